@@ -16,7 +16,7 @@
  *    passed as void*; NULL means the legacy default stream) and is
  *    asynchronous. No call synchronises, except conduit_read_status.
  *  - Conditions found on the device (a non-finite score, a bounded wait that
- *    ran out) are OR-ed into a caller-provided device int32 status word as
+ *    ran out, an index outside of its array) are OR-ed into a caller-provided device int32 status word as
  *    CONDUIT_FLAG_* bits; conduit_read_status turns the word into a status.
  *  - conduit_last_error_string() describes the last failure of the calling
  *    thread.
@@ -46,7 +46,8 @@ enum {
   CONDUIT_ERR_CUDA = 3,        /* a CUDA runtime call failed */
   CONDUIT_ERR_NONFINITE = 4,   /* device found a NaN / Inf score (status word) */
   CONDUIT_ERR_TIMEOUT = 5,     /* a bounded device wait ran out (status word) */
-  CONDUIT_ERR_WORKSPACE = 6    /* workspace pointer missing, misaligned or short */
+  CONDUIT_ERR_WORKSPACE = 6,   /* workspace pointer missing, misaligned or short */
+  CONDUIT_ERR_INDEX = 7        /* device found a position, length or page outside of its range (status word) */
 };
 
 /*
@@ -58,6 +59,7 @@ enum {
 enum {
   CONDUIT_FLAG_NONFINITE = 1,
   CONDUIT_FLAG_TIMEOUT = 2,
+  CONDUIT_FLAG_INDEX = 4,
   CONDUIT_SITE_LOAD = 1 << 8,
   CONDUIT_SITE_MMA = 1 << 9,
   CONDUIT_SITE_FINAL = 1 << 10
@@ -467,6 +469,170 @@ conduit_status conduit_staleness_iso(const conduit_kv* kv, const conduit_batch* 
                                      size_t workspace_bytes, int32_t* status, void* stream);
 
 /*
+ * Rotary positions with several axes (time, height, width of images and
+ * video). The first rot_dim dims of a head rotate as rot_dim / 2 pairs; pair p
+ * turns by the angle of the position on the axis axis[p], whose cosine and
+ * sine are row pos[axis[p]][t] of a table:
+ *   (cos, sin) = table[pos[axis[p]][t]][p]
+ *   y1 = x1 cos - x2 sin,   y2 = x2 cos + x1 sin           (fp32, rounded once)
+ *   CONDUIT_ROPE_HALVES  (x1, x2) = (x[p], x[p + rot_dim / 2])
+ *   CONDUIT_ROPE_PAIRS   (x1, x2) = (x[2 p], x[2 p + 1])
+ * Dims from rot_dim on pass unchanged. `axis` covers both ways of dealing the
+ * pairs out to the axes (consecutive sections and interleaved).
+ * A row with a position outside [0, table_len) is not written and sets
+ * CONDUIT_FLAG_INDEX.
+ */
+enum { CONDUIT_ROPE_HALVES = 0, CONDUIT_ROPE_PAIRS = 1 };
+#define CONDUIT_MAX_AXES 4
+
+typedef struct conduit_rotary {
+  int32_t rot_dim;       /* even, in [2, head_dim] */
+  int32_t num_axes;      /* A in [1, CONDUIT_MAX_AXES] */
+  int32_t layout;        /* CONDUIT_ROPE_* */
+  int32_t table_len;     /* rows of the table */
+  const float* table;    /* device fp32 [table_len][rot_dim / 2][2], 16-byte aligned */
+  const int32_t* axis;   /* host [rot_dim / 2], each in [0, A) */
+} conduit_rotary;
+
+/*
+ * Rows x[l][t][h][:] of a call (queries, keys, values, outputs): a base pointer
+ * and strides in elements, so that a row may be part of a fused projection.
+ * The head_dim elements of a row are contiguous. Strides >= 0, base aligned to
+ * the element (16-byte aligned bases and strides take wider copies).
+ */
+typedef struct conduit_rows {
+  void* data;            /* device */
+  int64_t layer_stride;
+  int64_t row_stride;
+  int64_t head_stride;
+} conduit_rows;
+
+/*
+ * out[l][t][h] = rotation of x[l][t][h] for l < L, t < T, h < H. `inverse`
+ * turns back (sin -> -sin), which is also the gradient: dx = inverse of dout.
+ *  pos  device int32 [A][T]
+ *  out  may be x itself (same data and strides); other overlaps are not allowed
+ * T = 0 is no work. Errors: INVALID_ARG (sizes, pointers, strides, axis),
+ * UNSUPPORTED (head_dim outside [2, 256], more than 65535 layers).
+ */
+conduit_status conduit_rope(const conduit_rotary* rope, const int32_t* pos, int32_t num_layers,
+                            int32_t num_rows, int32_t num_heads, int32_t head_dim, int32_t dtype,
+                            const conduit_rows* x, const conduit_rows* out, int32_t inverse,
+                            int32_t* status, void* stream);
+
+/*
+ * Requests of one call on a growing cache. Request r has the call's rows
+ * row_off[r] .. row_off[r+1]-1 (its newest tokens) and len[r] cached tokens,
+ * those rows included: row i of n_r is the token len[r] - n_r + i. len lives on
+ * the device only, so that a captured decoding step can be replayed with
+ * lengths that grow; max_len bounds them on the host (grids, workspaces). A
+ * length outside [0, min(max_len, page-table row)] is clamped for reading and
+ * sets CONDUIT_FLAG_INDEX.
+ */
+typedef struct conduit_seqs {
+  int32_t num_requests;        /* R >= 1 */
+  int32_t max_len;             /* >= 0 */
+  const int32_t* row_off;      /* host [R+1] */
+  const int32_t* row_off_dev;  /* device [R+1], equal contents */
+  const int32_t* len_dev;      /* device [R] */
+} conduit_seqs;
+
+/*
+ * Append to a paged cache (conduit_kv with page_size > 0), keys rotated on the
+ * way: for every layer and row of the call at token j of its request,
+ *   K[l][g][j] = rotation of k[l][t][g],  V[l][g][j] = v[l][t][g]
+ * and, where q is given, q_out[l][t][h] = rotation of q[l][t][h], in one launch.
+ *  rope    NULL: no rotation (pos is then ignored)
+ *  pos     device int32 [A][T], T = row_off[R]
+ *  q, q_out  both NULL or both given; q_out may be q itself
+ * A row whose position, token index or page (outside [0, num_pages)) is out of
+ * range is not written and sets CONDUIT_FLAG_INDEX. Rows of one call must have
+ * distinct slots. kv->num_layers layers are appended to.
+ */
+conduit_status conduit_kv_append(const conduit_kv* kv, const conduit_seqs* seqs,
+                                 const conduit_rotary* rope, const int32_t* pos,
+                                 const conduit_rows* k, const conduit_rows* v, const conduit_rows* q,
+                                 const conduit_rows* q_out, int32_t* status, void* stream);
+
+/*
+ * A cache held in 4 bits, for contexts kept between requests and read by
+ * decoding steps. Each token's head row is cut into groups of 32 dims:
+ *   x clipped to +-61440; lo, hi = its least and largest value
+ *   s = fp16((hi - lo) * fp32(1/15)),  m = fp16(lo + 8 s)
+ *   c = clamp(round_half_even((x - m) * (1/s)), -8, 7)   (0 where s = 0)
+ *   the group stands for m + s c;  c + 8 is stored in 4 bits
+ * all in fp32. A group with a NaN stands for NaNs (append sets NONFINITE for
+ * NaN and infinities).
+ * pool is [L][P][Hkv][page bytes], page bytes = page_size (d + d/4): page_size
+ * K rows of d/2 bytes, page_size V rows of d/2 bytes, then page_size rows of
+ * d/32 (s, m) fp16 pairs for K, and the same for V.
+ *   K row: dim 32 g + 8 c + e is nibble e of its 32-bit word c (d/32) + g
+ *   V row: dim 32 g + 4 q + e is nibble e of its 16-bit word q (d/32) + g
+ * so that a lane that multiplies group by group finds its words side by side.
+ * Rows that no token has may hold anything; they reach no result.
+ */
+typedef struct conduit_packed_kv {
+  int32_t num_layers;        /* L */
+  int32_t num_q_heads;       /* Hq, a multiple of Hkv */
+  int32_t num_kv_heads;      /* Hkv */
+  int32_t head_dim;          /* d, a multiple of 32 in [32, 256] */
+  int32_t page_size;         /* a power of two in [8, 1024] */
+  int32_t num_pages;         /* P */
+  int32_t max_pages_per_req; /* row length of page_table */
+  void* pool;                /* device, 16-byte aligned */
+  const int32_t* page_table; /* device [R][max_pages_per_req] */
+} conduit_packed_kv;
+
+/* Bytes of one page of one layer and KV head; -1 for sizes that are not supported. */
+int64_t conduit_packed_page_bytes(int32_t head_dim, int32_t page_size);
+
+/*
+ * conduit_kv_append into a 4-bit cache. dtype is that of k, v, q and q_out
+ * (CONDUIT_F32 or CONDUIT_BF16); the rotated key is packed from fp32.
+ */
+conduit_status conduit_packed_append(const conduit_packed_kv* kv, const conduit_seqs* seqs,
+                                     const conduit_rotary* rope, const int32_t* pos, int32_t dtype,
+                                     const conduit_rows* k, const conduit_rows* v,
+                                     const conduit_rows* q, const conduit_rows* q_out,
+                                     int32_t* status, void* stream);
+
+/*
+ * Take tokens up from a 4-bit cache into a cache that the scoring and refresh
+ * calls read: token t < N_r of batch request r becomes
+ *   dst K[l][g][t], V[l][g][t] = values of 4-bit token first[r] + t, in dst's dtype
+ * dst is contiguous or paged with packed's layers, KV heads and head_dim.
+ *  first  device int32 [R] or NULL (0)
+ * Tokens outside the page-table row or with a page outside [0, num_pages) of
+ * either cache are not written and set CONDUIT_FLAG_INDEX.
+ */
+conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* first,
+                                   const conduit_kv* dst, const conduit_batch* batch,
+                                   int32_t* status, void* stream);
+
+/*
+ * Attention of the call's rows over a 4-bit cache, from one row per request
+ * (decoding) to many (drafts, query prefixes, recomputed rows):
+ *   x_j = scale <q[l][t][h], K[l][h/G][j]>  for j < limit(t)
+ *   out[l][t][h] = sum_j softmax(x)_j V[l][h/G][j],  lse[l][h][t] = ln sum_j exp(x_j)
+ * with K, V the values that the cache stands for and softmax statistics and
+ * sums in fp32. A row that sees no key has out 0 and lse -inf.
+ *  scale   0: 1/sqrt(d); else finite and > 0
+ *  limits  device int32 [T] visible keys of each row (clamped to [0, len[r]]),
+ *          or NULL: row i of n_r sees max(0, len[r] - n_r + i + 1) (causal at the end)
+ *  lse     device fp32 [L][Hq][T] or NULL (the extra_lse of conduit_score_opts)
+ *  workspace  device, 256-byte aligned, conduit_packed_attn_workspace_size bytes
+ *          (fp32 partial results of key chunks); calls that overlap on the GPU
+ *          need workspaces of their own
+ * Results are deterministic.
+ */
+conduit_status conduit_packed_attn_workspace_size(const conduit_packed_kv* kv, const conduit_seqs* seqs,
+                                                  int32_t dtype, size_t* bytes);
+conduit_status conduit_packed_attn(const conduit_packed_kv* kv, const conduit_seqs* seqs, int32_t dtype,
+                                   const conduit_rows* q, float scale, const int32_t* limits,
+                                   const conduit_rows* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
  * Number of kernels this library has enqueued in this process (launched, or
  * recorded into a stream capture) since it was loaded. Diagnostic only.
  */
@@ -477,7 +643,8 @@ conduit_status conduit_clear_status(int32_t* status, void* stream);
 
 /*
  * Synchronise `stream`, copy the status word to *word (host) and return
- * CONDUIT_OK, CONDUIT_ERR_NONFINITE or CONDUIT_ERR_TIMEOUT (timeout wins).
+ * CONDUIT_OK, CONDUIT_ERR_NONFINITE, CONDUIT_ERR_INDEX or CONDUIT_ERR_TIMEOUT
+ * (timeout wins, then index).
  */
 conduit_status conduit_read_status(const int32_t* status, void* stream, int32_t* word);
 

@@ -18,8 +18,8 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libconduit.so")
 
-OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_NONFINITE, ERR_TIMEOUT, ERR_WORKSPACE = range(7)
-FLAG_NONFINITE, FLAG_TIMEOUT = 1, 2
+OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_NONFINITE, ERR_TIMEOUT, ERR_WORKSPACE, ERR_INDEX = range(8)
+FLAG_NONFINITE, FLAG_TIMEOUT, FLAG_INDEX = 1, 2, 4
 # with FLAG_TIMEOUT, the wait that ran out: a TMA tile, an MMA completion, an item's final MMA
 SITE_LOAD, SITE_MMA, SITE_FINAL = 1 << 8, 1 << 9, 1 << 10
 F32, BF16 = 0, 1
@@ -27,10 +27,12 @@ MAX_LAYERS = 512
 STAT_MEAN, STAT_RMS = 0, 1
 VNORM_FROM_V, VNORM_SIDE_CACHE, VNORM_NONE = 0, 1, 2
 _STATS = {"mean": STAT_MEAN, "rms": STAT_RMS}
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+_ROPE_LAYOUTS = {"halves": ROPE_HALVES, "pairs": ROPE_PAIRS}
 _VNORMS = {"v": VNORM_FROM_V, "side_cache": VNORM_SIDE_CACHE, "none": VNORM_NONE}
 
 _STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "CUDA", 4: "NONFINITE",
-                 5: "TIMEOUT", 6: "WORKSPACE"}
+                 5: "TIMEOUT", 6: "WORKSPACE", 7: "INDEX"}
 
 
 class ConduitError(RuntimeError):
@@ -53,6 +55,38 @@ class ConduitScoreOpts(ctypes.Structure):
     _fields_ = [
         ("statistic", ctypes.c_int32), ("value_norm", ctypes.c_int32),
         ("vnorm", ctypes.c_void_p), ("extra_lse", ctypes.c_void_p),
+    ]
+
+
+class ConduitRotary(ctypes.Structure):
+    _fields_ = [
+        ("rot_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32),
+        ("layout", ctypes.c_int32), ("table_len", ctypes.c_int32),
+        ("table", ctypes.c_void_p), ("axis", ctypes.c_void_p),
+    ]
+
+
+class ConduitRows(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+    ]
+
+
+class ConduitSeqs(ctypes.Structure):
+    _fields_ = [
+        ("num_requests", ctypes.c_int32), ("max_len", ctypes.c_int32),
+        ("row_off", ctypes.c_void_p), ("row_off_dev", ctypes.c_void_p), ("len_dev", ctypes.c_void_p),
+    ]
+
+
+class ConduitPackedKV(ctypes.Structure):
+    _fields_ = [
+        ("num_layers", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+        ("max_pages_per_req", ctypes.c_int32),
+        ("pool", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
     ]
 
 
@@ -101,6 +135,13 @@ def _load():
         "conduit_kv_exchange": (st, [P, P, P, P, P, P, P, P, P, P]),
         "conduit_refresh_workspace_size": (st, [P, P, P, ctypes.POINTER(SZ)]),
         "conduit_refresh_attn": (st, [P, P, P, P, P, P, P, P, SZ, P, P]),
+        "conduit_rope": (st, [P, P, I32, I32, I32, I32, I32, P, P, I32, P, P]),
+        "conduit_kv_append": (st, [P, P, P, P, P, P, P, P, P, P]),
+        "conduit_packed_page_bytes": (ctypes.c_int64, [I32, I32]),
+        "conduit_packed_append": (st, [P, P, P, P, I32, P, P, P, P, P, P]),
+        "conduit_packed_read": (st, [P, P, P, P, P, P]),
+        "conduit_packed_attn_workspace_size": (st, [P, P, I32, ctypes.POINTER(SZ)]),
+        "conduit_packed_attn": (st, [P, P, I32, P, ctypes.c_float, P, P, P, P, SZ, P, P]),
         "conduit_launch_count": (ctypes.c_int64, []),
         "conduit_clear_status": (st, [P, P]),
         "conduit_read_status": (st, [P, P, ctypes.POINTER(I32)]),
@@ -518,14 +559,211 @@ def conduit_refresh_attn(kv: KvCache, batch: Batch, idx, idx_off, idx_off_dev, q
     return out
 
 
+def rope_table(theta: float, rot_dim: int, max_pos: int, device="cuda") -> torch.Tensor:
+    """Cosines and sines of positions 0 .. max_pos - 1 for frequencies theta^(-2 p / rot_dim), fp32
+    [max_pos, rot_dim/2, 2]; the angles are formed in fp64."""
+    half = rot_dim // 2
+    freq = float(theta) ** (-torch.arange(half, dtype=torch.float64, device=device) / half)
+    angle = torch.arange(max_pos, dtype=torch.float64, device=device)[:, None] * freq
+    return torch.stack([angle.cos(), angle.sin()], dim=-1).float().contiguous()
+
+
+class Rope:
+    """Rotary positions with several axes (conduit_rotary): a table fp32 [max_pos, rot_dim/2, 2] of
+    (cos, sin) and the axis of every pair."""
+
+    def __init__(self, table: torch.Tensor, axis: Sequence[int], layout: str = "halves"):
+        if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, "table must be contiguous fp32 [max_pos, rot_dim/2, 2]")
+        if len(axis) != table.shape[1]:
+            raise ConduitError(ERR_INVALID_ARG, "axis needs one entry per pair of the table")
+        if layout not in _ROPE_LAYOUTS:
+            raise ConduitError(ERR_INVALID_ARG, "layout must be 'halves' or 'pairs'")
+        self.table = table
+        self.axis = (ctypes.c_int32 * len(axis))(*axis)
+        self.num_axes = max(axis, default=-1) + 1
+        self.rot_dim = 2 * table.shape[1]
+        self.struct = ConduitRotary(self.rot_dim, self.num_axes, _ROPE_LAYOUTS[layout], table.shape[0],
+                                    table.data_ptr(), ctypes.addressof(self.axis))
+
+    def ref(self):
+        return ctypes.byref(self.struct)
+
+    def positions(self, pos: Optional[torch.Tensor], rows: int) -> torch.Tensor:
+        if pos is None or pos.dtype != torch.int32 or not pos.is_contiguous() or \
+                tuple(pos.shape) != (self.num_axes, rows):
+            raise ConduitError(ERR_INVALID_ARG, f"pos must be contiguous int32 [{self.num_axes}, {rows}]")
+        return pos
+
+
+class Seqs:
+    """Requests of a call on a growing cache (conduit_seqs): rows row_off[r] .. row_off[r+1]-1 are the
+    newest of lens[r] cached tokens. lens (int32, device) is kept by reference: a decoding loop
+    advances it in place; max_len bounds it."""
+
+    def __init__(self, row_off, lens: torch.Tensor, max_len: int):
+        self.row_off = torch.as_tensor(row_off, dtype=torch.int32).contiguous().cpu()
+        if lens.dtype != torch.int32 or lens.numel() != self.row_off.numel() - 1 or not lens.is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, "lens must be contiguous int32 with one entry per request")
+        self.lens = lens
+        self.row_off_dev = self.row_off.to(lens.device)
+        self.num_requests, self.num_rows = lens.numel(), int(self.row_off[-1])
+        self.max_len = int(max_len)
+        self.struct = ConduitSeqs(self.num_requests, self.max_len, self.row_off.data_ptr(),
+                                  self.row_off_dev.data_ptr(), lens.data_ptr())
+
+    def ref(self):
+        return ctypes.byref(self.struct)
+
+
+def packed_page_bytes(head_dim: int, page_size: int) -> int:
+    """Bytes of one page of one layer and KV head of a 4-bit cache (-1: sizes not supported)."""
+    return int(_lib.conduit_packed_page_bytes(int(head_dim), int(page_size)))
+
+
+class PackedKv:
+    """A paged cache held in 4 bits (conduit_packed_kv): pool uint8 [L][P][Hkv][page bytes]."""
+
+    def __init__(self, pool: torch.Tensor, num_q_heads: int, head_dim: int, page_size: int,
+                 page_table: torch.Tensor):
+        if pool.dtype != torch.uint8 or pool.dim() != 4 or not pool.is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, "pool must be contiguous uint8 [L, P, Hkv, page bytes]")
+        L, P, Hkv, nbytes = pool.shape
+        want = packed_page_bytes(head_dim, page_size)
+        if want >= 0 and nbytes != want:
+            raise ConduitError(ERR_INVALID_ARG, f"a page of the pool has {nbytes} bytes, {want} needed")
+        if page_table.dim() != 2:
+            raise ConduitError(ERR_INVALID_ARG, "page_table must be [R, max_pages]")
+        self.pool = pool
+        self.page_table = page_table.to(device=pool.device, dtype=torch.int32).contiguous()
+        self.num_layers, self.num_kv_heads, self.num_q_heads = L, Hkv, num_q_heads
+        self.head_dim, self.page_size = head_dim, page_size
+        self.struct = ConduitPackedKV(L, num_q_heads, Hkv, head_dim, page_size, P, self.page_table.shape[1],
+                                      pool.data_ptr(), self.page_table.data_ptr())
+
+    @classmethod
+    def empty(cls, num_layers: int, num_pages: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
+              page_size: int, page_table: torch.Tensor, device="cuda"):
+        """A cache with a pool of its own."""
+        nbytes = packed_page_bytes(head_dim, page_size)
+        if nbytes < 0:
+            raise ConduitError(ERR_UNSUPPORTED, "head_dim must be a multiple of 32 in [32, 256], "
+                                                "page_size a power of two in [8, 1024]")
+        pool = torch.empty((num_layers, num_pages, num_kv_heads, nbytes), dtype=torch.uint8, device=device)
+        return cls(pool, num_q_heads, head_dim, page_size, page_table)
+
+    def ref(self):
+        return ctypes.byref(self.struct)
+
+
+def _rows(t: torch.Tensor, name: str, layers: int, rows: int, heads: int, d: int, dtype=None):
+    """Strided rows [L][T][H][d] (or [T][H][d] of one layer) as a conduit_rows reference."""
+    if t.dim() == 3:
+        (n, h, w), (rs, hs, es), L, ls = t.shape, t.stride(), 1, 0
+    elif t.dim() == 4:
+        (L, n, h, w), (ls, rs, hs, es) = t.shape, t.stride()
+    else:
+        raise ConduitError(ERR_INVALID_ARG, f"{name} must be [L, T, H, d] or [T, H, d]")
+    if (L, n, h, w) != (layers, rows, heads, d):
+        raise ConduitError(ERR_INVALID_ARG, f"{name} is {tuple(t.shape)}, not [{layers}, {rows}, {heads}, {d}]")
+    if es != 1 and w > 1:
+        raise ConduitError(ERR_INVALID_ARG, f"the elements of a head of {name} must be contiguous")
+    if dtype is not None and t.dtype != dtype:
+        raise ConduitError(ERR_INVALID_ARG, f"{name} is {t.dtype}, not {dtype}")
+    return ctypes.byref(ConduitRows(t.data_ptr(), ls, rs, hs))
+
+
+def conduit_rope(rope: Rope, x: torch.Tensor, pos: torch.Tensor, out=None, inverse: bool = False, status=None,
+                 stream=None) -> torch.Tensor:
+    """Rows x [T, H, d] or [L, T, H, d] (any strides, contiguous heads) turned by their positions
+    pos int32 [A, T]; inverse turns back (the gradient). out may be x."""
+    if x.dim() not in (3, 4):
+        raise ConduitError(ERR_INVALID_ARG, "x must be [L, T, H, d] or [T, H, d]")
+    L = x.shape[0] if x.dim() == 4 else 1
+    T, H, d = x.shape[-3:]
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    _check(_lib.conduit_rope(rope.ref(), _ptr(rope.positions(pos, T)), L, T, H, d, _dtype_code(x),
+                             _rows(x, "x", L, T, H, d), _rows(out, "out", L, T, H, d, x.dtype), int(inverse),
+                             _ptr(status), _stream_ptr(stream)))
+    return out
+
+
+def _append_args(kv, seqs: Seqs, k, v, rope, pos, q, q_out):
+    L, T, Hkv, d = kv.num_layers, seqs.num_rows, kv.num_kv_heads, kv.head_dim
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    rows = [_rows(k, "k", L, T, Hkv, d), _rows(v, "v", L, T, Hkv, d, k.dtype)]
+    rows += [None if t is None else _rows(t, name, L, T, kv.num_q_heads, d, k.dtype)
+             for t, name in ((q, "q"), (q_out, "q_out"))]
+    return (None if rope is None else rope.ref(), None if rope is None else _ptr(rope.positions(pos, T))), rows, q_out
+
+
+def conduit_kv_append(kv: KvCache, seqs: Seqs, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
+                      pos=None, q=None, q_out=None, status=None, stream=None):
+    """Append rows k, v [L, T, Hkv, d] to a paged cache, keys turned by rope on the way; q
+    [L, T, Hq, d] is turned in the same launch. Returns q_out (None without q)."""
+    if k.dtype != kv.dtype:
+        raise ConduitError(ERR_INVALID_ARG, f"k is {k.dtype}, the cache {kv.dtype}")
+    turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out)
+    _check(_lib.conduit_kv_append(kv.ref(), seqs.ref(), *turn, *rows, _ptr(status), _stream_ptr(stream)))
+    return q_out
+
+
+def conduit_packed_append(kv: PackedKv, seqs: Seqs, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
+                          pos=None, q=None, q_out=None, status=None, stream=None):
+    """conduit_kv_append into a 4-bit cache. Returns q_out (None without q)."""
+    turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out)
+    _check(_lib.conduit_packed_append(kv.ref(), seqs.ref(), *turn, _dtype_code(k), *rows, _ptr(status),
+                                      _stream_ptr(stream)))
+    return q_out
+
+
+def conduit_packed_read(kv: PackedKv, batch: Batch, dst: KvCache, first=None, status=None, stream=None):
+    """Tokens first[r] .. of every request of a 4-bit cache into dst, as the batch lays it out."""
+    if first is not None and (first.dtype != torch.int32 or first.numel() != batch.num_requests):
+        raise ConduitError(ERR_INVALID_ARG, "first must be int32 with one entry per request")
+    if batch.num_requests > kv.page_table.shape[0]:
+        raise ConduitError(ERR_INVALID_ARG, "the page table has fewer rows than the batch has requests")
+    _check(_lib.conduit_packed_read(kv.ref(), _ptr(first), dst.ref(), batch.ref(), _ptr(status),
+                                    _stream_ptr(stream)))
+
+
+def conduit_packed_attn_workspace_size(kv: PackedKv, seqs: Seqs, dtype: Optional[torch.dtype] = None) -> int:
+    """Workspace of conduit_packed_attn for rows of `dtype` (None: enough for either)."""
+    n, most = ctypes.c_size_t(0), 0
+    for code in ((F32, BF16) if dtype is None else (F32,) if dtype == torch.float32 else (BF16,)):
+        _check(_lib.conduit_packed_attn_workspace_size(kv.ref(), seqs.ref(), code, ctypes.byref(n)))
+        most = max(most, int(n.value))
+    return most
+
+
+def conduit_packed_attn(kv: PackedKv, seqs: Seqs, q: torch.Tensor, scale: Optional[float] = None, limits=None,
+                        out=None, lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
+    """Attention of rows q [L, T, Hq, d] over a 4-bit cache. limits int32 [T]: keys each row sees
+    (None: causal at the end of the context); lse fp32 [L, Hq, T] receives the log-sum-exp."""
+    L, T, Hq, d = kv.num_layers, seqs.num_rows, kv.num_q_heads, kv.head_dim
+    if seqs.num_requests > kv.page_table.shape[0]:
+        raise ConduitError(ERR_INVALID_ARG, "the page table has fewer rows than there are requests")
+    if limits is not None and (limits.dtype != torch.int32 or limits.numel() != T or not limits.is_contiguous()):
+        raise ConduitError(ERR_INVALID_ARG, "limits must be contiguous int32 with one entry per row")
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != L * Hq * T or not lse.is_contiguous()):
+        raise ConduitError(ERR_INVALID_ARG, "lse must be contiguous fp32 [L, Hq, T]")
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    rows = _rows(q, "q", L, T, Hq, d), _rows(out, "out", L, T, Hq, d, q.dtype)
+    ws = _workspace(lambda: conduit_packed_attn_workspace_size(kv, seqs, q.dtype), q.device, workspace)
+    _check(_lib.conduit_packed_attn(kv.ref(), seqs.ref(), _dtype_code(q), rows[0], scale or 0.0, _ptr(limits),
+                                    rows[1], _ptr(lse), _ptr(ws), ws.numel(), _ptr(status), _stream_ptr(stream)))
+    return out
+
+
 def conduit_clear_status(status: torch.Tensor, stream=None):
     _check(_lib.conduit_clear_status(_ptr(status), _stream_ptr(stream)))
 
 
 def conduit_read_status(status: torch.Tensor, stream=None) -> int:
-    """Synchronises the stream; returns OK, ERR_NONFINITE or ERR_TIMEOUT (no raise)."""
+    """Synchronises the stream; returns OK, ERR_NONFINITE, ERR_INDEX or ERR_TIMEOUT (no raise)."""
     word = ctypes.c_int32(0)
     code = _lib.conduit_read_status(_ptr(status), _stream_ptr(stream), ctypes.byref(word))
-    if code not in (OK, ERR_NONFINITE, ERR_TIMEOUT):
+    if code not in (OK, ERR_NONFINITE, ERR_INDEX, ERR_TIMEOUT):
         _check(code)
     return int(code)

@@ -6,15 +6,21 @@
 #include <cstdio>
 #include <string>
 
-#include "internal.cuh"
+#include "abi_checks.cuh"
 
 using namespace conduit;
+using namespace conduit::abi;
 
 namespace {
 
 std::atomic<int64_t> g_launches{0};
 
 thread_local std::string g_last_error;
+
+}  // namespace
+
+namespace conduit {
+namespace abi {
 
 conduit_status fail(conduit_status code, const char* fmt, ...) {
   char buf[512];
@@ -29,11 +35,6 @@ conduit_status fail(conduit_status code, const char* fmt, ...) {
 conduit_status cuda_fail(cudaError_t err, const char* what) {
   return fail(CONDUIT_ERR_CUDA, "%s: %s", what, cudaGetErrorString(err));
 }
-
-constexpr size_t kAlign = 256;
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 conduit_status check_batch(const conduit_batch* b) {
   if (!b) return fail(CONDUIT_ERR_INVALID_ARG, "batch is NULL");
@@ -118,6 +119,21 @@ BatchDev make_batch(const conduit_batch* b) {
   return BatchDev{b->num_requests, b->num_images, b->tok_off_dev, b->img_off_dev,
                   b->req_img_off_dev, b->q_off_dev};
 }
+
+conduit_status check_workspace(void* ws, size_t have, size_t need) {
+  if (need == 0) return CONDUIT_OK;
+  if (!ws) return fail(CONDUIT_ERR_WORKSPACE, "workspace is NULL but %zu bytes are needed", need);
+  if (reinterpret_cast<uintptr_t>(ws) % kAlign)
+    return fail(CONDUIT_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (have < need)
+    return fail(CONDUIT_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", have, need);
+  return CONDUIT_OK;
+}
+
+}  // namespace abi
+}  // namespace conduit
+
+namespace {
 
 conduit_status make_layers(const conduit_kv* kv, const int32_t* layers, int32_t n_layers,
                            LayerList* out) {
@@ -224,16 +240,6 @@ int max_tokens(const conduit_batch* b) {
   int m = 0;
   for (int r = 0; r < b->num_requests; ++r) m = std::max(m, b->tok_off[r + 1] - b->tok_off[r]);
   return m;
-}
-
-conduit_status check_workspace(void* ws, size_t have, size_t need) {
-  if (need == 0) return CONDUIT_OK;
-  if (!ws) return fail(CONDUIT_ERR_WORKSPACE, "workspace is NULL but %zu bytes are needed", need);
-  if (reinterpret_cast<uintptr_t>(ws) % kAlign)
-    return fail(CONDUIT_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (have < need)
-    return fail(CONDUIT_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", have, need);
-  return CONDUIT_OK;
 }
 
 conduit_status check_selection(const conduit_batch* b, const int32_t* idx_off,
@@ -733,6 +739,7 @@ conduit_status conduit_read_status(const int32_t* status, void* stream, int32_t*
   err = cudaMemcpy(word, status, sizeof(int32_t), cudaMemcpyDeviceToHost);
   if (err) return cuda_fail(err, "read_status (copy)");
   if (*word & CONDUIT_FLAG_TIMEOUT) return CONDUIT_ERR_TIMEOUT;
+  if (*word & CONDUIT_FLAG_INDEX) return CONDUIT_ERR_INDEX;
   if (*word & CONDUIT_FLAG_NONFINITE) return CONDUIT_ERR_NONFINITE;
   return CONDUIT_OK;
 }

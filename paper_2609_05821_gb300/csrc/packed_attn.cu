@@ -1,0 +1,221 @@
+// Attention over the 4-bit cache: how a call is cut, the CUDA-core kernel (fp32
+// rows, bf16 rows), and the join of key chunks.
+//
+// Mathematics: x_j = scale <q, K_j>, out = sum_j e^(x_j - M) V_j / sum_j e^(x_j - M) in
+// one pass with a running M per (row, head); chunks of keys give (M, sum, O) that
+// combine_kernel joins in order. Columns: the call's rows of a request times the G
+// query heads of a KV head, column j = i G + h.
+#include <algorithm>
+
+#include "packed_attn.cuh"
+
+namespace conduit {
+namespace {
+
+// ------------------------------------------------------------- CUDA cores
+// A CTA of four warps, two columns a warp, 32 keys at a time as fp32 in shared
+// memory: lanes are keys for the logits and dims for the sums.
+constexpr int kSimtKeys = 32;
+
+template <typename T, int NG>
+__global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
+  constexpr int D = NG * 32, KS = D + 1;
+  extern __shared__ float simt_smem[];
+  float *ks = simt_smem, *vs = ks + kSimtKeys * KS, *qs = vs + kSimtKeys * D;
+  Item it;
+  if (!item_of(a, &it)) return;
+  const int tid = threadIdx.x, w = tid / 32, lane = tid % 32;
+  for (int e = tid; e < kCols * D; e += 128) {
+    const int j = it.cb * kCols + e / D;
+    float x = 0.f;
+    if (j < it.n * a.kv.G) {
+      const int i = j / a.kv.G, h = it.g * a.kv.G + j % a.kv.G;
+      x = to_float(static_cast<const T*>(a.q.p)[it.l * a.q.ls + int64_t(it.t0 + i) * a.q.rs + h * a.q.hs + e % D]);
+    }
+    qs[e] = x;
+  }
+  int lim[2], most = 0;
+  for (int c = 0; c < kCols; ++c) most = max(most, limit_of(a, it, it.cb * kCols + c));
+#pragma unroll
+  for (int c = 0; c < 2; ++c) lim[c] = limit_of(a, it, it.cb * kCols + 2 * w + c);
+  const int k0 = it.chunk * a.chunk, k1 = min(k0 + a.chunk, most);
+  const float to_log2 = a.scale * kLog2e;
+  float m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, o[2][NG];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int e = 0; e < NG; ++e) o[c][e] = 0.f;
+  for (int kb = k0; kb < k1; kb += kSimtKeys) {
+    __syncthreads();
+    for (int e = tid; e < kSimtKeys * (D / 8); e += 128) {  // 8 dims of a key, K and V
+      const int key = e / (D / 8), u = e % (D / 8), j = kb + key, grp = u / 4, c = u % 4;
+      float* ko = ks + key * KS + 8 * u;
+      float* vo = vs + key * D + 8 * u;
+      if (j < k1) {
+        const uint8_t* at = a.kv.page(it.l, it.g, page_of(a, it.r, j));
+        const int row = j & ((1 << a.kv.page_shift) - 1);
+        const uint32_t kw = reinterpret_cast<const uint32_t*>(at + a.kv.codes(0, row))[c * NG + grp];
+        const uint16_t* vh = reinterpret_cast<const uint16_t*>(at + a.kv.codes(1, row));
+        const uint32_t vw = vh[2 * c * NG + grp] | uint32_t(vh[(2 * c + 1) * NG + grp]) << 16;
+        const float2 kp = __half22float2(reinterpret_cast<const __half2*>(at + a.kv.params(0, row))[grp]);
+        const float2 vp = __half22float2(reinterpret_cast<const __half2*>(at + a.kv.params(1, row))[grp]);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          ko[x] = fmaf(kp.x, float(int((kw >> (4 * x)) & 15u) - 8), kp.y);
+          vo[x] = fmaf(vp.x, float(int((vw >> (4 * x)) & 15u) - 8), vp.y);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) ko[x] = vo[x] = 0.f;
+      }
+    }
+    __syncthreads();
+    float x[2] = {0.f, 0.f};
+    const float* k = ks + lane * KS;
+    const float* q0 = qs + 2 * w * D;
+#pragma unroll 8
+    for (int e = 0; e < D; ++e) {
+      x[0] = fmaf(q0[e], k[e], x[0]);
+      x[1] = fmaf(q0[D + e], k[e], x[1]);
+    }
+    float p[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const float y = kb + lane < lim[c] ? x[c] * to_log2 : -INFINITY;
+      float top = y;
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+      const float mn = fmaxf(m[c], top), base = mn == -INFINITY ? 0.f : mn;
+      p[c] = exp2f(y - base);
+      float add = p[c];
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) add += __shfl_xor_sync(0xffffffffu, add, s);
+      const float corr = exp2f(m[c] - base);
+      sum[c] = sum[c] * corr + add;
+      m[c] = mn;
+#pragma unroll
+      for (int e = 0; e < NG; ++e) o[c][e] *= corr;
+    }
+    for (int key = 0; key < kSimtKeys; ++key) {
+      const float p0 = __shfl_sync(0xffffffffu, p[0], key), p1 = __shfl_sync(0xffffffffu, p[1], key);
+      const bool s0 = kb + key < lim[0], s1 = kb + key < lim[1];  // a NaN value reaches only rows that see it
+#pragma unroll
+      for (int e = 0; e < NG; ++e) {
+        const float v = vs[key * D + e * 32 + lane];
+        if (s0) o[0][e] = fmaf(p0, v, o[0][e]);
+        if (s1) o[1][e] = fmaf(p1, v, o[1][e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int j = it.cb * kCols + 2 * w + c;
+    if (j >= it.n * a.kv.G) continue;
+#pragma unroll
+    for (int e = 0; e < NG; ++e) store_out<T>(a, it, j, e * 32 + lane, o[c][e], sum[c]);
+    if (lane == 0) store_stats(a, it, j, m[c], sum[c]);
+  }
+}
+
+constexpr int simt_smem_bytes(int d) { return (kSimtKeys * (2 * d + 1) + kCols * d) * int(sizeof(float)); }
+
+// ---------------------------------------------------------------- the join
+// A warp per (layer, row, head): weights 2^(M_c - M) over the chunks of the
+// request's context, then the sums in chunk order.
+template <typename T, int NG>
+__global__ void __launch_bounds__(128) combine_kernel(AttnArgs a) {
+  const int64_t col = int64_t(blockIdx.x) * 4 + threadIdx.x / 32;
+  const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
+  if (col >= cols) return;
+  const int lane = threadIdx.x % 32;
+  const int h = int(col % a.kv.Hq), t = int(col / a.kv.Hq % a.s.T), l = int(col / a.kv.Hq / a.s.T);
+  const int r = request_of(a.s.row_off, a.s.R, t);
+  const int len = cached_len(a.s, a.kv.capacity(), r, nullptr, false);
+  const int n = max(1, (len + a.chunk - 1) / a.chunk);
+  float top = -INFINITY;
+  for (int c = lane; c < n; c += 32) top = fmaxf(top, a.part_ml[c * cols + col].x);
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, o[NG];
+#pragma unroll
+  for (int e = 0; e < NG; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int c = 0; c < n; ++c) {
+    const float2 ml = a.part_ml[c * cols + col];
+    const float wgt = exp2f(ml.x - base);
+    sum = fmaf(wgt, ml.y, sum);
+    const float* po = a.part_o + (c * cols + col) * (NG * 32) + lane;
+#pragma unroll
+    for (int e = 0; e < NG; ++e) o[e] = fmaf(wgt, po[e * 32], o[e]);
+  }
+  T* to = static_cast<T*>(a.out.p) + l * a.out.ls + int64_t(t) * a.out.rs + h * a.out.hs;
+#pragma unroll
+  for (int e = 0; e < NG; ++e) to[e * 32 + lane] = from_float<T>(sum == 0.f ? 0.f : o[e] / sum);
+  if (lane == 0 && a.lse)
+    a.lse[(int64_t(l) * a.kv.Hq + h) * a.s.T + t] = sum == 0.f ? -INFINITY : kLn2 * (base + log2f(sum));
+}
+
+template <typename T, int NG>
+cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
+  constexpr int kSmem = simt_smem_bytes(NG * 32);
+  cudaError_t err = cudaFuncSetAttribute(packed_attn_simt<T, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (err) return err;
+  packed_attn_simt<T, NG><<<unsigned(plan.items), 128, kSmem, stream>>>(a);
+  count_launches(1);
+  err = cudaGetLastError();
+  if (err || a.chunks == 1) return err;
+  const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
+  combine_kernel<T, NG><<<unsigned((cols + 3) / 4), 128, 0, stream>>>(a);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_t(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
+  switch (a.kv.d / 32) {
+    case 1: return launch_ng<T, 1>(a, plan, stream);
+    case 2: return launch_ng<T, 2>(a, plan, stream);
+    case 3: return launch_ng<T, 3>(a, plan, stream);
+    case 4: return launch_ng<T, 4>(a, plan, stream);
+    case 5: return launch_ng<T, 5>(a, plan, stream);
+    case 6: return launch_ng<T, 6>(a, plan, stream);
+    case 7: return launch_ng<T, 7>(a, plan, stream);
+    default: return launch_ng<T, 8>(a, plan, stream);
+  }
+}
+
+int64_t items_of(const PackedDev& kv, const SeqsDev& s, int chunks) {
+  const int64_t blocks = (int64_t(s.max_rows) * kv.G + kCols - 1) / kCols;
+  return int64_t(kv.L) * s.R * kv.Hkv * blocks * chunks;
+}
+
+}  // namespace
+
+PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype) {
+  PackedAttnPlan p{};
+  const int most = int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
+  // four CTAs for each of the two that an SM holds, at least 256 keys each
+  const int64_t items = std::max<int64_t>(1, items_of(kv, s, 1));
+  const int64_t want = std::min<int64_t>((8 * 152 + items - 1) / items, (most + 255) / 256);
+  p.chunks = int(std::max<int64_t>(1, want));
+  p.chunk = std::max(256, (most + p.chunks - 1) / p.chunks);
+  p.chunk = (p.chunk + 255) / 256 * 256;
+  p.chunks = std::max(1, (most + p.chunk - 1) / p.chunk);
+  p.items = items_of(kv, s, p.chunks);
+  if (p.chunks > 1) p.scratch = size_t(p.chunks) * kv.L * s.T * kv.Hq * (size_t(kv.d) + 2) * sizeof(float);
+  return p;
+}
+
+cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const PackedAttnPlan& plan, int dtype,
+                               const RowsDev& q, float scale, const int32_t* limits, const RowsDev& out,
+                               float* lse, void* scratch, int32_t* status, cudaStream_t stream) {
+  AttnArgs a{kv, s, q, out, lse, limits, scale, plan.chunk, plan.chunks, 0, nullptr, nullptr, status};
+  a.col_blocks = int((int64_t(s.max_rows) * kv.G + kCols - 1) / kCols);
+  a.part_ml = static_cast<float2*>(scratch);
+  a.part_o = reinterpret_cast<float*>(a.part_ml + size_t(plan.chunks) * kv.L * s.T * kv.Hq);
+  return dtype == CONDUIT_BF16 ? launch_t<__nv_bfloat16>(a, plan, stream)
+                               : launch_t<float>(a, plan, stream);
+}
+
+}  // namespace conduit
