@@ -623,7 +623,9 @@ conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* f
  *  workspace  device, 256-byte aligned, conduit_packed_attn_workspace_size bytes
  *          (fp32 partial results of key chunks); calls that overlap on the GPU
  *          need workspaces of their own
- * Results are deterministic.
+ * bf16 rows with head_dim 64, 96 or 128 run on the tensor cores (fp16 operands:
+ * codes and queries exact, values and weights within 2^-11); fp32 rows and other
+ * head sizes on the CUDA cores in fp32. Results are deterministic.
  */
 conduit_status conduit_packed_attn_workspace_size(const conduit_packed_kv* kv, const conduit_seqs* seqs,
                                                   int32_t dtype, size_t* bytes);

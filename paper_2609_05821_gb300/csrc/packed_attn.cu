@@ -1,5 +1,5 @@
 // Attention over the 4-bit cache: how a call is cut, the CUDA-core kernel (fp32
-// rows, bf16 rows), and the join of key chunks.
+// rows, head sizes without a tensor-core kernel), and the join of key chunks.
 //
 // Mathematics: x_j = scale <q, K_j>, out = sum_j e^(x_j - M) V_j / sum_j e^(x_j - M) in
 // one pass with a running M per (row, head); chunks of keys give (M, sum, O) that
@@ -157,13 +157,18 @@ __global__ void __launch_bounds__(128) combine_kernel(AttnArgs a) {
 }
 
 template <typename T, int NG>
-cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
-  constexpr int kSmem = simt_smem_bytes(NG * 32);
-  cudaError_t err = cudaFuncSetAttribute(packed_attn_simt<T, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-  if (err) return err;
-  packed_attn_simt<T, NG><<<unsigned(plan.items), 128, kSmem, stream>>>(a);
-  count_launches(1);
-  err = cudaGetLastError();
+cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, bool mma, cudaStream_t stream) {
+  cudaError_t err;
+  if (mma) {
+    err = launch_packed_attn_mma(a, plan.items, stream);
+  } else {
+    constexpr int kSmem = simt_smem_bytes(NG * 32);
+    err = cudaFuncSetAttribute(packed_attn_simt<T, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (err) return err;
+    packed_attn_simt<T, NG><<<unsigned(plan.items), 128, kSmem, stream>>>(a);
+    count_launches(1);
+    err = cudaGetLastError();
+  }
   if (err || a.chunks == 1) return err;
   const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
   combine_kernel<T, NG><<<unsigned((cols + 3) / 4), 128, 0, stream>>>(a);
@@ -172,16 +177,16 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
 }
 
 template <typename T>
-cudaError_t launch_t(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
+cudaError_t launch_t(const AttnArgs& a, const PackedAttnPlan& plan, bool mma, cudaStream_t stream) {
   switch (a.kv.d / 32) {
-    case 1: return launch_ng<T, 1>(a, plan, stream);
-    case 2: return launch_ng<T, 2>(a, plan, stream);
-    case 3: return launch_ng<T, 3>(a, plan, stream);
-    case 4: return launch_ng<T, 4>(a, plan, stream);
-    case 5: return launch_ng<T, 5>(a, plan, stream);
-    case 6: return launch_ng<T, 6>(a, plan, stream);
-    case 7: return launch_ng<T, 7>(a, plan, stream);
-    default: return launch_ng<T, 8>(a, plan, stream);
+    case 1: return launch_ng<T, 1>(a, plan, mma, stream);
+    case 2: return launch_ng<T, 2>(a, plan, mma, stream);
+    case 3: return launch_ng<T, 3>(a, plan, mma, stream);
+    case 4: return launch_ng<T, 4>(a, plan, mma, stream);
+    case 5: return launch_ng<T, 5>(a, plan, mma, stream);
+    case 6: return launch_ng<T, 6>(a, plan, mma, stream);
+    case 7: return launch_ng<T, 7>(a, plan, mma, stream);
+    default: return launch_ng<T, 8>(a, plan, mma, stream);
   }
 }
 
@@ -214,8 +219,8 @@ cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const Pack
   a.col_blocks = int((int64_t(s.max_rows) * kv.G + kCols - 1) / kCols);
   a.part_ml = static_cast<float2*>(scratch);
   a.part_o = reinterpret_cast<float*>(a.part_ml + size_t(plan.chunks) * kv.L * s.T * kv.Hq);
-  return dtype == CONDUIT_BF16 ? launch_t<__nv_bfloat16>(a, plan, stream)
-                               : launch_t<float>(a, plan, stream);
+  return dtype == CONDUIT_BF16 ? launch_t<__nv_bfloat16>(a, plan, packed_attn_mma_supported(kv, dtype), stream)
+                               : launch_t<float>(a, plan, false, stream);
 }
 
 }  // namespace conduit

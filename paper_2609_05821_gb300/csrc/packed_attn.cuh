@@ -86,4 +86,8 @@ __device__ __forceinline__ void store_stats(const AttnArgs& a, const Item& it, i
   }
 }
 
+// Warp-level tensor-core kernel (packed_attn_mma.cu): bf16 rows, head_dim 64, 96, 128.
+bool packed_attn_mma_supported(const PackedDev& kv, int dtype);
+cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, cudaStream_t stream);
+
 }  // namespace conduit
