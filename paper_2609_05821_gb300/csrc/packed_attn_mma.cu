@@ -1,21 +1,23 @@
 // Attention over the 4-bit cache for few rows (decoding, drafts): warp-level tensor
 // cores, one pass over the packed keys and values.
 //
-// Mathematics. A group of 32 dims of token t is m_t + s_t c, c in -8..7. Logits come
-// group by group: x = sum_g s_tg (sum c q) + m_tg (sum q), with the codes exact in fp16 and
-// the queries exact too (bf16 scaled to fp16's range by a power of two per row), so
-// only fp32 sums round. Values are formed as fp16 m + s c (2^-11 relative), weights
-// rounded to fp16: both below the rounding of a bf16 output.
+// Mathematics. A group of 32 dims of token t is m_t + s_t (u - 8), u in 0..15. Logits come
+// group by group: x = sum_g s_tg (sum (u - 8) q) + m_tg (sum q). A nibble under the
+// exponent of 1024 is 1024 + u (or 1024 + 16 u) in fp16, one masked word for two codes; the
+// offsets are sums of the query alone and are taken off in fp32 (the products and their
+// sums are exact to 2^-23 of 1024 |q|: 10^-4 of a logit's own unit). Values are formed as
+// fp16 m + s c (2^-11 relative), weights rounded to fp16: both below the rounding of a
+// bf16 output.
 //
-// Shape. mma m16n8k16 with the tokens (then the dims) as the 16 rows and up to 8
-// (row, query head) columns as n, so that a KV head's group of 7 or 8 query heads
-// wastes nothing. The logits' accumulators hold tokens by lane / 4; movmatrix turns them
-// into the operand of the value product. Each warp owns tiles of 32 tokens with a ring
-// of its own: bulk copies of whole page runs, so no block-wide barrier is met before the
-// end, where the warps' results are joined.
+// Shape. mma with the tokens (then the dims) as the 16 rows and up to 8 (row, query head)
+// columns as n, so that a KV head's group of 7 or 8 query heads wastes nothing. The
+// logits' accumulators hold tokens by lane / 4; movmatrix turns them into the operand of
+// the value product. Each warp owns tiles of 32 tokens with a ring of its own: bulk copies
+// of whole page runs, so no block-wide barrier is met before the end, where the warps'
+// results are joined.
 //
-// Bound: 1.25 d bytes per token and KV head from HBM; next to it the unpacking, about
-// two instructions a value and lane.
+// Bound: 1.25 d bytes per token and KV head from HBM; next to it the unpacking of the
+// values, whose integer and fp16 instructions issue at half rate.
 #include "packed_attn.cuh"
 
 namespace conduit {
@@ -23,19 +25,26 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kStages = 2;
-constexpr int kTile = 32;  // tokens of a tile
+constexpr int kTile = 32;  // tokens of a tile (2^5)
 constexpr int kBoxBytes(int d) { return kTile * (d + d / 4); }
 
 __device__ __forceinline__ uint32_t h2u(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
 __device__ __forceinline__ __half2 u2h(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
 
-// Codes of two nibbles as fp16: bits 0-3 and 16-19 (lo) or 4-7 and 20-23 (hi) of w.
-// 0x6400 | n is 1024 + n (or 1024 + 16 n), so one fp16 instruction gives n - 8 exactly.
+// Two nibbles u of w as fp16: 1024 + u of bits 0-3 and 16-19, 1024 + 16 u of bits 4-7 and 20-23.
+__device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t mask) {  // (w & mask) | 0x64006400
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(w), "r"(mask), "r"(0x64006400u));
+  return y;
+}
+__device__ __forceinline__ uint32_t raw_lo(uint32_t w) { return masked(w, 0x000F000Fu); }
+__device__ __forceinline__ uint32_t raw_hi(uint32_t w) { return masked(w, 0x00F000F0u); }
+// The same as u - 8, exactly.
 __device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
-  return h2u(__hadd2(u2h((w & 0x000F000Fu) | 0x64006400u), __float2half2_rn(-1032.f)));
+  return h2u(__hadd2(u2h(raw_lo(w)), __float2half2_rn(-1032.f)));
 }
 __device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
-  return h2u(__hfma2(u2h((w & 0x00F000F0u) | 0x64006400u), __float2half2_rn(0.0625f), __float2half2_rn(-72.f)));
+  return h2u(__hfma2(u2h(raw_hi(w)), __float2half2_rn(0.0625f), __float2half2_rn(-72.f)));
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -44,6 +53,15 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The same from zero, without registers for it.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
@@ -96,6 +114,155 @@ __device__ __forceinline__ bool finite_pair(uint32_t p) {
   return (p & 0x7C00u) != 0x7C00u && (p & 0x7C000000u) != 0x7C000000u;
 }
 
+// The mids of groups 2 (c & 1) and + 1 of a token's parameters.
+template <int NG>
+__device__ __forceinline__ uint32_t mids(const uint8_t* p, int c) {
+  static_assert(NG <= 4, "two lanes hold the groups");
+  if constexpr (NG == 4) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p + 8 * (c & 1));
+    return __byte_perm(w.x, w.y, 0x7632);
+  } else {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+    uint32_t y = __byte_perm(w[0], w[1], 0x7632);
+    if (c & 1) y = NG == 3 ? w[NG - 1] >> 16 : 0;
+    return y;
+  }
+}
+
+// State of a warp's running softmax for the two columns of a lane.
+template <int NG>
+struct Running {
+  float ref[2], sum[2];  // reference exponent (log2 units), sum of weights of this lane's tokens
+  float o[2 * NG][4];    // dims 32 g + 4 q + {0, 1} and {2, 3} of both columns in o[2 g], o[2 g + 1]
+};
+
+// The weights' reference moves only when a logit passes it by more than this (log2
+// units): weights stay below 2^8, which fp16 and the fp32 sums hold as well as 1.
+constexpr float kSlack = 8.f;
+
+// One tile of 32 tokens. kEdge: some column does not see all of it.
+template <int NG, bool kEdge>
+__device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, const uint32_t (&bq)[NG][4],
+                                          uint32_t qsum, const float (&qoff)[NG][2],
+                                          const float (&to_log2)[2], int kb, int k1, int least, const int (&lim)[2], int c, int q, int key_lo) {
+  constexpr int D = NG * 32;
+  const uint8_t *kc = box, *vc = box + kTile * (D / 2), *kp = box + kTile * D, *vp = kp + kTile * (D / 8);
+  float x[2][4];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int lo = 16 * t + key_lo, hi = lo + 8;
+    uint32_t wl[NG], wh[NG], pl[NG], ph[NG];
+    load_words<NG>(kc + lo * (D / 2) + c * (D / 8), wl);
+    load_words<NG>(kc + hi * (D / 2) + c * (D / 8), wh);
+    load_words<NG>(kp + lo * (D / 8), pl);
+    load_words<NG>(kp + hi * (D / 8), ph);
+    // sum_g m_tg (sum q): one product over the groups, the query sums in two fp16 parts
+    mma_f16_first(x[t], mids<NG>(kp + lo * (D / 8), c), mids<NG>(kp + hi * (D / 8), c), 0, 0, qsum, 0);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      float acc[4];
+      mma_f16_first(acc, raw_lo(wl[g]), raw_lo(wh[g]), raw_hi(wl[g]), raw_hi(wh[g]), bq[g][0], bq[g][1]);
+      const uint32_t l8 = wl[g] >> 8, h8 = wh[g] >> 8;
+      mma_f16(acc, raw_lo(l8), raw_lo(h8), raw_hi(l8), raw_hi(h8), bq[g][2], bq[g][3]);
+      const float sl = __low2float(u2h(pl[g])), sh = __low2float(u2h(ph[g]));
+      x[t][0] = fmaf(sl, acc[0] - qoff[g][0], x[t][0]);
+      x[t][1] = fmaf(sl, acc[1] - qoff[g][1], x[t][1]);
+      x[t][2] = fmaf(sh, acc[2] - qoff[g][0], x[t][2]);
+      x[t][3] = fmaf(sh, acc[3] - qoff[g][1], x[t][3]);
+    }
+    if (kEdge) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (kb + (e < 2 ? lo : hi) >= lim[e & 1]) x[t][e] = -INFINITY;
+    }
+  }
+  float top[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    top[e] = fmaxf(fmaxf(x[0][e], x[0][e + 2]), fmaxf(x[1][e], x[1][e + 2])) * to_log2[e];
+  if (__any_sync(0xffffffffu, top[0] > st.ref[0] + kSlack || top[1] > st.ref[1] + kSlack)) {
+    float corr[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int s = 4; s < 32; s <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], s));
+      const float moved = fmaxf(st.ref[e], top[e]);
+      corr[e] = moved == -INFINITY ? 1.f : tc::ex2(st.ref[e] - moved);
+      st.ref[e] = moved;
+      st.sum[e] *= corr[e];
+    }
+#pragma unroll
+    for (int t = 0; t < 2 * NG; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st.o[t][e] *= corr[e & 1];
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const float base = kEdge && st.ref[e] == -INFINITY ? 0.f : st.ref[e];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      x[t][e] = tc::ex2(fmaf(x[t][e], to_log2[e], -base));
+      x[t][e + 2] = tc::ex2(fmaf(x[t][e + 2], to_log2[e], -base));
+      st.sum[e] += x[t][e] + x[t][e + 2];
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint32_t b0 = transpose8x8(h2u(__floats2half2_rn(x[t][0], x[t][1])));
+    const uint32_t b1 = transpose8x8(h2u(__floats2half2_rn(x[t][2], x[t][3])));
+    // tokens of this lane's operand slots 2 c, 2 c + 1, and eight on
+    uint32_t v[4][(NG + 1) / 2], p[4][NG];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int key = 16 * t + (e & 1 ? (4 + c) ^ 1 : c) + (e & 2 ? 8 : 0);
+      load_halves<NG>(vc + key * (D / 2) + q * (D / 16), v[e]);
+      load_words<NG>(vp + key * (D / 8), p[e]);
+      if (kEdge) {
+        // tokens that some column does not see: their weight there is 0, and 0 times NaN must not be
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+          if (kb + key >= k1 || (kb + key >= least && !finite_pair(p[e][g]))) p[e][g] = 0;
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const uint32_t pick = g & 1 ? 0x7632u : 0x5410u;
+      const uint32_t xl = __byte_perm(v[0][g / 2], v[1][g / 2], pick), xh = __byte_perm(v[2][g / 2], v[3][g / 2], pick);
+      const __half2 sl = u2h(__byte_perm(p[0][g], p[1][g], 0x5410)), ml = u2h(__byte_perm(p[0][g], p[1][g], 0x7632));
+      const __half2 sh = u2h(__byte_perm(p[2][g], p[3][g], 0x5410)), mh = u2h(__byte_perm(p[2][g], p[3][g], 0x7632));
+      auto value = [](uint32_t code, __half2 s, __half2 mid) { return h2u(__hfma2(s, u2h(code), mid)); };
+      mma_f16(st.o[2 * g], value(codes_lo(xl), sl, ml), value(codes_hi(xl), sl, ml), value(codes_lo(xh), sh, mh),
+              value(codes_hi(xh), sh, mh), b0, b1);
+      const uint32_t yl = xl >> 8, yh = xh >> 8;
+      mma_f16(st.o[2 * g + 1], value(codes_lo(yl), sl, ml), value(codes_hi(yl), sl, ml), value(codes_lo(yh), sh, mh),
+              value(codes_hi(yh), sh, mh), b0, b1);
+    }
+  }
+  if (kEdge) {
+    // a value that is not finite makes the outputs of the columns that see it NaN
+    uint32_t poison = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int key = 8 * t + key_lo;
+      uint32_t p[NG];
+      load_words<NG>(vp + key * (D / 8), p);
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (kb + key < min(lim[e], k1) && !finite_pair(p[g])) poison |= 1u << (2 * g + e);
+    }
+    poison = __reduce_or_sync(0x11111111u << c, poison);
+    if (poison) {
+#pragma unroll
+      for (int t = 0; t < 2 * NG; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (poison >> (2 * (t / 2) + (e & 1)) & 1u) st.o[t][e] = NAN;
+    }
+  }
+}
+
 template <int NG>
 __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   constexpr int D = NG * 32, kBox = kBoxBytes(D);
@@ -105,8 +272,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   if (!item_of(a, &it)) return;
   const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int c = lane & 3, q = lane >> 2;
-  // a row of the logits' accumulator is the token row_of(lane / 4) of its half tile; with
-  // this order the value loads of a warp touch two banks' halves evenly
+  // a row of the logits' accumulator is the token key_lo (+ 8) of its half tile; with this
+  // order the value loads of a warp are spread evenly over the banks
   const int key_lo = (q & 1) ? (4 + (q >> 1)) ^ 1 : q >> 1;
 
   // keys that this lane's two columns see; columns past the last see all (their result is dropped)
@@ -135,31 +302,42 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   }
   __syncwarp();
 
-  const int run = min(kTile, 1 << a.kv.page_shift);  // tokens of a tile that lie in one page
-  auto fill = [&](int stage, int tile) {
-    const int kb = k0 + tile * kTile;
-    const int runs = (min(k1 - kb, kTile) + run - 1) / run;
-    if (lane == 0) tc::mbar_arrive_expect_tx(&full[w][stage], uint32_t(runs * run * (D + D / 4)));
+  // A lane copies one part (K codes, V codes, K and V parameters) of one run, the tokens of
+  // a tile that lie in one page.
+  const int run_shift = min(5, a.kv.page_shift), run = 1 << run_shift;
+  const int part = lane & 3, at_tile = (lane >> 2) << run_shift;
+  const int row_bytes = part < 2 ? D / 2 : D / 8;
+  const uint32_t dst = tc::smem_u32(ring) + (part < 2 ? part * kTile * (D / 2) : kTile * D + (part - 2) * kTile * (D / 8)) +
+                       at_tile * row_bytes;
+  const uint8_t* from = a.kv.page(it.l, it.g, 0) + (part < 2 ? a.kv.codes(part, 0) : a.kv.params(part - 2, 0));
+  const int64_t page_stride = a.kv.Hkv * a.kv.page_bytes;
+  // the page of this lane's run in a tile, looked up one fill ahead
+  auto page_in = [&](int n) {
+    const int j = k0 + (w + n * kWarps) * kTile + at_tile;
+    return n < mine && j < k1 && at_tile < kTile ? page_of(a, it.r, j) : 0;
+  };
+  int next_page = page_in(0);
+  auto fill = [&](int n) {
+    const int stage = n % kStages, kb = k0 + (w + n * kWarps) * kTile;
+    const int runs = (min(k1 - kb, kTile) + run - 1) >> run_shift;
+    if (lane == 0) tc::mbar_arrive_expect_tx(&full[w][stage], uint32_t((runs << run_shift) * (D + D / 4)));
     __syncwarp();
     if (lane < 4 * runs) {
-      const int part = lane & 3, j = kb + (lane >> 2) * run, row = j & ((1 << a.kv.page_shift) - 1);
-      const uint8_t* at = a.kv.page(it.l, it.g, page_of(a, it.r, j));
-      const uint32_t base = tc::smem_u32(ring + stage * kBox);
-      const int at_tile = (lane >> 2) * run;
-      if (part < 2)
-        bulk_load(base + (part * kTile + at_tile) * (D / 2), at + a.kv.codes(part, row), run * (D / 2), &full[w][stage]);
-      else
-        bulk_load(base + kTile * D + ((part - 2) * kTile + at_tile) * (D / 8), at + a.kv.params(part - 2, row),
-                  run * (D / 8), &full[w][stage]);
+      const int j = kb + at_tile, row = j & ((1 << a.kv.page_shift) - 1);
+      bulk_load(dst + stage * kBox, from + next_page * page_stride + row * row_bytes, row_bytes << run_shift,
+                &full[w][stage]);
     }
+    next_page = page_in(n + 1);
   };
 #pragma unroll
   for (int s = 0; s < kStages; ++s)
-    if (s < mine) fill(s, w + s * kWarps);
+    if (s < mine) fill(s);
 
-  // Queries of column q (operand layout), scaled to [256, 512) at most by 2^-shift.
+  // Queries of column q in the operand layout, scaled by 2^-shift so that the largest lies in
+  // [256, 512): exact in fp16 down to 2^-22 of it. Odd dims meet 16 u and are divided by 16.
   uint32_t bq[NG][4];
-  float qsum[NG][2], to_log2[2];
+  uint32_t qsum = 0;
+  float qoff[NG][2], to_log2[2];
   {
     const int j = it.cb * kCols + q;
     float x[NG][8], top = 0.f;
@@ -190,164 +368,60 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     int shift = int(__float_as_uint(top) >> 23) - 127 - 8;  // top < 2^(shift + 9)
     if (!(top < INFINITY) || top == 0.f) shift = 0;
-    // 2^-shift in two factors, each a normal number
+    // 2^-shift and 2^shift in two factors, each a normal number
     const float f1 = __uint_as_float(uint32_t(127 - shift / 2) << 23);
     const float f2 = __uint_as_float(uint32_t(127 - (shift - shift / 2)) << 23);
     const float g1 = __uint_as_float(uint32_t(127 + shift / 2) << 23);
     const float g2 = __uint_as_float(uint32_t(127 + (shift - shift / 2)) << 23);
-    const float back = a.scale * kLog2e * g1 * g2;
-    float part[NG];
+    // positive, so that a masked logit stays -inf under it
+    const float back = fmaxf(a.scale * kLog2e * g1 * g2, 1.1754944e-38f);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) to_log2[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e));
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      part[g] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[g][e] = x[g][e] * f1 * f2;
-        part[g] += x[g][e];
+      for (int e = 0; e < 8; ++e) x[g][e] = x[g][e] * f1 * f2;
+      float even = (x[g][0] + x[g][2]) + (x[g][4] + x[g][6]), odd = (x[g][1] + x[g][3]) + (x[g][5] + x[g][7]);
+#pragma unroll
+      for (int s = 1; s < 4; s <<= 1) {
+        even += __shfl_xor_sync(0xffffffffu, even, s);
+        odd += __shfl_xor_sync(0xffffffffu, odd, s);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) bq[g][e] = h2u(__floats2half2_rn(x[g][e], x[g][e + 4]));
-      part[g] += __shfl_xor_sync(0xffffffffu, part[g], 1);
-      part[g] += __shfl_xor_sync(0xffffffffu, part[g], 2);
-    }
+      for (int e = 0; e < 4; ++e) {  // word e: dims e and e + 4
+        const float f = e & 1 ? 0.0625f : 1.f;
+        bq[g][e] = h2u(__floats2half2_rn(x[g][e] * f, x[g][e + 4] * f));
+      }
+      const float off = 1032.f * even + 72.f * odd;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      to_log2[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e));
-#pragma unroll
-      for (int g = 0; g < NG; ++g) qsum[g][e] = __shfl_sync(0xffffffffu, part[g], 4 * (2 * c + e));
+      for (int e = 0; e < 2; ++e) qoff[g][e] = __shfl_sync(0xffffffffu, off, 4 * (2 * c + e));
+      // slots 2 c, 2 c + 1 of the product with the mids: groups 0, 1, 2, 3, then the same in a second part
+      const float total = even + odd, first = __half2float(__float2half_rn(total));
+      if (g / 2 == (c & 1))
+        qsum |= uint32_t(__half_as_ushort(__float2half_rn(c < 2 ? first : total - first))) << (16 * (g & 1));
     }
   }
 
-  float m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-  float o[2 * NG][4];
+  Running<NG> st;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) st.ref[e] = -INFINITY, st.sum[e] = 0.f;
 #pragma unroll
   for (int t = 0; t < 2 * NG; ++t)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[t][e] = 0.f;
+    for (int e = 0; e < 4; ++e) st.o[t][e] = 0.f;
 
   bool ok = true;
-  for (int n = 0; n < mine && ok; ++n) {
+  for (int n = 0; n < mine; ++n) {
     const int stage = n % kStages, kb = k0 + (w + n * kWarps) * kTile;
-    if (!tc::mbar_wait(&full[w][stage], uint32_t(n / kStages) & 1u)) {
-      ok = false;
-      break;
-    }
+    ok = tc::mbar_wait(&full[w][stage], uint32_t(n / kStages) & 1u);
+    if (!ok) break;
     const uint8_t* box = ring + stage * kBox;
-    const uint8_t *kc = box, *vc = box + kTile * (D / 2), *kp = box + kTile * D, *vp = kp + kTile * (D / 8);
-    const bool edge = kb + kTile > least;  // some column does not see the whole tile
-
-    float x[2][4];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int lo = 16 * t + key_lo, hi = lo + 8;
-      uint32_t wl[NG], wh[NG], pl[NG], ph[NG];
-      load_words<NG>(kc + lo * (D / 2) + c * (D / 8), wl);
-      load_words<NG>(kc + hi * (D / 2) + c * (D / 8), wh);
-      load_words<NG>(kp + lo * (D / 8), pl);
-      load_words<NG>(kp + hi * (D / 8), ph);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[t][e] = 0.f;
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        mma_f16(acc, codes_lo(wl[g]), codes_lo(wh[g]), codes_hi(wl[g]), codes_hi(wh[g]), bq[g][0], bq[g][1]);
-        const uint32_t l8 = wl[g] >> 8, h8 = wh[g] >> 8;
-        mma_f16(acc, codes_lo(l8), codes_lo(h8), codes_hi(l8), codes_hi(h8), bq[g][2], bq[g][3]);
-        const float2 fl = __half22float2(u2h(pl[g])), fh = __half22float2(u2h(ph[g]));
-        x[t][0] = fmaf(fl.x, acc[0], fmaf(fl.y, qsum[g][0], x[t][0]));
-        x[t][1] = fmaf(fl.x, acc[1], fmaf(fl.y, qsum[g][1], x[t][1]));
-        x[t][2] = fmaf(fh.x, acc[2], fmaf(fh.y, qsum[g][0], x[t][2]));
-        x[t][3] = fmaf(fh.x, acc[3], fmaf(fh.y, qsum[g][1], x[t][3]));
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[t][e] *= to_log2[e & 1];
-        if (edge && kb + (e < 2 ? lo : hi) >= lim[e & 1]) x[t][e] = -INFINITY;
-      }
-    }
-    float corr[2];
-    bool moved = false;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float top = fmaxf(fmaxf(x[0][e], x[0][e + 2]), fmaxf(x[1][e], x[1][e + 2]));
-#pragma unroll
-      for (int s = 4; s < 32; s <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-      const float mn = fmaxf(m[e], top), base = mn == -INFINITY ? 0.f : mn;
-      corr[e] = tc::ex2(m[e] - base);
-      moved |= mn != m[e];
-      m[e] = mn;
-      sum[e] *= corr[e];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        x[t][e] = tc::ex2(x[t][e] - base);
-        x[t][e + 2] = tc::ex2(x[t][e + 2] - base);
-        sum[e] += x[t][e] + x[t][e + 2];
-      }
-    }
-    if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-      for (int t = 0; t < 2 * NG; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[t][e] *= corr[e & 1];
-    }
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint32_t b0 = transpose8x8(h2u(__floats2half2_rn(x[t][0], x[t][1])));
-      const uint32_t b1 = transpose8x8(h2u(__floats2half2_rn(x[t][2], x[t][3])));
-      // tokens of this lane's operand slots 2 c, 2 c + 1, and eight on
-      uint32_t v[4][(NG + 1) / 2], p[4][NG];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = 16 * t + (e & 1 ? (4 + c) ^ 1 : c) + (e & 2 ? 8 : 0);
-        load_halves<NG>(vc + key * (D / 2) + q * (D / 16), v[e]);
-        load_words<NG>(vp + key * (D / 8), p[e]);
-        if (edge) {
-          // tokens that some column does not see: their weight there is 0, and 0 times NaN must not be
-#pragma unroll
-          for (int g = 0; g < NG; ++g)
-            if (kb + key >= k1 || (kb + key >= least && !finite_pair(p[e][g]))) p[e][g] = 0;
-        }
-      }
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const uint32_t pick = g & 1 ? 0x7632u : 0x5410u;
-        const uint32_t xl = __byte_perm(v[0][g / 2], v[1][g / 2], pick), xh = __byte_perm(v[2][g / 2], v[3][g / 2], pick);
-        const __half2 sl = u2h(__byte_perm(p[0][g], p[1][g], 0x5410)), ml = u2h(__byte_perm(p[0][g], p[1][g], 0x7632));
-        const __half2 sh = u2h(__byte_perm(p[2][g], p[3][g], 0x5410)), mh = u2h(__byte_perm(p[2][g], p[3][g], 0x7632));
-        auto value = [](uint32_t code, __half2 s, __half2 mid) { return h2u(__hfma2(s, u2h(code), mid)); };
-        mma_f16(o[2 * g], value(codes_lo(xl), sl, ml), value(codes_hi(xl), sl, ml), value(codes_lo(xh), sh, mh),
-                value(codes_hi(xh), sh, mh), b0, b1);
-        const uint32_t yl = xl >> 8, yh = xh >> 8;
-        mma_f16(o[2 * g + 1], value(codes_lo(yl), sl, ml), value(codes_hi(yl), sl, ml), value(codes_lo(yh), sh, mh),
-                value(codes_hi(yh), sh, mh), b0, b1);
-      }
-    }
-    if (edge) {
-      // a value that is not finite makes the outputs of the columns that see it NaN
-      uint32_t poison = 0;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int key = 8 * t + key_lo;
-        uint32_t p[NG];
-        load_words<NG>(vp + key * (D / 8), p);
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (kb + key < min(lim[e], k1) && !finite_pair(p[g])) poison |= 1u << (2 * g + e);
-      }
-#pragma unroll
-      for (int s = 4; s < 32; s <<= 1) poison |= __shfl_xor_sync(0xffffffffu, poison, s);
-      if (poison) {
-#pragma unroll
-        for (int t = 0; t < 2 * NG; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (poison >> (2 * (t / 2) + (e & 1)) & 1u) o[t][e] = NAN;
-      }
-    }
+    if (kb + kTile > least)
+      tile_step<NG, true>(st, box, bq, qsum, qoff, to_log2, kb, k1, least, lim, c, q, key_lo);
+    else
+      tile_step<NG, false>(st, box, bq, qsum, qoff, to_log2, kb, k1, least, lim, c, q, key_lo);
     __syncwarp();
-    if (n + kStages < mine) fill(stage, w + (n + kStages) * kWarps);
+    if (n + kStages < mine) fill(n + kStages);
   }
   if (!ok) {  // bounded waits for the copies that are still under way
     flag_status(a.status, CONDUIT_FLAG_TIMEOUT | CONDUIT_SITE_LOAD);
@@ -358,20 +432,20 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
 #pragma unroll
   for (int e = 0; e < 2; ++e)
 #pragma unroll
-    for (int s = 4; s < 32; s <<= 1) sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], s);
+    for (int s = 4; s < 32; s <<= 1) st.sum[e] += __shfl_xor_sync(0xffffffffu, st.sum[e], s);
   __syncthreads();
   constexpr int kRow = D + 4;
   float* ow = reinterpret_cast<float*>(smem);          // [warps][columns][kRow]
-  float2* st = reinterpret_cast<float2*>(ow + kWarps * kCols * kRow);  // [warps][columns] (M, sum)
+  float2* ml = reinterpret_cast<float2*>(ow + kWarps * kCols * kRow);  // [warps][columns] (reference, sum)
   static_assert(kWarps * kCols * (kRow * 4 + 8) <= kWarps * kStages * kBox, "the join fits the ring");
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int col = 2 * c + e;
-    if (q == 0) st[w * kCols + col] = make_float2(m[e], sum[e]);
+    if (q == 0) ml[w * kCols + col] = make_float2(st.ref[e], st.sum[e]);
 #pragma unroll
     for (int g = 0; g < NG; ++g)
       *reinterpret_cast<float4*>(ow + (w * kCols + col) * kRow + 32 * g + 4 * q) =
-          make_float4(o[2 * g][e], o[2 * g][e + 2], o[2 * g + 1][e], o[2 * g + 1][e + 2]);
+          make_float4(st.o[2 * g][e], st.o[2 * g][e + 2], st.o[2 * g + 1][e], st.o[2 * g + 1][e + 2]);
   }
   __syncthreads();
   for (int e = threadIdx.x; e < kCols * D; e += kWarps * 32) {
@@ -379,12 +453,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     if (j >= it.n * a.kv.G) break;
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) top = fmaxf(top, st[i * kCols + col].x);
+    for (int i = 0; i < kWarps; ++i) top = fmaxf(top, ml[i * kCols + col].x);
     const float base = top == -INFINITY ? 0.f : top;
     float total = 0.f, out = 0.f;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
-      const float2 s = st[i * kCols + col];
+      const float2 s = ml[i * kCols + col];
       const float wgt = tc::ex2(s.x - base);
       total = fmaf(wgt, s.y, total);
       out = fmaf(wgt, ow[(i * kCols + col) * kRow + dd], out);
