@@ -4,6 +4,8 @@
 // Mathematics: y1 = x1 c - x2 s, y2 = x2 c + x1 s for each pair, in fp32, rounded
 // once. Bound: every row is read once and written once; the cosines of a row
 // (8 bytes a pair) are shared by all of its heads.
+#include <algorithm>
+
 #include "rotate.cuh"
 
 namespace conduit {
@@ -19,7 +21,7 @@ struct AppendArgs {
 // A thread owns a unit (VEC pairs) of a row and walks over heads hg, hg + HG, ...
 // Heads count q, then (append) k, then v.
 template <typename T, int VEC, bool kAppend>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
     rotate_kernel(RopeDev rope, AppendArgs ap, int T_rows, int nq, int d, int HG, RowsDev x, RowsDev out, RowsDev k,
                   RowsDev v, int32_t* status) {
   using C = Chunk<T, VEC>;
@@ -30,55 +32,54 @@ __global__ void __launch_bounds__(kThreads)
   const int i = int(rest / uint32_t(HG)), hg = int(rest % uint32_t(HG));
   const int r = blockIdx.y, l = blockIdx.z;
   int64_t t = i, slot_off = 0;
+  int slot = 0, pos[CONDUIT_MAX_AXES];
   bool ok = true;
+  // Loads that do not wait for one another go out together: a row's length, then its
+  // positions and its page, then its cosines and the first head.
   if (kAppend) {
-    const int t0 = ap.s.row_off[r], n = ap.s.row_off[r + 1] - t0;
-    if (i >= n) return;
+    const int t0 = ap.s.row_off[r], t1 = ap.s.row_off[r + 1], len = ap.s.len[r];
+    if (i >= t1 - t0) return;
     t = t0 + i;
-    const int len = ap.s.len[r], slot = len - n + i;
-    ok = slot >= 0 && slot < ap.s.max_len && slot / ap.kv.page_size < ap.kv.max_pages;
-    if (ok) {
-      const int page = ap.kv.page_table[int64_t(r) * ap.kv.max_pages + slot / ap.kv.page_size];
-      ok = page >= 0 && page < ap.kv.num_pages;
-      slot_off = ((int64_t(l) * ap.kv.num_pages + page) * ap.kv.Hkv * ap.kv.page_size + slot % ap.kv.page_size) * d;
-    }
+    slot = len - (t1 - t0) + i;
+    const int in_req = slot / ap.kv.page_size;
+    ok = slot >= 0 && slot < ap.s.max_len && in_req < ap.kv.max_pages;
+    const int page = ap.kv.page_table[int64_t(r) * ap.kv.max_pages + (ok ? in_req : 0)];
+    ok &= page >= 0 && page < ap.kv.num_pages;
+    slot_off = ((int64_t(l) * ap.kv.num_pages + page) * ap.kv.Hkv * ap.kv.page_size + slot % ap.kv.page_size) * d;
   } else if (i >= T_rows) {
     return;
   }
-  const Unit un = unit_of<VEC>(rope, u);
-  float2 cs[VEC];
-  if (rope.rot && ok) {
-    // a unit that only copies checks the positions too: a row is written whole or not at all
-    ok = load_turn<VEC>(rope, t, un.turns ? u * VEC : 0, cs);
-  }
-  if (!ok) {
+  const Unit un = unit_of<VEC>(rope, d, u);
+  const int Hkv = kAppend ? ap.kv.Hkv : 0, H = nq + 2 * Hkv;
+  C a, b;
+  auto load = [&](int h) {
+    const bool is_q = h < nq, is_k = h < nq + Hkv;
+    const RowsDev& from = is_q ? x : is_k ? k : v;
+    const T* src = static_cast<const T*>(from.p) + l * from.ls + t * from.rs + (is_q ? h : is_k ? h - nq : h - nq - Hkv) * from.hs;
+    a = *reinterpret_cast<const C*>(src + un.a);
+    if (un.b >= 0) b = *reinterpret_cast<const C*>(src + un.b);
+  };
+  if (rope.rot) ok &= load_positions(rope, t, pos);
+  load(hg);
+  if (!ok) {  // the row is left out, in all of its parts
     if (u == 0 && hg == 0) flag_status(status, CONDUIT_FLAG_INDEX);
     return;
   }
-  const int Hkv = kAppend ? ap.kv.Hkv : 0, H = nq + 2 * Hkv;
-#pragma unroll 4
+  float2 cs[VEC];
+  if (un.turns) load_turn<VEC>(rope, pos, u * VEC, cs);
   for (int h = hg; h < H; h += HG) {
-    const T* src;
+    C y = a, z = b;
+    if (h + HG < H) load(h + HG);
+    if (un.turns && h < nq + Hkv) turn_chunks<T, VEC>(rope, cs, y, z);
     T* dst;
-    bool turns = un.turns;
-    if (h < nq) {
-      src = static_cast<const T*>(x.p) + l * x.ls + t * x.rs + h * x.hs;
+    if (h < nq)
       dst = static_cast<T*>(out.p) + l * out.ls + t * out.rs + h * out.hs;
-    } else {
-      const bool is_v = h >= nq + Hkv;
-      const int g = is_v ? h - nq - Hkv : h - nq;
-      const RowsDev& from = is_v ? v : k;
-      src = static_cast<const T*>(from.p) + l * from.ls + t * from.rs + g * from.hs;
-      dst = static_cast<T*>(is_v ? ap.kv.v : ap.kv.k) + slot_off + int64_t(g) * ap.kv.page_size * d;
-      turns &= !is_v;
-    }
-    C a = *reinterpret_cast<const C*>(src + un.a);
-    if (un.turns) {
-      C b = *reinterpret_cast<const C*>(src + un.b);
-      if (turns) turn_chunks<T, VEC>(rope, cs, a, b);
-      *reinterpret_cast<C*>(dst + un.b) = b;
-    }
-    *reinterpret_cast<C*>(dst + un.a) = a;
+    else if (h < nq + Hkv)
+      dst = static_cast<T*>(ap.kv.k) + slot_off + int64_t(h - nq) * ap.kv.page_size * d;
+    else
+      dst = static_cast<T*>(ap.kv.v) + slot_off + int64_t(h - nq - Hkv) * ap.kv.page_size * d;
+    *reinterpret_cast<C*>(dst + un.a) = y;
+    if (un.b >= 0) *reinterpret_cast<C*>(dst + un.b) = z;
   }
 }
 
@@ -86,7 +87,10 @@ template <typename T, int VEC, bool kAppend>
 cudaError_t launch(const RopeDev& rope, const AppendArgs& ap, int L, int R, int rows, int nq, int d, const RowsDev& x,
                    const RowsDev& out, const RowsDev& k, const RowsDev& v, int32_t* status, cudaStream_t stream) {
   const int H = nq + (kAppend ? 2 * ap.kv.Hkv : 0), nu = units_per_row<VEC>(rope, d);
-  const int HG = H;
+  // Heads per thread: one while the launch does not fill the SMs twice, then up to 16.
+  const int64_t wide = int64_t(rows) * R * L * H * nu / (2 * 152 * 2048);
+  const int per = int(std::min<int64_t>(16, std::max<int64_t>(1, wide)));
+  const int HG = (H + per - 1) / per;
   const int64_t threads = int64_t(rows) * HG * nu;
   const dim3 grid(unsigned((threads + kThreads - 1) / kThreads), R, L);
   rotate_kernel<T, VEC, kAppend><<<grid, kThreads, 0, stream>>>(rope, ap, rows, nq, d, HG, x, out, k, v, status);

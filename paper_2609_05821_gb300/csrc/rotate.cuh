@@ -11,47 +11,66 @@ struct alignas(sizeof(T) * VEC) Chunk {
   T v[VEC];
 };
 
-// Unit u of a row: u < half / VEC are rotating units with their chunks at `a` and
-// `b`; the others copy the chunk at `a`.
+// Unit u of a row: two chunks of VEC elements at `a` and `b` that rotate, or that pass
+// (the last of those may be one chunk: b < 0).
 struct Unit {
   int a, b;
   bool turns;
 };
 
 template <int VEC>
-__device__ __forceinline__ Unit unit_of(const RopeDev& rope, int u) {
+__device__ __forceinline__ Unit unit_of(const RopeDev& rope, int d, int u) {
   const int nr = rope.half / VEC;
-  if (u >= nr) return Unit{rope.rot + (u - nr) * VEC, 0, false};
+  if (u >= nr) {
+    const int at = rope.rot + (u - nr) * 2 * VEC;
+    return Unit{at, at + VEC < d ? at + VEC : -1, false};
+  }
   if (rope.layout == CONDUIT_ROPE_HALVES) return Unit{u * VEC, rope.half + u * VEC, true};
   return Unit{2 * u * VEC, 2 * u * VEC + VEC, true};
 }
 
 template <int VEC>
 __host__ __device__ __forceinline__ int units_per_row(const RopeDev& rope, int d) {
-  return rope.half / VEC + (d - rope.rot) / VEC;
+  return rope.half / VEC + ((d - rope.rot) / VEC + 1) / 2;
 }
 
-// Cosines and (signed) sines of pairs p0 .. p0 + VEC - 1 for row t; false if one of
-// the positions lies outside of the table.
-template <int VEC>
-__device__ __forceinline__ bool load_turn(const RopeDev& rope, int64_t t, int p0, float2 (&cs)[VEC]) {
-  int pos[CONDUIT_MAX_AXES];
+// The positions of row t on the axes; false if one lies outside of the table.
+__device__ __forceinline__ bool load_positions(const RopeDev& rope, int64_t t, int (&pos)[CONDUIT_MAX_AXES]) {
   bool ok = true;
 #pragma unroll
-  for (int a = 0; a < CONDUIT_MAX_AXES; ++a) {
-    pos[a] = a < rope.axes ? rope.pos[int64_t(a) * rope.T + t] : 0;
-    ok &= pos[a] >= 0 && pos[a] < rope.len;
+  for (int a = 0; a < CONDUIT_MAX_AXES; ++a) pos[a] = a < rope.axes ? rope.pos[int64_t(a) * rope.T + t] : 0;
+#pragma unroll
+  for (int a = 0; a < CONDUIT_MAX_AXES; ++a) ok &= pos[a] >= 0 && (pos[a] < rope.len || a >= rope.axes);
+  return ok;
+}
+
+// Cosines and (signed) sines of pairs p0 .. p0 + VEC - 1 at positions inside the table.
+template <int VEC>
+__device__ __forceinline__ void load_turn(const RopeDev& rope, const int (&pos)[CONDUIT_MAX_AXES], int p0,
+                                          float2 (&cs)[VEC]) {
+  auto row_of = [&](int p) {
+    const int a = (rope.axis[p >> 4] >> (2 * (p & 15))) & 3;
+    return int64_t(a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : pos[3]) * rope.half;
+  };
+  if constexpr (VEC % 4 == 0) {
+    // pairs of one axis (p0 is a multiple of VEC, so they share a word of `axis`) lie side by side in the table
+    const uint32_t axes = (rope.axis[p0 >> 4] >> (2 * (p0 & 15))) & ((1u << (2 * VEC)) - 1);
+    if (axes == (axes & 3) * (0x5555u & ((1u << (2 * VEC)) - 1)) && (rope.half & 1) == 0) {
+      const float4* row = reinterpret_cast<const float4*>(rope.table + row_of(p0) + p0);
+#pragma unroll
+      for (int e = 0; e < VEC / 2; ++e) {
+        const float4 x = row[e];
+        cs[2 * e] = make_float2(x.x, x.y * rope.sign);
+        cs[2 * e + 1] = make_float2(x.z, x.w * rope.sign);
+      }
+      return;
+    }
   }
-  if (!ok) return false;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    const int p = p0 + e;
-    const int a = (rope.axis[p >> 4] >> (2 * (p & 15))) & 3;
-    const int at = a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : pos[3];
-    cs[e] = rope.table[int64_t(at) * rope.half + p];
+    cs[e] = rope.table[row_of(p0 + e) + p0 + e];
     cs[e].y *= rope.sign;
   }
-  return true;
 }
 
 // The products are rounded before they are added: the value of the formula's own
