@@ -8,12 +8,19 @@
 #include <algorithm>
 
 #include "rotate.cuh"
+#include "tc_common.cuh"
 
 namespace conduit {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr float kClip = 61440.f;  // m +- 8 s stays inside fp16
+
+// a + b of products that were rounded before. A packed multiply followed by a packed
+// add comes out as one fused operation; two scalar additions do not merge with it.
+__device__ __forceinline__ float2 add_rounded(float2 a, float2 b) {
+  return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y));
+}
 
 // 8 elements from p as fp32.
 template <typename T>
@@ -93,59 +100,108 @@ __device__ __forceinline__ void turn8(const RopeDev& rope, const T* row, int i0,
       other[e] = i < rope.rot ? to_float(row[j]) : 0.f;
     }
   }
+  if (kPairing == kAnywhere) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (kPairing != kAnywhere || i0 + e < rope.rot)
-      x[e] = __fadd_rn(__fmul_rn(x[e], cs[e].x), __fmul_rn(other[e], cs[e].y));
+    for (int e = 0; e < 8; ++e)
+      if (i0 + e < rope.rot) x[e] = __fadd_rn(__fmul_rn(x[e], cs[e].x), __fmul_rn(other[e], cs[e].y));
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const float2 own = tc::fmul2(make_float2(x[e], x[e + 1]), make_float2(cs[e].x, cs[e + 1].x));
+    const float2 add = tc::fmul2(make_float2(other[e], other[e + 1]), make_float2(cs[e].y, cs[e + 1].y));
+    const float2 y = add_rounded(own, add);
+    x[e] = y.x;
+    x[e + 1] = y.y;
+  }
 }
 
-// Four neighbouring lanes hold a group of 32 dims; returns this lane's eight codes
-// (0..15) as nibbles of a word, and the group's (s, m). Called by whole warps.
-// x is clipped only where some group of the warp needs it.
-__device__ __forceinline__ uint32_t pack8(float (&x)[8], __half2* param, bool* nonfinite) {
-  float lo = x[0], hi = x[0], zero = 0.f;
+// Least and largest of eight values; true if one of them is not finite.
+__device__ __forceinline__ bool range8(const float (&x)[8], float* lo, float* hi) {
+  *lo = fminf(x[0], x[1]);
+  *hi = fmaxf(x[0], x[1]);
+  float2 zero = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    lo = fminf(lo, x[e]);
-    hi = fmaxf(hi, x[e]);
-    zero = fmaf(x[e], 0.f, zero);  // NaN if one of them is not finite
-  }
-  *nonfinite = zero != 0.f;
-  bool nan = false;
-  if (__any_sync(0xffffffffu, zero != 0.f || hi > kClip || lo < -kClip)) {
-    lo = INFINITY;
-    hi = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      nan |= x[e] != x[e];
-      x[e] = fminf(fmaxf(x[e], -kClip), kClip);
-      lo = fminf(lo, x[e]);
-      hi = fmaxf(hi, x[e]);
+  for (int e = 0; e < 8; e += 2) {
+    if (e) {
+      *lo = tc::fmin3(*lo, x[e], x[e + 1]);
+      *hi = tc::fmax3(*hi, x[e], x[e + 1]);
     }
-    int any = nan;
-    any |= __shfl_xor_sync(0xffffffffu, any, 1);
-    any |= __shfl_xor_sync(0xffffffffu, any, 2);
-    nan = any;
+    zero = tc::ffma2(make_float2(x[e], x[e + 1]), make_float2(0.f, 0.f), zero);  // NaN from NaN and infinities
   }
-#pragma unroll
-  for (int o = 1; o < 4; o <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
-  const __half s = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f));
-  const __half m = __float2half_rn(__fadd_rn(lo, 8.f * __half2float(s)));
-  const float sf = __half2float(s), mf = __half2float(m);
-  const float inv = sf > 0.f ? __frcp_rn(sf) : 0.f;
+  return !(zero.x + zero.y == 0.f);
+}
+
+// Codes c + 8 of eight values as nibbles: c = rint((x - m) inv), clamped where `clamp`.
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float m, float inv, bool clamp) {
   uint32_t w = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    // 1.5 x 2^23 + 8 + c, rounded to an integer: its low nibble is c + 8
-    const float c = fminf(fmaxf(__fmul_rn(__fsub_rn(x[e], mf), inv), -8.f), 7.f);
-    const uint32_t bits = __float_as_uint(__fadd_rn(c, 12582920.f));
-    w |= (bits << (4 * e)) & (15u << (4 * e));
+  for (int e = 0; e < 8; e += 2) {
+    float2 c = tc::fmul2(tc::fadd2(make_float2(x[e], x[e + 1]), make_float2(-m, -m)), make_float2(inv, inv));
+    if (clamp) c = make_float2(fminf(fmaxf(c.x, -8.f), 7.f), fminf(fmaxf(c.y, -8.f), 7.f));
+    // 1.5 x 2^23 + 8 + c, rounded to an integer: bits 0x4B400000 + 8 + c, whose upper part is taken off the sum below
+    c = add_rounded(c, make_float2(12582920.f, 12582920.f));
+    w += __float_as_uint(c.x) << (4 * e);
+    w += __float_as_uint(c.y) << (4 * e + 4);
   }
-  *param = nan ? __halves2half2(__float2half_rn(0.f), __float2half_rn(NAN)) : __halves2half2(s, m);
-  return w;
+  constexpr uint32_t kUpper = 0x4B400000u * 0x11111111u;
+  return w - kUpper;
+}
+
+// Four neighbouring lanes hold a group of 32 dims of a key (x) and of a value (y).
+// Returns this lane's eight codes of each and the groups' (s, m); true if one of this
+// lane's values is not finite. Called by whole warps. The lower two lanes of a group
+// work out the key's s and m, the upper two the value's.
+__device__ __forceinline__ bool pack8(float (&x)[8], float (&y)[8], int c, uint32_t* kw, uint32_t* vw, __half2* kp,
+                                      __half2* vp) {
+  constexpr unsigned kAll = 0xffffffffu;
+  float lo[2], hi[2];
+  const bool bad_x = range8(x, &lo[0], &hi[0]), bad_y = range8(y, &lo[1], &hi[1]);
+  const bool bad = bad_x || bad_y;
+  int nan = 0;
+  const bool wild = bad || fmaxf(hi[0], hi[1]) > kClip || fminf(lo[0], lo[1]) < -kClip;
+  if (__any_sync(kAll, wild)) {  // clip and look for NaN only where a group of the warp needs it
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float(&z)[8] = b ? y : x;
+      lo[b] = INFINITY;
+      hi[b] = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        nan |= int(z[e] != z[e]) << b;
+        z[e] = fminf(fmaxf(z[e], -kClip), kClip);
+        lo[b] = fminf(lo[b], z[e]);
+        hi[b] = fmaxf(hi[b], z[e]);
+      }
+    }
+    nan |= __shfl_xor_sync(kAll, nan, 1);
+    nan |= __shfl_xor_sync(kAll, nan, 2);
+  }
+  // one lane of each pair carries the key's range on, the other the value's
+  const bool is_v = c & 2;
+  float l = is_v ? lo[1] : lo[0], h = is_v ? hi[1] : hi[0];
+  l = fminf(l, __shfl_xor_sync(kAll, is_v ? lo[0] : lo[1], 2));
+  h = fmaxf(h, __shfl_xor_sync(kAll, is_v ? hi[0] : hi[1], 2));
+  l = fminf(l, __shfl_xor_sync(kAll, l, 1));
+  h = fmaxf(h, __shfl_xor_sync(kAll, h, 1));
+  const __half s = __float2half_rn(__fmul_rn(__fsub_rn(h, l), 1.f / 15.f));
+  const __half m = __float2half_rn(__fadd_rn(l, 8.f * __half2float(s)));
+  const float sf = __half2float(s), mf = __half2float(m);
+  const float inv = sf > 0.f ? __frcp_rn(sf) : 0.f;
+  // codes leave -8 .. 7 only where the rounding of m is coarse next to s
+  const bool clamp = __any_sync(kAll, !(__fmul_rn(__fsub_rn(l, mf), inv) > -8.5f && __fmul_rn(__fsub_rn(h, mf), inv) < 7.5f));
+  __half2 own = __halves2half2(s, m);
+  uint32_t other = __shfl_xor_sync(kAll, *reinterpret_cast<uint32_t*>(&own), 2);
+  const float inv2 = __shfl_xor_sync(kAll, inv, 2);
+  const __half2 theirs = *reinterpret_cast<__half2*>(&other);
+  *kp = is_v ? theirs : own;
+  *vp = is_v ? own : theirs;
+  *kw = codes8(x, __high2float(*kp), is_v ? inv2 : inv, clamp);
+  *vw = codes8(y, __high2float(*vp), is_v ? inv : inv2, clamp);
+  const __half2 none = __halves2half2(__float2half_rn(0.f), __float2half_rn(NAN));
+  if (nan & 1) *kp = none;
+  if (nan & 2) *vp = none;
+  return bad;
 }
 
 // Blocks below kv_blocks pack keys and values: a thread owns 8 dims of a row's heads hg,
@@ -192,30 +248,31 @@ __global__ void __launch_bounds__(kThreads, 4)
   if (ok) load_turn8<kPairing>(rope, pos, 8 * u, cs);
   const int row = slot & ((1 << kv.page_shift) - 1), groups = kv.d / 32, grp = u / 4, c = u % 4;
   bool bad = false;
+  const T* kr = static_cast<const T*>(k.p) + l * k.ls + t * k.rs + h0 * k.hs;
+  const T* vr = static_cast<const T*>(v.p) + l * v.ls + t * v.rs + h0 * v.hs;
+  uint8_t* at = kv.page(l, h0, page);
   for (int g = h0; g - h0 < kv.Hkv; g += HG) {  // the same count for every thread of a warp
     const bool on = ok && g < kv.Hkv;
     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (on) {
-      const T* kr = static_cast<const T*>(k.p) + l * k.ls + t * k.rs + g * k.hs;
-      const T* vr = static_cast<const T*>(v.p) + l * v.ls + t * v.rs + g * v.hs;
       load8(kr + 8 * u, wide, x);
       load8(vr + 8 * u, wide, y);
       turn8<kPairing>(rope, kr, 8 * u, wide, cs, x);
     }
+    uint32_t kw, vw;
     __half2 kp, vp;
-    bool bad_k, bad_v;
-    const uint32_t kw = pack8(x, &kp, &bad_k), vw = pack8(y, &vp, &bad_v);
-    if (!on) continue;
-    bad |= bad_k || bad_v;
-    uint8_t* at = kv.page(l, g, page);
-    reinterpret_cast<uint32_t*>(at + kv.codes(0, row))[c * groups + grp] = kw;
-    uint16_t* half_words = reinterpret_cast<uint16_t*>(at + kv.codes(1, row));
-    half_words[(2 * c) * groups + grp] = uint16_t(vw);
-    half_words[(2 * c + 1) * groups + grp] = uint16_t(vw >> 16);
-    if (c == 0) {
-      reinterpret_cast<__half2*>(at + kv.params(0, row))[grp] = kp;
-      reinterpret_cast<__half2*>(at + kv.params(1, row))[grp] = vp;
+    const bool wild = pack8(x, y, c, &kw, &vw, &kp, &vp);
+    if (on) {
+      bad |= wild;
+      reinterpret_cast<uint32_t*>(at + kv.codes(0, row))[c * groups + grp] = kw;
+      uint16_t* half_words = reinterpret_cast<uint16_t*>(at + kv.codes(1, row));
+      half_words[(2 * c) * groups + grp] = uint16_t(vw);
+      half_words[(2 * c + 1) * groups + grp] = uint16_t(vw >> 16);
+      if ((c & 1) == 0) reinterpret_cast<__half2*>(at + kv.params(c >> 1, row))[grp] = c ? vp : kp;
     }
+    kr += HG * k.hs;
+    vr += HG * v.hs;
+    at += HG * kv.page_bytes;
   }
   if (bad) flag_status(status, CONDUIT_FLAG_NONFINITE);
 }
@@ -229,10 +286,13 @@ __device__ __forceinline__ void store_values(T* to, uint32_t w, __half2 param) {
   for (int p = 0; p < 8 / N; ++p) {
     Chunk<T, N> y;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      // 2^23 + u
-      const float u = __uint_as_float(((w >> (4 * (p * N + e))) & 15u) | 0x4B000000u);
-      y.v[e] = from_float<T>(fmaf(sm.x, u - 8388616.f, sm.y));
+    for (int e = 0; e < N; e += 2) {
+      const int at = 4 * (p * N + e);  // the nibbles under the exponent of 2^23 are 2^23 + u
+      float2 u = make_float2(__uint_as_float(((w >> at) & 15u) | 0x4B000000u),
+                             __uint_as_float(((w >> (at + 4)) & 15u) | 0x4B000000u));
+      u = tc::ffma2(make_float2(sm.x, sm.x), tc::fadd2(u, make_float2(-8388616.f, -8388616.f)), make_float2(sm.y, sm.y));
+      y.v[e] = from_float<T>(u.x);
+      y.v[e + 1] = from_float<T>(u.y);
     }
     *reinterpret_cast<Chunk<T, N>*>(to + p * N) = y;
   }
