@@ -71,7 +71,10 @@ cudaError_t launch_packed_read(const PackedDev& kv, const int32_t* first, const 
 
 // Attention over the 4-bit cache. A plan says how a call is cut; `scratch` bytes
 // of workspace hold the partial results of `chunks` key chunks.
+enum { kAttnSimt = 0, kAttnMma = 1, kAttnTc = 2 };
 struct PackedAttnPlan {
+  int kernel;     // CUDA cores, warp-level tensor cores, tcgen05
+  int cols;       // columns (rows of the call times query heads of a KV head) per CTA
   int chunk;      // keys per chunk
   int chunks;     // of the longest context
   int64_t items;  // CTAs

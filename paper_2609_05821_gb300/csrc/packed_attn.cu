@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
   extern __shared__ float simt_smem[];
   float *ks = simt_smem, *vs = ks + kSimtKeys * KS, *qs = vs + kSimtKeys * D;
   Item it;
-  if (!item_of(a, &it)) return;
+  if (!item_of<kCols>(a, &it)) return;
   const int tid = threadIdx.x, w = tid / 32, lane = tid % 32;
   for (int e = tid; e < kCols * D; e += 128) {
     const int j = it.cb * kCols + e / D;
@@ -172,9 +172,11 @@ __global__ void __launch_bounds__(kJoin * NG * 8) combine_kernel(AttnArgs a) {
 }
 
 template <typename T, int NG>
-cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, bool mma, cudaStream_t stream) {
+cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
   cudaError_t err;
-  if (mma) {
+  if (plan.kernel == kAttnTc) {
+    err = launch_packed_attn_tc(a, plan.items, stream);
+  } else if (plan.kernel == kAttnMma) {
     err = launch_packed_attn_mma(a, plan.items, stream);
   } else {
     constexpr int kSmem = simt_smem_bytes(NG * 32);
@@ -192,21 +194,21 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, bool mma, c
 }
 
 template <typename T>
-cudaError_t launch_t(const AttnArgs& a, const PackedAttnPlan& plan, bool mma, cudaStream_t stream) {
+cudaError_t launch_t(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
   switch (a.kv.d / 32) {
-    case 1: return launch_ng<T, 1>(a, plan, mma, stream);
-    case 2: return launch_ng<T, 2>(a, plan, mma, stream);
-    case 3: return launch_ng<T, 3>(a, plan, mma, stream);
-    case 4: return launch_ng<T, 4>(a, plan, mma, stream);
-    case 5: return launch_ng<T, 5>(a, plan, mma, stream);
-    case 6: return launch_ng<T, 6>(a, plan, mma, stream);
-    case 7: return launch_ng<T, 7>(a, plan, mma, stream);
-    default: return launch_ng<T, 8>(a, plan, mma, stream);
+    case 1: return launch_ng<T, 1>(a, plan, stream);
+    case 2: return launch_ng<T, 2>(a, plan, stream);
+    case 3: return launch_ng<T, 3>(a, plan, stream);
+    case 4: return launch_ng<T, 4>(a, plan, stream);
+    case 5: return launch_ng<T, 5>(a, plan, stream);
+    case 6: return launch_ng<T, 6>(a, plan, stream);
+    case 7: return launch_ng<T, 7>(a, plan, stream);
+    default: return launch_ng<T, 8>(a, plan, stream);
   }
 }
 
-int64_t items_of(const PackedDev& kv, const SeqsDev& s, int chunks) {
-  const int64_t blocks = (int64_t(s.max_rows) * kv.G + kCols - 1) / kCols;
+int64_t items_of(const PackedDev& kv, const SeqsDev& s, int cols, int chunks) {
+  const int64_t blocks = (int64_t(s.max_rows) * kv.G + cols - 1) / cols;
   return int64_t(kv.L) * s.R * kv.Hkv * blocks * chunks;
 }
 
@@ -217,19 +219,25 @@ size_t stats_bytes(const PackedDev& kv, const SeqsDev& s, int chunks) {
 
 }  // namespace
 
+#ifndef TC_FROM
+#define TC_FROM 16
+#endif
 PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype) {
   PackedAttnPlan p{};
   const int most = int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
-  // An SM holds two CTAs. One request: one wave of equal chunks. More: four CTAs for each
-  // place, so that contexts of unequal lengths fill it. At least 256 keys each.
-  const int64_t items = std::max<int64_t>(1, items_of(kv, s, 1)), places = 2 * 152;
+  const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
+  p.kernel = !mma ? kAttnSimt : int64_t(s.max_rows) * kv.G > TC_FROM ? kAttnTc : kAttnMma;
+  p.cols = p.kernel == kAttnTc ? 256 : kCols;
+  // An SM holds two CTAs (tcgen05: one). One request: one wave of equal chunks. More: four
+  // CTAs for each place, so that contexts of unequal lengths fill it. At least 256 keys each.
+  const int64_t items = std::max<int64_t>(1, items_of(kv, s, p.cols, 1)), places = p.kernel == kAttnTc ? 152 : 2 * 152;
   const int64_t even = s.R == 1 ? places / items : (4 * places + items - 1) / items;
   const int64_t want = std::min<int64_t>(even, (most + 255) / 256);
   p.chunks = int(std::max<int64_t>(1, want));
   p.chunk = std::max(256, (most + p.chunks - 1) / p.chunks);
   p.chunk = (p.chunk + 255) / 256 * 256;
   p.chunks = std::max(1, (most + p.chunk - 1) / p.chunk);
-  p.items = items_of(kv, s, p.chunks);
+  p.items = items_of(kv, s, p.cols, p.chunks);
   if (p.chunks > 1)
     p.scratch = stats_bytes(kv, s, p.chunks) + size_t(p.chunks) * kv.L * s.T * kv.Hq * size_t(kv.d) * sizeof(float);
   return p;
@@ -239,11 +247,10 @@ cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const Pack
                                const RowsDev& q, float scale, const int32_t* limits, const RowsDev& out,
                                float* lse, void* scratch, int32_t* status, cudaStream_t stream) {
   AttnArgs a{kv, s, q, out, lse, limits, scale, plan.chunk, plan.chunks, 0, nullptr, nullptr, status};
-  a.col_blocks = int((int64_t(s.max_rows) * kv.G + kCols - 1) / kCols);
+  a.col_blocks = int((int64_t(s.max_rows) * kv.G + plan.cols - 1) / plan.cols);
   a.part_ml = static_cast<float2*>(scratch);
   a.part_o = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats_bytes(kv, s, plan.chunks));
-  return dtype == CONDUIT_BF16 ? launch_t<__nv_bfloat16>(a, plan, packed_attn_mma_supported(kv, dtype), stream)
-                               : launch_t<float>(a, plan, false, stream);
+  return dtype == CONDUIT_BF16 ? launch_t<__nv_bfloat16>(a, plan, stream) : launch_t<float>(a, plan, stream);
 }
 
 }  // namespace conduit

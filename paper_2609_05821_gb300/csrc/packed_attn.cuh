@@ -6,7 +6,7 @@
 #include "tc_common.cuh"
 
 namespace conduit {
-constexpr int kCols = 8;  // columns per CTA
+constexpr int kCols = 8;  // columns per CTA of the warp-level and CUDA-core kernels
 
 struct AttnArgs {
   PackedDev kv;
@@ -26,6 +26,7 @@ struct Item {
   int l, r, g, cb, chunk, t0, n, len;
 };
 
+template <int kBlockCols>
 __device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
   uint32_t x = blockIdx.x;
   it->cb = int(x % uint32_t(a.col_blocks));
@@ -39,7 +40,7 @@ __device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
   it->t0 = a.s.row_off[it->r];
   it->n = a.s.row_off[it->r + 1] - it->t0;
   it->len = cached_len(a.s, a.kv.capacity(), it->r, a.status, threadIdx.x == 0);
-  if (it->cb * kCols >= it->n * a.kv.G) return false;
+  if (it->cb * kBlockCols >= it->n * a.kv.G) return false;
   return it->chunk == 0 || it->chunk * a.chunk < it->len;
 }
 
@@ -86,8 +87,60 @@ __device__ __forceinline__ void store_stats(const AttnArgs& a, const Item& it, i
   }
 }
 
-// Warp-level tensor-core kernel (packed_attn_mma.cu): bf16 rows, head_dim 64, 96, 128.
-bool packed_attn_mma_supported(const PackedDev& kv, int dtype);
+__device__ __forceinline__ uint32_t h2u(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+__device__ __forceinline__ __half2 u2h(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
+
+// Two nibbles u of w as fp16: 1024 + u of bits 0-3 and 16-19, 1024 + 16 u of bits 4-7 and 20-23.
+__device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t mask) {  // (w & mask) | 0x64006400
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(w), "r"(mask), "r"(0x64006400u));
+  return y;
+}
+__device__ __forceinline__ uint32_t raw_lo(uint32_t w) { return masked(w, 0x000F000Fu); }
+__device__ __forceinline__ uint32_t raw_hi(uint32_t w) { return masked(w, 0x00F000F0u); }
+// The same as u - 8, exactly.
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
+  return h2u(__hadd2(u2h(raw_lo(w)), __float2half2_rn(-1032.f)));
+}
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
+  return h2u(__hfma2(u2h(raw_hi(w)), __float2half2_rn(0.0625f), __float2half2_rn(-72.f)));
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(tc::smem_u32(bar))
+               : "memory");
+}
+
+// N consecutive 32-bit words, N * 4 bytes aligned to the widest load that divides them.
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const uint4 x = reinterpret_cast<const uint4*>(p)[i];
+      w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+    }
+  } else if constexpr (N % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const uint2 x = reinterpret_cast<const uint2*>(p)[i];
+      w[2 * i] = x.x, w[2 * i + 1] = x.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+  }
+}
+
+// Neither s nor m of a parameter pair is infinite or NaN.
+__device__ __forceinline__ bool finite_pair(uint32_t p) {
+  return (p & 0x7C00u) != 0x7C00u && (p & 0x7C000000u) != 0x7C000000u;
+}
+
+// Warp-level tensor-core kernel (packed_attn_mma.cu) and tcgen05 kernel
+// (packed_attn_tc.cu): bf16 rows, head_dim 64, 96, 128.
 cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, cudaStream_t stream);
+cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream);
 
 }  // namespace conduit

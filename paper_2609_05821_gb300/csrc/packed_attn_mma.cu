@@ -28,25 +28,6 @@ constexpr int kStages = 2;
 constexpr int kTile = 32;  // tokens of a tile (2^5)
 constexpr int kBoxBytes(int d) { return kTile * (d + d / 4); }
 
-__device__ __forceinline__ uint32_t h2u(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
-__device__ __forceinline__ __half2 u2h(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
-
-// Two nibbles u of w as fp16: 1024 + u of bits 0-3 and 16-19, 1024 + 16 u of bits 4-7 and 20-23.
-__device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t mask) {  // (w & mask) | 0x64006400
-  uint32_t y;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(w), "r"(mask), "r"(0x64006400u));
-  return y;
-}
-__device__ __forceinline__ uint32_t raw_lo(uint32_t w) { return masked(w, 0x000F000Fu); }
-__device__ __forceinline__ uint32_t raw_hi(uint32_t w) { return masked(w, 0x00F000F0u); }
-// The same as u - 8, exactly.
-__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
-  return h2u(__hadd2(u2h(raw_lo(w)), __float2half2_rn(-1032.f)));
-}
-__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
-  return h2u(__hfma2(u2h(raw_hi(w)), __float2half2_rn(0.0625f), __float2half2_rn(-72.f)));
-}
-
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
   asm volatile(
@@ -70,33 +51,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(src), "r"(bytes), "r"(tc::smem_u32(bar))
-               : "memory");
-}
-
-// N consecutive 32-bit words, N * 4 bytes aligned to the widest load that divides them.
-template <int N>
-__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
-  if constexpr (N % 4 == 0) {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-      const uint4 x = reinterpret_cast<const uint4*>(p)[i];
-      w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
-    }
-  } else if constexpr (N % 2 == 0) {
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-      const uint2 x = reinterpret_cast<const uint2*>(p)[i];
-      w[2 * i] = x.x, w[2 * i + 1] = x.y;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
-  }
-}
-
 // N 16-bit words in the low halves (even) and high halves (odd) of (N + 1) / 2 words.
 template <int N>
 __device__ __forceinline__ void load_halves(const uint8_t* p, uint32_t (&w)[(N + 1) / 2]) {
@@ -108,10 +62,6 @@ __device__ __forceinline__ void load_halves(const uint8_t* p, uint32_t (&w)[(N +
     for (int i = 0; i < N / 2; ++i) w[i] = h[2 * i] | uint32_t(h[2 * i + 1]) << 16;
     w[N / 2] = h[N - 1];
   }
-}
-
-__device__ __forceinline__ bool finite_pair(uint32_t p) {
-  return (p & 0x7C00u) != 0x7C00u && (p & 0x7C000000u) != 0x7C000000u;
 }
 
 // The mids of groups 2 (c & 1) and + 1 of a token's parameters.
@@ -269,7 +219,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[kWarps][kStages];
   Item it;
-  if (!item_of(a, &it)) return;
+  if (!item_of<kCols>(a, &it)) return;
   const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int c = lane & 3, q = lane >> 2;
   // a row of the logits' accumulator is the token key_lo (+ 8) of its half tile; with this
@@ -479,10 +429,6 @@ cudaError_t launch(const AttnArgs& a, int64_t items, cudaStream_t stream) {
 }
 
 }  // namespace
-
-bool packed_attn_mma_supported(const PackedDev& kv, int dtype) {
-  return dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
-}
 
 cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, cudaStream_t stream) {
   switch (a.kv.d) {

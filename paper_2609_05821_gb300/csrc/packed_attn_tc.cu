@@ -1,0 +1,495 @@
+// Attention over the 4-bit cache for many rows (query prefixes, recomputed rows): tcgen05.
+//
+// Mathematics: as in packed_attn_mma.cu, with keys and values as fp16 m + s c (2^-11
+// relative), the query scaled by a power of two per row into fp16, weights rounded to
+// fp16; logits, statistics and outputs in fp32 (tensor memory).
+//
+// Shape. A CTA holds two tiles of 128 columns (A and B: rows of the call times query
+// heads of one KV head) and walks over the keys in tiles of 128. Each key tile is
+// unpacked once into shared memory for both. Roles (512 threads):
+//   warps 0-3, 4-7  softmax of A and of B: a thread owns a column and all 128 keys
+//   warps 8-11      unpack: four lanes a token, a word of eight codes at a time
+//   warp 12         bulk copies of page runs into two small buffers, keys and values
+//   warp 13         MMAs: P_x(t) V(t), then S_x(t + 1), for x = A, B; one lane issues
+// One column tile's softmax runs beside the other's MMAs. MMAs of one thread complete in
+// order, so S_x(t + 1) may overwrite P_x(t), and S_x(t + 1) says that P_x(t) V(t) is done.
+// The dims of keys and queries are permuted alike (a word's nibbles come out as dims
+// e, e + 4), those of the values as they unpack (two groups side by side); the output rows
+// are put back in order. TMEM: S_A, S_B at columns [0, 256) with P over their upper halves,
+// O_A, O_B at [256, 512).
+//
+// Bound: the issue slots that unpacking (about 2 300 warp instructions per 128 keys) and
+// softmax (1 800 per column tile) share, next to 2 048 cycles of tensor work.
+#include "packed_attn.cuh"
+
+namespace conduit {
+namespace {
+
+constexpr int kThreads = 512;                 // warps 14 and 15 only give up registers
+constexpr int kKeys = 128;                    // keys of a tile
+constexpr int kTileCols = 128;                // columns of a tile
+constexpr int kTcCols = 2 * kTileCols;
+constexpr int kUnpackWarp = 8, kLoadWarp = 12, kMmaWarp = 13;
+constexpr uint32_t kBlock = 128 * 128;        // 128 rows of 64 fp16, swizzled
+constexpr uint32_t kSCols = 128, kPCol = 64, kOCol = 256;
+constexpr float kSlack = 8.f;                 // as in packed_attn_mma.cu
+
+template <int NG>
+struct Sizes {
+  static constexpr int D = 32 * NG;
+  static constexpr uint32_t kTile = (D + 63) / 64 * kBlock;  // a query, key or value tile
+  static constexpr uint32_t kRaw = kKeys * (D / 2 + D / 8);   // packed keys (or values) of a tile
+  static constexpr uint32_t kSmem = 1024 + 6 * kTile + 2 * kRaw;
+};
+
+struct Bars {
+  uint64_t raw_full[2], raw_free[2];    // packed keys, packed values
+  uint64_t k_full[2], k_free[2], v_full[2], v_free[2];
+  uint64_t q_full, s_full[2], p_full[2], o_full[2], drained;
+};
+
+// The eight values of a word: nibbles (0, 4), (1, 5), (2, 6), (3, 7).
+__device__ __forceinline__ uint4 values8(uint32_t w, __half2 s, __half2 m) {
+  const uint32_t w8 = w >> 8;
+  return make_uint4(h2u(__hfma2(s, u2h(codes_lo(w)), m)), h2u(__hfma2(s, u2h(codes_hi(w)), m)),
+                    h2u(__hfma2(s, u2h(codes_lo(w8)), m)), h2u(__hfma2(s, u2h(codes_hi(w8)), m)));
+}
+// kind::f16 with fp16 operands, fp32 sums; B key-major or dim-major.
+constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
+  return (1u << 4) | (uint32_t(b_mn_major) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
+}
+
+// Bounded wait of a converged warp; false after a second or once another role gave up.
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  bool ok = tc::mbar_probe(bar, parity);
+  if (!ok) {
+    const uint64_t t0 = tc::globaltimer_ns();
+    for (uint32_t i = 1; !ok && i < tc::kSpinLimit; ++i) {
+      ok = tc::mbar_try_wait(bar, parity);
+      if (!ok && (i & 7u) == 0 && (*abort || tc::globaltimer_ns() - t0 > tc::kWaitNs)) break;
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
+}
+
+__device__ __forceinline__ void give_up(const AttnArgs& a, volatile int* abort, int32_t site) {
+  if (!*abort) flag_status(a.status, CONDUIT_FLAG_TIMEOUT | site);
+  *abort = 1;
+}
+
+template <int NG>
+__global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
+  using Z = Sizes<NG>;
+  constexpr int D = Z::D;
+  extern __shared__ uint8_t dynamic[];
+  __shared__ Bars bars;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int seen_most, seen_least, poison[NG], abort_flag;
+  Item it;
+  if (!item_of<kTcCols>(a, &it)) return;
+  uint8_t* base = dynamic + (1024 - (tc::smem_u32(dynamic) & 1023u)) % 1024;
+  uint8_t *qt = base, *kt = qt + 2 * Z::kTile, *vt = kt + 2 * Z::kTile, *raw = vt + 2 * Z::kTile;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  volatile int* abort = &abort_flag;
+
+  if (tid == 0) {
+    for (int s = 0; s < 2; ++s) {
+      tc::mbar_init(&bars.raw_full[s], 1);
+      tc::mbar_init(&bars.raw_free[s], 4);
+      tc::mbar_init(&bars.k_full[s], 4);
+      tc::mbar_init(&bars.v_full[s], 4);
+      tc::mbar_init(&bars.k_free[s], 1);
+      tc::mbar_init(&bars.v_free[s], 1);
+      tc::mbar_init(&bars.s_full[s], 1);
+      tc::mbar_init(&bars.p_full[s], 4);
+      tc::mbar_init(&bars.o_full[s], 1);
+    }
+    tc::mbar_init(&bars.q_full, 8);
+    tc::mbar_init(&bars.drained, 1);
+    tc::fence_barrier_init();
+    seen_most = 0;
+    seen_least = INT32_MAX;
+    for (int g = 0; g < NG; ++g) poison[g] = INT32_MAX;
+    abort_flag = 0;
+  }
+  if (warp == kMmaWarp) tc::tmem_alloc(&tmem_slot, 512);
+  __syncthreads();
+  // keys that a column sees; columns past the last see all (their result is dropped)
+  const int col = it.cb * kTcCols + tid;
+  const bool live = tid < kTcCols && col < it.n * a.kv.G;
+  const int lim = live ? limit_of(a, it, col) : INT32_MAX;
+  if (warp < kUnpackWarp) {
+    const int hi = __reduce_max_sync(0xffffffffu, live ? lim : 0), lo = __reduce_min_sync(0xffffffffu, lim);
+    if (lane == 0) {
+      atomicMax(&seen_most, hi);
+      atomicMin(&seen_least, lo);
+    }
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const int least = seen_least, k0 = it.chunk * a.chunk, k1 = min(k0 + a.chunk, seen_most);
+  const int tiles = k1 > k0 ? (k1 - k0 + kKeys - 1) / kKeys : 0;
+  const int streams = it.cb * kTcCols + kTileCols < it.n * a.kv.G ? 2 : 1;
+
+  // 128 registers a thread at launch: 2 x 88 + 2 x 168 per four warpgroups
+  if (warp >= kUnpackWarp)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;" ::: "memory");
+  else
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;" ::: "memory");
+  if (warp == kLoadWarp) {
+    // ---------------------------------------------------------------- copies
+    const int run_shift = min(7, a.kv.page_shift), run = 1 << run_shift;
+    const int part = lane & 1, at_tile = (lane >> 1) << run_shift;  // codes or parameters of one run
+    const int row_bytes = part ? D / 8 : D / 2;
+    const uint32_t dst = tc::smem_u32(raw) + (part ? kKeys * (D / 2) : 0) + at_tile * row_bytes;
+    const int64_t page_stride = a.kv.Hkv * a.kv.page_bytes;
+    const uint8_t* head = a.kv.page(it.l, it.g, 0);
+    int issued[2] = {0, 0};
+    for (int t = 0; t < tiles; ++t) {
+      const int kb = k0 + t * kKeys, runs = (min(k1 - kb, kKeys) + run - 1) >> run_shift;
+      const bool mine = lane < 2 * runs;
+      const int j = kb + at_tile, row = j & ((1 << a.kv.page_shift) - 1);
+      const uint8_t* page = mine ? head + page_of(a, it.r, j) * page_stride : head;
+      bool ok = true;
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        if (t > 0 && !(ok = wait_warp(&bars.raw_free[v], (t - 1) & 1, abort))) break;
+        if (lane == 0) tc::mbar_arrive_expect_tx(&bars.raw_full[v], uint32_t(runs << run_shift) * (D / 2 + D / 8));
+        __syncwarp();
+        if (mine)
+          bulk_load(dst + v * Z::kRaw, page + (part ? a.kv.params(v, row) : a.kv.codes(v, row)), row_bytes << run_shift,
+                    &bars.raw_full[v]);
+        ++issued[v];
+      }
+      if (!ok) {
+        if (lane == 0) give_up(a, abort, CONDUIT_SITE_MMA);
+        break;
+      }
+    }
+    for (int v = 0; v < 2; ++v)  // the last copies (all have landed unless a role gave up)
+      if (issued[v]) tc::mbar_wait(&bars.raw_full[v], (issued[v] - 1) & 1);
+  } else if (warp >= kUnpackWarp && warp < kLoadWarp) {
+    // ---------------------------------------------------------------- unpack
+    // Four lanes a token. Keys: the two tokens of eight lanes are four apart, so that their
+    // chunks fall into different banks of the swizzled tile; values: next to each other.
+    const int c = lane & 3, i8 = lane >> 2;
+    const int first = 32 * (warp - kUnpackWarp) + (i8 & 1) * 4 + (i8 >> 1);
+    for (int t = 0; t < tiles; ++t) {
+      const int kb = k0 + t * kKeys, stage = t & 1;
+      bool ok = wait_warp(&bars.raw_full[0], t & 1, abort);
+      if (ok && t >= 2) ok = wait_warp(&bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
+      if (!ok) {
+        if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
+        break;
+      }
+      uint8_t* tile = kt + stage * Z::kTile;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int token = first + 8 * i;
+        uint32_t w[NG], p[NG];
+        load_words<NG>(raw + token * (D / 2) + c * (D / 8), w);
+        load_words<NG>(raw + kKeys * (D / 2) + token * (D / 8), p);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const int ch = 4 * g + c;
+          *reinterpret_cast<uint4*>(tile + (ch >> 3) * kBlock + tc::sw128_offset(token, ch & 7)) =
+              values8(w[g], u2h(__byte_perm(p[g], p[g], 0x1010)), u2h(__byte_perm(p[g], p[g], 0x3232)));
+        }
+      }
+      tc::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tc::mbar_arrive(&bars.raw_free[0]);
+        tc::mbar_arrive(&bars.k_full[stage]);
+      }
+      ok = wait_warp(&bars.raw_full[1], t & 1, abort);
+      if (ok && t >= 2) ok = wait_warp(&bars.v_free[stage], ((t >> 1) - 1) & 1, abort);
+      if (!ok) {
+        if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
+        break;
+      }
+      tile = vt + stage * Z::kTile;
+      const bool edge = kb + kKeys > least;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int token = 32 * (warp - kUnpackWarp) + 8 * i + i8, j = kb + token;
+        const uint8_t* row = raw + Z::kRaw + token * (D / 2);
+        uint32_t w[NG], p[NG];
+        if constexpr (NG == 3) {  // words c, c + 4, c + 8
+#pragma unroll
+          for (int n = 0; n < NG; ++n) w[n] = *reinterpret_cast<const uint32_t*>(row + 4 * (4 * n + c));
+        } else {  // words NG c on
+          load_words<NG>(row + c * (D / 8), w);
+        }
+        load_words<NG>(raw + Z::kRaw + kKeys * (D / 2) + token * (D / 8), p);
+        if (edge) {
+          // tokens that some column does not see: their weight there is 0, and 0 times NaN must not be
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            if (j >= least && j < k1 && !finite_pair(p[g])) atomicMin(&poison[g], j), p[g] = 0;
+            if (j >= k1) p[g] = 0;
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          // word ch of the row: the groups g0 and g1 side by side
+          int ch = NG * c + n;
+          uint32_t word = w[n], p0 = p[2 * n % NG], p1 = p[(2 * n + 1) % NG];
+          if constexpr (NG == 4) {  // the lanes of a token in different banks
+            ch = 4 * c + (n ^ (c & 2));
+            word = c & 2 ? w[n ^ 2] : w[n];
+          } else if constexpr (NG == 3) {
+            ch = 4 * n + c;
+            const int g0 = 2 * ch % 3, g1 = (2 * ch + 1) % 3;
+            p0 = g0 == 0 ? p[0] : g0 == 1 ? p[1] : p[2];
+            p1 = g1 == 0 ? p[0] : g1 == 1 ? p[1] : p[2];
+          }
+          *reinterpret_cast<uint4*>(tile + (ch >> 3) * kBlock + tc::sw128_offset(token, ch & 7)) =
+              values8(word, u2h(__byte_perm(p0, p1, 0x5410)), u2h(__byte_perm(p0, p1, 0x7632)));
+        }
+      }
+      tc::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tc::mbar_arrive(&bars.raw_free[1]);
+        tc::mbar_arrive(&bars.v_full[stage]);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ------------------------------------------------------------------ MMAs
+    const uint32_t leader = lane == 0;
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    constexpr uint32_t idesc_s = idesc_f16(kTileCols, kKeys, false), idesc_o = idesc_f16(kTileCols, D, true);
+    const uint64_t dq = tc::desc_sw128(tc::smem_u32(qt));
+    auto score = [&](int x, int stage) {
+      const uint64_t dk = tc::desc_sw128(tc::smem_u32(kt) + stage * Z::kTile);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
+        tc::mma_bf16_if(leader, tm + x * kSCols, dq + ((x * Z::kTile) >> 4) + off, dk + off, idesc_s, kk > 0);
+      }
+      tc::mma_commit_if(leader, &bars.s_full[x]);
+    };
+    bool ok = tiles == 0 || wait_warp(&bars.q_full, 0, abort);
+    if (ok && tiles > 0 && (ok = wait_warp(&bars.k_full[0], 0, abort))) {
+      tc::tc_fence_after();
+      for (int x = 0; x < streams; ++x) score(x, 0);
+      tc::mma_commit_if(leader, &bars.k_free[0]);
+    }
+    for (int t = 0; ok && t < tiles; ++t) {
+      const int stage = t & 1, next = stage ^ 1;
+      const bool more = t + 1 < tiles;
+      const uint64_t dv = tc::desc_sw128_mn(tc::smem_u32(vt) + stage * Z::kTile, kBlock);
+      if (!(ok = wait_warp(&bars.v_full[stage], (t >> 1) & 1, abort))) break;
+      if (more && !(ok = wait_warp(&bars.k_full[next], ((t + 1) >> 1) & 1, abort))) break;
+      for (int x = 0; x < streams; ++x) {
+        if (!(ok = wait_warp(&bars.p_full[x], t & 1, abort))) break;
+        tc::tc_fence_after();
+#pragma unroll
+        for (int kk = 0; kk < kKeys / 16; ++kk)
+          tc::mma_bf16_ts_if(leader, tm + kOCol + x * kSCols, tm + x * kSCols + kPCol + kk * 8, dv + kk * (2048 >> 4),
+                             idesc_o, t > 0 || kk > 0);
+        if (x + 1 == streams) tc::mma_commit_if(leader, &bars.v_free[stage]);
+        if (more)
+          score(x, next);
+        else
+          tc::mma_commit_if(leader, &bars.o_full[x]);
+      }
+      if (ok && more) tc::mma_commit_if(leader, &bars.k_free[next]);
+    }
+    if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_MMA);
+    tc::mma_commit_if(leader, &bars.drained);  // every MMA issued above is done once this arrives
+    tc::mbar_wait(&bars.drained, 0);
+    __syncwarp();
+  } else if (warp < kUnpackWarp) {
+    // --------------------------------------------------------------- softmax
+    const int x = warp >> 2, row = tid & 127;
+    const int i = live ? col / a.kv.G : 0, h = live ? it.g * a.kv.G + col % a.kv.G : 0;
+    float to_log2;
+    {
+      // the column's query, scaled so that its largest lies in [256, 512), into the swizzled tile
+      const __nv_bfloat16* src =
+          static_cast<const __nv_bfloat16*>(a.q.p) + it.l * a.q.ls + int64_t(it.t0 + i) * a.q.rs + h * a.q.hs;
+      const bool wide = ((reinterpret_cast<uintptr_t>(a.q.p) | uint64_t(2 * (a.q.ls | a.q.rs | a.q.hs))) & 15u) == 0;
+      uint4 v[D / 8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int b = 0; b < D / 8; ++b) {
+        if (!live) {
+          v[b] = make_uint4(0, 0, 0, 0);
+        } else if (wide) {
+          v[b] = *reinterpret_cast<const uint4*>(src + 8 * b);
+        } else {
+          __nv_bfloat16 e8[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) e8[e] = src[8 * b + e];
+          v[b] = *reinterpret_cast<uint4*>(e8);
+        }
+        const uint32_t w[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFF0000u, (w[e] & 0x7FFFu) << 16));  // |q| as fp32 bits
+      }
+      int shift = int(top >> 23) - 127 - 8;
+      if (top >= 0x7F800000u || top == 0) shift = 0;
+      // 2^-shift and 2^shift in two factors, each a normal number
+      const float f1 = __uint_as_float(uint32_t(127 - shift / 2) << 23);
+      const float f2 = __uint_as_float(uint32_t(127 - (shift - shift / 2)) << 23);
+      const float g1 = __uint_as_float(uint32_t(127 + shift / 2) << 23);
+      const float g2 = __uint_as_float(uint32_t(127 + (shift - shift / 2)) << 23);
+      to_log2 = fmaxf(a.scale * kLog2e * g1 * g2, 1.1754944e-38f);  // positive, so that a masked logit stays -inf
+#pragma unroll
+      for (int b = 0; b < D / 8; ++b) {
+        const uint32_t w[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f[2 * e] = __uint_as_float(w[e] << 16) * f1 * f2;
+          f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u) * f1 * f2;
+        }
+        uint4 y;  // in the order in which a word's nibbles unpack
+        y.x = h2u(__floats2half2_rn(f[0], f[4]));
+        y.y = h2u(__floats2half2_rn(f[1], f[5]));
+        y.z = h2u(__floats2half2_rn(f[2], f[6]));
+        y.w = h2u(__floats2half2_rn(f[3], f[7]));
+        *reinterpret_cast<uint4*>(qt + x * Z::kTile + (b >> 3) * kBlock + tc::sw128_offset(row, b & 7)) = y;
+      }
+      tc::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars.q_full);
+    }
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    const uint32_t sb = tmem + lanes + x * kSCols, ob = tmem + lanes + kOCol + x * kSCols;
+    float ref = -INFINITY;
+    float2 sum = make_float2(0.f, 0.f);
+    const float2 up = make_float2(to_log2, to_log2);
+    bool ok = true;
+    const int count = x < streams ? tiles : 0;
+    for (int t = 0; t < count; ++t) {
+      if (!(ok = wait_warp(&bars.s_full[x], t & 1, abort))) break;
+      tc::tc_fence_after();
+      const int left = lim - (k0 + t * kKeys);  // keys of the tile that the column sees
+      const bool edge = k0 + (t + 1) * kKeys > least;
+      uint32_t p[4][16];
+      float2 add;
+      for (int pass = 0;; ++pass) {
+        const float low = ref == -INFINITY ? 0.f : -ref;
+        const float2 down = make_float2(low, low);
+        float top = -INFINITY;
+        add = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          float s[32];
+          tc::tmem_ld32(sb + 32 * b, s);
+          if (edge) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (32 * b + e >= left) s[e] = -INFINITY;
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            top = tc::fmax3(top, s[e], s[e + 1]);
+            const float2 y = tc::ffma2(make_float2(s[e], s[e + 1]), up, down);
+            const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
+            add = tc::fadd2(add, w);
+            p[b][e / 2] = h2u(__float22half2_rn(w));
+          }
+        }
+        top *= to_log2;
+        if (pass || !__any_sync(0xffffffffu, top > ref + kSlack)) break;
+        // the reference moves: what was summed so far is scaled, and the weights are taken again
+        const float moved = fmaxf(ref, top), corr = moved == -INFINITY ? 1.f : tc::ex2(ref - moved);
+        ref = moved;
+        sum = make_float2(sum.x * corr, sum.y * corr);
+        if (t > 0) {
+#pragma unroll 1
+          for (int b = 0; b < D / 32; ++b) {
+            float o[32];
+            tc::tmem_ld32(ob + 32 * b, o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] *= corr;
+            tc::tmem_st32(ob + 32 * b, o);
+          }
+        }
+      }
+      sum = tc::fadd2(sum, add);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) tc::tmem_st16_nowait(sb + kPCol + 16 * b, p[b]);
+      tc::tmem_wait_st();
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars.p_full[x]);
+    }
+    if (ok && count > 0) ok = wait_warp(&bars.o_full[x], 0, abort);
+    if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_FINAL);
+    tc::tc_fence_after();
+    const float total = sum.x + sum.y;
+    if (live) store_stats(a, it, col, ref, total);
+    const float inv = a.chunks > 1 ? 1.f : total == 0.f ? 0.f : 1.f / total;
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out.p) + it.l * a.out.ls + int64_t(it.t0 + i) * a.out.rs + h * a.out.hs;
+    const bool by_four =
+        ((reinterpret_cast<uintptr_t>(a.out.p) | uint64_t(2 * (a.out.ls | a.out.rs | a.out.hs))) & 7u) == 0;
+    const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
+    float* part = a.part_o + (it.chunk * cols + (int64_t(it.l) * a.s.T + it.t0 + i) * a.kv.Hq + h) * D;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+      float o[32];
+      if (ok && count > 0) {
+        tc::tmem_ld32(ob + 32 * b, o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = 0.f;
+      }
+      if (live) {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          // four neighbouring dims of group g: every other column of a word of the value rows
+          const int word = 4 * b + n / 2, hw = 2 * word + (n & 1), g = hw % NG, dim = 32 * g + 4 * (hw / NG);
+          float y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            y[e] = o[8 * (n / 2) + 2 * e + (n & 1)] * inv;
+            if (poison[g] < lim) y[e] = NAN;  // a value that is not finite reaches the columns that see it
+          }
+          if (a.chunks > 1) {
+            *reinterpret_cast<float4*>(part + dim) = make_float4(y[0], y[1], y[2], y[3]);
+          } else if (by_four) {
+            __nv_bfloat162 z[2] = {__floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
+            *reinterpret_cast<uint2*>(to + dim) = *reinterpret_cast<uint2*>(z);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[dim + e] = __float2bfloat16_rn(y[e]);
+          }
+        }
+      }
+    }
+    tc::tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc::tc_fence_after();
+    tc::tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int NG>
+cudaError_t launch(const AttnArgs& a, int64_t items, cudaStream_t stream) {
+  cudaError_t err = cudaFuncSetAttribute(packed_attn_tc<NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<NG>::kSmem);
+  if (err) return err;
+  packed_attn_tc<NG><<<unsigned(items), kThreads, Sizes<NG>::kSmem, stream>>>(a);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream) {
+  switch (a.kv.d) {
+    case 64: return launch<2>(a, items, stream);
+    case 96: return launch<3>(a, items, stream);
+    default: return launch<4>(a, items, stream);
+  }
+}
+
+}  // namespace conduit
