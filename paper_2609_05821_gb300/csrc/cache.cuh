@@ -29,6 +29,7 @@ struct SeqsDev {
   int32_t R, T, max_len, max_rows;
   const int32_t* row_off;
   const int32_t* len;
+  const int32_t* row_off_host;
 };
 
 struct PackedDev {
@@ -74,7 +75,6 @@ cudaError_t launch_packed_read(const PackedDev& kv, const int32_t* first, const 
 enum { kAttnSimt = 0, kAttnMma = 1, kAttnTc = 2 };
 struct PackedAttnPlan {
   int kernel;     // CUDA cores, warp-level tensor cores, tcgen05
-  int cols;       // columns (rows of the call times query heads of a KV head) per CTA
   int chunk;      // keys per chunk
   int chunks;     // of the longest context
   int64_t items;  // CTAs

@@ -76,7 +76,7 @@ conduit_status make_seqs(const conduit_seqs* s, SeqsDev* out) {
   if (!s->row_off || !s->row_off_dev || !s->len_dev)
     return fail(CONDUIT_ERR_INVALID_ARG, "row_off, row_off_dev and len_dev are required");
   if (s->row_off[0] != 0) return fail(CONDUIT_ERR_INVALID_ARG, "row_off must start at 0");
-  *out = SeqsDev{s->num_requests, 0, s->max_len, 0, s->row_off_dev, s->len_dev};
+  *out = SeqsDev{s->num_requests, 0, s->max_len, 0, s->row_off_dev, s->len_dev, s->row_off};
   for (int r = 0; r < s->num_requests; ++r) {
     if (s->row_off[r + 1] < s->row_off[r])
       return fail(CONDUIT_ERR_INVALID_ARG, "row_off must be non-decreasing (request %d)", r);

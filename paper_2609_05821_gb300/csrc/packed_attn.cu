@@ -6,6 +6,7 @@
 // combine_kernel joins in order. Columns: the call's rows of a request times the G
 // query heads of a KV head, column j = i G + h.
 #include <algorithm>
+#include <cmath>
 
 #include "packed_attn.cuh"
 
@@ -23,7 +24,7 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
   extern __shared__ float simt_smem[];
   float *ks = simt_smem, *vs = ks + kSimtKeys * KS, *qs = vs + kSimtKeys * D;
   Item it;
-  if (!item_of<kCols>(a, &it)) return;
+  if (!item_of(a, &it)) return;
   const int tid = threadIdx.x, w = tid / 32, lane = tid % 32;
   for (int e = tid; e < kCols * D; e += 128) {
     const int j = it.cb * kCols + e / D;
@@ -52,7 +53,7 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
       float* ko = ks + key * KS + 8 * u;
       float* vo = vs + key * D + 8 * u;
       if (j < k1) {
-        const uint8_t* at = a.kv.page(it.l, it.g, page_of(a, it.r, j));
+        const uint8_t* at = a.kv.page(it.l, it.g, page_in_pool(a, page_entry(a, it.r, j)));
         const int row = j & ((1 << a.kv.page_shift) - 1);
         const uint32_t kw = reinterpret_cast<const uint32_t*>(at + a.kv.codes(0, row))[c * NG + grp];
         const uint16_t* vh = reinterpret_cast<const uint16_t*>(at + a.kv.codes(1, row));
@@ -120,31 +121,38 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
 constexpr int simt_smem_bytes(int d) { return (kSimtKeys * (2 * d + 1) + kCols * d) * int(sizeof(float)); }
 
 // ---------------------------------------------------------------- the join
-// A block per (layer, row, head): eight groups of threads take every eighth chunk of
-// the request's context, four dims a thread, then join in order. One warp that walked
-// over all chunks took 60 us for 147 chunks; this takes 5.
-constexpr int kJoin = 8;
-
-template <typename T, int NG>
-__global__ void __launch_bounds__(kJoin * NG * 8) combine_kernel(AttnArgs a) {
-  constexpr int D = NG * 32, kLanes = NG * 8;
-  __shared__ float4 part[kJoin][kLanes];
-  __shared__ float part_sum[kJoin];
-  const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq, col = blockIdx.x;
-  const int lane = threadIdx.x % kLanes, grp = threadIdx.x / kLanes;
-  const int h = int(col % a.kv.Hq), t = int(col / a.kv.Hq % a.s.T), l = int(col / a.kv.Hq / a.s.T);
-  const int r = request_of(a.s.row_off, a.s.R, t);
-  const int len = cached_len(a.s, a.kv.capacity(), r, nullptr, false);
-  const int n = max(1, (len + a.chunk - 1) / a.chunk);
+// Groups of threads with four dims a thread: kJoin groups share a (layer, row, head) and
+// take every kJoin-th chunk of the request's context, then join in order. One group that
+// walked over 147 chunks took 60 us, eight take 5; over two chunks of 73 000 (row, head)
+// pairs eight groups each (six of them idle) took 200 us.
+template <typename T, int NG, int kJoin>
+__global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
+  constexpr int D = NG * 32, kLanes = NG * 8, kPer = 8 / kJoin;
+  __shared__ float4 part[8][kLanes];
+  __shared__ float part_sum[8];
+  const int lane = threadIdx.x % kLanes, grp = threadIdx.x / kLanes, of = grp % kJoin;
+  const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq, col = int64_t(blockIdx.x) * kPer + grp / kJoin;
+  const bool on = col < cols;
+  int h = 0, t = 0, l = 0, n = 0;
+  if (on) {
+    h = int(col % a.kv.Hq), t = int(col / a.kv.Hq % a.s.T), l = int(col / a.kv.Hq / a.s.T);
+    const int r = request_of(a.s.row_off, a.s.R, t);
+    const int len = cached_len(a.s, a.kv.capacity(), r, nullptr, false);
+    n = max(1, (len + a.chunk - 1) / a.chunk);
+  }
   float top = -INFINITY;
-  for (int c = threadIdx.x % 32; c < n; c += 32) top = fmaxf(top, a.part_ml[c * cols + col].x);
+  if (kJoin == 8) {  // one column in the block: its warps look for the reference lane by lane
+    for (int c = threadIdx.x % 32; c < n; c += 32) top = fmaxf(top, a.part_ml[c * cols + col].x);
 #pragma unroll
-  for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+    for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  } else {
+    for (int c = 0; c < n; ++c) top = fmaxf(top, a.part_ml[c * cols + col].x);
+  }
   const float base = top == -INFINITY ? 0.f : top;
   float sum = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int c = grp; c < n; c += kJoin) {
+  for (int c = of; c < n; c += kJoin) {
     const float2 ml = a.part_ml[c * cols + col];
     const float wgt = exp2f(ml.x - base);
     sum = fmaf(wgt, ml.y, sum);
@@ -154,20 +162,26 @@ __global__ void __launch_bounds__(kJoin * NG * 8) combine_kernel(AttnArgs a) {
     o.z = fmaf(wgt, po.z, o.z);
     o.w = fmaf(wgt, po.w, o.w);
   }
-  part[grp][lane] = o;
-  if (lane == 0) part_sum[grp] = sum;
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  sum = 0.f;
-  float out = 0.f;
+  if (kJoin > 1) {
+    part[grp][lane] = o;
+    if (lane == 0) part_sum[grp] = sum;
+    __syncthreads();
+    if (of != 0 || !on) return;
 #pragma unroll
-  for (int c = 0; c < kJoin; ++c) {
-    sum += part_sum[c];
-    out += reinterpret_cast<const float*>(part[c])[threadIdx.x];
+    for (int c = 1; c < kJoin; ++c) {
+      const float4 y = part[grp + c][lane];
+      sum += part_sum[grp + c];
+      o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
+    }
   }
-  T* to = static_cast<T*>(a.out.p) + l * a.out.ls + int64_t(t) * a.out.rs + h * a.out.hs;
-  to[threadIdx.x] = from_float<T>(sum == 0.f ? 0.f : out / sum);
-  if (threadIdx.x == 0 && a.lse)
+  if (!on) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  T* to = static_cast<T*>(a.out.p) + l * a.out.ls + int64_t(t) * a.out.rs + h * a.out.hs + 4 * lane;
+  to[0] = from_float<T>(o.x * inv);
+  to[1] = from_float<T>(o.y * inv);
+  to[2] = from_float<T>(o.z * inv);
+  to[3] = from_float<T>(o.w * inv);
+  if (lane == 0 && a.lse)
     a.lse[(int64_t(l) * a.kv.Hq + h) * a.s.T + t] = sum == 0.f ? -INFINITY : kLn2 * (base + log2f(sum));
 }
 
@@ -188,7 +202,10 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
   }
   if (err || a.chunks == 1) return err;
   const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
-  combine_kernel<T, NG><<<unsigned(cols), kJoin * NG * 8, 0, stream>>>(a);
+  if (a.chunks >= 8)
+    combine_kernel<T, NG, 8><<<unsigned(cols), NG * 64, 0, stream>>>(a);
+  else
+    combine_kernel<T, NG, 1><<<unsigned((cols + 7) / 8), NG * 64, 0, stream>>>(a);
   count_launches(1);
   return cudaGetLastError();
 }
@@ -207,9 +224,14 @@ cudaError_t launch_t(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t
   }
 }
 
-int64_t items_of(const PackedDev& kv, const SeqsDev& s, int cols, int chunks) {
-  const int64_t blocks = (int64_t(s.max_rows) * kv.G + cols - 1) / cols;
-  return int64_t(kv.L) * s.R * kv.Hkv * blocks * chunks;
+// Column blocks of the request with most rows. tcgen05: pairs of column tiles and a rank for
+// blocks with one.
+int64_t blocks_of(const PackedDev& kv, const SeqsDev& s, int kernel) {
+  const int64_t cols = int64_t(s.max_rows) * kv.G;
+  return kernel == kAttnTc ? (cols + 127) / 128 / 2 + 1 : (cols + kCols - 1) / kCols;
+}
+int64_t items_of(const PackedDev& kv, const SeqsDev& s, int kernel, int chunks) {
+  return int64_t(kv.L) * s.R * kv.Hkv * blocks_of(kv, s, kernel) * chunks;
 }
 
 // (reference, sum) of every chunk and (row, head), to a multiple of 16 bytes.
@@ -227,17 +249,33 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   const int most = int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
   const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
   p.kernel = !mma ? kAttnSimt : int64_t(s.max_rows) * kv.G > TC_FROM ? kAttnTc : kAttnMma;
-  p.cols = p.kernel == kAttnTc ? 256 : kCols;
-  // An SM holds two CTAs (tcgen05: one). One request: one wave of equal chunks. More: four
-  // CTAs for each place, so that contexts of unequal lengths fill it. At least 256 keys each.
-  const int64_t items = std::max<int64_t>(1, items_of(kv, s, p.cols, 1)), places = p.kernel == kAttnTc ? 152 : 2 * 152;
-  const int64_t even = s.R == 1 ? places / items : (4 * places + items - 1) / items;
-  const int64_t want = std::min<int64_t>(even, (most + 255) / 256);
-  p.chunks = int(std::max<int64_t>(1, want));
+  const int64_t largest = std::max(1, (most + 255) / 256);
+  if (p.kernel == kAttnTc) {
+    // One CTA per SM: the number of chunks with the least time by a model of one pass, 6 us for
+    // a CTA and 1.8 us for 128 keys of two column tiles, and of the join, 12 bytes a partial
+    // value at 5 TB/s after a launch of 5 us.
+    int64_t blocks = 0;
+    for (int r = 0; r < s.R; ++r)
+      blocks += (int64_t(s.row_off_host[r + 1] - s.row_off_host[r]) * kv.G + 255) / 256;
+    const double items = double(kv.L) * kv.Hkv * blocks, values = double(kv.L) * s.T * kv.Hq * kv.d;
+    double best = 0;
+    for (int64_t c = 1; c <= std::min<int64_t>(largest, 64); ++c) {
+      const double waves = std::ceil(items * c / 152.);
+      const double us = waves * (6. + 1.8 / 128. * most / c) + (c > 1 ? 5. + c * values * 12. / 5e6 : 0.);
+      if (c == 1 || us < best) best = us, p.chunks = int(c);
+    }
+  } else {
+    // An SM holds two CTAs. One request: one wave of equal chunks. More: eight CTAs for each
+    // place, so that contexts of unequal lengths fill it (64 requests of 2-30k tokens: four 186,
+    // eight 180, sixteen 190 us). At least 256 keys each.
+    const int64_t items = std::max<int64_t>(1, items_of(kv, s, p.kernel, 1)), places = 2 * 152;
+    const int64_t even = s.R == 1 ? places / items : (8 * places + items - 1) / items;
+    p.chunks = int(std::max<int64_t>(1, std::min(even, largest)));
+  }
   p.chunk = std::max(256, (most + p.chunks - 1) / p.chunks);
   p.chunk = (p.chunk + 255) / 256 * 256;
   p.chunks = std::max(1, (most + p.chunk - 1) / p.chunk);
-  p.items = items_of(kv, s, p.cols, p.chunks);
+  p.items = items_of(kv, s, p.kernel, p.chunks);
   if (p.chunks > 1)
     p.scratch = stats_bytes(kv, s, p.chunks) + size_t(p.chunks) * kv.L * s.T * kv.Hq * size_t(kv.d) * sizeof(float);
   return p;
@@ -247,7 +285,7 @@ cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const Pack
                                const RowsDev& q, float scale, const int32_t* limits, const RowsDev& out,
                                float* lse, void* scratch, int32_t* status, cudaStream_t stream) {
   AttnArgs a{kv, s, q, out, lse, limits, scale, plan.chunk, plan.chunks, 0, nullptr, nullptr, status};
-  a.col_blocks = int((int64_t(s.max_rows) * kv.G + plan.cols - 1) / plan.cols);
+  a.col_blocks = int(blocks_of(kv, s, plan.kernel));
   a.part_ml = static_cast<float2*>(scratch);
   a.part_o = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats_bytes(kv, s, plan.chunks));
   return dtype == CONDUIT_BF16 ? launch_t<__nv_bfloat16>(a, plan, stream) : launch_t<float>(a, plan, stream);

@@ -26,11 +26,8 @@ struct Item {
   int l, r, g, cb, chunk, t0, n, len;
 };
 
-template <int kBlockCols>
-__device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
-  uint32_t x = blockIdx.x;
-  it->cb = int(x % uint32_t(a.col_blocks));
-  x /= uint32_t(a.col_blocks);
+// The chunk, KV head, request and layer of unit x, and the request's rows and length.
+__device__ __forceinline__ void decode(const AttnArgs& a, uint32_t x, Item* it) {
   it->chunk = int(x % uint32_t(a.chunks));
   x /= uint32_t(a.chunks);
   it->g = int(x % uint32_t(a.kv.Hkv));
@@ -40,7 +37,13 @@ __device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
   it->t0 = a.s.row_off[it->r];
   it->n = a.s.row_off[it->r + 1] - it->t0;
   it->len = cached_len(a.s, a.kv.capacity(), it->r, a.status, threadIdx.x == 0);
-  if (it->cb * kBlockCols >= it->n * a.kv.G) return false;
+}
+
+// Column blocks of kCols, side by side so that they share the keys in L2.
+__device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
+  it->cb = int(blockIdx.x % uint32_t(a.col_blocks));
+  decode(a, blockIdx.x / uint32_t(a.col_blocks), it);
+  if (it->cb * kCols >= it->n * a.kv.G) return false;
   return it->chunk == 0 || it->chunk * a.chunk < it->len;
 }
 
@@ -52,9 +55,12 @@ __device__ __forceinline__ int limit_of(const AttnArgs& a, const Item& it, int j
   return min(max(lim, 0), it.len);
 }
 
-// Page of token j of request r, clamped into the pool (out of range: flagged).
-__device__ __forceinline__ int page_of(const AttnArgs& a, int r, int j) {
-  const int id = a.kv.page_table[int64_t(r) * a.kv.max_pages + (j >> a.kv.page_shift)];
+// Page of token j of request r as the table has it, and the same clamped into the pool
+// (out of range: flagged). Two steps, so that a lookup can be under way before its use.
+__device__ __forceinline__ int page_entry(const AttnArgs& a, int r, int j) {
+  return a.kv.page_table[int64_t(r) * a.kv.max_pages + (j >> a.kv.page_shift)];
+}
+__device__ __forceinline__ int page_in_pool(const AttnArgs& a, int id) {
   if (id >= 0 && id < a.kv.P) return id;
   flag_status(a.status, CONDUIT_FLAG_INDEX);
   return 0;

@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[kWarps][kStages];
   Item it;
-  if (!item_of<kCols>(a, &it)) return;
+  if (!item_of(a, &it)) return;
   const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int c = lane & 3, q = lane >> 2;
   // a row of the logits' accumulator is the token key_lo (+ 8) of its half tile; with this
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   // the page of this lane's run in a tile, looked up one fill ahead
   auto page_in = [&](int n) {
     const int j = k0 + (w + n * kWarps) * kTile + at_tile;
-    return n < mine && j < k1 && at_tile < kTile ? page_of(a, it.r, j) : 0;
+    return n < mine && j < k1 && at_tile < kTile ? page_entry(a, it.r, j) : 0;
   };
   int next_page = page_in(0);
   auto fill = [&](int n) {
@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     __syncwarp();
     if (lane < 4 * runs) {
       const int j = kb + at_tile, row = j & ((1 << a.kv.page_shift) - 1);
-      bulk_load(dst + stage * kBox, from + next_page * page_stride + row * row_bytes, row_bytes << run_shift,
+      bulk_load(dst + stage * kBox, from + page_in_pool(a, next_page) * page_stride + row * row_bytes, row_bytes << run_shift,
                 &full[w][stage]);
     }
     next_page = page_in(n + 1);

@@ -7,10 +7,12 @@
 // Shape. A CTA holds two tiles of 128 columns (A and B: rows of the call times query
 // heads of one KV head) and walks over the keys in tiles of 128. Each key tile is
 // unpacked once into shared memory for both. Roles (512 threads):
-//   warps 0-3, 4-7  softmax of A and of B: a thread owns a column and all 128 keys
-//   warps 8-11      unpack: four lanes a token, a word of eight codes at a time
-//   warp 12         bulk copies of page runs into two small buffers, keys and values
-//   warp 13         MMAs: P_x(t) V(t), then S_x(t + 1), for x = A, B; one lane issues
+//   warp 0            MMAs: P_x(t) V(t), then S_x(t + 1), for x = A, B; one lane issues.
+//                     The first warp, because the schedulers favour it: as warp 13 it took
+//                     120 cycles to issue an MMA of 64
+//   warp 1            bulk copies of page runs into a small ring, keys and values in turn
+//   warps 4-7         unpack: four lanes a token, a word of eight codes at a time
+//   warps 8-11, 12-15 softmax of A and of B: a thread owns a column and all 128 keys
 // One column tile's softmax runs beside the other's MMAs. MMAs of one thread complete in
 // order, so S_x(t + 1) may overwrite P_x(t), and S_x(t + 1) says that P_x(t) V(t) is done.
 // The dims of keys and queries are permuted alike (a word's nibbles come out as dims
@@ -25,13 +27,14 @@
 namespace conduit {
 namespace {
 
-constexpr int kThreads = 512;                 // warps 14 and 15 only give up registers
+constexpr int kThreads = 512;                 // warps 2 and 3 only give up registers
 constexpr int kKeys = 128;                    // keys of a tile
 constexpr int kTileCols = 128;                // columns of a tile
 constexpr int kTcCols = 2 * kTileCols;
-constexpr int kUnpackWarp = 8, kLoadWarp = 12, kMmaWarp = 13;
+constexpr int kMmaWarp = 0, kLoadWarp = 1, kUnpackWarp = 4, kSoftWarp = 8;
 constexpr uint32_t kBlock = 128 * 128;        // 128 rows of 64 fp16, swizzled
 constexpr uint32_t kSCols = 128, kPCol = 64, kOCol = 256;
+constexpr int kRing = 3;                      // packed keys and values in turn
 constexpr float kSlack = 8.f;                 // as in packed_attn_mma.cu
 
 template <int NG>
@@ -39,11 +42,11 @@ struct Sizes {
   static constexpr int D = 32 * NG;
   static constexpr uint32_t kTile = (D + 63) / 64 * kBlock;  // a query, key or value tile
   static constexpr uint32_t kRaw = kKeys * (D / 2 + D / 8);   // packed keys (or values) of a tile
-  static constexpr uint32_t kSmem = 1024 + 6 * kTile + 2 * kRaw;
+  static constexpr uint32_t kSmem = 1024 + 6 * kTile + kRing * kRaw;
 };
 
 struct Bars {
-  uint64_t raw_full[2], raw_free[2];    // packed keys, packed values
+  uint64_t raw_full[kRing], raw_free[kRing];
   uint64_t k_full[2], k_free[2], v_full[2], v_free[2];
   uint64_t q_full, s_full[2], p_full[2], o_full[2], drained;
 };
@@ -77,6 +80,89 @@ __device__ __forceinline__ void give_up(const AttnArgs& a, volatile int* abort, 
   *abort = 1;
 }
 
+// The item of this CTA: a.col_blocks - 1 ranks of blocks with two column tiles, then one rank
+// of blocks with one.
+__device__ __forceinline__ bool tc_item(const AttnArgs& a, Item* it) {
+  const uint32_t pairs = a.col_blocks - 1, units = uint32_t(a.chunks) * a.kv.Hkv * a.s.R * a.kv.L;
+  const bool single = blockIdx.x >= units * pairs;
+  uint32_t x = single ? blockIdx.x - units * pairs : blockIdx.x / pairs;
+  const int rank = single ? 0 : int(blockIdx.x % pairs);
+  decode(a, x, it);
+  const int tiles = (it->n * a.kv.G + kTileCols - 1) / kTileCols;  // column tiles of the request
+  it->cb = single ? tiles / 2 : rank;
+  if (single ? !(tiles & 1) : rank >= tiles / 2) return false;
+  return it->chunk == 0 || it->chunk * a.chunk < it->len;
+}
+
+// One lane's share of a token's values. kEdge: the tile holds tokens that some column does
+// not see. Their weight there is 0, and 0 times NaN must not be: a parameter pair that is not
+// finite becomes 0 and its first token is noted for the group.
+template <int NG, bool kEdge>
+__device__ __forceinline__ void unpack_values(uint8_t* tile, const uint8_t* box, int token, int c, int kb, int k1,
+                                              int least, int* poison) {
+  constexpr int D = 32 * NG;
+  const uint8_t* row = box + token * (D / 2);
+  uint32_t w[NG], p[NG];
+  if constexpr (NG == 3) {  // words c, c + 4, c + 8
+#pragma unroll
+    for (int n = 0; n < NG; ++n) w[n] = *reinterpret_cast<const uint32_t*>(row + 4 * (4 * n + c));
+  } else {  // words NG c on
+    load_words<NG>(row + c * (D / 8), w);
+  }
+  load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), p);
+  if (kEdge) {
+    const int j = kb + token;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      if (j >= least && j < k1 && !finite_pair(p[g])) atomicMin(&poison[g], j), p[g] = 0;
+      if (j >= k1) p[g] = 0;
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NG; ++n) {
+    // word ch of the row: the groups g0 and g1 side by side
+    int ch = NG * c + n;
+    uint32_t word = w[n], p0 = p[2 * n % NG], p1 = p[(2 * n + 1) % NG];
+    if constexpr (NG == 4) {  // the lanes of a token in different banks
+      ch = 4 * c + (n ^ (c & 2));
+      word = c & 2 ? w[n ^ 2] : w[n];
+    } else if constexpr (NG == 3) {
+      ch = 4 * n + c;
+      const int g0 = 2 * ch % 3, g1 = (2 * ch + 1) % 3;
+      p0 = g0 == 0 ? p[0] : g0 == 1 ? p[1] : p[2];
+      p1 = g1 == 0 ? p[0] : g1 == 1 ? p[1] : p[2];
+    }
+    *reinterpret_cast<uint4*>(tile + (ch >> 3) * kBlock + tc::sw128_offset(token, ch & 7)) =
+        values8(word, u2h(__byte_perm(p0, p1, 0x5410)), u2h(__byte_perm(p0, p1, 0x7632)));
+  }
+}
+
+// Weights 2^(s up + down) of the 128 logits at sb: packed into p, summed into add; returns the
+// largest logit (unscaled). kEdge: only the first `left` are seen.
+template <bool kEdge>
+__device__ __forceinline__ float weigh(uint32_t sb, float2 up, float2 down, int left, uint32_t (&p)[4][16], float2* add) {
+  float top = -INFINITY;
+  *add = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    float s[32];
+    tc::tmem_ld32(sb + 32 * b, s);
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      if (kEdge) {
+        if (32 * b + e >= left) s[e] = -INFINITY;
+        if (32 * b + e + 1 >= left) s[e + 1] = -INFINITY;
+      }
+      top = tc::fmax3(top, s[e], s[e + 1]);
+      const float2 y = tc::ffma2(make_float2(s[e], s[e + 1]), up, down);
+      const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
+      *add = tc::fadd2(*add, w);
+      p[b][e / 2] = h2u(__float22half2_rn(w));
+    }
+  }
+  return top;
+}
+
 template <int NG>
 __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   using Z = Sizes<NG>;
@@ -85,17 +171,20 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   __shared__ Bars bars;
   __shared__ uint32_t tmem_slot;
   __shared__ int seen_most, seen_least, poison[NG], abort_flag;
+  // Blocks with two column tiles come first and those with one, which take 3/4 of the time, last.
   Item it;
-  if (!item_of<kTcCols>(a, &it)) return;
+  if (!tc_item(a, &it)) return;
   uint8_t* base = dynamic + (1024 - (tc::smem_u32(dynamic) & 1023u)) % 1024;
   uint8_t *qt = base, *kt = qt + 2 * Z::kTile, *vt = kt + 2 * Z::kTile, *raw = vt + 2 * Z::kTile;
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
   volatile int* abort = &abort_flag;
 
   if (tid == 0) {
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kRing; ++s) {
       tc::mbar_init(&bars.raw_full[s], 1);
       tc::mbar_init(&bars.raw_free[s], 4);
+    }
+    for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&bars.k_full[s], 4);
       tc::mbar_init(&bars.v_full[s], 4);
       tc::mbar_init(&bars.k_free[s], 1);
@@ -115,10 +204,10 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   if (warp == kMmaWarp) tc::tmem_alloc(&tmem_slot, 512);
   __syncthreads();
   // keys that a column sees; columns past the last see all (their result is dropped)
-  const int col = it.cb * kTcCols + tid;
-  const bool live = tid < kTcCols && col < it.n * a.kv.G;
+  const int at = tid - 32 * kSoftWarp, col = it.cb * kTcCols + at;
+  const bool live = at >= 0 && col < it.n * a.kv.G;
   const int lim = live ? limit_of(a, it, col) : INT32_MAX;
-  if (warp < kUnpackWarp) {
+  if (warp >= kSoftWarp) {
     const int hi = __reduce_max_sync(0xffffffffu, live ? lim : 0), lo = __reduce_min_sync(0xffffffffu, lim);
     if (lane == 0) {
       atomicMax(&seen_most, hi);
@@ -134,10 +223,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   const int streams = it.cb * kTcCols + kTileCols < it.n * a.kv.G ? 2 : 1;
 
   // 128 registers a thread at launch: 2 x 88 + 2 x 168 per four warpgroups
-  if (warp >= kUnpackWarp)
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;" ::: "memory");
-  else
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;" ::: "memory");
+  if (warp < kSoftWarp) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;" ::: "memory");
   if (warp == kLoadWarp) {
     // ---------------------------------------------------------------- copies
     const int run_shift = min(7, a.kv.page_shift), run = 1 << run_shift;
@@ -146,31 +233,34 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     const uint32_t dst = tc::smem_u32(raw) + (part ? kKeys * (D / 2) : 0) + at_tile * row_bytes;
     const int64_t page_stride = a.kv.Hkv * a.kv.page_bytes;
     const uint8_t* head = a.kv.page(it.l, it.g, 0);
-    int issued[2] = {0, 0};
-    for (int t = 0; t < tiles; ++t) {
+    auto page_at = [&](int t) {  // page of this lane's run in tile t, looked up a tile ahead
+      const int j = k0 + t * kKeys + at_tile;
+      return at_tile < kKeys && j < k1 ? page_entry(a, it.r, j) : 0;
+    };
+    int issued = 0, next = page_at(0);
+    bool ok = true;
+    for (int t = 0; ok && t < tiles; ++t) {
       const int kb = k0 + t * kKeys, runs = (min(k1 - kb, kKeys) + run - 1) >> run_shift;
       const bool mine = lane < 2 * runs;
-      const int j = kb + at_tile, row = j & ((1 << a.kv.page_shift) - 1);
-      const uint8_t* page = mine ? head + page_of(a, it.r, j) * page_stride : head;
-      bool ok = true;
+      const int row = (kb + at_tile) & ((1 << a.kv.page_shift) - 1);
+      const uint8_t* page = head + (mine ? page_in_pool(a, next) : 0) * page_stride;
+      next = page_at(t + 1);
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
-        if (t > 0 && !(ok = wait_warp(&bars.raw_free[v], (t - 1) & 1, abort))) break;
-        if (lane == 0) tc::mbar_arrive_expect_tx(&bars.raw_full[v], uint32_t(runs << run_shift) * (D / 2 + D / 8));
+        const int slot = issued % kRing;
+        if (issued >= kRing && !(ok = wait_warp(&bars.raw_free[slot], (issued / kRing - 1) & 1, abort))) break;
+        if (lane == 0) tc::mbar_arrive_expect_tx(&bars.raw_full[slot], uint32_t(runs << run_shift) * (D / 2 + D / 8));
         __syncwarp();
         if (mine)
-          bulk_load(dst + v * Z::kRaw, page + (part ? a.kv.params(v, row) : a.kv.codes(v, row)), row_bytes << run_shift,
-                    &bars.raw_full[v]);
-        ++issued[v];
-      }
-      if (!ok) {
-        if (lane == 0) give_up(a, abort, CONDUIT_SITE_MMA);
-        break;
+          bulk_load(dst + slot * Z::kRaw, page + (part ? a.kv.params(v, row) : a.kv.codes(v, row)),
+                    row_bytes << run_shift, &bars.raw_full[slot]);
+        ++issued;
       }
     }
-    for (int v = 0; v < 2; ++v)  // the last copies (all have landed unless a role gave up)
-      if (issued[v]) tc::mbar_wait(&bars.raw_full[v], (issued[v] - 1) & 1);
-  } else if (warp >= kUnpackWarp && warp < kLoadWarp) {
+    if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_MMA);
+    for (int n = max(0, issued - kRing); n < issued; ++n)  // the last copies (all have landed unless a role gave up)
+      tc::mbar_wait(&bars.raw_full[n % kRing], (n / kRing) & 1);
+  } else if (warp >= kUnpackWarp) {
     // ---------------------------------------------------------------- unpack
     // Four lanes a token. Keys: the two tokens of eight lanes are four apart, so that their
     // chunks fall into different banks of the swizzled tile; values: next to each other.
@@ -178,7 +268,9 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     const int first = 32 * (warp - kUnpackWarp) + (i8 & 1) * 4 + (i8 >> 1);
     for (int t = 0; t < tiles; ++t) {
       const int kb = k0 + t * kKeys, stage = t & 1;
-      bool ok = wait_warp(&bars.raw_full[0], t & 1, abort);
+      int slot = 2 * t % kRing;
+      const uint8_t* box = raw + slot * Z::kRaw;
+      bool ok = wait_warp(&bars.raw_full[slot], (2 * t / kRing) & 1, abort);
       if (ok && t >= 2) ok = wait_warp(&bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
       if (!ok) {
         if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
@@ -189,8 +281,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       for (int i = 0; i < 4; ++i) {
         const int token = first + 8 * i;
         uint32_t w[NG], p[NG];
-        load_words<NG>(raw + token * (D / 2) + c * (D / 8), w);
-        load_words<NG>(raw + kKeys * (D / 2) + token * (D / 8), p);
+        load_words<NG>(box + token * (D / 2) + c * (D / 8), w);
+        load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), p);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
           const int ch = 4 * g + c;
@@ -201,159 +293,162 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       tc::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        tc::mbar_arrive(&bars.raw_free[0]);
+        tc::mbar_arrive(&bars.raw_free[slot]);
         tc::mbar_arrive(&bars.k_full[stage]);
       }
-      ok = wait_warp(&bars.raw_full[1], t & 1, abort);
+      slot = (2 * t + 1) % kRing;
+      box = raw + slot * Z::kRaw;
+      ok = wait_warp(&bars.raw_full[slot], ((2 * t + 1) / kRing) & 1, abort);
       if (ok && t >= 2) ok = wait_warp(&bars.v_free[stage], ((t >> 1) - 1) & 1, abort);
       if (!ok) {
         if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
         break;
       }
       tile = vt + stage * Z::kTile;
-      const bool edge = kb + kKeys > least;
+      const int token0 = 32 * (warp - kUnpackWarp) + i8;
+      if (kb + kKeys > least) {  // some column does not see the whole tile
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) unpack_values<NG, true>(tile, box, token0 + 8 * i, c, kb, k1, least, poison);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int token = 32 * (warp - kUnpackWarp) + 8 * i + i8, j = kb + token;
-        const uint8_t* row = raw + Z::kRaw + token * (D / 2);
-        uint32_t w[NG], p[NG];
-        if constexpr (NG == 3) {  // words c, c + 4, c + 8
-#pragma unroll
-          for (int n = 0; n < NG; ++n) w[n] = *reinterpret_cast<const uint32_t*>(row + 4 * (4 * n + c));
-        } else {  // words NG c on
-          load_words<NG>(row + c * (D / 8), w);
-        }
-        load_words<NG>(raw + Z::kRaw + kKeys * (D / 2) + token * (D / 8), p);
-        if (edge) {
-          // tokens that some column does not see: their weight there is 0, and 0 times NaN must not be
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            if (j >= least && j < k1 && !finite_pair(p[g])) atomicMin(&poison[g], j), p[g] = 0;
-            if (j >= k1) p[g] = 0;
-          }
-        }
-#pragma unroll
-        for (int n = 0; n < NG; ++n) {
-          // word ch of the row: the groups g0 and g1 side by side
-          int ch = NG * c + n;
-          uint32_t word = w[n], p0 = p[2 * n % NG], p1 = p[(2 * n + 1) % NG];
-          if constexpr (NG == 4) {  // the lanes of a token in different banks
-            ch = 4 * c + (n ^ (c & 2));
-            word = c & 2 ? w[n ^ 2] : w[n];
-          } else if constexpr (NG == 3) {
-            ch = 4 * n + c;
-            const int g0 = 2 * ch % 3, g1 = (2 * ch + 1) % 3;
-            p0 = g0 == 0 ? p[0] : g0 == 1 ? p[1] : p[2];
-            p1 = g1 == 0 ? p[0] : g1 == 1 ? p[1] : p[2];
-          }
-          *reinterpret_cast<uint4*>(tile + (ch >> 3) * kBlock + tc::sw128_offset(token, ch & 7)) =
-              values8(word, u2h(__byte_perm(p0, p1, 0x5410)), u2h(__byte_perm(p0, p1, 0x7632)));
-        }
+        for (int i = 0; i < 4; ++i) unpack_values<NG, false>(tile, box, token0 + 8 * i, c, kb, k1, least, poison);
       }
       tc::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        tc::mbar_arrive(&bars.raw_free[1]);
+        tc::mbar_arrive(&bars.raw_free[slot]);
         tc::mbar_arrive(&bars.v_full[stage]);
       }
     }
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------------ MMAs
+    // the whole warp walks the schedule on values from one lane, so that the operands live in
+    // uniform registers
     const uint32_t leader = lane == 0;
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const int count = __shfl_sync(0xffffffffu, tiles, 0);
+    const bool both = __shfl_sync(0xffffffffu, streams, 0) == 2;
+    const uint32_t q_at = __shfl_sync(0xffffffffu, tc::smem_u32(qt), 0);
+    const uint32_t k_at = q_at + 2 * Z::kTile, v_at = k_at + 2 * Z::kTile;
     constexpr uint32_t idesc_s = idesc_f16(kTileCols, kKeys, false), idesc_o = idesc_f16(kTileCols, D, true);
-    const uint64_t dq = tc::desc_sw128(tc::smem_u32(qt));
-    auto score = [&](int x, int stage) {
-      const uint64_t dk = tc::desc_sw128(tc::smem_u32(kt) + stage * Z::kTile);
+    const uint64_t dq = tc::desc_sw128(q_at);
+    // S_x(t) = Q_x K(t)^T. With `last`, the values of tile t and the keys of tile t + 1 are waited
+    // for half-way: a wait costs 130 to 200 cycles, which the MMAs already issued cover.
+    bool ok = true;
+    auto score = [&](int x, int t, bool last) {
+      const int stage = t & 1;
+      const uint64_t dk = tc::desc_sw128(k_at + stage * Z::kTile);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
+        if (kk == D / 32 && last)
+          ok = wait_warp(&bars.v_full[stage], (t >> 1) & 1, abort) &&
+               (t + 1 == count || wait_warp(&bars.k_full[stage ^ 1], ((t + 1) >> 1) & 1, abort));
         const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
         tc::mma_bf16_if(leader, tm + x * kSCols, dq + ((x * Z::kTile) >> 4) + off, dk + off, idesc_s, kk > 0);
       }
       tc::mma_commit_if(leader, &bars.s_full[x]);
+      if (last) tc::mma_commit_if(leader, &bars.k_free[stage]);
     };
-    bool ok = tiles == 0 || wait_warp(&bars.q_full, 0, abort);
-    if (ok && tiles > 0 && (ok = wait_warp(&bars.k_full[0], 0, abort))) {
+    if (count > 0 && (ok = wait_warp(&bars.q_full, 0, abort) && wait_warp(&bars.k_full[0], 0, abort))) {
       tc::tc_fence_after();
-      for (int x = 0; x < streams; ++x) score(x, 0);
-      tc::mma_commit_if(leader, &bars.k_free[0]);
+      score(0, 0, !both);
+      if (both) score(1, 0, true);
     }
-    for (int t = 0; ok && t < tiles; ++t) {
-      const int stage = t & 1, next = stage ^ 1;
-      const bool more = t + 1 < tiles;
-      const uint64_t dv = tc::desc_sw128_mn(tc::smem_u32(vt) + stage * Z::kTile, kBlock);
-      if (!(ok = wait_warp(&bars.v_full[stage], (t >> 1) & 1, abort))) break;
-      if (more && !(ok = wait_warp(&bars.k_full[next], ((t + 1) >> 1) & 1, abort))) break;
-      for (int x = 0; x < streams; ++x) {
+    for (int t = 0; ok && t < count; ++t) {
+      const int stage = t & 1;
+      const bool more = t + 1 < count;
+      const uint64_t dv = tc::desc_sw128_mn(v_at + stage * Z::kTile, kBlock);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (x == 1 && !both) break;
         if (!(ok = wait_warp(&bars.p_full[x], t & 1, abort))) break;
         tc::tc_fence_after();
 #pragma unroll
         for (int kk = 0; kk < kKeys / 16; ++kk)
           tc::mma_bf16_ts_if(leader, tm + kOCol + x * kSCols, tm + x * kSCols + kPCol + kk * 8, dv + kk * (2048 >> 4),
                              idesc_o, t > 0 || kk > 0);
-        if (x + 1 == streams) tc::mma_commit_if(leader, &bars.v_free[stage]);
+        if (x == 1 || !both) tc::mma_commit_if(leader, &bars.v_free[stage]);
         if (more)
-          score(x, next);
+          score(x, t + 1, x == 1 || !both);
         else
           tc::mma_commit_if(leader, &bars.o_full[x]);
+        if (!ok) break;
       }
-      if (ok && more) tc::mma_commit_if(leader, &bars.k_free[next]);
     }
     if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_MMA);
     tc::mma_commit_if(leader, &bars.drained);  // every MMA issued above is done once this arrives
     tc::mbar_wait(&bars.drained, 0);
     __syncwarp();
-  } else if (warp < kUnpackWarp) {
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;" ::: "memory");
     // --------------------------------------------------------------- softmax
-    const int x = warp >> 2, row = tid & 127;
-    const int i = live ? col / a.kv.G : 0, h = live ? it.g * a.kv.G + col % a.kv.G : 0;
+    const int x = (warp - kSoftWarp) >> 2;
+    uint8_t* tile = qt + x * Z::kTile;  // this stream's queries, and at the end its rows on their way out
+    const int row0 = (warp & 3) * 32;   // this warp's columns of the tile
     float to_log2;
     {
-      // the column's query, scaled so that its largest lies in [256, 512), into the swizzled tile
-      const __nv_bfloat16* src =
-          static_cast<const __nv_bfloat16*>(a.q.p) + it.l * a.q.ls + int64_t(it.t0 + i) * a.q.rs + h * a.q.hs;
+      // Queries into the swizzled tile: 16 lanes a column, two columns at a time, each scaled by
+      // a power of two so that its largest lies in [256, 512).
+      constexpr int kUse = D / 8;  // lanes with eight dims of a column
+      const int part = lane & 15, side = lane >> 4;
       const bool wide = ((reinterpret_cast<uintptr_t>(a.q.p) | uint64_t(2 * (a.q.ls | a.q.rs | a.q.hs))) & 15u) == 0;
-      uint4 v[D / 8];
-      uint32_t top = 0;
+      to_log2 = 0.f;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        uint4 v[8];
 #pragma unroll
-      for (int b = 0; b < D / 8; ++b) {
-        if (!live) {
-          v[b] = make_uint4(0, 0, 0, 0);
-        } else if (wide) {
-          v[b] = *reinterpret_cast<const uint4*>(src + 8 * b);
-        } else {
-          __nv_bfloat16 e8[8];
+        for (int k = 0; k < 8; ++k) {
+          const int c = it.cb * kTcCols + x * kTileCols + row0 + 16 * half + 2 * k + side;
+          v[k] = make_uint4(0, 0, 0, 0);
+          if (part < kUse && c < it.n * a.kv.G) {
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.p) + it.l * a.q.ls +
+                                       int64_t(it.t0 + c / a.kv.G) * a.q.rs + (it.g * a.kv.G + c % a.kv.G) * a.q.hs + 8 * part;
+            if (wide) {
+              v[k] = *reinterpret_cast<const uint4*>(src);
+            } else {
+              __nv_bfloat16 e8[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) e8[e] = src[8 * b + e];
-          v[b] = *reinterpret_cast<uint4*>(e8);
+              for (int e = 0; e < 8; ++e) e8[e] = src[e];
+              v[k] = *reinterpret_cast<uint4*>(e8);
+            }
+          }
         }
-        const uint32_t w[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFF0000u, (w[e] & 0x7FFFu) << 16));  // |q| as fp32 bits
-      }
-      int shift = int(top >> 23) - 127 - 8;
-      if (top >= 0x7F800000u || top == 0) shift = 0;
-      // 2^-shift and 2^shift in two factors, each a normal number
-      const float f1 = __uint_as_float(uint32_t(127 - shift / 2) << 23);
-      const float f2 = __uint_as_float(uint32_t(127 - (shift - shift / 2)) << 23);
-      const float g1 = __uint_as_float(uint32_t(127 + shift / 2) << 23);
-      const float g2 = __uint_as_float(uint32_t(127 + (shift - shift / 2)) << 23);
-      to_log2 = fmaxf(a.scale * kLog2e * g1 * g2, 1.1754944e-38f);  // positive, so that a masked logit stays -inf
+        for (int k = 0; k < 8; ++k) {
+          const int row = row0 + 16 * half + 2 * k + side;
+          const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+          uint32_t top = 0;  // the largest |q| as fp32 bits
 #pragma unroll
-      for (int b = 0; b < D / 8; ++b) {
-        const uint32_t w[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
-        float f[8];
+          for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFF0000u, (w[e] & 0x7FFFu) << 16));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          f[2 * e] = __uint_as_float(w[e] << 16) * f1 * f2;
-          f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u) * f1 * f2;
+          for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          int shift = int(top >> 23) - 127 - 8;
+          if (top >= 0x7F800000u || top == 0) shift = 0;
+          // 2^-shift and 2^shift in two factors, each a normal number
+          const float f1 = __uint_as_float(uint32_t(127 - shift / 2) << 23);
+          const float f2 = __uint_as_float(uint32_t(127 - (shift - shift / 2)) << 23);
+          const float g1 = __uint_as_float(uint32_t(127 + shift / 2) << 23);
+          const float g2 = __uint_as_float(uint32_t(127 + (shift - shift / 2)) << 23);
+          // positive, so that a masked logit stays -inf under it; to the column's own lane
+          const float back = fmaxf(a.scale * kLog2e * g1 * g2, 1.1754944e-38f);
+          const float even = __shfl_sync(0xffffffffu, back, 0), odd = __shfl_sync(0xffffffffu, back, 16);
+          if (lane == 16 * half + 2 * k) to_log2 = even;
+          if (lane == 16 * half + 2 * k + 1) to_log2 = odd;
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f[2 * e] = __uint_as_float(w[e] << 16) * f1 * f2;
+            f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u) * f1 * f2;
+          }
+          uint4 y;  // in the order in which a word's nibbles unpack
+          y.x = h2u(__floats2half2_rn(f[0], f[4]));
+          y.y = h2u(__floats2half2_rn(f[1], f[5]));
+          y.z = h2u(__floats2half2_rn(f[2], f[6]));
+          y.w = h2u(__floats2half2_rn(f[3], f[7]));
+          if (part < kUse)
+            *reinterpret_cast<uint4*>(tile + (part >> 3) * kBlock + tc::sw128_offset(row, part & 7)) = y;
         }
-        uint4 y;  // in the order in which a word's nibbles unpack
-        y.x = h2u(__floats2half2_rn(f[0], f[4]));
-        y.y = h2u(__floats2half2_rn(f[1], f[5]));
-        y.z = h2u(__floats2half2_rn(f[2], f[6]));
-        y.w = h2u(__floats2half2_rn(f[3], f[7]));
-        *reinterpret_cast<uint4*>(qt + x * Z::kTile + (b >> 3) * kBlock + tc::sw128_offset(row, b & 7)) = y;
       }
       tc::fence_proxy_async_smem();
       __syncwarp();
@@ -376,26 +471,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       for (int pass = 0;; ++pass) {
         const float low = ref == -INFINITY ? 0.f : -ref;
         const float2 down = make_float2(low, low);
-        float top = -INFINITY;
-        add = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          float s[32];
-          tc::tmem_ld32(sb + 32 * b, s);
-          if (edge) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (32 * b + e >= left) s[e] = -INFINITY;
-          }
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            top = tc::fmax3(top, s[e], s[e + 1]);
-            const float2 y = tc::ffma2(make_float2(s[e], s[e + 1]), up, down);
-            const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
-            add = tc::fadd2(add, w);
-            p[b][e / 2] = h2u(__float22half2_rn(w));
-          }
-        }
+        float top = edge ? weigh<true>(sb, up, down, left, p, &add) : weigh<false>(sb, up, down, left, p, &add);
         top *= to_log2;
         if (pass || !__any_sync(0xffffffffu, top > ref + kSlack)) break;
         // the reference moves: what was summed so far is scaled, and the weights are taken again
@@ -427,11 +503,21 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     const float total = sum.x + sum.y;
     if (live) store_stats(a, it, col, ref, total);
     const float inv = a.chunks > 1 ? 1.f : total == 0.f ? 0.f : 1.f / total;
-    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out.p) + it.l * a.out.ls + int64_t(it.t0 + i) * a.out.rs + h * a.out.hs;
-    const bool by_four =
-        ((reinterpret_cast<uintptr_t>(a.out.p) | uint64_t(2 * (a.out.ls | a.out.rs | a.out.hs))) & 7u) == 0;
+    // The rows go out through the query tile (every product that read it is done), so that
+    // neighbouring lanes write neighbouring dims.
+    const bool partial = a.chunks > 1;
     const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
-    float* part = a.part_o + (it.chunk * cols + (int64_t(it.l) * a.s.T + it.t0 + i) * a.kv.Hq + h) * D;
+    const bool by_16 = ((reinterpret_cast<uintptr_t>(a.out.p) | uint64_t(2 * (a.out.ls | a.out.rs | a.out.hs))) & 15u) == 0;
+    const int row = row0 + lane;
+    // 16-byte chunk c of a row, in a place that spreads the rows over the banks
+    constexpr int kRowBytes = D == 64 ? 128 : 256;  // 128 rows fit the tile
+    auto chunk_at = [&](int r, int c) { return tile + r * kRowBytes + ((c ^ (r & 7)) << 4); };
+    auto row_of = [&](int r, int* i, int* h) {
+      const int c = it.cb * kTcCols + x * kTileCols + r;
+      *i = c / a.kv.G;
+      *h = it.g * a.kv.G + c % a.kv.G;
+      return c < it.n * a.kv.G;
+    };
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) {
       float o[32];
@@ -441,25 +527,53 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = 0.f;
       }
-      if (live) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-          // four neighbouring dims of group g: every other column of a word of the value rows
-          const int word = 4 * b + n / 2, hw = 2 * word + (n & 1), g = hw % NG, dim = 32 * g + 4 * (hw / NG);
-          float y[4];
+      for (int n = 0; n < 8; ++n) {
+        // four neighbouring dims of group g: every other column of a word of the value rows
+        const int word = 4 * b + n / 2, hw = 2 * word + (n & 1), g = hw % NG, dim = 32 * g + 4 * (hw / NG);
+        float y[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y[e] = o[8 * (n / 2) + 2 * e + (n & 1)] * inv;
-            if (poison[g] < lim) y[e] = NAN;  // a value that is not finite reaches the columns that see it
-          }
-          if (a.chunks > 1) {
-            *reinterpret_cast<float4*>(part + dim) = make_float4(y[0], y[1], y[2], y[3]);
-          } else if (by_four) {
-            __nv_bfloat162 z[2] = {__floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
-            *reinterpret_cast<uint2*>(to + dim) = *reinterpret_cast<uint2*>(z);
+        for (int e = 0; e < 4; ++e) {
+          y[e] = o[8 * (n / 2) + 2 * e + (n & 1)] * inv;
+          if (poison[g] < lim) y[e] = NAN;  // a value that is not finite reaches the columns that see it
+        }
+        if (partial) {  // a block's 32 dims, in the order in which they come
+          *reinterpret_cast<float4*>(chunk_at(row, n)) = make_float4(y[0], y[1], y[2], y[3]);
+        } else {
+          const __nv_bfloat162 z[2] = {__floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
+          *reinterpret_cast<uint2*>(chunk_at(row, dim / 8) + (dim & 4) * 2) = *reinterpret_cast<const uint2*>(z);
+        }
+      }
+      if (!partial) continue;
+      __syncwarp();
+#pragma unroll 1
+      for (int k = 0; k < 8; ++k) {  // four rows at a time, eight lanes a row
+        const int r = row0 + 4 * k + (lane >> 3), n = lane & 7;
+        const int hw = 2 * (4 * b + n / 2) + (n & 1), dim = 32 * (hw % NG) + 4 * (hw / NG);
+        int i, h;
+        if (row_of(r, &i, &h)) {
+          float* part = a.part_o + (it.chunk * cols + (int64_t(it.l) * a.s.T + it.t0 + i) * a.kv.Hq + h) * D;
+          *reinterpret_cast<float4*>(part + dim) = *reinterpret_cast<const float4*>(chunk_at(r, n));
+        }
+      }
+      __syncwarp();
+    }
+    if (!partial) {
+      __syncwarp();
+#pragma unroll 4
+      for (int k = 0; k < 16; ++k) {
+        const int r = row0 + 2 * k + (lane >> 4), c = lane & 15;
+        int i, h;
+        if (row_of(r, &i, &h) && c < D / 8) {
+          __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out.p) + it.l * a.out.ls + int64_t(it.t0 + i) * a.out.rs +
+                              h * a.out.hs + 8 * c;
+          const uint4 y = *reinterpret_cast<const uint4*>(chunk_at(r, c));
+          if (by_16) {
+            *reinterpret_cast<uint4*>(to) = y;
           } else {
+            const __nv_bfloat16* e8 = reinterpret_cast<const __nv_bfloat16*>(&y);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) to[dim + e] = __float2bfloat16_rn(y[e]);
+            for (int e = 0; e < 8; ++e) to[e] = e8[e];
           }
         }
       }
@@ -493,3 +607,4 @@ cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t
 }
 
 }  // namespace conduit
+
