@@ -11,7 +11,7 @@
 //                     The first warp, because the schedulers favour it: as warp 13 it took
 //                     120 cycles to issue an MMA of 64
 //   warp 1            bulk copies of page runs into a small ring, keys and values in turn
-//   warps 4-7         unpack: four lanes a token, a word of eight codes at a time
+//   warps 2-7         unpack: four lanes a token, a word of eight codes at a time
 //   warps 8-11, 12-15 softmax of A and of B: a thread owns a column and all 128 keys
 // One column tile's softmax runs beside the other's MMAs. MMAs of one thread complete in
 // order, so S_x(t + 1) may overwrite P_x(t), and S_x(t + 1) says that P_x(t) V(t) is done.
@@ -27,11 +27,11 @@
 namespace conduit {
 namespace {
 
-constexpr int kThreads = 512;                 // warps 2 and 3 only give up registers
+constexpr int kThreads = 512;
 constexpr int kKeys = 128;                    // keys of a tile
 constexpr int kTileCols = 128;                // columns of a tile
 constexpr int kTcCols = 2 * kTileCols;
-constexpr int kMmaWarp = 0, kLoadWarp = 1, kUnpackWarp = 4, kSoftWarp = 8;
+constexpr int kMmaWarp = 0, kLoadWarp = 1, kUnpackWarp = 2, kUnpackWarps = 6, kSoftWarp = 8;
 constexpr uint32_t kBlock = 128 * 128;        // 128 rows of 64 fp16, swizzled
 constexpr uint32_t kSCols = 128, kPCol = 64, kOCol = 256;
 constexpr int kRing = 3;                      // packed keys and values in turn
@@ -48,7 +48,7 @@ struct Sizes {
 struct Bars {
   uint64_t raw_full[kRing], raw_free[kRing];
   uint64_t k_full[2], k_free[2], v_full[2], v_free[2];
-  uint64_t q_full, s_full[2], p_full[2], o_full[2], drained;
+  uint64_t q_full, s_full[2], p_full[2], o_full[2], joined, drained;
 };
 
 // The eight values of a word: nibbles (0, 4), (1, 5), (2, 6), (3, 7).
@@ -92,6 +92,21 @@ __device__ __forceinline__ bool tc_item(const AttnArgs& a, Item* it) {
   it->cb = single ? tiles / 2 : rank;
   if (single ? !(tiles & 1) : rank >= tiles / 2) return false;
   return it->chunk == 0 || it->chunk * a.chunk < it->len;
+}
+
+// One lane's share of a token's keys: words NG c on, a word's values in chunk 4 g + c.
+template <int NG>
+__device__ __forceinline__ void unpack_keys(uint8_t* tile, const uint8_t* box, int token, int c) {
+  constexpr int D = 32 * NG;
+  uint32_t w[NG], p[NG];
+  load_words<NG>(box + token * (D / 2) + c * (D / 8), w);
+  load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), p);
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const int ch = 4 * g + c;
+    *reinterpret_cast<uint4*>(tile + (ch >> 3) * kBlock + tc::sw128_offset(token, ch & 7)) =
+        values8(w[g], u2h(__byte_perm(p[g], p[g], 0x1010)), u2h(__byte_perm(p[g], p[g], 0x3232)));
+  }
 }
 
 // One lane's share of a token's values. kEdge: the tile holds tokens that some column does
@@ -171,9 +186,12 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   __shared__ Bars bars;
   __shared__ uint32_t tmem_slot;
   __shared__ int seen_most, seen_least, poison[NG], abort_flag;
-  // Blocks with two column tiles come first and those with one, which take 3/4 of the time, last.
+  __shared__ float2 of_b[kTileCols];  // split: B's (reference, sum)
+  // Blocks with two column tiles come first and those with one, which take half of the time, last.
   Item it;
   if (!tc_item(a, &it)) return;
+  // One column tile: A takes its even key tiles and B its odd ones, joined at the end.
+  const bool split = it.cb * kTcCols + kTileCols >= it.n * a.kv.G;
   uint8_t* base = dynamic + (1024 - (tc::smem_u32(dynamic) & 1023u)) % 1024;
   uint8_t *qt = base, *kt = qt + 2 * Z::kTile, *vt = kt + 2 * Z::kTile, *raw = vt + 2 * Z::kTile;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
@@ -194,6 +212,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       tc::mbar_init(&bars.o_full[s], 1);
     }
     tc::mbar_init(&bars.q_full, 8);
+    tc::mbar_init(&bars.joined, 4);
     tc::mbar_init(&bars.drained, 1);
     tc::fence_barrier_init();
     seen_most = 0;
@@ -204,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   if (warp == kMmaWarp) tc::tmem_alloc(&tmem_slot, 512);
   __syncthreads();
   // keys that a column sees; columns past the last see all (their result is dropped)
-  const int at = tid - 32 * kSoftWarp, col = it.cb * kTcCols + at;
+  const int at = tid - 32 * kSoftWarp, col = it.cb * kTcCols + (split ? at & (kTileCols - 1) : at);
   const bool live = at >= 0 && col < it.n * a.kv.G;
   const int lim = live ? limit_of(a, it, col) : INT32_MAX;
   if (warp >= kSoftWarp) {
@@ -220,7 +239,6 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   const uint32_t tmem = tmem_slot;
   const int least = seen_least, k0 = it.chunk * a.chunk, k1 = min(k0 + a.chunk, seen_most);
   const int tiles = k1 > k0 ? (k1 - k0 + kKeys - 1) / kKeys : 0;
-  const int streams = it.cb * kTcCols + kTileCols < it.n * a.kv.G ? 2 : 1;
 
   // 128 registers a thread at launch: 2 x 88 + 2 x 168 per four warpgroups
   if (warp < kSoftWarp) {
@@ -260,64 +278,39 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_MMA);
     for (int n = max(0, issued - kRing); n < issued; ++n)  // the last copies (all have landed unless a role gave up)
       tc::mbar_wait(&bars.raw_full[n % kRing], (n / kRing) & 1);
-  } else if (warp >= kUnpackWarp) {
+  } else if (warp != kMmaWarp) {
     // ---------------------------------------------------------------- unpack
-    // Four lanes a token. Keys: the two tokens of eight lanes are four apart, so that their
-    // chunks fall into different banks of the swizzled tile; values: next to each other.
+    // A unit is a quarter (32 tokens) of a tile's keys, then of its values; six warps take
+    // them in turn. Four lanes a token. Keys: the two tokens of eight lanes are four apart, so
+    // that their chunks fall into different banks of the swizzled tile; values: side by side.
     const int c = lane & 3, i8 = lane >> 2;
-    const int first = 32 * (warp - kUnpackWarp) + (i8 & 1) * 4 + (i8 >> 1);
-    for (int t = 0; t < tiles; ++t) {
-      const int kb = k0 + t * kKeys, stage = t & 1;
-      int slot = 2 * t % kRing;
+    for (int n = warp - kUnpackWarp; n < 8 * tiles; n += kUnpackWarps) {
+      const int t = n >> 3, v = (n >> 2) & 1, token0 = 32 * (n & 3), stage = t & 1;
+      const int load = 2 * t + v, slot = load % kRing;
       const uint8_t* box = raw + slot * Z::kRaw;
-      bool ok = wait_warp(&bars.raw_full[slot], (2 * t / kRing) & 1, abort);
-      if (ok && t >= 2) ok = wait_warp(&bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
+      bool ok = wait_warp(&bars.raw_full[slot], (load / kRing) & 1, abort);
+      if (ok && t >= 2) ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
       if (!ok) {
         if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
         break;
       }
-      uint8_t* tile = kt + stage * Z::kTile;
+      uint8_t* tile = (v ? vt : kt) + stage * Z::kTile;
+      const int kb = k0 + t * kKeys;
+      if (!v) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int token = first + 8 * i;
-        uint32_t w[NG], p[NG];
-        load_words<NG>(box + token * (D / 2) + c * (D / 8), w);
-        load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), p);
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const int ch = 4 * g + c;
-          *reinterpret_cast<uint4*>(tile + (ch >> 3) * kBlock + tc::sw128_offset(token, ch & 7)) =
-              values8(w[g], u2h(__byte_perm(p[g], p[g], 0x1010)), u2h(__byte_perm(p[g], p[g], 0x3232)));
-        }
-      }
-      tc::fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        tc::mbar_arrive(&bars.raw_free[slot]);
-        tc::mbar_arrive(&bars.k_full[stage]);
-      }
-      slot = (2 * t + 1) % kRing;
-      box = raw + slot * Z::kRaw;
-      ok = wait_warp(&bars.raw_full[slot], ((2 * t + 1) / kRing) & 1, abort);
-      if (ok && t >= 2) ok = wait_warp(&bars.v_free[stage], ((t >> 1) - 1) & 1, abort);
-      if (!ok) {
-        if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
-        break;
-      }
-      tile = vt + stage * Z::kTile;
-      const int token0 = 32 * (warp - kUnpackWarp) + i8;
-      if (kb + kKeys > least) {  // some column does not see the whole tile
+        for (int i = 0; i < 4; ++i) unpack_keys<NG>(tile, box, token0 + (i8 & 1) * 4 + (i8 >> 1) + 8 * i, c);
+      } else if (kb + kKeys > least) {  // some column does not see the whole tile
 #pragma unroll 1
-        for (int i = 0; i < 4; ++i) unpack_values<NG, true>(tile, box, token0 + 8 * i, c, kb, k1, least, poison);
+        for (int i = 0; i < 4; ++i) unpack_values<NG, true>(tile, box, token0 + i8 + 8 * i, c, kb, k1, least, poison);
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) unpack_values<NG, false>(tile, box, token0 + 8 * i, c, kb, k1, least, poison);
+        for (int i = 0; i < 4; ++i) unpack_values<NG, false>(tile, box, token0 + i8 + 8 * i, c, kb, k1, least, poison);
       }
       tc::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
         tc::mbar_arrive(&bars.raw_free[slot]);
-        tc::mbar_arrive(&bars.v_full[stage]);
+        tc::mbar_arrive(v ? &bars.v_full[stage] : &bars.k_full[stage]);
       }
     }
   } else if (warp == kMmaWarp) {
@@ -326,50 +319,52 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     // uniform registers
     const uint32_t leader = lane == 0;
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-    const int count = __shfl_sync(0xffffffffu, tiles, 0);
-    const bool both = __shfl_sync(0xffffffffu, streams, 0) == 2;
+    const int all = __shfl_sync(0xffffffffu, tiles, 0);
+    const bool halves = __shfl_sync(0xffffffffu, int(split), 0) != 0;
     const uint32_t q_at = __shfl_sync(0xffffffffu, tc::smem_u32(qt), 0);
     const uint32_t k_at = q_at + 2 * Z::kTile, v_at = k_at + 2 * Z::kTile;
     constexpr uint32_t idesc_s = idesc_f16(kTileCols, kKeys, false), idesc_o = idesc_f16(kTileCols, D, true);
     const uint64_t dq = tc::desc_sw128(q_at);
-    // S_x(t) = Q_x K(t)^T. With `last`, the values of tile t and the keys of tile t + 1 are waited
-    // for half-way: a wait costs 130 to 200 cycles, which the MMAs already issued cover.
+    // S_x = Q K^T for the key tile `tile`; a tile's keys and values are waited for by the first
+    // stream that reads it and freed by the last.
     bool ok = true;
-    auto score = [&](int x, int t, bool last) {
-      const int stage = t & 1;
+    auto score = [&](int x, int tile) {
+      const int stage = tile & 1;
+      if (halves || x == 0) {
+        if (!(ok = wait_warp(&bars.k_full[stage], (tile >> 1) & 1, abort))) return;
+        tc::tc_fence_after();
+      }
       const uint64_t dk = tc::desc_sw128(k_at + stage * Z::kTile);
+      const uint64_t dx = dq + (halves ? 0 : (x * Z::kTile) >> 4);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        if (kk == D / 32 && last)
-          ok = wait_warp(&bars.v_full[stage], (t >> 1) & 1, abort) &&
-               (t + 1 == count || wait_warp(&bars.k_full[stage ^ 1], ((t + 1) >> 1) & 1, abort));
         const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
-        tc::mma_bf16_if(leader, tm + x * kSCols, dq + ((x * Z::kTile) >> 4) + off, dk + off, idesc_s, kk > 0);
+        tc::mma_bf16_if(leader, tm + x * kSCols, dx + off, dk + off, idesc_s, kk > 0);
       }
       tc::mma_commit_if(leader, &bars.s_full[x]);
-      if (last) tc::mma_commit_if(leader, &bars.k_free[stage]);
+      if (halves || x == 1) tc::mma_commit_if(leader, &bars.k_free[stage]);
     };
-    if (count > 0 && (ok = wait_warp(&bars.q_full, 0, abort) && wait_warp(&bars.k_full[0], 0, abort))) {
-      tc::tc_fence_after();
-      score(0, 0, !both);
-      if (both) score(1, 0, true);
+    const int count[2] = {halves ? (all + 1) / 2 : all, halves ? all / 2 : all};
+    if (all > 0 && (ok = wait_warp(&bars.q_full, 0, abort))) {
+      score(0, 0);
+      if (ok && count[1] > 0) score(1, halves ? 1 : 0);
     }
-    for (int t = 0; ok && t < count; ++t) {
-      const int stage = t & 1;
-      const bool more = t + 1 < count;
-      const uint64_t dv = tc::desc_sw128_mn(v_at + stage * Z::kTile, kBlock);
+    for (int t = 0; ok && t < count[0]; ++t) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        if (x == 1 && !both) break;
+        if (t >= count[x]) break;
+        const int tile = halves ? 2 * t + x : t, stage = tile & 1;
+        if ((halves || x == 0) && !(ok = wait_warp(&bars.v_full[stage], (tile >> 1) & 1, abort))) break;
         if (!(ok = wait_warp(&bars.p_full[x], t & 1, abort))) break;
         tc::tc_fence_after();
+        const uint64_t dv = tc::desc_sw128_mn(v_at + stage * Z::kTile, kBlock);
 #pragma unroll
         for (int kk = 0; kk < kKeys / 16; ++kk)
           tc::mma_bf16_ts_if(leader, tm + kOCol + x * kSCols, tm + x * kSCols + kPCol + kk * 8, dv + kk * (2048 >> 4),
                              idesc_o, t > 0 || kk > 0);
-        if (x == 1 || !both) tc::mma_commit_if(leader, &bars.v_free[stage]);
-        if (more)
-          score(x, t + 1, x == 1 || !both);
+        if (halves || x == 1) tc::mma_commit_if(leader, &bars.v_free[stage]);
+        if (t + 1 < count[x])
+          score(x, halves ? tile + 2 : tile + 1);
         else
           tc::mma_commit_if(leader, &bars.o_full[x]);
         if (!ok) break;
@@ -384,7 +379,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 168;" ::: "memory");
     // --------------------------------------------------------------- softmax
     const int x = (warp - kSoftWarp) >> 2;
-    uint8_t* tile = qt + x * Z::kTile;  // this stream's queries, and at the end its rows on their way out
+    const bool owner = !split || x == 0;  // of the column: its query and its output row
+    uint8_t* tile = qt + (split ? 0 : x) * Z::kTile;  // the queries, and at the end the rows on their way out
     const int row0 = (warp & 3) * 32;   // this warp's columns of the tile
     float to_log2;
     {
@@ -399,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
         uint4 v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int c = it.cb * kTcCols + x * kTileCols + row0 + 16 * half + 2 * k + side;
+          const int c = it.cb * kTcCols + (split ? 0 : x * kTileCols) + row0 + 16 * half + 2 * k + side;
           v[k] = make_uint4(0, 0, 0, 0);
           if (part < kUse && c < it.n * a.kv.G) {
             const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.p) + it.l * a.q.ls +
@@ -446,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
           y.y = h2u(__floats2half2_rn(f[1], f[5]));
           y.z = h2u(__floats2half2_rn(f[2], f[6]));
           y.w = h2u(__floats2half2_rn(f[3], f[7]));
-          if (part < kUse)
+          if (part < kUse && owner)
             *reinterpret_cast<uint4*>(tile + (part >> 3) * kBlock + tc::sw128_offset(row, part & 7)) = y;
         }
       }
@@ -460,12 +456,13 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     float2 sum = make_float2(0.f, 0.f);
     const float2 up = make_float2(to_log2, to_log2);
     bool ok = true;
-    const int count = x < streams ? tiles : 0;
+    const int count = split ? (tiles + 1 - x) / 2 : tiles;
     for (int t = 0; t < count; ++t) {
       if (!(ok = wait_warp(&bars.s_full[x], t & 1, abort))) break;
       tc::tc_fence_after();
-      const int left = lim - (k0 + t * kKeys);  // keys of the tile that the column sees
-      const bool edge = k0 + (t + 1) * kKeys > least;
+      const int kb = k0 + (split ? 2 * t + x : t) * kKeys;
+      const int left = lim - kb;  // keys of the tile that the column sees
+      const bool edge = kb + kKeys > least;
       uint32_t p[4][16];
       float2 add;
       for (int pass = 0;; ++pass) {
@@ -498,11 +495,31 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       if (lane == 0) tc::mbar_arrive(&bars.p_full[x]);
     }
     if (ok && count > 0) ok = wait_warp(&bars.o_full[x], 0, abort);
+    float total = sum.x + sum.y, own_w = 1.f, b_w = 0.f;
+    bool join = false;
+    if (split) {
+      if (x == 1) {
+        of_b[at & (kTileCols - 1)] = make_float2(ref, total);
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars.joined);
+      } else if (ok && (ok = wait_warp(&bars.joined, 0, abort)) && tiles > 1) {
+        ok = wait_warp(&bars.o_full[1], 0, abort);
+        join = true;
+        const float2 b = of_b[at];
+        const float top = fmaxf(ref, b.x), base = top == -INFINITY ? 0.f : top;
+        own_w = tc::ex2(ref - base);
+        b_w = tc::ex2(b.x - base);
+        total = own_w * total + b_w * b.y;
+        ref = top;
+      }
+    }
     if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_FINAL);
     tc::tc_fence_after();
-    const float total = sum.x + sum.y;
+    if (owner) {
     if (live) store_stats(a, it, col, ref, total);
     const float inv = a.chunks > 1 ? 1.f : total == 0.f ? 0.f : 1.f / total;
+    own_w *= inv;
+    b_w *= inv;
     // The rows go out through the query tile (every product that read it is done), so that
     // neighbouring lanes write neighbouring dims.
     const bool partial = a.chunks > 1;
@@ -513,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     constexpr int kRowBytes = D == 64 ? 128 : 256;  // 128 rows fit the tile
     auto chunk_at = [&](int r, int c) { return tile + r * kRowBytes + ((c ^ (r & 7)) << 4); };
     auto row_of = [&](int r, int* i, int* h) {
-      const int c = it.cb * kTcCols + x * kTileCols + r;
+      const int c = it.cb * kTcCols + (split ? 0 : x * kTileCols) + r;
       *i = c / a.kv.G;
       *h = it.g * a.kv.G + c % a.kv.G;
       return c < it.n * a.kv.G;
@@ -523,9 +540,17 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       float o[32];
       if (ok && count > 0) {
         tc::tmem_ld32(ob + 32 * b, o);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] *= own_w;
       } else {
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = 0.f;
+      }
+      if (ok && join) {
+        float other[32];
+        tc::tmem_ld32(ob + kSCols + 32 * b, other);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = fmaf(other[e], b_w, o[e]);
       }
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
@@ -534,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
         float y[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          y[e] = o[8 * (n / 2) + 2 * e + (n & 1)] * inv;
+          y[e] = o[8 * (n / 2) + 2 * e + (n & 1)];
           if (poison[g] < lim) y[e] = NAN;  // a value that is not finite reaches the columns that see it
         }
         if (partial) {  // a block's 32 dims, in the order in which they come
@@ -577,6 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
           }
         }
       }
+    }
     }
     tc::tc_fence_before();
   }
