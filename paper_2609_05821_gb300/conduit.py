@@ -590,8 +590,8 @@ class Rope:
         return ctypes.byref(self.struct)
 
     def positions(self, pos: Optional[torch.Tensor], rows: int) -> torch.Tensor:
-        if pos is None or pos.dtype != torch.int32 or not pos.is_contiguous() or \
-                tuple(pos.shape) != (self.num_axes, rows):
+        if pos is None or pos.dtype is not torch.int32 or pos.shape != (self.num_axes, rows) or \
+                not pos.is_contiguous():
             raise ConduitError(ERR_INVALID_ARG, f"pos must be contiguous int32 [{self.num_axes}, {rows}]")
         return pos
 
@@ -656,35 +656,39 @@ class PackedKv:
         return ctypes.byref(self.struct)
 
 
+def _addr(t: Optional[torch.Tensor]):
+    """A tensor's address for a void* parameter (as an int, which costs less than an object)."""
+    return None if t is None else t.data_ptr()
+
+
 def _rows(t: torch.Tensor, name: str, layers: int, rows: int, heads: int, d: int, dtype=None):
     """Strided rows [L][T][H][d] (or [T][H][d] of one layer) as a conduit_rows reference."""
-    if t.dim() == 3:
-        (n, h, w), (rs, hs, es), L, ls = t.shape, t.stride(), 1, 0
-    elif t.dim() == 4:
-        (L, n, h, w), (ls, rs, hs, es) = t.shape, t.stride()
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 4:
+        fits, layer = shape == (layers, rows, heads, d), stride[0]
     else:
-        raise ConduitError(ERR_INVALID_ARG, f"{name} must be [L, T, H, d] or [T, H, d]")
-    if (L, n, h, w) != (layers, rows, heads, d):
-        raise ConduitError(ERR_INVALID_ARG, f"{name} is {tuple(t.shape)}, not [{layers}, {rows}, {heads}, {d}]")
-    if es != 1 and w > 1:
+        fits, layer = layers == 1 and shape == (rows, heads, d), 0
+    if not fits:
+        raise ConduitError(ERR_INVALID_ARG, f"{name} is {tuple(shape)}, not [{layers}, {rows}, {heads}, {d}]")
+    if stride[-1] != 1 and d > 1:
         raise ConduitError(ERR_INVALID_ARG, f"the elements of a head of {name} must be contiguous")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise ConduitError(ERR_INVALID_ARG, f"{name} is {t.dtype}, not {dtype}")
-    return ctypes.byref(ConduitRows(t.data_ptr(), ls, rs, hs))
+    return ctypes.byref(ConduitRows(t.data_ptr(), layer, stride[-3], stride[-2]))
 
 
 def conduit_rope(rope: Rope, x: torch.Tensor, pos: torch.Tensor, out=None, inverse: bool = False, status=None,
                  stream=None) -> torch.Tensor:
     """Rows x [T, H, d] or [L, T, H, d] (any strides, contiguous heads) turned by their positions
     pos int32 [A, T]; inverse turns back (the gradient). out may be x."""
-    if x.dim() not in (3, 4):
+    shape = x.shape
+    if len(shape) not in (3, 4):
         raise ConduitError(ERR_INVALID_ARG, "x must be [L, T, H, d] or [T, H, d]")
-    L = x.shape[0] if x.dim() == 4 else 1
-    T, H, d = x.shape[-3:]
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    _check(_lib.conduit_rope(rope.ref(), _ptr(rope.positions(pos, T)), L, T, H, d, _dtype_code(x),
+    L, (T, H, d) = (shape[0], shape[1:]) if len(shape) == 4 else (1, shape)
+    out = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    _check(_lib.conduit_rope(rope.ref(), _addr(rope.positions(pos, T)), L, T, H, d, _dtype_code(x),
                              _rows(x, "x", L, T, H, d), _rows(out, "out", L, T, H, d, x.dtype), int(inverse),
-                             _ptr(status), _stream_ptr(stream)))
+                             _addr(status), _stream_ptr(stream)))
     return out
 
 
@@ -695,7 +699,7 @@ def _append_args(kv, seqs: Seqs, k, v, rope, pos, q, q_out):
     rows = [_rows(k, "k", L, T, Hkv, d), _rows(v, "v", L, T, Hkv, d, k.dtype)]
     rows += [None if t is None else _rows(t, name, L, T, kv.num_q_heads, d, k.dtype)
              for t, name in ((q, "q"), (q_out, "q_out"))]
-    return (None if rope is None else rope.ref(), None if rope is None else _ptr(rope.positions(pos, T))), rows, q_out
+    return (None if rope is None else rope.ref(), None if rope is None else _addr(rope.positions(pos, T))), rows, q_out
 
 
 def conduit_kv_append(kv: KvCache, seqs: Seqs, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
@@ -705,7 +709,7 @@ def conduit_kv_append(kv: KvCache, seqs: Seqs, k: torch.Tensor, v: torch.Tensor,
     if k.dtype != kv.dtype:
         raise ConduitError(ERR_INVALID_ARG, f"k is {k.dtype}, the cache {kv.dtype}")
     turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out)
-    _check(_lib.conduit_kv_append(kv.ref(), seqs.ref(), *turn, *rows, _ptr(status), _stream_ptr(stream)))
+    _check(_lib.conduit_kv_append(kv.ref(), seqs.ref(), *turn, *rows, _addr(status), _stream_ptr(stream)))
     return q_out
 
 
@@ -713,7 +717,7 @@ def conduit_packed_append(kv: PackedKv, seqs: Seqs, k: torch.Tensor, v: torch.Te
                           pos=None, q=None, q_out=None, status=None, stream=None):
     """conduit_kv_append into a 4-bit cache. Returns q_out (None without q)."""
     turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out)
-    _check(_lib.conduit_packed_append(kv.ref(), seqs.ref(), *turn, _dtype_code(k), *rows, _ptr(status),
+    _check(_lib.conduit_packed_append(kv.ref(), seqs.ref(), *turn, _dtype_code(k), *rows, _addr(status),
                                       _stream_ptr(stream)))
     return q_out
 
@@ -724,7 +728,7 @@ def conduit_packed_read(kv: PackedKv, batch: Batch, dst: KvCache, first=None, st
         raise ConduitError(ERR_INVALID_ARG, "first must be int32 with one entry per request")
     if batch.num_requests > kv.page_table.shape[0]:
         raise ConduitError(ERR_INVALID_ARG, "the page table has fewer rows than the batch has requests")
-    _check(_lib.conduit_packed_read(kv.ref(), _ptr(first), dst.ref(), batch.ref(), _ptr(status),
+    _check(_lib.conduit_packed_read(kv.ref(), _addr(first), dst.ref(), batch.ref(), _addr(status),
                                     _stream_ptr(stream)))
 
 
@@ -751,8 +755,8 @@ def conduit_packed_attn(kv: PackedKv, seqs: Seqs, q: torch.Tensor, scale: Option
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
     rows = _rows(q, "q", L, T, Hq, d), _rows(out, "out", L, T, Hq, d, q.dtype)
     ws = _workspace(lambda: conduit_packed_attn_workspace_size(kv, seqs, q.dtype), q.device, workspace)
-    _check(_lib.conduit_packed_attn(kv.ref(), seqs.ref(), _dtype_code(q), rows[0], scale or 0.0, _ptr(limits),
-                                    rows[1], _ptr(lse), _ptr(ws), ws.numel(), _ptr(status), _stream_ptr(stream)))
+    _check(_lib.conduit_packed_attn(kv.ref(), seqs.ref(), _dtype_code(q), rows[0], scale or 0.0, _addr(limits),
+                                    rows[1], _addr(lse), _addr(ws), ws.numel(), _addr(status), _stream_ptr(stream)))
     return out
 
 

@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
   constexpr int D = NG * 32, KS = D + 1;
   extern __shared__ float simt_smem[];
   float *ks = simt_smem, *vs = ks + kSimtKeys * KS, *qs = vs + kSimtKeys * D;
+  let_join_start();
   Item it;
   if (!item_of(a, &it)) return;
   const int tid = threadIdx.x, w = tid / 32, lane = tid % 32;
@@ -140,6 +141,7 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
     const int len = cached_len(a.s, a.kv.capacity(), r, nullptr, false);
     n = max(1, (len + a.chunk - 1) / a.chunk);
   }
+  wait_for_chunks();
   float top = -INFINITY;
   if (kJoin == 8) {  // one column in the block: its warps look for the reference lane by lane
     for (int c = threadIdx.x % 32; c < n; c += 32) top = fmaxf(top, a.part_ml[c * cols + col].x);
@@ -202,12 +204,18 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
   }
   if (err || a.chunks == 1) return err;
   const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
-  if (a.chunks >= 8)
-    combine_kernel<T, NG, 8><<<unsigned(cols), NG * 64, 0, stream>>>(a);
-  else
-    combine_kernel<T, NG, 1><<<unsigned((cols + 7) / 8), NG * 64, 0, stream>>>(a);
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(a.chunks >= 8 ? cols : (cols + 7) / 8));
+  cfg.blockDim = dim3(NG * 64);
+  cfg.stream = stream;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
   count_launches(1);
-  return cudaGetLastError();
+  return a.chunks >= 8 ? cudaLaunchKernelEx(&cfg, combine_kernel<T, NG, 8>, a)
+                       : cudaLaunchKernelEx(&cfg, combine_kernel<T, NG, 1>, a);
 }
 
 template <typename T>
@@ -249,7 +257,12 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   const int most = int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
   const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
   p.kernel = !mma ? kAttnSimt : int64_t(s.max_rows) * kv.G > TC_FROM ? kAttnTc : kAttnMma;
-  const int64_t largest = std::max(1, (most + 255) / 256);
+#ifndef MINC
+#define MINC 256
+#define MINS 64
+#endif
+  const int step = p.kernel == kAttnSimt ? MINS : p.kernel == kAttnMma ? MINC : 256;  // least keys of a chunk
+  const int64_t largest = std::max(1, (most + step - 1) / step);
   if (p.kernel == kAttnTc) {
     // One CTA per SM: the number of chunks with the least time by a model of one pass, 6 us for
     // a CTA and 1.8 us for 128 keys of two column tiles, and of the join, 12 bytes a partial
@@ -272,8 +285,8 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
     const int64_t even = s.R == 1 ? places / items : (8 * places + items - 1) / items;
     p.chunks = int(std::max<int64_t>(1, std::min(even, largest)));
   }
-  p.chunk = std::max(256, (most + p.chunks - 1) / p.chunks);
-  p.chunk = (p.chunk + 255) / 256 * 256;
+  p.chunk = std::max(step, (most + p.chunks - 1) / p.chunks);
+  p.chunk = (p.chunk + step - 1) / step * step;
   p.chunks = std::max(1, (most + p.chunk - 1) / p.chunk);
   p.items = items_of(kv, s, p.kernel, p.chunks);
   if (p.chunks > 1)

@@ -21,6 +21,10 @@ struct AttnArgs {
   int32_t* status;
 };
 
+// The join is launched while the chunks are still worked on; it waits for all of them.
+__device__ __forceinline__ void let_join_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_chunks() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // What a CTA works on.
 struct Item {
   int l, r, g, cb, chunk, t0, n, len;
@@ -77,6 +81,24 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const Item& it, int
     const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
     const int64_t col = (int64_t(it.l) * a.s.T + it.t0 + i) * a.kv.Hq + h;
     a.part_o[(it.chunk * cols + col) * a.kv.d + dd] = o;
+  }
+}
+
+// The same for dims dd .. dd + 3.
+template <typename T>
+__device__ __forceinline__ void store_out4(const AttnArgs& a, const Item& it, int j, int dd, float4 o, float sum) {
+  const int i = j / a.kv.G, h = it.g * a.kv.G + j % a.kv.G;
+  if (a.chunks == 1) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T* to = static_cast<T*>(a.out.p) + it.l * a.out.ls + int64_t(it.t0 + i) * a.out.rs + h * a.out.hs + dd;
+    to[0] = from_float<T>(o.x * inv);
+    to[1] = from_float<T>(o.y * inv);
+    to[2] = from_float<T>(o.z * inv);
+    to[3] = from_float<T>(o.w * inv);
+  } else {
+    const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
+    const int64_t col = (int64_t(it.l) * a.s.T + it.t0 + i) * a.kv.Hq + h;
+    *reinterpret_cast<float4*>(a.part_o + (it.chunk * cols + col) * a.kv.d + dd) = o;
   }
 }
 

@@ -215,9 +215,11 @@ __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, c
 
 template <int NG>
 __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
+  static_assert(kCols * NG * 8 <= kWarps * 32, "four dims a thread");
   constexpr int D = NG * 32, kBox = kBoxBytes(D);
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[kWarps][kStages];
+  let_join_start();
   Item it;
   if (!item_of(a, &it)) return;
   const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -225,6 +227,33 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   // a row of the logits' accumulator is the token key_lo (+ 8) of its half tile; with this
   // order the value loads of a warp are spread evenly over the banks
   const int key_lo = (q & 1) ? (4 + (q >> 1)) ^ 1 : q >> 1;
+
+  // Loads that wait for nothing but the request go out first: the page of this lane's first
+  // copy, then the column's query.
+  const int run_shift = min(5, a.kv.page_shift), at_tile = (lane >> 2) << run_shift, k0 = it.chunk * a.chunk;
+  const int first_j = k0 + w * kTile + at_tile;
+  int next_page = at_tile < kTile && first_j < it.len ? page_entry(a, it.r, first_j) : 0;
+  uint4 qv[NG];
+  {
+    const int j = it.cb * kCols + q;
+    const bool live = j < it.n * a.kv.G;
+    const int i = live ? j / a.kv.G : 0, h = live ? it.g * a.kv.G + j % a.kv.G : 0;
+    const __nv_bfloat16* src =
+        static_cast<const __nv_bfloat16*>(a.q.p) + it.l * a.q.ls + int64_t(it.t0 + i) * a.q.rs + h * a.q.hs + 8 * c;
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.q.p) | uint64_t(2 * (a.q.ls | a.q.rs | a.q.hs))) & 15u) == 0;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      qv[g] = make_uint4(0, 0, 0, 0);
+      if (live && wide) {
+        qv[g] = *reinterpret_cast<const uint4*>(src + 32 * g);
+      } else if (live) {
+        __nv_bfloat16 v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = src[32 * g + e];
+        qv[g] = *reinterpret_cast<uint4*>(v);
+      }
+    }
+  }
 
   // keys that this lane's two columns see; columns past the last see all (their result is dropped)
   int lim[2], most = 0, least = INT32_MAX;
@@ -240,7 +269,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     most = max(most, __shfl_xor_sync(0xffffffffu, most, s));
     least = min(least, __shfl_xor_sync(0xffffffffu, least, s));
   }
-  const int k0 = it.chunk * a.chunk, k1 = min(k0 + a.chunk, most);
+  const int k1 = min(k0 + a.chunk, most);
   const int tiles = k1 > k0 ? (k1 - k0 + kTile - 1) / kTile : 0;
   const int mine = tiles > w ? (tiles - w + kWarps - 1) / kWarps : 0;
 
@@ -254,8 +283,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
 
   // A lane copies one part (K codes, V codes, K and V parameters) of one run, the tokens of
   // a tile that lie in one page.
-  const int run_shift = min(5, a.kv.page_shift), run = 1 << run_shift;
-  const int part = lane & 3, at_tile = (lane >> 2) << run_shift;
+  const int run = 1 << run_shift, part = lane & 3;
   const int row_bytes = part < 2 ? D / 2 : D / 8;
   const uint32_t dst = tc::smem_u32(ring) + (part < 2 ? part * kTile * (D / 2) : kTile * D + (part - 2) * kTile * (D / 8)) +
                        at_tile * row_bytes;
@@ -266,7 +294,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     const int j = k0 + (w + n * kWarps) * kTile + at_tile;
     return n < mine && j < k1 && at_tile < kTile ? page_entry(a, it.r, j) : 0;
   };
-  int next_page = page_in(0);
   auto fill = [&](int n) {
     const int stage = n % kStages, kb = k0 + (w + n * kWarps) * kTile;
     const int runs = (min(k1 - kb, kTile) + run - 1) >> run_shift;
@@ -289,25 +316,10 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   uint32_t qsum = 0;
   float qoff[NG][2], to_log2[2];
   {
-    const int j = it.cb * kCols + q;
     float x[NG][8], top = 0.f;
-    const bool live = j < it.n * a.kv.G;
-    const int i = live ? j / a.kv.G : 0, h = live ? it.g * a.kv.G + j % a.kv.G : 0;
-    const __nv_bfloat16* src =
-        static_cast<const __nv_bfloat16*>(a.q.p) + it.l * a.q.ls + int64_t(it.t0 + i) * a.q.rs + h * a.q.hs + 8 * c;
-    const bool wide = ((reinterpret_cast<uintptr_t>(a.q.p) | uint64_t(2 * (a.q.ls | a.q.rs | a.q.hs))) & 15u) == 0;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      __nv_bfloat16 v[8];
-      if (!live) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __float2bfloat16_rn(0.f);
-      } else if (wide) {
-        *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(src + 32 * g);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = src[32 * g + e];
-      }
+      const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(&qv[g]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         x[g][e] = __bfloat162float(v[e]);
@@ -387,7 +399,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   constexpr int kRow = D + 4;
   float* ow = reinterpret_cast<float*>(smem);          // [warps][columns][kRow]
   float2* ml = reinterpret_cast<float2*>(ow + kWarps * kCols * kRow);  // [warps][columns] (reference, sum)
-  static_assert(kWarps * kCols * (kRow * 4 + 8) <= kWarps * kStages * kBox, "the join fits the ring");
+  static_assert(kWarps * kCols * (kRow * 4 + 8) + (kWarps + 1) * kCols * 4 <= kWarps * kStages * kBox, "the join fits the ring");
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int col = 2 * c + e;
@@ -398,23 +410,40 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
           make_float4(st.o[2 * g][e], st.o[2 * g][e + 2], st.o[2 * g + 1][e], st.o[2 * g + 1][e + 2]);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < kCols * D; e += kWarps * 32) {
-    const int col = e / D, dd = e % D, j = it.cb * kCols + col;
-    if (j >= it.n * a.kv.G) break;
+  // weights of the warps once per column, then four dims a thread
+  float* weight = reinterpret_cast<float*>(ml + kWarps * kCols);  // [warps + 1][columns], the sum last
+  if (threadIdx.x < kWarps * kCols) {
+    const int col = threadIdx.x % kCols, i = threadIdx.x / kCols;
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) top = fmaxf(top, ml[i * kCols + col].x);
+    for (int k = 0; k < kWarps; ++k) top = fmaxf(top, ml[k * kCols + col].x);
     const float base = top == -INFINITY ? 0.f : top;
-    float total = 0.f, out = 0.f;
+    weight[i * kCols + col] = tc::ex2(ml[i * kCols + col].x - base);
+    if (i == 0) {
+      float total = 0.f;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      const float2 s = ml[i * kCols + col];
-      const float wgt = tc::ex2(s.x - base);
-      total = fmaf(wgt, s.y, total);
-      out = fmaf(wgt, ow[(i * kCols + col) * kRow + dd], out);
+      for (int k = 0; k < kWarps; ++k) total = fmaf(tc::ex2(ml[k * kCols + col].x - base), ml[k * kCols + col].y, total);
+      weight[kWarps * kCols + col] = total;
+      const int j = it.cb * kCols + col;
+      if (j < it.n * a.kv.G) store_stats(a, it, j, top, total);
     }
-    store_out<__nv_bfloat16>(a, it, j, dd, out, total);
-    if (dd == 0) store_stats(a, it, j, top, total);
+  }
+  __syncthreads();
+  if (threadIdx.x < kCols * D / 4) {
+    const int col = threadIdx.x / (D / 4), dd = 4 * (threadIdx.x % (D / 4)), j = it.cb * kCols + col;
+    if (j < it.n * a.kv.G) {
+      float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        const float wgt = weight[i * kCols + col];
+        const float4 o = *reinterpret_cast<const float4*>(ow + (i * kCols + col) * kRow + dd);
+        out.x = fmaf(wgt, o.x, out.x);
+        out.y = fmaf(wgt, o.y, out.y);
+        out.z = fmaf(wgt, o.z, out.z);
+        out.w = fmaf(wgt, o.w, out.w);
+      }
+      store_out4<__nv_bfloat16>(a, it, j, dd, out, weight[kWarps * kCols + col]);
+    }
   }
 }
 

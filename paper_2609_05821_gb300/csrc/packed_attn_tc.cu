@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   __shared__ uint32_t tmem_slot;
   __shared__ int seen_most, seen_least, poison[NG], abort_flag;
   __shared__ float2 of_b[kTileCols];  // split: B's (reference, sum)
+  let_join_start();
   // Blocks with two column tiles come first and those with one, which take half of the time, last.
   Item it;
   if (!tc_item(a, &it)) return;
