@@ -78,6 +78,7 @@ struct PackedAttnPlan {
   int chunk;      // keys per chunk
   int chunks;     // of the longest context
   int64_t items;  // CTAs
+  bool cluster;   // the chunks of a context join inside a cluster
   size_t scratch;
 };
 PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype);

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
     if (j >= it.n * a.kv.G) continue;
 #pragma unroll
     for (int e = 0; e < NG; ++e) store_out<T>(a, it, j, e * 32 + lane, o[c][e], sum[c]);
-    if (lane == 0) store_stats(a, it, j, m[c], sum[c]);
+    if (lane == 0) store_stats(a, it, j, m[c], sum[c], a.chunks == 1);
   }
 }
 
@@ -193,7 +193,7 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
   if (plan.kernel == kAttnTc) {
     err = launch_packed_attn_tc(a, plan.items, stream);
   } else if (plan.kernel == kAttnMma) {
-    err = launch_packed_attn_mma(a, plan.items, stream);
+    err = launch_packed_attn_mma(a, plan.items, plan.cluster, stream);
   } else {
     constexpr int kSmem = simt_smem_bytes(NG * 32);
     err = cudaFuncSetAttribute(packed_attn_simt<T, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
@@ -202,7 +202,7 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
     count_launches(1);
     err = cudaGetLastError();
   }
-  if (err || a.chunks == 1) return err;
+  if (err || a.chunks == 1 || plan.cluster) return err;
   const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
   cudaLaunchAttribute early{};
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -289,7 +289,11 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   p.chunk = (p.chunk + step - 1) / step * step;
   p.chunks = std::max(1, (most + p.chunk - 1) / p.chunk);
   p.items = items_of(kv, s, p.kernel, p.chunks);
-  if (p.chunks > 1)
+  // Up to eight chunks join inside a cluster: one launch and no partial results in memory. More
+  // CTAs than places and the clusters wait for one another (16 requests of 1 025 tokens: 15.8 us
+  // with the join, 18.0 us in clusters; one request: 9.4 and 8.5 us).
+  p.cluster = p.kernel == kAttnMma && p.chunks > 1 && p.chunks <= 8 && p.items <= 2 * 152;
+  if (p.chunks > 1 && !p.cluster)
     p.scratch = stats_bytes(kv, s, p.chunks) + size_t(p.chunks) * kv.L * s.T * kv.Hq * size_t(kv.d) * sizeof(float);
   return p;
 }

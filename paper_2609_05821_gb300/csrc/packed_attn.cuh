@@ -43,12 +43,21 @@ __device__ __forceinline__ void decode(const AttnArgs& a, uint32_t x, Item* it) 
   it->len = cached_len(a.s, a.kv.capacity(), it->r, a.status, threadIdx.x == 0);
 }
 
-// Column blocks of kCols, side by side so that they share the keys in L2.
+// Column blocks of kCols, side by side so that they share the keys in L2; in clusters, the
+// chunks of a context side by side.
+template <bool kCluster = false>
 __device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
-  it->cb = int(blockIdx.x % uint32_t(a.col_blocks));
-  decode(a, blockIdx.x / uint32_t(a.col_blocks), it);
+  const uint32_t inner = kCluster ? a.chunks : a.col_blocks;
+  uint32_t x = blockIdx.x / inner;
+  if (kCluster) {
+    it->cb = int(x % uint32_t(a.col_blocks));
+    decode(a, x / uint32_t(a.col_blocks) * a.chunks + blockIdx.x % inner, it);
+  } else {
+    it->cb = int(blockIdx.x % inner);
+    decode(a, x, it);
+  }
   if (it->cb * kCols >= it->n * a.kv.G) return false;
-  return it->chunk == 0 || it->chunk * a.chunk < it->len;
+  return kCluster || it->chunk == 0 || it->chunk * a.chunk < it->len;
 }
 
 // Keys that column j of the item sees (0 for columns past the last).
@@ -86,9 +95,10 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const Item& it, int
 
 // The same for dims dd .. dd + 3.
 template <typename T>
-__device__ __forceinline__ void store_out4(const AttnArgs& a, const Item& it, int j, int dd, float4 o, float sum) {
+__device__ __forceinline__ void store_out4(const AttnArgs& a, const Item& it, int j, int dd, float4 o, float sum,
+                                           bool last) {
   const int i = j / a.kv.G, h = it.g * a.kv.G + j % a.kv.G;
-  if (a.chunks == 1) {
+  if (last) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T* to = static_cast<T*>(a.out.p) + it.l * a.out.ls + int64_t(it.t0 + i) * a.out.rs + h * a.out.hs + dd;
     to[0] = from_float<T>(o.x * inv);
@@ -104,9 +114,9 @@ __device__ __forceinline__ void store_out4(const AttnArgs& a, const Item& it, in
 
 constexpr float kLn2 = 0.69314718055994531f;
 
-__device__ __forceinline__ void store_stats(const AttnArgs& a, const Item& it, int j, float m, float sum) {
+__device__ __forceinline__ void store_stats(const AttnArgs& a, const Item& it, int j, float m, float sum, bool last) {
   const int i = j / a.kv.G, h = it.g * a.kv.G + j % a.kv.G;
-  if (a.chunks == 1) {
+  if (last) {
     if (a.lse)
       a.lse[(int64_t(it.l) * a.kv.Hq + h) * a.s.T + it.t0 + i] = sum == 0.f ? -INFINITY : kLn2 * (m + log2f(sum));
   } else {
@@ -168,7 +178,8 @@ __device__ __forceinline__ bool finite_pair(uint32_t p) {
 
 // Warp-level tensor-core kernel (packed_attn_mma.cu) and tcgen05 kernel
 // (packed_attn_tc.cu): bf16 rows, head_dim 64, 96, 128.
-cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, cudaStream_t stream);
+// `cluster`: the chunks of a context form a cluster, which joins them itself.
+cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, bool cluster, cudaStream_t stream);
 cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream);
 
 }  // namespace conduit

@@ -213,15 +213,36 @@ __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, c
   }
 }
 
-template <int NG>
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The value at p's place in the shared memory of CTA `rank` of the cluster.
+template <typename T>
+__device__ __forceinline__ T read_of(const T* p, int rank) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(rank));
+  T y;
+  if constexpr (sizeof(T) == 8)
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(y.x), "=f"(y.y) : "r"(at) : "memory");
+  else
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(y.x), "=f"(y.y), "=f"(y.z), "=f"(y.w)
+                 : "r"(at)
+                 : "memory");
+  return y;
+}
+
+// kCluster: the CTAs of a cluster take the chunks of a context and join them in shared memory.
+template <int NG, bool kCluster>
 __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   static_assert(kCols * NG * 8 <= kWarps * 32, "four dims a thread");
   constexpr int D = NG * 32, kBox = kBoxBytes(D);
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[kWarps][kStages];
-  let_join_start();
+  if (!kCluster) let_join_start();
   Item it;
-  if (!item_of(a, &it)) return;
+  if (!item_of<kCluster>(a, &it)) return;
   const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int c = lane & 3, q = lane >> 2;
   // a row of the logits' accumulator is the token key_lo (+ 8) of its half tile; with this
@@ -269,7 +290,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     most = max(most, __shfl_xor_sync(0xffffffffu, most, s));
     least = min(least, __shfl_xor_sync(0xffffffffu, least, s));
   }
-  const int k1 = min(k0 + a.chunk, most);
+  const int k1 = min(k0 + a.chunk, most);  // at or before k0 for a chunk past the context
   const int tiles = k1 > k0 ? (k1 - k0 + kTile - 1) / kTile : 0;
   const int mine = tiles > w ? (tiles - w + kWarps - 1) / kWarps : 0;
 
@@ -399,7 +420,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   constexpr int kRow = D + 4;
   float* ow = reinterpret_cast<float*>(smem);          // [warps][columns][kRow]
   float2* ml = reinterpret_cast<float2*>(ow + kWarps * kCols * kRow);  // [warps][columns] (reference, sum)
-  static_assert(kWarps * kCols * (kRow * 4 + 8) + (kWarps + 1) * kCols * 4 <= kWarps * kStages * kBox, "the join fits the ring");
+  static_assert(kWarps * kCols * (kRow * 4 + 8) + (kWarps + 1) * kCols * 4 + kCols * (8 + D * 4) <= kWarps * kStages * kBox, "the join fits the ring");
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int col = 2 * c + e;
@@ -412,6 +433,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   __syncthreads();
   // weights of the warps once per column, then four dims a thread
   float* weight = reinterpret_cast<float*>(ml + kWarps * kCols);  // [warps + 1][columns], the sum last
+  float2* joined_ml = reinterpret_cast<float2*>(weight + (kWarps + 1) * kCols);  // [columns] (clusters)
+  float4* joined = reinterpret_cast<float4*>(joined_ml + kCols);                 // [columns][D / 4]
   if (threadIdx.x < kWarps * kCols) {
     const int col = threadIdx.x % kCols, i = threadIdx.x / kCols;
     float top = -INFINITY;
@@ -425,45 +448,99 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
       for (int k = 0; k < kWarps; ++k) total = fmaf(tc::ex2(ml[k * kCols + col].x - base), ml[k * kCols + col].y, total);
       weight[kWarps * kCols + col] = total;
       const int j = it.cb * kCols + col;
-      if (j < it.n * a.kv.G) store_stats(a, it, j, top, total);
+      if (kCluster)
+        joined_ml[col] = make_float2(top, total);
+      else if (j < it.n * a.kv.G)
+        store_stats(a, it, j, top, total, a.chunks == 1);
     }
   }
   __syncthreads();
+  const int col = threadIdx.x / (D / 4), dd = 4 * (threadIdx.x % (D / 4));
   if (threadIdx.x < kCols * D / 4) {
-    const int col = threadIdx.x / (D / 4), dd = 4 * (threadIdx.x % (D / 4)), j = it.cb * kCols + col;
-    if (j < it.n * a.kv.G) {
+    const int j = it.cb * kCols + col;
+    float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float wgt = weight[i * kCols + col];
+      const float4 o = *reinterpret_cast<const float4*>(ow + (i * kCols + col) * kRow + dd);
+      out.x = fmaf(wgt, o.x, out.x);
+      out.y = fmaf(wgt, o.y, out.y);
+      out.z = fmaf(wgt, o.z, out.z);
+      out.w = fmaf(wgt, o.w, out.w);
+    }
+    if (kCluster)
+      joined[threadIdx.x] = out;
+    else if (j < it.n * a.kv.G)
+      store_out4<__nv_bfloat16>(a, it, j, dd, out, weight[kWarps * kCols + col], a.chunks == 1);
+  }
+  if constexpr (kCluster) {
+    // every CTA finishes a slice of the columns' dims over all chunks, in chunk order
+    cluster_sync();
+    constexpr int kUnits = kCols * D / 4;
+    const int C = a.chunks, slice = (kUnits + C - 1) / C, u = it.chunk * slice + threadIdx.x;
+    if (int(threadIdx.x) < slice && u < kUnits) {
+      const int uc = u / (D / 4), ud = 4 * (u % (D / 4)), j = it.cb * kCols + uc;
+      float2 st[8];
+      float4 o[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {  // every load under way before the first use
+        const int from = min(k, C - 1);
+        st[k] = read_of<float2>(&joined_ml[uc], from);
+        o[k] = read_of<float4>(&joined[u], from);
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = fmaxf(top, st[k].x);
+      const float base = top == -INFINITY ? 0.f : top;
+      float total = 0.f;
       float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < kWarps; ++i) {
-        const float wgt = weight[i * kCols + col];
-        const float4 o = *reinterpret_cast<const float4*>(ow + (i * kCols + col) * kRow + dd);
-        out.x = fmaf(wgt, o.x, out.x);
-        out.y = fmaf(wgt, o.y, out.y);
-        out.z = fmaf(wgt, o.z, out.z);
-        out.w = fmaf(wgt, o.w, out.w);
+      for (int k = 0; k < 8; ++k) {
+        if (k >= C) continue;
+        const float wgt = tc::ex2(st[k].x - base);
+        total = fmaf(wgt, st[k].y, total);
+        out.x = fmaf(wgt, o[k].x, out.x);
+        out.y = fmaf(wgt, o[k].y, out.y);
+        out.z = fmaf(wgt, o[k].z, out.z);
+        out.w = fmaf(wgt, o[k].w, out.w);
       }
-      store_out4<__nv_bfloat16>(a, it, j, dd, out, weight[kWarps * kCols + col]);
+      if (j < it.n * a.kv.G) {
+        store_out4<__nv_bfloat16>(a, it, j, ud, out, total, true);
+        if (ud == 0) store_stats(a, it, j, top, total, true);
+      }
     }
+    cluster_sync();  // nobody leaves while its results are read
   }
 }
 
-template <int NG>
+template <int NG, bool kCluster>
 cudaError_t launch(const AttnArgs& a, int64_t items, cudaStream_t stream) {
   constexpr int kSmem = kWarps * kStages * kBoxBytes(NG * 32);
-  cudaError_t err = cudaFuncSetAttribute(packed_attn_mma<NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  cudaError_t err =
+      cudaFuncSetAttribute(packed_attn_mma<NG, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (err) return err;
-  packed_attn_mma<NG><<<unsigned(items), kWarps * 32, kSmem, stream>>>(a);
+  cudaLaunchAttribute cluster{};
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = kCluster ? a.chunks : 1;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(items));
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = stream;
+  cfg.attrs = &cluster;
+  cfg.numAttrs = kCluster ? 1 : 0;
   count_launches(1);
-  return cudaGetLastError();
+  return cudaLaunchKernelEx(&cfg, packed_attn_mma<NG, kCluster>, a);
 }
 
 }  // namespace
 
-cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, cudaStream_t stream) {
+cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, bool cluster, cudaStream_t stream) {
   switch (a.kv.d) {
-    case 64: return launch<2>(a, items, stream);
-    case 96: return launch<3>(a, items, stream);
-    default: return launch<4>(a, items, stream);
+    case 64: return cluster ? launch<2, true>(a, items, stream) : launch<2, false>(a, items, stream);
+    case 96: return cluster ? launch<3, true>(a, items, stream) : launch<3, false>(a, items, stream);
+    default: return cluster ? launch<4, true>(a, items, stream) : launch<4, false>(a, items, stream);
   }
 }
 

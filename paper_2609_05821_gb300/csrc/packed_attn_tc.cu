@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_FINAL);
     tc::tc_fence_after();
     if (owner) {
-    if (live) store_stats(a, it, col, ref, total);
+    if (live) store_stats(a, it, col, ref, total, a.chunks == 1);
     const float inv = a.chunks > 1 ? 1.f : total == 0.f ? 0.f : 1.f / total;
     own_w *= inv;
     b_w *= inv;
