@@ -187,11 +187,18 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
     a.lse[(int64_t(l) * a.kv.Hq + h) * a.s.T + t] = sum == 0.f ? -INFINITY : kLn2 * (base + log2f(sum));
 }
 
+// The tcgen05 kernel's keys are within 2^-12 of their values, and so a logit within 2^-12 of sum
+// |q||k|: nothing beside the rounding of a bf16 output, and in a log-sum-exp an error that falls
+// with the number of keys that count (2 x 10^-4 of it for one key, 5 x 10^-6 for 2 000, 2 x 10^-6
+// for 8 192). For shorter contexts keys come as two fp16 numbers, whether or not a log-sum-exp is
+// asked for, so that outputs do not depend on that.
+constexpr int kExactBelow = 2048;
+
 template <typename T, int NG>
 cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
   cudaError_t err;
   if (plan.kernel == kAttnTc) {
-    err = launch_packed_attn_tc(a, plan.items, stream);
+    err = launch_packed_attn_tc(a, plan.items, a.s.max_len < kExactBelow, stream);
   } else if (plan.kernel == kAttnMma) {
     err = launch_packed_attn_mma(a, plan.items, plan.cluster, stream);
   } else {

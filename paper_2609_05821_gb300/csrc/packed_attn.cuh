@@ -180,6 +180,7 @@ __device__ __forceinline__ bool finite_pair(uint32_t p) {
 // (packed_attn_tc.cu): bf16 rows, head_dim 64, 96, 128.
 // `cluster`: the chunks of a context form a cluster, which joins them itself.
 cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, bool cluster, cudaStream_t stream);
-cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream);
+// `exact`: logits in fp32's precision.
+cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, bool exact, cudaStream_t stream);
 
 }  // namespace conduit

@@ -3,11 +3,12 @@
 //
 // Mathematics. A group of 32 dims of token t is m_t + s_t (u - 8), u in 0..15. Logits come
 // group by group: x = sum_g s_tg (sum (u - 8) q) + m_tg (sum q). A nibble under the
-// exponent of 1024 is 1024 + u (or 1024 + 16 u) in fp16, one masked word for two codes; the
-// offsets are sums of the query alone and are taken off in fp32 (the products and their
-// sums are exact to 2^-23 of 1024 |q|: 10^-4 of a logit's own unit). Values are formed as
-// fp16 m + s c (2^-11 relative), weights rounded to fp16: both below the rounding of a
-// bf16 output.
+// exponent of 128 is 128 + u in bf16, one masked word for two codes, and a bf16 query is an
+// operand as it is; the offsets are sums of the query alone and are taken off in fp32. (The
+// tensor cores cut each sum off at 2^-23 of its size: at most 10^-6 of the log-sum-exp. With
+// fp16's 1024 + u, which needs a shift less per word, it was 6 x 10^-6.) Values are formed as
+// fp16 m + s c (2^-11 relative), weights rounded to fp16: both below the rounding of a bf16
+// output.
 //
 // Shape. mma with the tokens (then the dims) as the 16 rows and up to 8 (row, query head)
 // columns as n, so that a KV head's group of 7 or 8 query heads wastes nothing. The
@@ -36,7 +37,22 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
 // The same from zero, without registers for it.
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                               uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                               uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -79,6 +95,13 @@ __device__ __forceinline__ uint32_t mids(const uint8_t* p, int c) {
   }
 }
 
+// The nibbles at bits 0-3 and 16-19 as bf16 128 + u.
+__device__ __forceinline__ uint32_t raw(uint32_t w) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(w), "r"(0x000F000Fu), "r"(0x43004300u));
+  return y;
+}
+
 // State of a warp's running softmax for the two columns of a lane.
 template <int NG>
 struct Running {
@@ -111,9 +134,8 @@ __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, c
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       float acc[4];
-      mma_f16_first(acc, raw_lo(wl[g]), raw_lo(wh[g]), raw_hi(wl[g]), raw_hi(wh[g]), bq[g][0], bq[g][1]);
-      const uint32_t l8 = wl[g] >> 8, h8 = wh[g] >> 8;
-      mma_f16(acc, raw_lo(l8), raw_lo(h8), raw_hi(l8), raw_hi(h8), bq[g][2], bq[g][3]);
+      mma_bf16_first(acc, raw(wl[g]), raw(wh[g]), raw(wl[g] >> 4), raw(wh[g] >> 4), bq[g][0], bq[g][1]);
+      mma_bf16(acc, raw(wl[g] >> 8), raw(wh[g] >> 8), raw(wl[g] >> 12), raw(wh[g] >> 12), bq[g][2], bq[g][3]);
       const float sl = __low2float(u2h(pl[g])), sh = __low2float(u2h(ph[g]));
       x[t][0] = fmaf(sl, acc[0] - qoff[g][0], x[t][0]);
       x[t][1] = fmaf(sl, acc[1] - qoff[g][1], x[t][1]);
@@ -332,7 +354,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     if (s < mine) fill(s);
 
   // Queries of column q in the operand layout, scaled by 2^-shift so that the largest lies in
-  // [256, 512): exact in fp16 down to 2^-22 of it. Odd dims meet 16 u and are divided by 16.
+  // [256, 512): their sums then fit fp16.
   uint32_t bq[NG][4];
   uint32_t qsum = 0;
   float qoff[NG][2], to_log2[2];
@@ -364,22 +386,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     for (int g = 0; g < NG; ++g) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[g][e] = x[g][e] * f1 * f2;
-      float even = (x[g][0] + x[g][2]) + (x[g][4] + x[g][6]), odd = (x[g][1] + x[g][3]) + (x[g][5] + x[g][7]);
+      float total = ((x[g][0] + x[g][1]) + (x[g][2] + x[g][3])) + ((x[g][4] + x[g][5]) + (x[g][6] + x[g][7]));
 #pragma unroll
-      for (int s = 1; s < 4; s <<= 1) {
-        even += __shfl_xor_sync(0xffffffffu, even, s);
-        odd += __shfl_xor_sync(0xffffffffu, odd, s);
-      }
+      for (int s = 1; s < 4; s <<= 1) total += __shfl_xor_sync(0xffffffffu, total, s);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {  // word e: dims e and e + 4
-        const float f = e & 1 ? 0.0625f : 1.f;
-        bq[g][e] = h2u(__floats2half2_rn(x[g][e] * f, x[g][e + 4] * f));
+        const __nv_bfloat162 two = __floats2bfloat162_rn(x[g][e], x[g][e + 4]);
+        bq[g][e] = *reinterpret_cast<const uint32_t*>(&two);
       }
-      const float off = 1032.f * even + 72.f * odd;
+      const float off = 136.f * total;
 #pragma unroll
       for (int e = 0; e < 2; ++e) qoff[g][e] = __shfl_sync(0xffffffffu, off, 4 * (2 * c + e));
       // slots 2 c, 2 c + 1 of the product with the mids: groups 0, 1, 2, 3, then the same in a second part
-      const float total = even + odd, first = __half2float(__float2half_rn(total));
+      const float first = __half2float(__float2half_rn(total));
       if (g / 2 == (c & 1))
         qsum |= uint32_t(__half_as_ushort(__float2half_rn(c < 2 ? first : total - first))) << (16 * (g & 1));
     }

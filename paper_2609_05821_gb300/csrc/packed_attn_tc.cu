@@ -109,6 +109,33 @@ __device__ __forceinline__ void unpack_keys(uint8_t* tile, const uint8_t* box, i
   }
 }
 
+// The same in two parts: hi is the value in fp16, lo what is missing from it.
+template <int NG>
+__device__ __forceinline__ void unpack_keys_exact(uint8_t* hi, uint8_t* lo, const uint8_t* box, int token, int c) {
+  constexpr int D = 32 * NG;
+  uint32_t w[NG], p[NG];
+  load_words<NG>(box + token * (D / 2) + c * (D / 8), w);
+  load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), p);
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const float2 sm = __half22float2(u2h(p[g]));
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float a = fmaf(sm.x, float(int((w[g] >> (4 * e)) & 15u) - 8), sm.y);
+      const float b = fmaf(sm.x, float(int((w[g] >> (4 * e + 16)) & 15u) - 8), sm.y);
+      const __half2 top = __floats2half2_rn(a, b);
+      const float2 back = __half22float2(top);
+      h[e] = h2u(top);
+      l[e] = h2u(__floats2half2_rn(a - back.x, b - back.y));
+    }
+    const int ch = 4 * g + c;
+    const uint32_t at = (ch >> 3) * kBlock + tc::sw128_offset(token, ch & 7);
+    *reinterpret_cast<uint4*>(hi + at) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4*>(lo + at) = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+
 // One lane's share of a token's values. kEdge: the tile holds tokens that some column does
 // not see. Their weight there is 0, and 0 times NaN must not be: a parameter pair that is not
 // finite becomes 0 and its first token is noted for the group.
@@ -178,7 +205,9 @@ __device__ __forceinline__ float weigh(uint32_t sb, float2 up, float2 down, int 
   return top;
 }
 
-template <int NG>
+// kExact: keys as the sum of two fp16 numbers (a tile in both key buffers), so that logits keep
+// fp32's precision.
+template <int NG, bool kExact>
 __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   using Z = Sizes<NG>;
   constexpr int D = Z::D;
@@ -268,6 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       for (int v = 0; v < 2; ++v) {
         const int slot = issued % kRing;
         if (issued >= kRing && !(ok = wait_warp(&bars.raw_free[slot], (issued / kRing - 1) & 1, abort))) break;
+        if (kExact && !v && t > 0 && !(ok = wait_warp(&bars.k_free[0], (t - 1) & 1, abort))) break;
         if (lane == 0) tc::mbar_arrive_expect_tx(&bars.raw_full[slot], uint32_t(runs << run_shift) * (D / 2 + D / 8));
         __syncwarp();
         if (mine)
@@ -290,14 +320,23 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       const int load = 2 * t + v, slot = load % kRing;
       const uint8_t* box = raw + slot * Z::kRaw;
       bool ok = wait_warp(&bars.raw_full[slot], (load / kRing) & 1, abort);
-      if (ok && t >= 2) ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
+      // A buffer is free once its last tile but one has been used. A warp takes only some of the
+      // units, but cannot take a phase for the one two before it: the ring lets no unit begin
+      // before every unit three copies back is done, and those waited for that earlier phase.
+      // kExact has one key buffer, for which that would not hold; there the copies wait.
+      if (ok && t >= 2 && !(kExact && !v))
+        ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
       if (!ok) {
         if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
         break;
       }
-      uint8_t* tile = (v ? vt : kt) + stage * Z::kTile;
+      uint8_t* tile = v ? vt + stage * Z::kTile : kExact ? kt : kt + stage * Z::kTile;
       const int kb = k0 + t * kKeys;
-      if (!v) {
+      if (!v && kExact) {
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i)
+          unpack_keys_exact<NG>(tile, tile + Z::kTile, box, token0 + (i8 & 1) * 4 + (i8 >> 1) + 8 * i, c);
+      } else if (!v) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) unpack_keys<NG>(tile, box, token0 + (i8 & 1) * 4 + (i8 >> 1) + 8 * i, c);
       } else if (kb + kKeys > least) {  // some column does not see the whole tile
@@ -311,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       __syncwarp();
       if (lane == 0) {
         tc::mbar_arrive(&bars.raw_free[slot]);
-        tc::mbar_arrive(v ? &bars.v_full[stage] : &bars.k_full[stage]);
+        tc::mbar_arrive(v ? &bars.v_full[stage] : &bars.k_full[kExact ? 0 : stage]);
       }
     }
   } else if (warp == kMmaWarp) {
@@ -330,9 +369,9 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     // stream that reads it and freed by the last.
     bool ok = true;
     auto score = [&](int x, int tile) {
-      const int stage = tile & 1;
+      const int stage = kExact ? 0 : tile & 1;
       if (halves || x == 0) {
-        if (!(ok = wait_warp(&bars.k_full[stage], (tile >> 1) & 1, abort))) return;
+        if (!(ok = wait_warp(&bars.k_full[stage], (kExact ? tile : tile >> 1) & 1, abort))) return;
         tc::tc_fence_after();
       }
       const uint64_t dk = tc::desc_sw128(k_at + stage * Z::kTile);
@@ -341,6 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       for (int kk = 0; kk < D / 16; ++kk) {
         const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
         tc::mma_bf16_if(leader, tm + x * kSCols, dx + off, dk + off, idesc_s, kk > 0);
+        if (kExact) tc::mma_bf16_if(leader, tm + x * kSCols, dx + off, dk + off + (Z::kTile >> 4), idesc_s, true);
       }
       tc::mma_commit_if(leader, &bars.s_full[x]);
       if (halves || x == 1) tc::mma_commit_if(leader, &bars.k_free[stage]);
@@ -495,7 +535,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars.p_full[x]);
     }
-    if (ok && count > 0) ok = wait_warp(&bars.o_full[x], 0, abort);
+    // without keys there is nothing to wait for but the other warps' queries, over which the rows go out
+    if (ok) ok = count > 0 ? wait_warp(&bars.o_full[x], 0, abort) : wait_warp(&bars.q_full, 0, abort);
     float total = sum.x + sum.y, own_w = 1.f, b_w = 0.f;
     bool join = false;
     if (split) {
@@ -614,24 +655,24 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   }
 }
 
-template <int NG>
+template <int NG, bool kExact>
 cudaError_t launch(const AttnArgs& a, int64_t items, cudaStream_t stream) {
-  cudaError_t err = cudaFuncSetAttribute(packed_attn_tc<NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<NG>::kSmem);
+  constexpr uint32_t kSmem = Sizes<NG>::kSmem;
+  cudaError_t err = cudaFuncSetAttribute(packed_attn_tc<NG, kExact>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (err) return err;
-  packed_attn_tc<NG><<<unsigned(items), kThreads, Sizes<NG>::kSmem, stream>>>(a);
+  packed_attn_tc<NG, kExact><<<unsigned(items), kThreads, kSmem, stream>>>(a);
   count_launches(1);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream) {
+cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, bool exact, cudaStream_t stream) {
   switch (a.kv.d) {
-    case 64: return launch<2>(a, items, stream);
-    case 96: return launch<3>(a, items, stream);
-    default: return launch<4>(a, items, stream);
+    case 64: return exact ? launch<2, true>(a, items, stream) : launch<2, false>(a, items, stream);
+    case 96: return exact ? launch<3, true>(a, items, stream) : launch<3, false>(a, items, stream);
+    default: return exact ? launch<4, true>(a, items, stream) : launch<4, false>(a, items, stream);
   }
 }
 
 }  // namespace conduit
-

@@ -242,6 +242,24 @@ def test_lengths_and_pages_out_of_range(C):
     assert torch.equal(out[0, 1], good[0, 1])
 
 
+def test_many_rows_that_see_nothing(C):
+    """Contexts far shorter than the call's rows, in more CTAs than SMs: blocks of rows without a key are zeros."""
+    lens, rows = (1, 3, 0, 2) * 12, (90, 128, 60, 41) * 12
+    kv, groups = _cache(C, 31, 1, 28, 4, 128, 16, lens)
+    T = sum(rows)
+    q = torch.randn((1, T, 28, 128), generator=torch.Generator(device="cuda").manual_seed(6), device="cuda").to(BF)
+    seqs = C.Seqs(np.concatenate([[0], np.cumsum(rows)]), torch.tensor(lens, dtype=torch.int32, device="cuda"), 3)
+    lse = torch.zeros((1, 28, T), device="cuda")
+    for _ in range(4):
+        out = C.conduit_packed_attn(kv, seqs, q, lse=lse)
+        t = 0
+        for n, c in zip(lens, rows):
+            assert torch.all(out[0, t:t + c - n] == 0) and torch.all(lse[0, :, t:t + c - n] == -float("inf"))
+            t += c
+        assert torch.isfinite(out.float()).all()
+    _check(C, kv, groups, lens, rows, q, None, out, lse, 128 ** -0.5, True)
+
+
 def test_other_stream(C):
     kv, groups = _cache(C, 8, 1, 8, 2, 128, 16, (777,))
     q = torch.randn((1, 1, 8, 128), device="cuda").to(BF)
