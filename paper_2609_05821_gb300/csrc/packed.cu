@@ -206,13 +206,15 @@ __device__ __forceinline__ bool pack8(float (&x)[8], float (&y)[8], int c, uint3
 
 // Blocks below kv_blocks pack keys and values: a thread owns 8 dims of a row's heads hg,
 // hg + HG, ... (four threads a group). The blocks after them rotate queries, a unit of
-// pairs per thread.
+// pairs per thread. Either walks over layers blockIdx.z, + gridDim.z, ...: a row's place,
+// positions and cosines are worked out once for all of them.
 template <typename T, int VEC, int kPairing>
 __global__ void __launch_bounds__(kThreads, 4)
     packed_append_kernel(PackedDev kv, SeqsDev s, RopeDev rope, int kv_blocks, int HG, bool wide, RowsDev k, RowsDev v,
                          RowsDev q, RowsDev q_out, int32_t* status) {
-  const int r = blockIdx.y, l = blockIdx.z;
+  const int r = blockIdx.y;
   const int t0 = s.row_off[r], n = s.row_off[r + 1] - t0, len = s.len[r];
+  if (n == 0) return;
   const bool pack = int(blockIdx.x) < kv_blocks;
   const uint32_t lin = (pack ? blockIdx.x : blockIdx.x - kv_blocks) * uint32_t(kThreads) + threadIdx.x;
   const uint32_t per = pack ? kv.d / 8 : units_per_row<VEC>(rope, kv.d), heads = pack ? HG : kv.Hq;
@@ -225,54 +227,62 @@ __global__ void __launch_bounds__(kThreads, 4)
   const int page = kv.page_table[int64_t(r) * kv.max_pages + (ok ? slot >> kv.page_shift : 0)];
   ok &= page >= 0 && page < kv.P;
   int pos[CONDUIT_MAX_AXES];
-  if (rope.rot && n > 0) ok &= load_positions(rope, t, pos);
+  if (rope.rot) ok &= load_positions(rope, t, pos);
   if (live && !ok && u == 0 && h0 == 0) flag_status(status, CONDUIT_FLAG_INDEX);
   if (!pack) {
     if (!ok) return;
     using C = Chunk<T, VEC>;
     const Unit un = unit_of<VEC>(rope, kv.d, u);
-    const T* src = static_cast<const T*>(q.p) + l * q.ls + t * q.rs + h0 * q.hs;
-    T* dst = static_cast<T*>(q_out.p) + l * q_out.ls + t * q_out.rs + h0 * q_out.hs;
-    C a = *reinterpret_cast<const C*>(src + un.a), b;
-    if (un.b >= 0) b = *reinterpret_cast<const C*>(src + un.b);
-    if (un.turns) {
-      float2 cs[VEC];
-      load_turn<VEC>(rope, pos, u * VEC, cs);
-      turn_chunks<T, VEC>(rope, cs, a, b);
+    float2 cs[VEC];
+    if (un.turns) load_turn<VEC>(rope, pos, u * VEC, cs);
+    for (int l = blockIdx.z; l < kv.L; l += gridDim.z) {
+      const T* src = static_cast<const T*>(q.p) + l * q.ls + t * q.rs + h0 * q.hs;
+      T* dst = static_cast<T*>(q_out.p) + l * q_out.ls + t * q_out.rs + h0 * q_out.hs;
+      C a = *reinterpret_cast<const C*>(src + un.a), b;
+      if (un.b >= 0) b = *reinterpret_cast<const C*>(src + un.b);
+      if (un.turns) turn_chunks<T, VEC>(rope, cs, a, b);
+      *reinterpret_cast<C*>(dst + un.a) = a;
+      if (un.b >= 0) *reinterpret_cast<C*>(dst + un.b) = b;
     }
-    *reinterpret_cast<C*>(dst + un.a) = a;
-    if (un.b >= 0) *reinterpret_cast<C*>(dst + un.b) = b;
     return;
   }
   float2 cs[8];
   if (ok) load_turn8<kPairing>(rope, pos, 8 * u, cs);
   const int row = slot & ((1 << kv.page_shift) - 1), groups = kv.d / 32, grp = u / 4, c = u % 4;
   bool bad = false;
-  const T* kr = static_cast<const T*>(k.p) + l * k.ls + t * k.rs + h0 * k.hs;
-  const T* vr = static_cast<const T*>(v.p) + l * v.ls + t * v.rs + h0 * v.hs;
-  uint8_t* at = kv.page(l, h0, page);
-  for (int g = h0; g - h0 < kv.Hkv; g += HG) {  // the same count for every thread of a warp
-    const bool on = ok && g < kv.Hkv;
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (on) {
+  const int64_t page_step = HG * kv.page_bytes;
+  for (int l = blockIdx.z; l < kv.L; l += gridDim.z) {
+    // where the first head's rows come from and go to; a thread without a row reads row 0's
+    const T* kr = static_cast<const T*>(k.p) + l * k.ls + t * k.rs + h0 * k.hs;
+    const T* vr = static_cast<const T*>(v.p) + l * v.ls + t * v.rs + h0 * v.hs;
+    uint8_t* at = kv.page(l, h0, ok ? page : 0);
+    uint32_t* key_word = reinterpret_cast<uint32_t*>(at + kv.codes(0, row)) + c * groups + grp;
+    uint16_t* value_words = reinterpret_cast<uint16_t*>(at + kv.codes(1, row)) + 2 * c * groups + grp;
+    __half2* params = reinterpret_cast<__half2*>(at + kv.params(c >> 1, row)) + grp;
+    for (int g = h0; g - h0 < kv.Hkv; g += HG) {  // the same count for every thread of a warp
+      const bool past = g >= kv.Hkv;              // (reads its last head again)
+      float x[8], y[8];
       load8(kr + 8 * u, wide, x);
       load8(vr + 8 * u, wide, y);
-      turn8<kPairing>(rope, kr, 8 * u, wide, cs, x);
+      if (ok) turn8<kPairing>(rope, kr, 8 * u, wide, cs, x);
+      uint32_t kw, vw;
+      __half2 kp, vp;
+      const bool wild = pack8(x, y, c, &kw, &vw, &kp, &vp);
+      if (ok && !past) {
+        bad |= wild;
+        *key_word = kw;
+        value_words[0] = uint16_t(vw);
+        value_words[groups] = uint16_t(vw >> 16);
+        if ((c & 1) == 0) *params = c ? vp : kp;
+      }
+      if (g + HG < kv.Hkv) {
+        kr += HG * k.hs;
+        vr += HG * v.hs;
+      }
+      key_word += page_step / 4;
+      value_words += page_step / 2;
+      params += page_step / 4;
     }
-    uint32_t kw, vw;
-    __half2 kp, vp;
-    const bool wild = pack8(x, y, c, &kw, &vw, &kp, &vp);
-    if (on) {
-      bad |= wild;
-      reinterpret_cast<uint32_t*>(at + kv.codes(0, row))[c * groups + grp] = kw;
-      uint16_t* half_words = reinterpret_cast<uint16_t*>(at + kv.codes(1, row));
-      half_words[(2 * c) * groups + grp] = uint16_t(vw);
-      half_words[(2 * c + 1) * groups + grp] = uint16_t(vw >> 16);
-      if ((c & 1) == 0) reinterpret_cast<__half2*>(at + kv.params(c >> 1, row))[grp] = c ? vp : kp;
-    }
-    kr += HG * k.hs;
-    vr += HG * v.hs;
-    at += HG * kv.page_bytes;
   }
   if (bad) flag_status(status, CONDUIT_FLAG_NONFINITE);
 }
@@ -302,7 +312,7 @@ __device__ __forceinline__ void store_values(T* to, uint32_t w, __half2 param) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4)
     packed_read_kernel(PackedDev kv, const int32_t* first, KvDev dst, BatchDev b, int HG, int32_t* status) {
-  const int r = blockIdx.y, l = blockIdx.z;
+  const int r = blockIdx.y;
   const int t0 = b.tok_off[r], n = b.tok_off[r + 1] - t0;
   const uint32_t per = kv.d / 8, lin = blockIdx.x * uint32_t(kThreads) + threadIdx.x;
   const uint32_t rest = lin / per;
@@ -321,28 +331,36 @@ __global__ void __launch_bounds__(kThreads, 4)
     return;
   }
   const int row = int(from) & ((1 << kv.page_shift) - 1), groups = kv.d / 32, grp = u / 4, c = u % 4;
-  // head 0; a head is a page record further here, a slab of rows or a page further there
-  const uint8_t* at = kv.page(l, 0, page);
-  const int64_t out = dst.row(l, 0, r, int64_t(t0) + t, t) + 8 * u;
-  const int64_t step = (dst.page_size ? int64_t(dst.page_size) : dst.n_tot) * dst.d;
+  const int64_t step = (dst.page_size ? int64_t(dst.page_size) : dst.n_tot) * dst.d;  // a head of dst
+  for (int l = blockIdx.z; l < kv.L; l += gridDim.z) {
+    const uint8_t* at = kv.page(l, 0, page);
+    const int64_t out = dst.row(l, 0, r, int64_t(t0) + t, t) + 8 * u;
 #pragma unroll 2
-  for (int g = hg; g < kv.Hkv; g += HG) {
-    const uint8_t* p = at + g * kv.page_bytes;
-    const uint32_t kw = reinterpret_cast<const uint32_t*>(p + kv.codes(0, row))[c * groups + grp];
-    const uint16_t* half_words = reinterpret_cast<const uint16_t*>(p + kv.codes(1, row));
-    const uint32_t v0 = half_words[(2 * c) * groups + grp], v1 = half_words[(2 * c + 1) * groups + grp];
-    const __half2 kp = reinterpret_cast<const __half2*>(p + kv.params(0, row))[grp];
-    const __half2 vp = reinterpret_cast<const __half2*>(p + kv.params(1, row))[grp];
-    store_values(static_cast<T*>(dst.k) + out + g * step, kw, kp);
-    store_values(static_cast<T*>(dst.v) + out + g * step, v0 | v1 << 16, vp);
+    for (int g = hg; g < kv.Hkv; g += HG) {
+      const uint8_t* p = at + g * kv.page_bytes;
+      const uint32_t kw = reinterpret_cast<const uint32_t*>(p + kv.codes(0, row))[c * groups + grp];
+      const uint16_t* half_words = reinterpret_cast<const uint16_t*>(p + kv.codes(1, row));
+      const uint32_t v0 = half_words[(2 * c) * groups + grp], v1 = half_words[(2 * c + 1) * groups + grp];
+      const __half2 kp = reinterpret_cast<const __half2*>(p + kv.params(0, row))[grp];
+      const __half2 vp = reinterpret_cast<const __half2*>(p + kv.params(1, row))[grp];
+      store_values(static_cast<T*>(dst.k) + out + g * step, kw, kp);
+      store_values(static_cast<T*>(dst.v) + out + g * step, v0 | v1 << 16, vp);
+    }
   }
 }
 
-// Groups of heads: a thread takes one head while the launch does not fill the SMs twice,
-// then up to four (its positions, pages and cosines serve all of them).
-int head_groups(int64_t threads, int heads) {
-  const int per = int(std::min<int64_t>(4, std::max<int64_t>(1, threads / (2 * 152 * 1024))));
-  return (heads + per - 1) / per;
+// How many heads and layers a thread takes: one while the launch does not fill the SMs twice,
+// then up to four heads, then up to eight layers (8 192 tokens of 28 layers, 4 heads of 128
+// dims, append: one layer a thread 241 us, eight 203; one head and one layer 400).
+struct Share {
+  int head_groups, layer_groups;
+};
+Share share_of(int64_t rows, int heads, int layers) {
+  const int64_t full = 2 * 152 * 1024, threads = rows * heads * layers;
+  const int per_head = int(std::min<int64_t>(4, std::max<int64_t>(1, threads / full)));
+  const int groups = (heads + per_head - 1) / per_head;
+  const int per_layer = int(std::min<int64_t>(8, std::max<int64_t>(1, rows * groups * layers / full)));
+  return Share{groups, (layers + per_layer - 1) / per_layer};
 }
 
 template <typename T, int VEC, int kPairing>
@@ -351,10 +369,11 @@ cudaError_t append_with(const PackedDev& kv, const SeqsDev& s, const RopeDev& ro
                         cudaStream_t stream) {
   auto blocks = [&](int64_t threads) { return int((threads + kThreads - 1) / kThreads); };
   const int64_t rows = int64_t(s.max_rows) * (kv.d / 8);
-  const int HG = head_groups(rows * kv.Hkv * s.R * kv.L, kv.Hkv);
+  const Share share = share_of(rows * s.R, kv.Hkv, kv.L);
+  const int HG = share.head_groups;
   const int kv_blocks = blocks(rows * HG);
   const int q_blocks = q.p ? blocks(int64_t(s.max_rows) * kv.Hq * units_per_row<VEC>(rope, kv.d)) : 0;
-  packed_append_kernel<T, VEC, kPairing><<<dim3(kv_blocks + q_blocks, s.R, kv.L), kThreads, 0, stream>>>(
+  packed_append_kernel<T, VEC, kPairing><<<dim3(kv_blocks + q_blocks, s.R, share.layer_groups), kThreads, 0, stream>>>(
       kv, s, rope, kv_blocks, HG, wide, k, v, q, q_out, status);
   count_launches(1);
   return cudaGetLastError();
@@ -389,9 +408,10 @@ cudaError_t launch_packed_append(const PackedDev& kv, const SeqsDev& s, const Ro
 cudaError_t launch_packed_read(const PackedDev& kv, const int32_t* first, const KvDev& dst, const BatchDev& b,
                                int max_tokens, int32_t* status, cudaStream_t stream) {
   const int64_t rows = int64_t(max_tokens) * (kv.d / 8);
-  const int HG = head_groups(rows * kv.Hkv * b.R * kv.L, kv.Hkv);
+  const Share share = share_of(rows * b.R, kv.Hkv, kv.L);
+  const int HG = share.head_groups;
   const int64_t threads = rows * HG;
-  const dim3 grid(unsigned((threads + kThreads - 1) / kThreads), b.R, kv.L);
+  const dim3 grid(unsigned((threads + kThreads - 1) / kThreads), b.R, share.layer_groups);
   if (dst.dtype == CONDUIT_BF16)
     packed_read_kernel<__nv_bfloat16><<<grid, kThreads, 0, stream>>>(kv, first, dst, b, HG, status);
   else

@@ -256,19 +256,18 @@ size_t stats_bytes(const PackedDev& kv, const SeqsDev& s, int chunks) {
 
 }  // namespace
 
-#ifndef TC_FROM
-#define TC_FROM 16
-#endif
 PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype) {
   PackedAttnPlan p{};
   const int most = int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
   const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
-  p.kernel = !mma ? kAttnSimt : int64_t(s.max_rows) * kv.G > TC_FROM ? kAttnTc : kAttnMma;
-#ifndef MINC
-#define MINC 256
-#define MINS 64
-#endif
-  const int step = p.kernel == kAttnSimt ? MINS : p.kernel == kAttnMma ? MINC : 256;  // least keys of a chunk
+  // Up to eight columns: the warp-level kernel, whose one block reads the cache once. Then
+  // tcgen05 (16 requests of 8 192 tokens, 28 / 4 heads, both in us: 14 columns 69 and 66, 21: 89
+  // and 68, 63: 181 and 70), but for few columns over a short context, where its start shows
+  // (16 requests of 1 000 tokens: 28 columns 30 and 31, 56: 47 and 39).
+  const int64_t columns = int64_t(s.max_rows) * kv.G;
+  const bool few = columns <= kCols || (columns <= 4 * kCols && most < 2048);
+  p.kernel = !mma ? kAttnSimt : few ? kAttnMma : kAttnTc;
+  const int step = p.kernel == kAttnSimt ? 64 : 256;  // least keys of a chunk
   const int64_t largest = std::max(1, (most + step - 1) / step);
   if (p.kernel == kAttnTc) {
     // One CTA per SM: the number of chunks with the least time by a model of one pass, 6 us for
