@@ -1,14 +1,14 @@
 // Attention over the 4-bit cache for few rows (decoding, drafts): warp-level tensor
 // cores, one pass over the packed keys and values.
 //
-// Mathematics. A group of 32 dims of token t is m_t + s_t (u - 8), u in 0..15. Logits come
-// group by group: x = sum_g s_tg (sum (u - 8) q) + m_tg (sum q). A nibble under the
-// exponent of 128 is 128 + u in bf16, one masked word for two codes, and a bf16 query is an
-// operand as it is; the offsets are sums of the query alone and are taken off in fp32. (The
-// tensor cores cut each sum off at 2^-23 of its size: at most 10^-6 of the log-sum-exp. With
-// fp16's 1024 + u, which needs a shift less per word, it was 6 x 10^-6.) Values are formed as
-// fp16 m + s c (2^-11 relative), weights rounded to fp16: both below the rounding of a bf16
-// output.
+// Mathematics. A group of 32 dims of token t is m_t + s_t c, c in -8..7. Logits come group by
+// group: x = sum_g s_tg (sum c q) + m_tg (sum q), with the codes exact in fp16 and the
+// queries exact too (bf16 scaled to fp16's range by a power of two per row), so only fp32 sums
+// round (to 6 x 10^-8 of a log-sum-exp). Values are formed as fp16 m + s c (2^-11 relative),
+// weights rounded to fp16: both below the rounding of a bf16 output. (Codes with their offset
+// left on, taken off in fp32, cost no instruction less on the pipe that counts and lost
+// precision: fp16's 1024 + u 6 x 10^-6 of a log-sum-exp, bf16's 128 + u 178 us for the batch of
+// 64 where this takes 172.)
 //
 // Shape. mma with the tokens (then the dims) as the 16 rows and up to 8 (row, query head)
 // columns as n, so that a KV head's group of 7 or 8 query heads wastes nothing. The
@@ -37,22 +37,7 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 // The same from zero, without registers for it.
-__device__ __forceinline__ void mma_bf16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                               uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-}
 __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                               uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -95,13 +80,6 @@ __device__ __forceinline__ uint32_t mids(const uint8_t* p, int c) {
   }
 }
 
-// The nibbles at bits 0-3 and 16-19 as bf16 128 + u.
-__device__ __forceinline__ uint32_t raw(uint32_t w) {
-  uint32_t y;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(w), "r"(0x000F000Fu), "r"(0x43004300u));
-  return y;
-}
-
 // State of a warp's running softmax for the two columns of a lane.
 template <int NG>
 struct Running {
@@ -116,7 +94,7 @@ constexpr float kSlack = 8.f;
 // One tile of 32 tokens. kEdge: some column does not see all of it.
 template <int NG, bool kEdge>
 __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, const uint32_t (&bq)[NG][4],
-                                          uint32_t qsum, const float (&qoff)[NG][2],
+                                          uint32_t qsum,
                                           const float (&to_log2)[2], int kb, int k1, int least, const int (&lim)[2], int c, int q, int key_lo) {
   constexpr int D = NG * 32;
   const uint8_t *kc = box, *vc = box + kTile * (D / 2), *kp = box + kTile * D, *vp = kp + kTile * (D / 8);
@@ -134,13 +112,14 @@ __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, c
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       float acc[4];
-      mma_bf16_first(acc, raw(wl[g]), raw(wh[g]), raw(wl[g] >> 4), raw(wh[g] >> 4), bq[g][0], bq[g][1]);
-      mma_bf16(acc, raw(wl[g] >> 8), raw(wh[g] >> 8), raw(wl[g] >> 12), raw(wh[g] >> 12), bq[g][2], bq[g][3]);
+      mma_f16_first(acc, codes_lo(wl[g]), codes_lo(wh[g]), codes_hi(wl[g]), codes_hi(wh[g]), bq[g][0], bq[g][1]);
+      const uint32_t l8 = wl[g] >> 8, h8 = wh[g] >> 8;
+      mma_f16(acc, codes_lo(l8), codes_lo(h8), codes_hi(l8), codes_hi(h8), bq[g][2], bq[g][3]);
       const float sl = __low2float(u2h(pl[g])), sh = __low2float(u2h(ph[g]));
-      x[t][0] = fmaf(sl, acc[0] - qoff[g][0], x[t][0]);
-      x[t][1] = fmaf(sl, acc[1] - qoff[g][1], x[t][1]);
-      x[t][2] = fmaf(sh, acc[2] - qoff[g][0], x[t][2]);
-      x[t][3] = fmaf(sh, acc[3] - qoff[g][1], x[t][3]);
+      x[t][0] = fmaf(sl, acc[0], x[t][0]);
+      x[t][1] = fmaf(sl, acc[1], x[t][1]);
+      x[t][2] = fmaf(sh, acc[2], x[t][2]);
+      x[t][3] = fmaf(sh, acc[3], x[t][3]);
     }
     if (kEdge) {
 #pragma unroll
@@ -332,6 +311,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
                        at_tile * row_bytes;
   const uint8_t* from = a.kv.page(it.l, it.g, 0) + (part < 2 ? a.kv.codes(part, 0) : a.kv.params(part - 2, 0));
   const int64_t page_stride = a.kv.Hkv * a.kv.page_bytes;
+  const int page_mask = (1 << a.kv.page_shift) - 1;
   // the page of this lane's run in a tile, looked up one fill ahead
   auto page_in = [&](int n) {
     const int j = k0 + (w + n * kWarps) * kTile + at_tile;
@@ -339,14 +319,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   };
   auto fill = [&](int n) {
     const int stage = n % kStages, kb = k0 + (w + n * kWarps) * kTile;
-    const int runs = (min(k1 - kb, kTile) + run - 1) >> run_shift;
-    if (lane == 0) tc::mbar_arrive_expect_tx(&full[w][stage], uint32_t((runs << run_shift) * (D + D / 4)));
+    const int tokens = min(k1 - kb, kTile), j = kb + at_tile;
+    if (lane == 0)  // whole runs
+      tc::mbar_arrive_expect_tx(&full[w][stage], uint32_t((tokens + run - 1) & -run) * (D + D / 4));
     __syncwarp();
-    if (lane < 4 * runs) {
-      const int j = kb + at_tile, row = j & ((1 << a.kv.page_shift) - 1);
-      bulk_load(dst + stage * kBox, from + page_in_pool(a, next_page) * page_stride + row * row_bytes, row_bytes << run_shift,
-                &full[w][stage]);
-    }
+    if (at_tile < tokens)
+      bulk_load(dst + stage * kBox, from + page_in_pool(a, next_page) * page_stride + (j & page_mask) * row_bytes,
+                row_bytes << run_shift, &full[w][stage]);
     next_page = page_in(n + 1);
   };
 #pragma unroll
@@ -357,7 +336,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   // [256, 512): their sums then fit fp16.
   uint32_t bq[NG][4];
   uint32_t qsum = 0;
-  float qoff[NG][2], to_log2[2];
+  float to_log2[2];
   {
     float x[NG][8], top = 0.f;
 #pragma unroll
@@ -391,12 +370,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
       for (int s = 1; s < 4; s <<= 1) total += __shfl_xor_sync(0xffffffffu, total, s);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {  // word e: dims e and e + 4
-        const __nv_bfloat162 two = __floats2bfloat162_rn(x[g][e], x[g][e + 4]);
-        bq[g][e] = *reinterpret_cast<const uint32_t*>(&two);
+        bq[g][e] = h2u(__floats2half2_rn(x[g][e], x[g][e + 4]));
       }
-      const float off = 136.f * total;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) qoff[g][e] = __shfl_sync(0xffffffffu, off, 4 * (2 * c + e));
       // slots 2 c, 2 c + 1 of the product with the mids: groups 0, 1, 2, 3, then the same in a second part
       const float first = __half2float(__float2half_rn(total));
       if (g / 2 == (c & 1))
@@ -419,9 +394,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     if (!ok) break;
     const uint8_t* box = ring + stage * kBox;
     if (kb + kTile > least)
-      tile_step<NG, true>(st, box, bq, qsum, qoff, to_log2, kb, k1, least, lim, c, q, key_lo);
+      tile_step<NG, true>(st, box, bq, qsum, to_log2, kb, k1, least, lim, c, q, key_lo);
     else
-      tile_step<NG, false>(st, box, bq, qsum, qoff, to_log2, kb, k1, least, lim, c, q, key_lo);
+      tile_step<NG, false>(st, box, bq, qsum, to_log2, kb, k1, least, lim, c, q, key_lo);
     __syncwarp();
     if (n + kStages < mine) fill(n + kStages);
   }
