@@ -13,7 +13,7 @@
 namespace conduit {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr float kClip = 61440.f;  // m +- 8 s stays inside fp16
 
 // a + b of products that were rounded before. A packed multiply followed by a packed
@@ -22,21 +22,31 @@ __device__ __forceinline__ float2 add_rounded(float2 a, float2 b) {
   return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y));
 }
 
-// 8 elements from p as fp32.
+// 8 elements as they lie in memory, and as fp32.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool wide, float (&x)[8]) {
+struct Raw8 {
+  uint4 w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T* p, bool wide) {
+  Raw8<T> r;
   if (wide) {
-    constexpr int N = 16 / sizeof(T);
 #pragma unroll
-    for (int c = 0; c < 8 / N; ++c) {
-      const Chunk<T, N> w = *reinterpret_cast<const Chunk<T, N>*>(p + c * N);
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[c * N + e] = to_float(w.v[e]);
-    }
+    for (int c = 0; c < int(sizeof(T) / 2); ++c) r.w[c] = reinterpret_cast<const uint4*>(p)[c];
   } else {
+    T e8[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = to_float(p[e]);
+    for (int e = 0; e < 8; ++e) e8[e] = p[e];
+#pragma unroll
+    for (int c = 0; c < int(sizeof(T) / 2); ++c) r.w[c] = reinterpret_cast<const uint4*>(e8)[c];
   }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void to_floats(const Raw8<T>& r, float (&x)[8]) {
+  const T* e8 = reinterpret_cast<const T*>(r.w);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = to_float(e8[e]);
 }
 
 // How the pairs of a chunk of 8 dims lie: none, in the matching chunk of the other half
@@ -81,14 +91,15 @@ __device__ __forceinline__ void load_turn8(const RopeDev& rope, const int (&pos)
   }
 }
 
-// The chunk's dims after rotation. The products are rounded before they are added.
+// The chunk's dims after rotation; `far`: the matching chunk of the other half (kChunks). The
+// products are rounded before they are added.
 template <int kPairing, typename T>
-__device__ __forceinline__ void turn8(const RopeDev& rope, const T* row, int i0, bool wide, const float2 (&cs)[8],
-                                      float (&x)[8]) {
+__device__ __forceinline__ void turn8(const RopeDev& rope, const T* row, int i0, const Raw8<T>& far,
+                                      const float2 (&cs)[8], float (&x)[8]) {
   if (kPairing == kNoTurn || i0 >= rope.rot) return;
   float other[8];
   if (kPairing == kChunks) {
-    load8(row + (i0 < rope.half ? i0 + rope.half : i0 - rope.half), wide, other);
+    to_floats(far, other);
   } else if (kPairing == kNeighbours) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) other[e] = x[e ^ 1];
@@ -99,8 +110,6 @@ __device__ __forceinline__ void turn8(const RopeDev& rope, const T* row, int i0,
       const int j = rope.layout == CONDUIT_ROPE_PAIRS ? i ^ 1 : i < rope.half ? i + rope.half : i - rope.half;
       other[e] = i < rope.rot ? to_float(row[j]) : 0.f;
     }
-  }
-  if (kPairing == kAnywhere) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (i0 + e < rope.rot) x[e] = __fadd_rn(__fmul_rn(x[e], cs[e].x), __fmul_rn(other[e], cs[e].y));
@@ -209,7 +218,7 @@ __device__ __forceinline__ bool pack8(float (&x)[8], float (&y)[8], int c, uint3
 // pairs per thread. Either walks over layers blockIdx.z, + gridDim.z, ...: a row's place,
 // positions and cosines are worked out once for all of them.
 template <typename T, int VEC, int kPairing>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, 7)
     packed_append_kernel(PackedDev kv, SeqsDev s, RopeDev rope, int kv_blocks, int HG, bool wide, RowsDev k, RowsDev v,
                          RowsDev q, RowsDev q_out, int32_t* status) {
   const int r = blockIdx.y;
@@ -250,39 +259,54 @@ __global__ void __launch_bounds__(kThreads, 4)
   if (ok) load_turn8<kPairing>(rope, pos, 8 * u, cs);
   const int row = slot & ((1 << kv.page_shift) - 1), groups = kv.d / 32, grp = u / 4, c = u % 4;
   bool bad = false;
-  const int64_t page_step = HG * kv.page_bytes;
-  for (int l = blockIdx.z; l < kv.L; l += gridDim.z) {
-    // where the first head's rows come from and go to; a thread without a row reads row 0's
-    const T* kr = static_cast<const T*>(k.p) + l * k.ls + t * k.rs + h0 * k.hs;
-    const T* vr = static_cast<const T*>(v.p) + l * v.ls + t * v.rs + h0 * v.hs;
+  // Layer by layer and head by head, the next rows under way while one is packed. A thread without
+  // a row reads row 0's; the count of heads is the same for every thread of a warp, past the last
+  // one it is read again.
+  const int i0 = 8 * u, far0 = i0 >= rope.rot ? i0 : i0 < rope.half ? i0 + rope.half : i0 - rope.half;
+  const int steps = (kv.Hkv + HG - 1) / HG;
+  const T *kr = nullptr, *vr = nullptr;
+  Raw8<T> k_raw, far_raw, v_raw;
+  auto fetch = [&](int l, int step) {
+    const int g = min(h0 + step * HG, kv.Hkv - 1);
+    kr = static_cast<const T*>(k.p) + l * k.ls + t * k.rs + g * k.hs;
+    vr = static_cast<const T*>(v.p) + l * v.ls + t * v.rs + g * v.hs;
+    k_raw = load8(kr + i0, wide);
+    if (kPairing == kChunks) far_raw = load8(kr + far0, wide);
+    v_raw = load8(vr + i0, wide);
+  };
+  int l = blockIdx.z;
+  if (l < kv.L) fetch(l, 0);
+  while (l < kv.L) {
+    // the first head's places; a head is a page record further
     uint8_t* at = kv.page(l, h0, ok ? page : 0);
     uint32_t* key_word = reinterpret_cast<uint32_t*>(at + kv.codes(0, row)) + c * groups + grp;
     uint16_t* value_words = reinterpret_cast<uint16_t*>(at + kv.codes(1, row)) + 2 * c * groups + grp;
     __half2* params = reinterpret_cast<__half2*>(at + kv.params(c >> 1, row)) + grp;
-    for (int g = h0; g - h0 < kv.Hkv; g += HG) {  // the same count for every thread of a warp
-      const bool past = g >= kv.Hkv;              // (reads its last head again)
+    const int next_l = l + gridDim.z;
+    for (int step = 0; step < steps; ++step) {
       float x[8], y[8];
-      load8(kr + 8 * u, wide, x);
-      load8(vr + 8 * u, wide, y);
-      if (ok) turn8<kPairing>(rope, kr, 8 * u, wide, cs, x);
+      to_floats(k_raw, x);
+      to_floats(v_raw, y);
+      if (ok) turn8<kPairing>(rope, kr, i0, far_raw, cs, x);
+      if (step + 1 < steps)
+        fetch(l, step + 1);
+      else if (next_l < kv.L)
+        fetch(next_l, 0);
       uint32_t kw, vw;
       __half2 kp, vp;
       const bool wild = pack8(x, y, c, &kw, &vw, &kp, &vp);
-      if (ok && !past) {
+      if (ok && h0 + step * HG < kv.Hkv) {
         bad |= wild;
         *key_word = kw;
         value_words[0] = uint16_t(vw);
         value_words[groups] = uint16_t(vw >> 16);
         if ((c & 1) == 0) *params = c ? vp : kp;
       }
-      if (g + HG < kv.Hkv) {
-        kr += HG * k.hs;
-        vr += HG * v.hs;
-      }
-      key_word += page_step / 4;
-      value_words += page_step / 2;
-      params += page_step / 4;
+      key_word += HG * kv.page_bytes / 4;
+      value_words += HG * kv.page_bytes / 2;
+      params += HG * kv.page_bytes / 4;
     }
+    l = next_l;
   }
   if (bad) flag_status(status, CONDUIT_FLAG_NONFINITE);
 }
@@ -304,13 +328,13 @@ __device__ __forceinline__ void store_values(T* to, uint32_t w, __half2 param) {
       y.v[e] = from_float<T>(u.x);
       y.v[e + 1] = from_float<T>(u.y);
     }
-    *reinterpret_cast<Chunk<T, N>*>(to + p * N) = y;
+    store_once<T, N>(to + p * N, y);
   }
 }
 
 // A thread turns 8 dims of a token's K and V into values, for heads hg, hg + HG, ...
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, 10)
     packed_read_kernel(PackedDev kv, const int32_t* first, KvDev dst, BatchDev b, int HG, int32_t* status) {
   const int r = blockIdx.y;
   const int t0 = b.tok_off[r], n = b.tok_off[r + 1] - t0;
