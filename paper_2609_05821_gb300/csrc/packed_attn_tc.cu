@@ -94,13 +94,32 @@ __device__ __forceinline__ bool tc_item(const AttnArgs& a, Item* it) {
   return it->chunk == 0 || it->chunk * a.chunk < it->len;
 }
 
-// One lane's share of a token's keys: words NG c on, a word's values in chunk 4 g + c.
+// One lane's share of a packed token: NG words of codes, the parameters of its groups. Keys, and
+// values of 64 and 128 dims: words NG c on; values of 96 dims: words c, c + 4, c + 8.
 template <int NG>
-__device__ __forceinline__ void unpack_keys(uint8_t* tile, const uint8_t* box, int token, int c) {
-  constexpr int D = 32 * NG;
+struct Packed {
   uint32_t w[NG], p[NG];
-  load_words<NG>(box + token * (D / 2) + c * (D / 8), w);
-  load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), p);
+};
+template <int NG, bool kValues>
+__device__ __forceinline__ Packed<NG> take(const uint8_t* box, int token, int c) {
+  constexpr int D = 32 * NG;
+  Packed<NG> x;
+  const uint8_t* row = box + token * (D / 2);
+  if constexpr (kValues && NG == 3) {
+#pragma unroll
+    for (int n = 0; n < NG; ++n) x.w[n] = *reinterpret_cast<const uint32_t*>(row + 4 * (4 * n + c));
+  } else {
+    load_words<NG>(row + c * (D / 8), x.w);
+  }
+  load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), x.p);
+  return x;
+}
+
+// Keys: a word's values in chunk 4 g + c.
+template <int NG>
+__device__ __forceinline__ void unpack_keys(uint8_t* tile, const Packed<NG>& x, int token, int c) {
+  const uint32_t(&w)[NG] = x.w;
+  const uint32_t(&p)[NG] = x.p;
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const int ch = 4 * g + c;
@@ -111,11 +130,9 @@ __device__ __forceinline__ void unpack_keys(uint8_t* tile, const uint8_t* box, i
 
 // The same in two parts: hi is the value in fp16, lo what is missing from it.
 template <int NG>
-__device__ __forceinline__ void unpack_keys_exact(uint8_t* hi, uint8_t* lo, const uint8_t* box, int token, int c) {
-  constexpr int D = 32 * NG;
-  uint32_t w[NG], p[NG];
-  load_words<NG>(box + token * (D / 2) + c * (D / 8), w);
-  load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), p);
+__device__ __forceinline__ void unpack_keys_exact(uint8_t* hi, uint8_t* lo, const Packed<NG>& x, int token, int c) {
+  const uint32_t(&w)[NG] = x.w;
+  const uint32_t(&p)[NG] = x.p;
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const float2 sm = __half22float2(u2h(p[g]));
@@ -136,22 +153,14 @@ __device__ __forceinline__ void unpack_keys_exact(uint8_t* hi, uint8_t* lo, cons
   }
 }
 
-// One lane's share of a token's values. kEdge: the tile holds tokens that some column does
-// not see. Their weight there is 0, and 0 times NaN must not be: a parameter pair that is not
-// finite becomes 0 and its first token is noted for the group.
+// Values. kEdge: the tile holds tokens that some column does not see. Their weight there is 0,
+// and 0 times NaN must not be: a parameter pair that is not finite becomes 0 and its first
+// token is noted for the group.
 template <int NG, bool kEdge>
-__device__ __forceinline__ void unpack_values(uint8_t* tile, const uint8_t* box, int token, int c, int kb, int k1,
-                                              int least, int* poison) {
-  constexpr int D = 32 * NG;
-  const uint8_t* row = box + token * (D / 2);
-  uint32_t w[NG], p[NG];
-  if constexpr (NG == 3) {  // words c, c + 4, c + 8
-#pragma unroll
-    for (int n = 0; n < NG; ++n) w[n] = *reinterpret_cast<const uint32_t*>(row + 4 * (4 * n + c));
-  } else {  // words NG c on
-    load_words<NG>(row + c * (D / 8), w);
-  }
-  load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), p);
+__device__ __forceinline__ void unpack_values(uint8_t* tile, Packed<NG> x, int token, int c, int kb, int k1, int least,
+                                              int* poison) {
+  const uint32_t(&w)[NG] = x.w;
+  uint32_t(&p)[NG] = x.p;
   if (kEdge) {
     const int j = kb + token;
 #pragma unroll
@@ -230,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   if (tid == 0) {
     for (int s = 0; s < kRing; ++s) {
       tc::mbar_init(&bars.raw_full[s], 1);
-      tc::mbar_init(&bars.raw_free[s], 4);
+      tc::mbar_init(&bars.raw_free[s], kUnpackWarps);
     }
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&bars.k_full[s], 4);
@@ -297,6 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       for (int v = 0; v < 2; ++v) {
         const int slot = issued % kRing;
         if (issued >= kRing && !(ok = wait_warp(&bars.raw_free[slot], (issued / kRing - 1) & 1, abort))) break;
+        // kExact has one key buffer, whose phases the warps that unpack do not all see: the copies wait
         if (kExact && !v && t > 0 && !(ok = wait_warp(&bars.k_free[0], (t - 1) & 1, abort))) break;
         if (lane == 0) tc::mbar_arrive_expect_tx(&bars.raw_full[slot], uint32_t(runs << run_shift) * (D / 2 + D / 8));
         __syncwarp();
@@ -314,44 +324,58 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     // A unit is a quarter (32 tokens) of a tile's keys, then of its values; six warps take
     // them in turn. Four lanes a token. Keys: the two tokens of eight lanes are four apart, so
     // that their chunks fall into different banks of the swizzled tile; values: side by side.
+    // Every warp sees every copy land and says so before its slot is used again, also where
+    // another four warps unpack it: none can take a phase of a slot for the one two before it.
     const int c = lane & 3, i8 = lane >> 2;
-    for (int n = warp - kUnpackWarp; n < 8 * tiles; n += kUnpackWarps) {
-      const int t = n >> 3, v = (n >> 2) & 1, token0 = 32 * (n & 3), stage = t & 1;
-      const int load = 2 * t + v, slot = load % kRing;
-      const uint8_t* box = raw + slot * Z::kRaw;
+    int unit = warp - kUnpackWarp;  // the next one of this warp
+    for (int load = 0; load < 2 * tiles; ++load) {
+      const int t = load >> 1, v = load & 1, stage = t & 1, slot = load % kRing;
       bool ok = wait_warp(&bars.raw_full[slot], (load / kRing) & 1, abort);
-      // A buffer is free once its last tile but one has been used. A warp takes only some of the
-      // units, but cannot take a phase for the one two before it: the ring lets no unit begin
-      // before every unit three copies back is done, and those waited for that earlier phase.
-      // kExact has one key buffer, for which that would not hold; there the copies wait.
-      if (ok && t >= 2 && !(kExact && !v))
-        ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
+      const bool mine = unit < 4 * load + 4;
+      const int token = 32 * (unit & 3) + (v ? i8 : (i8 & 1) * 4 + (i8 >> 1));
+      // Into registers first, so that the next copy into the slot starts while this one is unpacked
+      // (held until the end, the ring gave the pace: 126 us for 8 192 keys of two column tiles).
+      Packed<NG> x[4];
+      if (ok) {
+        const uint8_t* box = raw + slot * Z::kRaw;
+        if (mine) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[i] = v ? take<NG, true>(box, token + 8 * i, c) : take<NG, false>(box, token + 8 * i, c);
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars.raw_free[slot]);
+        // A buffer is free once its last tile but one has been used. (A warp's unit before this one
+        // waited for a use at most a tile earlier, so this wait cannot mistake its phase either.)
+        if (mine && t >= 2 && !(kExact && !v))
+          ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
+      }
       if (!ok) {
         if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
         break;
       }
+      if (!mine) continue;
+      unit += kUnpackWarps;
       uint8_t* tile = v ? vt + stage * Z::kTile : kExact ? kt : kt + stage * Z::kTile;
       const int kb = k0 + t * kKeys;
-      if (!v && kExact) {
-#pragma unroll 1
-        for (int i = 0; i < 4; ++i)
-          unpack_keys_exact<NG>(tile, tile + Z::kTile, box, token0 + (i8 & 1) * 4 + (i8 >> 1) + 8 * i, c);
-      } else if (!v) {
+      if (!v) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) unpack_keys<NG>(tile, box, token0 + (i8 & 1) * 4 + (i8 >> 1) + 8 * i, c);
+        for (int i = 0; i < 4; ++i) {
+          if (kExact)
+            unpack_keys_exact<NG>(tile, tile + Z::kTile, x[i], token + 8 * i, c);
+          else
+            unpack_keys<NG>(tile, x[i], token + 8 * i, c);
+        }
       } else if (kb + kKeys > least) {  // some column does not see the whole tile
-#pragma unroll 1
-        for (int i = 0; i < 4; ++i) unpack_values<NG, true>(tile, box, token0 + i8 + 8 * i, c, kb, k1, least, poison);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack_values<NG, true>(tile, x[i], token + 8 * i, c, kb, k1, least, poison);
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) unpack_values<NG, false>(tile, box, token0 + i8 + 8 * i, c, kb, k1, least, poison);
+        for (int i = 0; i < 4; ++i) unpack_values<NG, false>(tile, x[i], token + 8 * i, c, kb, k1, least, poison);
       }
       tc::fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) {
-        tc::mbar_arrive(&bars.raw_free[slot]);
-        tc::mbar_arrive(v ? &bars.v_full[stage] : &bars.k_full[kExact ? 0 : stage]);
-      }
+      if (lane == 0) tc::mbar_arrive(v ? &bars.v_full[stage] : &bars.k_full[kExact ? 0 : stage]);
     }
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------------ MMAs
