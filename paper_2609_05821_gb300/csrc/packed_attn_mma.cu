@@ -8,14 +8,17 @@
 // weights rounded to fp16: both below the rounding of a bf16 output. (Codes with their offset
 // left on, taken off in fp32, cost no instruction less on the pipe that counts and lost
 // precision: fp16's 1024 + u 6 x 10^-6 of a log-sum-exp, bf16's 128 + u 178 us for the batch of
-// 64 where this takes 172.)
+// 64 where this took 172.)
 //
 // Shape. mma with the tokens (then the dims) as the 16 rows and up to 8 (row, query head)
 // columns as n, so that a KV head's group of 7 or 8 query heads wastes nothing. The
 // logits' accumulators hold tokens by lane / 4; movmatrix turns them into the operand of
-// the value product. Each warp owns tiles of 32 tokens with a ring of its own: bulk copies
-// of whole page runs, so no block-wide barrier is met before the end, where the warps'
-// results are joined.
+// the value product. Each warp owns tiles of 32 tokens with a ring of its own, so no
+// block-wide barrier is met before the end, where the warps' results are joined. A tile
+// comes in bulk copies of whole pages, or of four parts of a longer page: the lanes issue
+// theirs one after the other, about 100 cycles each. (Four parts of every page: 168 us for
+// the batch of 64 with pages of 16 tokens where this takes 157; 16-byte copies lane by lane,
+// whose instructions come out of the same issue slots, 174.)
 //
 // Bound: 1.25 d bytes per token and KV head from HBM; next to it the unpacking of the
 // values, whose integer and fp16 instructions issue at half rate.
@@ -91,24 +94,40 @@ struct Running {
 // units): weights stay below 2^8, which fp16 and the fp32 sums hold as well as 1.
 constexpr float kSlack = 8.f;
 
+// A tile in shared memory: page after page as in the pool, and of pages of more than 32 tokens
+// the 32 as a page of their own. Offsets of the codes and parameters of tokens 8 i.. of K (v = 0)
+// or V (v = 1); kRun: tokens of a page in the tile.
+template <int NG, int kRun>
+struct Box {
+  static constexpr int D = NG * 32, kPage = kRun * (D + D / 4);
+  __device__ static constexpr int codes(int v, int i) {
+    return 8 * i / kRun * kPage + v * kRun * (D / 2) + 8 * i % kRun * (D / 2);
+  }
+  __device__ static constexpr int params(int v, int i) {
+    return 8 * i / kRun * kPage + kRun * D + v * kRun * (D / 8) + 8 * i % kRun * (D / 8);
+  }
+};
+
 // One tile of 32 tokens. kEdge: some column does not see all of it.
-template <int NG, bool kEdge>
+template <int NG, int kRun, bool kEdge>
 __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, const uint32_t (&bq)[NG][4],
                                           uint32_t qsum,
                                           const float (&to_log2)[2], int kb, int k1, int least, const int (&lim)[2], int c, int q, int key_lo) {
   constexpr int D = NG * 32;
-  const uint8_t *kc = box, *vc = box + kTile * (D / 2), *kp = box + kTile * D, *vp = kp + kTile * (D / 8);
+  using B = Box<NG, kRun>;
   float x[2][4];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int lo = 16 * t + key_lo, hi = lo + 8;
+    const uint8_t* kp_lo = box + B::params(0, 2 * t) + key_lo * (D / 8);
+    const uint8_t* kp_hi = box + B::params(0, 2 * t + 1) + key_lo * (D / 8);
     uint32_t wl[NG], wh[NG], pl[NG], ph[NG];
-    load_words<NG>(kc + lo * (D / 2) + c * (D / 8), wl);
-    load_words<NG>(kc + hi * (D / 2) + c * (D / 8), wh);
-    load_words<NG>(kp + lo * (D / 8), pl);
-    load_words<NG>(kp + hi * (D / 8), ph);
+    load_words<NG>(box + B::codes(0, 2 * t) + key_lo * (D / 2) + c * (D / 8), wl);
+    load_words<NG>(box + B::codes(0, 2 * t + 1) + key_lo * (D / 2) + c * (D / 8), wh);
+    load_words<NG>(kp_lo, pl);
+    load_words<NG>(kp_hi, ph);
     // sum_g m_tg (sum q): one product over the groups, the query sums in two fp16 parts
-    mma_f16_first(x[t], mids<NG>(kp + lo * (D / 8), c), mids<NG>(kp + hi * (D / 8), c), 0, 0, qsum, 0);
+    mma_f16_first(x[t], mids<NG>(kp_lo, c), mids<NG>(kp_hi, c), 0, 0, qsum, 0);
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       float acc[4];
@@ -165,9 +184,9 @@ __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, c
     uint32_t v[4][(NG + 1) / 2], p[4][NG];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int key = 16 * t + (e & 1 ? (4 + c) ^ 1 : c) + (e & 2 ? 8 : 0);
-      load_halves<NG>(vc + key * (D / 2) + q * (D / 16), v[e]);
-      load_words<NG>(vp + key * (D / 8), p[e]);
+      const int block = 2 * t + (e >> 1), in = e & 1 ? (4 + c) ^ 1 : c, key = 8 * block + in;
+      load_halves<NG>(box + B::codes(1, block) + in * (D / 2) + q * (D / 16), v[e]);
+      load_words<NG>(box + B::params(1, block) + in * (D / 8), p[e]);
       if (kEdge) {
         // tokens that some column does not see: their weight there is 0, and 0 times NaN must not be
 #pragma unroll
@@ -196,7 +215,7 @@ __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, c
     for (int t = 0; t < 4; ++t) {
       const int key = 8 * t + key_lo;
       uint32_t p[NG];
-      load_words<NG>(vp + key * (D / 8), p);
+      load_words<NG>(box + B::params(1, t) + key_lo * (D / 8), p);
 #pragma unroll
       for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -235,9 +254,10 @@ __device__ __forceinline__ T read_of(const T* p, int rank) {
 }
 
 // kCluster: the CTAs of a cluster take the chunks of a context and join them in shared memory.
-template <int NG, bool kCluster>
+template <int NG, int kRun, bool kCluster>
 __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   static_assert(kCols * NG * 8 <= kWarps * 32, "four dims a thread");
+  using B = Box<NG, kRun>;
   constexpr int D = NG * 32, kBox = kBoxBytes(D);
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[kWarps][kStages];
@@ -251,10 +271,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   const int key_lo = (q & 1) ? (4 + (q >> 1)) ^ 1 : q >> 1;
 
   // Loads that wait for nothing but the request go out first: the page of this lane's first
-  // copy, then the column's query.
-  const int run_shift = min(5, a.kv.page_shift), at_tile = (lane >> 2) << run_shift, k0 = it.chunk * a.chunk;
+  // copy, then the column's query. A copy: a whole page (lane r page r of a tile), or a part of 32
+  // tokens of a longer one (lane p: K codes, V codes, K and V parameters).
+  const bool whole = a.kv.page_shift <= 5;
+  const int copies = whole ? kTile / kRun : 4, at_tile = whole ? lane * kRun : 0, k0 = it.chunk * a.chunk;
   const int first_j = k0 + w * kTile + at_tile;
-  int next_page = at_tile < kTile && first_j < it.len ? page_entry(a, it.r, first_j) : 0;
+  int next_page = lane < copies && first_j < it.len ? page_entry(a, it.r, first_j) : 0;
   uint4 qv[NG];
   {
     const int j = it.cb * kCols + q;
@@ -303,29 +325,28 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   }
   __syncwarp();
 
-  // A lane copies one part (K codes, V codes, K and V parameters) of one run, the tokens of
-  // a tile that lie in one page.
-  const int run = 1 << run_shift, part = lane & 3;
-  const int row_bytes = part < 2 ? D / 2 : D / 8;
-  const uint32_t dst = tc::smem_u32(ring) + (part < 2 ? part * kTile * (D / 2) : kTile * D + (part - 2) * kTile * (D / 8)) +
-                       at_tile * row_bytes;
-  const uint8_t* from = a.kv.page(it.l, it.g, 0) + (part < 2 ? a.kv.codes(part, 0) : a.kv.params(part - 2, 0));
+  const int row_bytes = whole ? 0 : lane < 2 ? D / 2 : D / 8;
+  const uint32_t bytes = whole ? B::kPage : kTile * row_bytes;
+  const uint32_t dst = tc::smem_u32(ring) + (whole     ? lane * B::kPage
+                                             : lane < 2 ? lane * kTile * (D / 2)
+                                                        : kTile * D + (lane - 2) * kTile * (D / 8));
+  const uint8_t* from = a.kv.page(it.l, it.g, 0) + (whole ? 0 : lane < 2 ? a.kv.codes(lane, 0) : a.kv.params(lane - 2, 0));
   const int64_t page_stride = a.kv.Hkv * a.kv.page_bytes;
   const int page_mask = (1 << a.kv.page_shift) - 1;
-  // the page of this lane's run in a tile, looked up one fill ahead
+  // the page of this lane's copy in a tile, looked up one fill ahead
   auto page_in = [&](int n) {
     const int j = k0 + (w + n * kWarps) * kTile + at_tile;
-    return n < mine && j < k1 && at_tile < kTile ? page_entry(a, it.r, j) : 0;
+    return n < mine && j < k1 && lane < copies ? page_entry(a, it.r, j) : 0;
   };
   auto fill = [&](int n) {
     const int stage = n % kStages, kb = k0 + (w + n * kWarps) * kTile;
-    const int tokens = min(k1 - kb, kTile), j = kb + at_tile;
+    const int tokens = min(k1 - kb, kTile);
     if (lane == 0)  // whole runs
-      tc::mbar_arrive_expect_tx(&full[w][stage], uint32_t((tokens + run - 1) & -run) * (D + D / 4));
+      tc::mbar_arrive_expect_tx(&full[w][stage], uint32_t((tokens + kRun - 1) & -kRun) * (D + D / 4));
     __syncwarp();
-    if (at_tile < tokens)
-      bulk_load(dst + stage * kBox, from + page_in_pool(a, next_page) * page_stride + (j & page_mask) * row_bytes,
-                row_bytes << run_shift, &full[w][stage]);
+    if (lane < copies && at_tile < tokens)
+      bulk_load(dst + stage * kBox, from + page_in_pool(a, next_page) * page_stride + (kb & page_mask) * row_bytes, bytes,
+                &full[w][stage]);
     next_page = page_in(n + 1);
   };
 #pragma unroll
@@ -394,9 +415,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
     if (!ok) break;
     const uint8_t* box = ring + stage * kBox;
     if (kb + kTile > least)
-      tile_step<NG, true>(st, box, bq, qsum, to_log2, kb, k1, least, lim, c, q, key_lo);
+      tile_step<NG, kRun, true>(st, box, bq, qsum, to_log2, kb, k1, least, lim, c, q, key_lo);
     else
-      tile_step<NG, false>(st, box, bq, qsum, to_log2, kb, k1, least, lim, c, q, key_lo);
+      tile_step<NG, kRun, false>(st, box, bq, qsum, to_log2, kb, k1, least, lim, c, q, key_lo);
     __syncwarp();
     if (n + kStages < mine) fill(n + kStages);
   }
@@ -507,11 +528,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   }
 }
 
-template <int NG, bool kCluster>
+template <int NG, int kRun, bool kCluster>
 cudaError_t launch(const AttnArgs& a, int64_t items, cudaStream_t stream) {
   constexpr int kSmem = kWarps * kStages * kBoxBytes(NG * 32);
   cudaError_t err =
-      cudaFuncSetAttribute(packed_attn_mma<NG, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+      cudaFuncSetAttribute(packed_attn_mma<NG, kRun, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (err) return err;
   cudaLaunchAttribute cluster{};
   cluster.id = cudaLaunchAttributeClusterDimension;
@@ -525,16 +546,25 @@ cudaError_t launch(const AttnArgs& a, int64_t items, cudaStream_t stream) {
   cfg.attrs = &cluster;
   cfg.numAttrs = kCluster ? 1 : 0;
   count_launches(1);
-  return cudaLaunchKernelEx(&cfg, packed_attn_mma<NG, kCluster>, a);
+  return cudaLaunchKernelEx(&cfg, packed_attn_mma<NG, kRun, kCluster>, a);
+}
+
+template <int NG>
+cudaError_t launch(const AttnArgs& a, int64_t items, bool cluster, cudaStream_t stream) {
+  switch (a.kv.page_shift) {
+    case 3: return cluster ? launch<NG, 8, true>(a, items, stream) : launch<NG, 8, false>(a, items, stream);
+    case 4: return cluster ? launch<NG, 16, true>(a, items, stream) : launch<NG, 16, false>(a, items, stream);
+    default: return cluster ? launch<NG, 32, true>(a, items, stream) : launch<NG, 32, false>(a, items, stream);
+  }
 }
 
 }  // namespace
 
 cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, bool cluster, cudaStream_t stream) {
   switch (a.kv.d) {
-    case 64: return cluster ? launch<2, true>(a, items, stream) : launch<2, false>(a, items, stream);
-    case 96: return cluster ? launch<3, true>(a, items, stream) : launch<3, false>(a, items, stream);
-    default: return cluster ? launch<4, true>(a, items, stream) : launch<4, false>(a, items, stream);
+    case 64: return launch<2>(a, items, cluster, stream);
+    case 96: return launch<3>(a, items, cluster, stream);
+    default: return launch<4>(a, items, cluster, stream);
   }
 }
 
