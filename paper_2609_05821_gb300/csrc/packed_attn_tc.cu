@@ -10,7 +10,7 @@
 //   warp 0            MMAs: P_x(t) V(t), then S_x(t + 1), for x = A, B; one lane issues.
 //                     The first warp, because the schedulers favour it: as warp 13 it took
 //                     120 cycles to issue an MMA of 64
-//   warp 1            bulk copies of page runs into a small ring, keys and values in turn
+//   warp 1            bulk copies of pages into a small ring, half a key tile at a time
 //   warps 2-7         unpack: four lanes a token, a word of eight codes at a time
 //   warps 8-11, 12-15 softmax of A and of B: a thread owns a column and all 128 keys
 // One column tile's softmax runs beside the other's MMAs. MMAs of one thread complete in
@@ -34,14 +34,15 @@ constexpr int kTcCols = 2 * kTileCols;
 constexpr int kMmaWarp = 0, kLoadWarp = 1, kUnpackWarp = 2, kUnpackWarps = 6, kSoftWarp = 8;
 constexpr uint32_t kBlock = 128 * 128;        // 128 rows of 64 fp16, swizzled
 constexpr uint32_t kSCols = 128, kPCol = 64, kOCol = 256;
-constexpr int kRing = 3;                      // packed keys and values in turn
+constexpr int kHalf = kKeys / 2;              // keys of a load
+constexpr int kRing = 3;                      // loads under way
 constexpr float kSlack = 8.f;                 // as in packed_attn_mma.cu
 
 template <int NG>
 struct Sizes {
   static constexpr int D = 32 * NG;
   static constexpr uint32_t kTile = (D + 63) / 64 * kBlock;  // a query, key or value tile
-  static constexpr uint32_t kRaw = kKeys * (D / 2 + D / 8);   // packed keys (or values) of a tile
+  static constexpr uint32_t kRaw = kHalf * (D + D / 4);      // packed keys and values of half a tile
   static constexpr uint32_t kSmem = 1024 + 6 * kTile + kRing * kRaw;
 };
 
@@ -101,17 +102,17 @@ struct Packed {
   uint32_t w[NG], p[NG];
 };
 template <int NG, bool kValues>
-__device__ __forceinline__ Packed<NG> take(const uint8_t* box, int token, int c) {
+__device__ __forceinline__ Packed<NG> take(const uint8_t* codes, const uint8_t* params, int token, int c) {
   constexpr int D = 32 * NG;
   Packed<NG> x;
-  const uint8_t* row = box + token * (D / 2);
+  const uint8_t* row = codes + token * (D / 2);
   if constexpr (kValues && NG == 3) {
 #pragma unroll
     for (int n = 0; n < NG; ++n) x.w[n] = *reinterpret_cast<const uint32_t*>(row + 4 * (4 * n + c));
   } else {
     load_words<NG>(row + c * (D / 8), x.w);
   }
-  load_words<NG>(box + kKeys * (D / 2) + token * (D / 8), x.p);
+  load_words<NG>(params + token * (D / 8), x.p);
   return x;
 }
 
@@ -284,55 +285,58 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;" ::: "memory");
   if (warp == kLoadWarp) {
     // ---------------------------------------------------------------- copies
-    const int run_shift = min(7, a.kv.page_shift), run = 1 << run_shift;
-    const int part = lane & 1, at_tile = (lane >> 1) << run_shift;  // codes or parameters of one run
-    const int row_bytes = part ? D / 8 : D / 2;
-    const uint32_t dst = tc::smem_u32(raw) + (part ? kKeys * (D / 2) : 0) + at_tile * row_bytes;
+    // A load: the packed keys and values of half a tile, in copies of whole pages (lane r page r)
+    // or, of a longer page, of four parts (lane p: K codes, V codes, K and V parameters). The lanes
+    // issue theirs one after the other, about 100 cycles each: with codes and parameters of keys
+    // and of values apart, a tile took as long to issue as its MMAs (377 us for 8 192 keys at 16
+    // tokens a page, 344 at 64).
+    const bool whole = a.kv.page_shift <= 6;
+    const int run_shift = min(6, a.kv.page_shift), copies = whole ? kHalf >> run_shift : 4;
+    const int at_half = whole ? lane << run_shift : 0, row_bytes = whole ? 0 : lane < 2 ? D / 2 : D / 8;
+    const uint32_t bytes = whole ? uint32_t(a.kv.page_bytes) : kHalf * row_bytes;
+    const uint32_t dst = tc::smem_u32(raw) + (whole     ? lane * bytes
+                                              : lane < 2 ? lane * kHalf * (D / 2)
+                                                         : kHalf * D + (lane - 2) * kHalf * (D / 8));
+    const uint8_t* from = a.kv.page(it.l, it.g, 0) + (whole ? 0 : lane < 2 ? a.kv.codes(lane, 0) : a.kv.params(lane - 2, 0));
     const int64_t page_stride = a.kv.Hkv * a.kv.page_bytes;
-    const uint8_t* head = a.kv.page(it.l, it.g, 0);
-    auto page_at = [&](int t) {  // page of this lane's run in tile t, looked up a tile ahead
-      const int j = k0 + t * kKeys + at_tile;
-      return at_tile < kKeys && j < k1 ? page_entry(a, it.r, j) : 0;
+    auto page_at = [&](int load) {  // page of this lane's copy, looked up a load ahead
+      const int j = k0 + load * kHalf + at_half;
+      return lane < copies && j < k1 ? page_entry(a, it.r, j) : 0;
     };
     int issued = 0, next = page_at(0);
     bool ok = true;
-    for (int t = 0; ok && t < tiles; ++t) {
-      const int kb = k0 + t * kKeys, runs = (min(k1 - kb, kKeys) + run - 1) >> run_shift;
-      const bool mine = lane < 2 * runs;
-      const int row = (kb + at_tile) & ((1 << a.kv.page_shift) - 1);
-      const uint8_t* page = head + (mine ? page_in_pool(a, next) : 0) * page_stride;
-      next = page_at(t + 1);
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        const int slot = issued % kRing;
-        if (issued >= kRing && !(ok = wait_warp(&bars.raw_free[slot], (issued / kRing - 1) & 1, abort))) break;
-        // kExact has one key buffer, whose phases the warps that unpack do not all see: the copies wait
-        if (kExact && !v && t > 0 && !(ok = wait_warp(&bars.k_free[0], (t - 1) & 1, abort))) break;
-        if (lane == 0) tc::mbar_arrive_expect_tx(&bars.raw_full[slot], uint32_t(runs << run_shift) * (D / 2 + D / 8));
-        __syncwarp();
-        if (mine)
-          bulk_load(dst + slot * Z::kRaw, page + (part ? a.kv.params(v, row) : a.kv.codes(v, row)),
-                    row_bytes << run_shift, &bars.raw_full[slot]);
-        ++issued;
-      }
+    for (; issued < 2 * tiles; ++issued) {
+      const int kb = k0 + issued * kHalf, tokens = max(0, min(k1 - kb, kHalf)), slot = issued % kRing;
+      const bool mine = lane < copies && at_half < tokens;
+      const uint8_t* src = from + (mine ? page_in_pool(a, next) : 0) * page_stride +
+                           (kb & ((1 << a.kv.page_shift) - 1)) * row_bytes;
+      next = page_at(issued + 1);
+      if (issued >= kRing && !(ok = wait_warp(&bars.raw_free[slot], (issued / kRing - 1) & 1, abort))) break;
+      // kExact has one key buffer, whose phases the warps that unpack do not all see: the copies wait
+      if (kExact && !(issued & 1) && issued > 0 && !(ok = wait_warp(&bars.k_free[0], (issued / 2 - 1) & 1, abort))) break;
+      if (lane == 0)  // whole runs
+        tc::mbar_arrive_expect_tx(&bars.raw_full[slot],
+                                  uint32_t((tokens + (1 << run_shift) - 1) >> run_shift << run_shift) * (D + D / 4));
+      __syncwarp();
+      if (mine) bulk_load(dst + slot * Z::kRaw, src, bytes, &bars.raw_full[slot]);
     }
     if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_MMA);
     for (int n = max(0, issued - kRing); n < issued; ++n)  // the last copies (all have landed unless a role gave up)
       tc::mbar_wait(&bars.raw_full[n % kRing], (n / kRing) & 1);
   } else if (warp != kMmaWarp) {
     // ---------------------------------------------------------------- unpack
-    // A unit is a quarter (32 tokens) of a tile's keys, then of its values; six warps take
-    // them in turn. Four lanes a token. Keys: the two tokens of eight lanes are four apart, so
+    // A unit is a half (32 tokens) of a load's keys, then of its values; six warps take them in
+    // turn. Four lanes a token. Keys: the two tokens of eight lanes are four apart, so
     // that their chunks fall into different banks of the swizzled tile; values: side by side.
     // Every warp sees every copy land and says so before its slot is used again, also where
     // another four warps unpack it: none can take a phase of a slot for the one two before it.
-    const int c = lane & 3, i8 = lane >> 2;
+    const int c = lane & 3, i8 = lane >> 2, run_shift = min(6, a.kv.page_shift);
     int unit = warp - kUnpackWarp;  // the next one of this warp
     for (int load = 0; load < 2 * tiles; ++load) {
-      const int t = load >> 1, v = load & 1, stage = t & 1, slot = load % kRing;
+      const int t = load >> 1, v = unit >> 1 & 1, stage = t & 1, slot = load % kRing;
       bool ok = wait_warp(&bars.raw_full[slot], (load / kRing) & 1, abort);
       const bool mine = unit < 4 * load + 4;
-      const int token = 32 * (unit & 3) + (v ? i8 : (i8 & 1) * 4 + (i8 >> 1));
+      const int in8 = v ? i8 : (i8 & 1) * 4 + (i8 >> 1), token = kHalf * (load & 1) + 32 * (unit & 1) + in8;
       // Into registers first, so that the next copy into the slot starts while this one is unpacked
       // (held until the end, the ring gave the pace: 126 us for 8 192 keys of two column tiles).
       Packed<NG> x[4];
@@ -340,13 +344,19 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
         const uint8_t* box = raw + slot * Z::kRaw;
         if (mine) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            x[i] = v ? take<NG, true>(box, token + 8 * i, c) : take<NG, false>(box, token + 8 * i, c);
+          for (int i = 0; i < 4; ++i) {  // page after page as in the pool
+            const int at = 32 * (unit & 1) + 8 * i, in_run = at & ((1 << run_shift) - 1);
+            const uint8_t* page = box + (at - in_run) * (D + D / 4);
+            const uint8_t* codes = page + ((v << run_shift) + in_run) * (D / 2);
+            const uint8_t* params = page + (D << run_shift) + ((v << run_shift) + in_run) * (D / 8);
+            x[i] = v ? take<NG, true>(codes, params, in8, c) : take<NG, false>(codes, params, in8, c);
+          }
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&bars.raw_free[slot]);
-        // A buffer is free once its last tile but one has been used. (A warp's unit before this one
-        // waited for a use at most a tile earlier, so this wait cannot mistake its phase either.)
+        // A buffer is free once its last tile but one has been used. (When a load lands, every warp is
+        // done with the load four before it, of the buffer's last tile, and so with the wait for the
+        // use before that: this wait cannot mistake its phase either.)
         if (mine && t >= 2 && !(kExact && !v))
           ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
       }
