@@ -58,6 +58,11 @@ __device__ __forceinline__ uint4 values8(uint32_t w, __half2 s, __half2 m) {
   return make_uint4(h2u(__hfma2(s, u2h(codes_lo(w)), m)), h2u(__hfma2(s, u2h(codes_hi(w)), m)),
                     h2u(__hfma2(s, u2h(codes_lo(w8)), m)), h2u(__hfma2(s, u2h(codes_hi(w8)), m)));
 }
+// The larger of two pairs of non-negative bf16, a NaN losing to a number.
+__device__ __forceinline__ uint32_t bf16_max2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 y = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&y);
+}
 // kind::f16 with fp16 operands, fp32 sums; B key-major or dim-major.
 constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
   return (1u << 4) | (uint32_t(b_mn_major) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
@@ -336,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       const int t = load >> 1, v = unit >> 1 & 1, stage = t & 1, slot = load % kRing;
       bool ok = wait_warp(&bars.raw_full[slot], (load / kRing) & 1, abort);
       const bool mine = unit < 4 * load + 4;
-      const int in8 = v ? i8 : (i8 & 1) * 4 + (i8 >> 1), token = kHalf * (load & 1) + 32 * (unit & 1) + in8;
+      const int in8 = v && NG != 3 ? i8 : (i8 & 1) * 4 + (i8 >> 1), token = kHalf * (load & 1) + 32 * (unit & 1) + in8;
       // Into registers first, so that the next copy into the slot starts while this one is unpacked
       // (held until the end, the ring gave the pace: 126 us for 8 192 keys of two column tiles).
       Packed<NG> x[4];
@@ -457,70 +462,70 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     const bool owner = !split || x == 0;  // of the column: its query and its output row
     uint8_t* tile = qt + (split ? 0 : x) * Z::kTile;  // the queries, and at the end the rows on their way out
     const int row0 = (warp & 3) * 32;   // this warp's columns of the tile
+    // Where this thread's column lies; a row moves by sixteen lanes together, which ask its lane.
+    const int own_i = live ? col / a.kv.G : 0, own_h = it.g * a.kv.G + (live ? col % a.kv.G : 0);
+    const uint32_t rows = __ballot_sync(0xffffffffu, live);
+    const int part = lane & 15, side = lane >> 4;
     float to_log2;
     {
-      // Queries into the swizzled tile: 16 lanes a column, two columns at a time, each scaled by
-      // a power of two so that its largest lies in [256, 512).
+      // Queries into the swizzled tile, two columns at a time, each scaled by a power of two so that
+      // its largest lies in [256, 512) (or below, if that takes more than 2^126).
       constexpr int kUse = D / 8;  // lanes with eight dims of a column
-      const int part = lane & 15, side = lane >> 4;
       const bool wide = ((reinterpret_cast<uintptr_t>(a.q.p) | uint64_t(2 * (a.q.ls | a.q.rs | a.q.hs))) & 15u) == 0;
-      to_log2 = 0.f;
-#pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        uint4 v[8];
+      const int64_t own = it.l * a.q.ls + int64_t(it.t0 + own_i) * a.q.rs + own_h * a.q.hs;
+      uint4 v[16];
+      // The usual loads stand apart: instructions that are not in a row come from memory one line
+      // after the other once the keys have passed through L2 (loads of both kinds side by side: 13 000
+      // cycles until the last was issued).
+      if (wide) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int c = it.cb * kTcCols + (split ? 0 : x * kTileCols) + row0 + 16 * half + 2 * k + side;
+        for (int k = 0; k < 16; ++k) {
+          const int r = 2 * k + side;
+          const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.p) + __shfl_sync(0xffffffffu, own, r) + 8 * part;
           v[k] = make_uint4(0, 0, 0, 0);
-          if (part < kUse && c < it.n * a.kv.G) {
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.p) + it.l * a.q.ls +
-                                       int64_t(it.t0 + c / a.kv.G) * a.q.rs + (it.g * a.kv.G + c % a.kv.G) * a.q.hs + 8 * part;
-            if (wide) {
-              v[k] = *reinterpret_cast<const uint4*>(src);
-            } else {
-              __nv_bfloat16 e8[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) e8[e] = src[e];
-              v[k] = *reinterpret_cast<uint4*>(e8);
-            }
-          }
+          if (part < kUse && (rows >> r & 1u)) v[k] = *reinterpret_cast<const uint4*>(src);
         }
+      } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int row = row0 + 16 * half + 2 * k + side;
-          const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-          uint32_t top = 0;  // the largest |q| as fp32 bits
+        for (int k = 0; k < 16; ++k) {
+          const int r = 2 * k + side;
+          const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.p) + __shfl_sync(0xffffffffu, own, r) + 8 * part;
+          __nv_bfloat16 e8[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFF0000u, (w[e] & 0x7FFFu) << 16));
-#pragma unroll
-          for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-          int shift = int(top >> 23) - 127 - 8;
-          if (top >= 0x7F800000u || top == 0) shift = 0;
-          // 2^-shift and 2^shift in two factors, each a normal number
-          const float f1 = __uint_as_float(uint32_t(127 - shift / 2) << 23);
-          const float f2 = __uint_as_float(uint32_t(127 - (shift - shift / 2)) << 23);
-          const float g1 = __uint_as_float(uint32_t(127 + shift / 2) << 23);
-          const float g2 = __uint_as_float(uint32_t(127 + (shift - shift / 2)) << 23);
-          // positive, so that a masked logit stays -inf under it; to the column's own lane
-          const float back = fmaxf(a.scale * kLog2e * g1 * g2, 1.1754944e-38f);
-          const float even = __shfl_sync(0xffffffffu, back, 0), odd = __shfl_sync(0xffffffffu, back, 16);
-          if (lane == 16 * half + 2 * k) to_log2 = even;
-          if (lane == 16 * half + 2 * k + 1) to_log2 = odd;
-          float f[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            f[2 * e] = __uint_as_float(w[e] << 16) * f1 * f2;
-            f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u) * f1 * f2;
-          }
-          uint4 y;  // in the order in which a word's nibbles unpack
-          y.x = h2u(__floats2half2_rn(f[0], f[4]));
-          y.y = h2u(__floats2half2_rn(f[1], f[5]));
-          y.z = h2u(__floats2half2_rn(f[2], f[6]));
-          y.w = h2u(__floats2half2_rn(f[3], f[7]));
-          if (part < kUse && owner)
-            *reinterpret_cast<uint4*>(tile + (part >> 3) * kBlock + tc::sw128_offset(row, part & 7)) = y;
+          for (int e = 0; e < 8; ++e) e8[e] = part < kUse && (rows >> r & 1u) ? src[e] : __nv_bfloat16(0.f);
+          v[k] = *reinterpret_cast<uint4*>(e8);
         }
       }
+      int own_shift = 0;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        // the largest |q|; a NaN counts where the row has nothing else
+        uint32_t top = bf16_max2(bf16_max2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), bf16_max2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) top = bf16_max2(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top = max(top & 0xFFFFu, top >> 16);
+        int shift = max(int(top >> 7) - 127 - 8, -126);
+        if (top >= 0x7F80u || top == 0) shift = 0;
+        const int got = __shfl_sync(0xffffffffu, shift, (lane & 1) << 4);
+        if (lane >> 1 == k) own_shift = got;
+        const float up = __uint_as_float(uint32_t(127 - shift) << 23);
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f[2 * e] = __uint_as_float(w[e] << 16) * up;
+          f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u) * up;
+        }
+        uint4 y;  // in the order in which a word's nibbles unpack
+        y.x = h2u(__floats2half2_rn(f[0], f[4]));
+        y.y = h2u(__floats2half2_rn(f[1], f[5]));
+        y.z = h2u(__floats2half2_rn(f[2], f[6]));
+        y.w = h2u(__floats2half2_rn(f[3], f[7]));
+        if (part < kUse && owner)
+          *reinterpret_cast<uint4*>(tile + (part >> 3) * kBlock + tc::sw128_offset(row0 + 2 * k + side, part & 7)) = y;
+      }
+      // positive, so that a masked logit stays -inf under it
+      to_log2 = fmaxf(a.scale * kLog2e * __uint_as_float(uint32_t(127 + own_shift) << 23), 1.1754944e-38f);
       tc::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars.q_full);
@@ -605,12 +610,15 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     // 16-byte chunk c of a row, in a place that spreads the rows over the banks
     constexpr int kRowBytes = D == 64 ? 128 : 256;  // 128 rows fit the tile
     auto chunk_at = [&](int r, int c) { return tile + r * kRowBytes + ((c ^ (r & 7)) << 4); };
-    auto row_of = [&](int r, int* i, int* h) {
-      const int c = it.cb * kTcCols + (split ? 0 : x * kTileCols) + r;
-      *i = c / a.kv.G;
-      *h = it.g * a.kv.G + c % a.kv.G;
-      return c < it.n * a.kv.G;
-    };
+    const int64_t own = partial ? (it.chunk * cols + (int64_t(it.l) * a.s.T + it.t0 + own_i) * a.kv.Hq + own_h) * D
+                                : it.l * a.out.ls + int64_t(it.t0 + own_i) * a.out.rs + own_h * a.out.hs;
+    bool tainted[NG], any_tainted = false;  // a value that is not finite reaches the columns that see it
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      tainted[g] = poison[g] < lim;
+      any_tainted |= tainted[g];
+    }
+    any_tainted = __any_sync(0xffffffffu, any_tainted);
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) {
       float o[32];
@@ -636,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           y[e] = o[8 * (n / 2) + 2 * e + (n & 1)];
-          if (poison[g] < lim) y[e] = NAN;  // a value that is not finite reaches the columns that see it
+          if (any_tainted && tainted[g]) y[e] = NAN;
         }
         if (partial) {  // a block's 32 dims, in the order in which they come
           *reinterpret_cast<float4*>(chunk_at(row, n)) = make_float4(y[0], y[1], y[2], y[3]);
@@ -649,13 +657,10 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       __syncwarp();
 #pragma unroll 1
       for (int k = 0; k < 8; ++k) {  // four rows at a time, eight lanes a row
-        const int r = row0 + 4 * k + (lane >> 3), n = lane & 7;
+        const int r = 4 * k + (lane >> 3), n = lane & 7;
         const int hw = 2 * (4 * b + n / 2) + (n & 1), dim = 32 * (hw % NG) + 4 * (hw / NG);
-        int i, h;
-        if (row_of(r, &i, &h)) {
-          float* part = a.part_o + (it.chunk * cols + (int64_t(it.l) * a.s.T + it.t0 + i) * a.kv.Hq + h) * D;
-          *reinterpret_cast<float4*>(part + dim) = *reinterpret_cast<const float4*>(chunk_at(r, n));
-        }
+        float* to = a.part_o + __shfl_sync(0xffffffffu, own, r) + dim;
+        if (rows >> r & 1u) *reinterpret_cast<float4*>(to) = *reinterpret_cast<const float4*>(chunk_at(row0 + r, n));
       }
       __syncwarp();
     }
@@ -663,12 +668,10 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       __syncwarp();
 #pragma unroll 4
       for (int k = 0; k < 16; ++k) {
-        const int r = row0 + 2 * k + (lane >> 4), c = lane & 15;
-        int i, h;
-        if (row_of(r, &i, &h) && c < D / 8) {
-          __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out.p) + it.l * a.out.ls + int64_t(it.t0 + i) * a.out.rs +
-                              h * a.out.hs + 8 * c;
-          const uint4 y = *reinterpret_cast<const uint4*>(chunk_at(r, c));
+        const int r = 2 * k + side;
+        __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out.p) + __shfl_sync(0xffffffffu, own, r) + 8 * part;
+        if ((rows >> r & 1u) && part < D / 8) {
+          const uint4 y = *reinterpret_cast<const uint4*>(chunk_at(row0 + r, part));
           if (by_16) {
             *reinterpret_cast<uint4*>(to) = y;
           } else {
