@@ -270,17 +270,24 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   const int step = p.kernel == kAttnSimt ? 64 : 256;  // least keys of a chunk
   const int64_t largest = std::max(1, (most + step - 1) / step);
   if (p.kernel == kAttnTc) {
-    // One CTA per SM: the number of chunks with the least time by a model of one pass, 6 us for
-    // a CTA and 1.8 us for 128 keys of two column tiles, and of the join, 12 bytes a partial
-    // value at 5 TB/s after a launch of 5 us.
-    int64_t blocks = 0;
-    for (int r = 0; r < s.R; ++r)
-      blocks += (int64_t(s.row_off_host[r + 1] - s.row_off_host[r]) * kv.G + 255) / 256;
-    const double items = double(kv.L) * kv.Hkv * blocks, values = double(kv.L) * s.T * kv.Hq * kv.d;
+    // One CTA per SM: the number of chunks with the least time by a model of one pass, 11 us for a
+    // CTA and 1.8 us for 128 keys of two column tiles (4.5 of keys in two parts), three quarters of
+    // it where the last wave has one column tile, and of the join, 12 bytes a partial value at
+    // 5 TB/s after a launch of 5 us. (Two layers x 16 requests x 8 192 keys, 28 / 4 heads of 96: one
+    // chunk 386 us, two 421.)
+    int64_t blocks = 0, singles = 0;
+    for (int r = 0; r < s.R; ++r) {
+      const int64_t tiles = (int64_t(s.row_off_host[r + 1] - s.row_off_host[r]) * kv.G + 127) / 128;
+      blocks += (tiles + 1) / 2;
+      singles += tiles & 1;
+    }
+    const int64_t heads = int64_t(kv.L) * kv.Hkv;
+    const double values = double(kv.L) * s.T * kv.Hq * kv.d, tile = most < kExactBelow ? 4.5 : 1.8;
     double best = 0;
     for (int64_t c = 1; c <= std::min<int64_t>(largest, 64); ++c) {
-      const double waves = std::ceil(items * c / 152.);
-      const double us = waves * (6. + 1.8 / 128. * most / c) + (c > 1 ? 5. + c * values * 12. / 5e6 : 0.);
+      const int64_t items = heads * c * blocks, before = (items - 1) / 152;
+      const double waves = before + (heads * c * singles >= items - 152 * before ? 0.75 : 1.);
+      const double us = waves * (11. + tile / 128. * most / c) + (c > 1 ? 5. + c * values * 12. / 5e6 : 0.);
       if (c == 1 || us < best) best = us, p.chunks = int(c);
     }
   } else {
