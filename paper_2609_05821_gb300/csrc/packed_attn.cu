@@ -271,7 +271,7 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   const int64_t largest = std::max(1, (most + step - 1) / step);
   if (p.kernel == kAttnTc) {
     // One CTA per SM: the number of chunks with the least time by a model of one pass, 11 us for a
-    // CTA and 1.8 us for 128 keys of two column tiles (4.5 of keys in two parts), three quarters of
+    // CTA and 1.8 us for 128 keys of two column tiles (3.3 of keys in two parts), three quarters of
     // it where the last wave has one column tile, and of the join, 12 bytes a partial value at
     // 5 TB/s after a launch of 5 us. (Two layers x 16 requests x 8 192 keys, 28 / 4 heads of 96: one
     // chunk 386 us, two 421.)
@@ -282,7 +282,7 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
       singles += tiles & 1;
     }
     const int64_t heads = int64_t(kv.L) * kv.Hkv;
-    const double values = double(kv.L) * s.T * kv.Hq * kv.d, tile = most < kExactBelow ? 4.5 : 1.8;
+    const double values = double(kv.L) * s.T * kv.Hq * kv.d, tile = most < kExactBelow ? 3.3 : 1.8;
     double best = 0;
     for (int64_t c = 1; c <= std::min<int64_t>(largest, 64); ++c) {
       const int64_t items = heads * c * blocks, before = (items - 1) / 152;

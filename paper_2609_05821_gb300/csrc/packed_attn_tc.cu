@@ -141,16 +141,15 @@ __device__ __forceinline__ void unpack_keys_exact(uint8_t* hi, uint8_t* lo, cons
   const uint32_t(&p)[NG] = x.p;
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    const float2 sm = __half22float2(u2h(p[g]));
+    const float2 sm = __half22float2(u2h(p[g])), s2 = make_float2(sm.x, sm.x), m2 = make_float2(sm.y, sm.y);
+    const uint32_t w8 = w[g] >> 8, u[4] = {codes_lo(w[g]), codes_hi(w[g]), codes_lo(w8), codes_hi(w8)};
     uint32_t h[4], l[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float a = fmaf(sm.x, float(int((w[g] >> (4 * e)) & 15u) - 8), sm.y);
-      const float b = fmaf(sm.x, float(int((w[g] >> (4 * e + 16)) & 15u) - 8), sm.y);
-      const __half2 top = __floats2half2_rn(a, b);
-      const float2 back = __half22float2(top);
+      const float2 x = tc::ffma2(s2, __half22float2(u2h(u[e])), m2);
+      const __half2 top = __float22half2_rn(x);
       h[e] = h2u(top);
-      l[e] = h2u(__floats2half2_rn(a - back.x, b - back.y));
+      l[e] = h2u(__float22half2_rn(tc::ffma2(__half22float2(top), make_float2(-1.f, -1.f), x)));
     }
     const int ch = 4 * g + c;
     const uint32_t at = (ch >> 3) * kBlock + tc::sw128_offset(token, ch & 7);
@@ -317,8 +316,6 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
                            (kb & ((1 << a.kv.page_shift) - 1)) * row_bytes;
       next = page_at(issued + 1);
       if (issued >= kRing && !(ok = wait_warp(&bars.raw_free[slot], (issued / kRing - 1) & 1, abort))) break;
-      // kExact has one key buffer, whose phases the warps that unpack do not all see: the copies wait
-      if (kExact && !(issued & 1) && issued > 0 && !(ok = wait_warp(&bars.k_free[0], (issued / 2 - 1) & 1, abort))) break;
       if (lane == 0)  // whole runs
         tc::mbar_arrive_expect_tx(&bars.raw_full[slot],
                                   uint32_t((tokens + (1 << run_shift) - 1) >> run_shift << run_shift) * (D + D / 4));
@@ -364,6 +361,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
         // use before that: this wait cannot mistake its phase either.)
         if (mine && t >= 2 && !(kExact && !v))
           ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
+        // kExact has one key buffer, whose every use every warp sees
+        if (kExact && ok && t >= 1 && !(load & 1)) ok = wait_warp(&bars.k_free[0], (t - 1) & 1, abort);
       }
       if (!ok) {
         if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
