@@ -624,8 +624,13 @@ conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* f
  *          (fp32 partial results of key chunks); calls that overlap on the GPU
  *          need workspaces of their own
  * bf16 rows with head_dim 64, 96 or 128 run on the tensor cores (fp16 operands:
- * codes and queries exact, values and weights within 2^-11); fp32 rows and other
- * head sizes on the CUDA cores in fp32. Results are deterministic.
+ * queries exact but for a power of two, values and weights within 2^-11, fp32
+ * sums); fp32 rows and other head sizes on the CUDA cores in fp32. Keys enter
+ * exactly, or as two fp16 numbers, where a request has at most 8 rows x (Hq/Hkv)
+ * or max_len < 2048: lse then carries fp32 rounding only. Else they are within
+ * 2^-11 of themselves (lse to about 2e-6 over 8192 keys). The kernel and the cut
+ * into key chunks follow from the sizes, max_len and row_off, so equal calls give
+ * equal bits.
  */
 conduit_status conduit_packed_attn_workspace_size(const conduit_packed_kv* kv, const conduit_seqs* seqs,
                                                   int32_t dtype, size_t* bytes);

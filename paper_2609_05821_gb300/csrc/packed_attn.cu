@@ -15,7 +15,9 @@ namespace {
 
 // ------------------------------------------------------------- CUDA cores
 // A CTA of four warps, two columns a warp, 32 keys at a time as fp32 in shared
-// memory: lanes are keys for the logits and dims for the sums.
+// memory: lanes are keys for the logits and dims for the sums. Bound by its fp32 products, one
+// shared-memory load each; in small calls by the chain of a tile's barriers. Measured: 1-5 rows of
+// 3 requests over 1 500 keys, 14 x 2 heads of 64 in fp32, 14 us with the join.
 constexpr int kSimtKeys = 32;
 
 template <typename T, int NG>
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
     a.lse[(int64_t(l) * a.kv.Hq + h) * a.s.T + t] = sum == 0.f ? -INFINITY : kLn2 * (base + log2f(sum));
 }
 
-// The tcgen05 kernel's keys are within 2^-12 of their values, and so a logit within 2^-12 of sum
+// The tcgen05 kernel's keys are within 2^-11 of their values, and so a logit within 2^-11 of sum
 // |q||k|: nothing beside the rounding of a bf16 output, and in a log-sum-exp an error that falls
 // with the number of keys that count (2 x 10^-4 of it for one key, 5 x 10^-6 for 2 000, 2 x 10^-6
 // for 8 192). For shorter contexts keys come as two fp16 numbers, whether or not a log-sum-exp is

@@ -21,7 +21,9 @@
 // whose instructions come out of the same issue slots, 174.)
 //
 // Bound: 1.25 d bytes per token and KV head from HBM; next to it the unpacking of the
-// values, whose integer and fp16 instructions issue at half rate.
+// values, whose integer and fp16 instructions issue at half rate. Measured: one row each of
+// 64 requests of 2 000-30 000 tokens, 28 x 4 heads of 128, 157 us with the join (4.2 TB/s, 66 %
+// of the issue slots); one of 262 145 tokens, 32 x 8 heads, 73 us (4.6 TB/s).
 #include "packed_attn.cuh"
 
 namespace conduit {
