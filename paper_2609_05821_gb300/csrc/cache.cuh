@@ -77,6 +77,8 @@ struct PackedAttnPlan {
   int kernel;     // CUDA cores, warp-level tensor cores, tcgen05
   int chunk;      // keys per chunk
   int chunks;     // of the longest context
+  int last_chunk, last_chunks;  // tcgen05: the same of the blocks with one column tile
+  int64_t part_cols;            // columns with partial results
   int64_t items;  // CTAs
   bool cluster;   // the chunks of a context join inside a cluster
   size_t scratch;

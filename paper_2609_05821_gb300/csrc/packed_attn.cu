@@ -134,14 +134,25 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
   __shared__ float4 part[8][kLanes];
   __shared__ float part_sum[8];
   const int lane = threadIdx.x % kLanes, grp = threadIdx.x / kLanes, of = grp % kJoin;
-  const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq, col = int64_t(blockIdx.x) * kPer + grp / kJoin;
-  const bool on = col < cols;
+  const int64_t cols = a.part_cols, col = int64_t(blockIdx.x) * kPer + grp / kJoin;
+  bool on = col < cols;
   int h = 0, t = 0, l = 0, n = 0;
   if (on) {
-    h = int(col % a.kv.Hq), t = int(col / a.kv.Hq % a.s.T), l = int(col / a.kv.Hq / a.s.T);
-    const int r = request_of(a.s.row_off, a.s.R, t);
+    int r, chunk = a.chunk;
+    if (a.chunks > 1) {
+      h = int(col % a.kv.Hq), t = int(col / a.kv.Hq % a.s.T), l = int(col / a.kv.Hq / a.s.T);
+      r = request_of(a.s.row_off, a.s.R, t);
+    } else {  // a column of the tile that a request has left over from its pairs
+      const int64_t unit = col / 128;
+      const int g = int(unit % a.kv.Hkv);
+      r = int(unit / a.kv.Hkv % a.s.R), l = int(unit / a.kv.Hkv / a.s.R);
+      const int t0 = a.s.row_off[r], all = (a.s.row_off[r + 1] - t0) * a.kv.G, tiles = (all + 127) / 128;
+      const int j = 128 * (tiles - 1) + int(col % 128);
+      on = (tiles & 1) && j < all;
+      t = t0 + j / a.kv.G, h = g * a.kv.G + j % a.kv.G, chunk = a.last_chunk;
+    }
     const int len = cached_len(a.s, a.kv.capacity(), r, nullptr, false);
-    n = max(1, (len + a.chunk - 1) / a.chunk);
+    n = on ? max(1, (len + chunk - 1) / chunk) : 0;
   }
   wait_for_chunks();
   float top = -INFINITY;
@@ -211,19 +222,19 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
     count_launches(1);
     err = cudaGetLastError();
   }
-  if (err || a.chunks == 1 || plan.cluster) return err;
-  const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
+  const int chunks = std::max(a.chunks, a.last_chunks);
+  if (err || chunks == 1 || plan.cluster) return err;
   cudaLaunchAttribute early{};
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(unsigned(a.chunks >= 8 ? cols : (cols + 7) / 8));
+  cfg.gridDim = dim3(unsigned(chunks >= 8 ? a.part_cols : (a.part_cols + 7) / 8));
   cfg.blockDim = dim3(NG * 64);
   cfg.stream = stream;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
   count_launches(1);
-  return a.chunks >= 8 ? cudaLaunchKernelEx(&cfg, combine_kernel<T, NG, 8>, a)
+  return chunks >= 8 ? cudaLaunchKernelEx(&cfg, combine_kernel<T, NG, 8>, a)
                        : cudaLaunchKernelEx(&cfg, combine_kernel<T, NG, 1>, a);
 }
 
@@ -247,13 +258,35 @@ int64_t blocks_of(const PackedDev& kv, const SeqsDev& s, int kernel) {
   const int64_t cols = int64_t(s.max_rows) * kv.G;
   return kernel == kAttnTc ? (cols + 127) / 128 / 2 + 1 : (cols + kCols - 1) / kCols;
 }
-int64_t items_of(const PackedDev& kv, const SeqsDev& s, int kernel, int chunks) {
-  return int64_t(kv.L) * s.R * kv.Hkv * blocks_of(kv, s, kernel) * chunks;
+int64_t items_of(const PackedDev& kv, const SeqsDev& s, int kernel, int chunks, int last_chunks) {
+  return int64_t(kv.L) * s.R * kv.Hkv * ((blocks_of(kv, s, kernel) - 1) * chunks + last_chunks);
 }
 
-// (reference, sum) of every chunk and (row, head), to a multiple of 16 bytes.
-size_t stats_bytes(const PackedDev& kv, const SeqsDev& s, int chunks) {
-  return (size_t(chunks) * kv.L * s.T * kv.Hq * sizeof(float2) + 15) / 16 * 16;
+// (reference, sum) of every chunk and column with partial results, to a multiple of 16 bytes.
+size_t stats_bytes(const PackedAttnPlan& p) {
+  return (size_t(std::max(p.chunks, p.last_chunks)) * p.part_cols * sizeof(float2) + 15) / 16 * 16;
+}
+
+// Time by which `places` SMs are done with `pairs` CTAs of tp each and then `singles` of ts.
+double pass_time(int64_t pairs, int64_t singles, double tp, double ts) {
+  constexpr int64_t places = 152;
+  double at[2] = {pairs / places * tp, (pairs / places + 1) * tp};
+  const int64_t n[2] = {places - pairs % places, pairs % places};
+  double end = n[1] ? at[1] : at[0];
+  while (singles > 0) {
+    const int i = n[1] && at[1] < at[0];
+    at[i] += ts;
+    singles -= n[i];
+    end = std::max(end, at[i]);
+  }
+  return end;
+}
+
+// Keys of a chunk (a multiple of step) and chunks of the longest context, from about `chunks`.
+void cut(int most, int step, int* chunk, int* chunks) {
+  *chunk = std::max(step, (most + *chunks - 1) / *chunks);
+  *chunk = (*chunk + step - 1) / step * step;
+  *chunks = std::max(1, (most + *chunk - 1) / *chunk);
 }
 
 }  // namespace
@@ -272,54 +305,62 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   const int step = p.kernel == kAttnSimt ? 64 : 256;  // least keys of a chunk
   const int64_t largest = std::max(1, (most + step - 1) / step);
   if (p.kernel == kAttnTc) {
-    // One CTA per SM: the number of chunks with the least time by a model of one pass, 11 us for a
-    // CTA and 1.8 us for 128 keys of two column tiles (3.3 of keys in two parts), three quarters of
-    // it where the last wave has one column tile, and of the join, 12 bytes a partial value at
-    // 5 TB/s after a launch of 5 us. (Two layers x 16 requests x 8 192 keys, 28 / 4 heads of 96: one
-    // chunk 386 us, two 421.)
-    int64_t blocks = 0, singles = 0;
+    // One CTA per SM: the chunks with the least time by a model of the pass, 11 us for a CTA and
+    // 1.8 us for 128 keys of two column tiles (3.3 of keys in two parts), three quarters of it for
+    // one, and of the join, 12 bytes a partial value at 5 TB/s after a launch of 5 us. Either all
+    // blocks have the same chunks (two layers x 16 requests x 8 192 keys, 28 / 4 heads of 96: one
+    // chunk 386 us, two 421) or only those with one column tile, which come last and fill up
+    // what the pairs leave of the SMs (the same with 128 dims: 350 us without, 317 with; 96: 329).
+    int64_t pairs = 0, singles = 0;
     for (int r = 0; r < s.R; ++r) {
       const int64_t tiles = (int64_t(s.row_off_host[r + 1] - s.row_off_host[r]) * kv.G + 127) / 128;
-      blocks += (tiles + 1) / 2;
+      pairs += tiles / 2;
       singles += tiles & 1;
     }
-    const int64_t heads = int64_t(kv.L) * kv.Hkv;
-    const double values = double(kv.L) * s.T * kv.Hq * kv.d, tile = most < kExactBelow ? 3.3 : 1.8;
+    const int64_t heads = int64_t(kv.L) * kv.Hkv, items = heads * (pairs + singles);
+    const double keys = (most < kExactBelow ? 3.3 : 1.8) / 128. * most, all = double(kv.L) * s.T * kv.Hq;
+    auto join = [&](int64_t c, double cols) { return c > 1 ? 5. + c * cols * kv.d * 12. / 5e6 : 0.; };
     double best = 0;
-    for (int64_t c = 1; c <= std::min<int64_t>(largest, 64); ++c) {
-      const int64_t items = heads * c * blocks, before = (items - 1) / 152;
-      const double waves = before + (heads * c * singles >= items - 152 * before ? 0.75 : 1.);
-      const double us = waves * (11. + tile / 128. * most / c) + (c > 1 ? 5. + c * values * 12. / 5e6 : 0.);
-      if (c == 1 || us < best) best = us, p.chunks = int(c);
+    for (int64_t c = 1; c <= std::min<int64_t>(largest, 64) && (c == 1 || items * c <= 8 * 152); ++c) {
+      const double tp = 11. + keys / c, ts = 11. + 0.75 * keys / c;
+      const double us = pass_time(heads * pairs * c, heads * singles * c, tp, ts) + join(c, all);
+      if (c == 1 || us < best) best = us, p.chunks = p.last_chunks = int(c);
     }
+    for (int64_t c = 2; pairs && singles && items <= 8 * 152 && c <= std::min<int64_t>(largest, 8); ++c) {
+      const double us = pass_time(heads * pairs, heads * singles * c, 11. + keys, 11. + 0.75 * keys / c) +
+                        join(c, double(heads * singles * 128));
+      if (us < best) best = us, p.chunks = 1, p.last_chunks = int(c);
+    }
+    cut(most, step, &p.last_chunk, &p.last_chunks);
   } else {
     // An SM holds two CTAs. One request: one wave of equal chunks. More: eight CTAs for each
     // place, so that contexts of unequal lengths fill it (64 requests of 2-30k tokens: four 186,
     // eight 180, sixteen 190 us). At least 256 keys each.
-    const int64_t items = std::max<int64_t>(1, items_of(kv, s, p.kernel, 1)), places = 2 * 152;
+    const int64_t items = std::max<int64_t>(1, items_of(kv, s, p.kernel, 1, 1)), places = 2 * 152;
     const int64_t even = s.R == 1 ? places / items : (8 * places + items - 1) / items;
     p.chunks = int(std::max<int64_t>(1, std::min(even, largest)));
   }
-  p.chunk = std::max(step, (most + p.chunks - 1) / p.chunks);
-  p.chunk = (p.chunk + step - 1) / step * step;
-  p.chunks = std::max(1, (most + p.chunk - 1) / p.chunk);
-  p.items = items_of(kv, s, p.kernel, p.chunks);
+  cut(most, step, &p.chunk, &p.chunks);
+  if (p.kernel != kAttnTc) p.last_chunk = p.chunk, p.last_chunks = p.chunks;
+  p.items = items_of(kv, s, p.kernel, p.chunks, p.last_chunks);
   // Up to eight chunks join inside a cluster: one launch and no partial results in memory. More
   // CTAs than places and the clusters wait for one another (16 requests of 1 025 tokens: 15.8 us
   // with the join, 18.0 us in clusters; one request: 9.4 and 8.5 us).
   p.cluster = p.kernel == kAttnMma && p.chunks > 1 && p.chunks <= 8 && p.items <= 2 * 152;
-  if (p.chunks > 1 && !p.cluster)
-    p.scratch = stats_bytes(kv, s, p.chunks) + size_t(p.chunks) * kv.L * s.T * kv.Hq * size_t(kv.d) * sizeof(float);
+  p.part_cols = p.chunks > 1 ? int64_t(kv.L) * s.T * kv.Hq : int64_t(kv.L) * s.R * kv.Hkv * 128;
+  if (p.last_chunks > 1 && !p.cluster)
+    p.scratch = stats_bytes(p) + size_t(std::max(p.chunks, p.last_chunks)) * p.part_cols * size_t(kv.d) * sizeof(float);
   return p;
 }
 
 cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const PackedAttnPlan& plan, int dtype,
                                const RowsDev& q, float scale, const int32_t* limits, const RowsDev& out,
                                float* lse, void* scratch, int32_t* status, cudaStream_t stream) {
-  AttnArgs a{kv, s, q, out, lse, limits, scale, plan.chunk, plan.chunks, 0, nullptr, nullptr, status};
+  AttnArgs a{kv, s, q, out, lse, limits, scale, plan.chunk, plan.chunks, 0, plan.last_chunk, plan.last_chunks,
+             plan.part_cols, nullptr, nullptr, status};
   a.col_blocks = int(blocks_of(kv, s, plan.kernel));
   a.part_ml = static_cast<float2*>(scratch);
-  a.part_o = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats_bytes(kv, s, plan.chunks));
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats_bytes(plan));
   return dtype == CONDUIT_BF16 ? launch_t<__nv_bfloat16>(a, plan, stream) : launch_t<float>(a, plan, stream);
 }
 

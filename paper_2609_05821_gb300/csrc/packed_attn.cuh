@@ -16,8 +16,10 @@ struct AttnArgs {
   const int32_t* limits;  // or NULL
   float scale;
   int chunk, chunks, col_blocks;
-  float2* part_ml;        // [chunks][L T Hq] (M in log2 units, sum)
-  float* part_o;          // [chunks][L T Hq][d]
+  int last_chunk, last_chunks;  // tcgen05: of blocks with one column tile
+  int64_t part_cols;      // columns with partial results: L T Hq, or L R Hkv 128 where only those blocks have them
+  float2* part_ml;        // [chunks][part_cols] (M in log2 units, sum)
+  float* part_o;          // [chunks][part_cols][d]
   int32_t* status;
 };
 
@@ -31,9 +33,9 @@ struct Item {
 };
 
 // The chunk, KV head, request and layer of unit x, and the request's rows and length.
-__device__ __forceinline__ void decode(const AttnArgs& a, uint32_t x, Item* it) {
-  it->chunk = int(x % uint32_t(a.chunks));
-  x /= uint32_t(a.chunks);
+__device__ __forceinline__ void decode(const AttnArgs& a, uint32_t x, int chunks, Item* it) {
+  it->chunk = int(x % uint32_t(chunks));
+  x /= uint32_t(chunks);
   it->g = int(x % uint32_t(a.kv.Hkv));
   x /= uint32_t(a.kv.Hkv);
   it->r = int(x % uint32_t(a.s.R));
@@ -51,10 +53,10 @@ __device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
   uint32_t x = blockIdx.x / inner;
   if (kCluster) {
     it->cb = int(x % uint32_t(a.col_blocks));
-    decode(a, x / uint32_t(a.col_blocks) * a.chunks + blockIdx.x % inner, it);
+    decode(a, x / uint32_t(a.col_blocks) * a.chunks + blockIdx.x % inner, a.chunks, it);
   } else {
     it->cb = int(blockIdx.x % inner);
-    decode(a, x, it);
+    decode(a, x, a.chunks, it);
   }
   if (it->cb * kCols >= it->n * a.kv.G) return false;
   return kCluster || it->chunk == 0 || it->chunk * a.chunk < it->len;

@@ -25,7 +25,7 @@
 // shared memory), 1 200-1 500 of softmax, 1 000 for each 32 tokens of keys or values that a warp
 // unpacks; a CTA another 20 000 (item and limits 2 500, queries 8 000-11 500, rows out 7 000, the
 // next CTA's launch 2 000). Measured: 32-128 rows of 16 requests over 8 192 keys, two layers of
-// 28 x 4 heads of 128, 350 us (0.91 PFLOP/s, 48 % of the tensor pipe); 96 dims 386, 64 dims 285.
+// 28 x 4 heads of 128, 317 us (1.0 PFLOP/s); 96 dims 329, 64 dims 250.
 #include "packed_attn.cuh"
 
 namespace conduit {
@@ -97,11 +97,11 @@ __device__ __forceinline__ bool tc_item(const AttnArgs& a, Item* it) {
   const bool single = blockIdx.x >= units * pairs;
   uint32_t x = single ? blockIdx.x - units * pairs : blockIdx.x / pairs;
   const int rank = single ? 0 : int(blockIdx.x % pairs);
-  decode(a, x, it);
+  decode(a, x, single ? a.last_chunks : a.chunks, it);
   const int tiles = (it->n * a.kv.G + kTileCols - 1) / kTileCols;  // column tiles of the request
   it->cb = single ? tiles / 2 : rank;
   if (single ? !(tiles & 1) : rank >= tiles / 2) return false;
-  return it->chunk == 0 || it->chunk * a.chunk < it->len;
+  return it->chunk == 0 || it->chunk * (single ? a.last_chunk : a.chunk) < it->len;
 }
 
 // One lane's share of a packed token: NG words of codes, the parameters of its groups. Keys, and
@@ -241,6 +241,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   if (!tc_item(a, &it)) return;
   // One column tile: A takes its even key tiles and B its odd ones, joined at the end.
   const bool split = it.cb * kTcCols + kTileCols >= it.n * a.kv.G;
+  const int chunk = split ? a.last_chunk : a.chunk;
+  const bool partial = (split ? a.last_chunks : a.chunks) > 1;
   uint8_t* base = dynamic + (1024 - (tc::smem_u32(dynamic) & 1023u)) % 1024;
   uint8_t *qt = base, *kt = qt + 2 * Z::kTile, *vt = kt + 2 * Z::kTile, *raw = vt + 2 * Z::kTile;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
@@ -286,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  const int least = seen_least, k0 = it.chunk * a.chunk, k1 = min(k0 + a.chunk, seen_most);
+  const int least = seen_least, k0 = it.chunk * chunk, k1 = min(k0 + chunk, seen_most);
   const int tiles = k1 > k0 ? (k1 - k0 + kKeys - 1) / kKeys : 0;
 
   // 128 registers a thread at launch: 2 x 88 + 2 x 168 per four warpgroups
@@ -601,20 +603,26 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     if (!ok && lane == 0) give_up(a, abort, CONDUIT_SITE_FINAL);
     tc::tc_fence_after();
     if (owner) {
-    if (live) store_stats(a, it, col, ref, total, a.chunks == 1);
-    const float inv = a.chunks > 1 ? 1.f : total == 0.f ? 0.f : 1.f / total;
+    // this column among those with partial results
+    const int64_t part_col = a.chunks > 1 ? (int64_t(it.l) * a.s.T + it.t0 + own_i) * a.kv.Hq + own_h
+                                          : ((int64_t(it.l) * a.s.R + it.r) * a.kv.Hkv + it.g) * kTileCols + row0 + lane;
+    if (live) {
+      if (partial)
+        a.part_ml[it.chunk * a.part_cols + part_col] = make_float2(ref, total);
+      else
+        store_stats(a, it, col, ref, total, true);
+    }
+    const float inv = partial ? 1.f : total == 0.f ? 0.f : 1.f / total;
     own_w *= inv;
     b_w *= inv;
     // The rows go out through the query tile (every product that read it is done), so that
     // neighbouring lanes write neighbouring dims.
-    const bool partial = a.chunks > 1;
-    const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
     const bool by_16 = ((reinterpret_cast<uintptr_t>(a.out.p) | uint64_t(2 * (a.out.ls | a.out.rs | a.out.hs))) & 15u) == 0;
     const int row = row0 + lane;
     // 16-byte chunk c of a row, in a place that spreads the rows over the banks
     constexpr int kRowBytes = D == 64 ? 128 : 256;  // 128 rows fit the tile
     auto chunk_at = [&](int r, int c) { return tile + r * kRowBytes + ((c ^ (r & 7)) << 4); };
-    const int64_t own = partial ? (it.chunk * cols + (int64_t(it.l) * a.s.T + it.t0 + own_i) * a.kv.Hq + own_h) * D
+    const int64_t own = partial ? (it.chunk * a.part_cols + part_col) * D
                                 : it.l * a.out.ls + int64_t(it.t0 + own_i) * a.out.rs + own_h * a.out.hs;
     bool tainted[NG], any_tainted = false;  // a value that is not finite reaches the columns that see it
 #pragma unroll

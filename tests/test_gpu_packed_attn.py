@@ -260,6 +260,24 @@ def test_many_rows_that_see_nothing(C):
     _check(C, kv, groups, lens, rows, q, None, out, lse, 128 ** -0.5, True)
 
 
+# Rows of an odd number of column tiles and more blocks than SMs: the blocks with one tile are cut into
+# key chunks of their own, those with two are not.
+LAST_IN_CHUNKS = [
+    (BF, 2, 16, 16, 64, 16, (1500, 1340, 700, 3, 1024), (44, 139, 28, 131, 146), "random"),
+    (BF, 2, 16, 16, 64, 32, (2300, 2049, 60, 769, 2300), (32, 41, 138, 142, 148), None),
+]
+
+
+@pytest.mark.parametrize("dtype,L,hq,hkv,d,ps,lens,rows,limits", LAST_IN_CHUNKS)
+def test_last_blocks_in_chunks(C, dtype, L, hq, hkv, d, ps, lens, rows, limits):
+    table = torch.zeros((len(lens), -(-max(lens) // ps)), dtype=torch.int32)
+    kv = C.PackedKv.empty(L, 1, hq, hkv, d, ps, table)
+    seqs = C.Seqs(np.concatenate([[0], np.cumsum(rows)]), torch.tensor(lens, dtype=torch.int32, device="cuda"), max(lens))
+    per_chunk = L * len(lens) * hkv * 128 * (4 * d + 8)  # partial results of one tile per request and KV head
+    assert 2 * per_chunk <= C.conduit_packed_attn_workspace_size(kv, seqs, dtype) <= 8 * per_chunk + 256
+    test_attention(C, dtype, L, hq, hkv, d, ps, lens, rows, limits)
+
+
 def test_other_stream(C):
     kv, groups = _cache(C, 8, 1, 8, 2, 128, 16, (777,))
     q = torch.randn((1, 1, 8, 128), device="cuda").to(BF)
