@@ -14,21 +14,68 @@ namespace conduit {
 namespace {
 
 // ------------------------------------------------------------- CUDA cores
-// A CTA of four warps, two columns a warp, 32 keys at a time as fp32 in shared
-// memory: lanes are keys for the logits and dims for the sums. Bound by its fp32 products, one
-// shared-memory load each; in small calls by the chain of a tile's barriers. Measured: 1-5 rows of
-// 3 requests over 1 500 keys, 14 x 2 heads of 64 in fp32, 14 us with the join.
+// A CTA of four warps, two columns a warp, 32 keys at a time as fp32 in shared memory: lanes are
+// keys for the logits and dims for the sums. The next 32 keys' codes are on their way into
+// registers meanwhile, and the pages of the 32 after them. Bound by the loads from shared memory
+// beside the products (three of 16 bytes for eight products of the logits); in small calls by the
+// chain of a tile. Measured, 14 x 2 heads of 64 in fp32 with the join: 1-5 rows of 3 requests over
+// 1 500 keys 11.4 us (64 keys a chunk; 32: 12.5, 128: 13.4), 10-16 rows over 4 096 keys 49 us.
 constexpr int kSimtKeys = 32;
+constexpr int kSimtRow(int d) { return d + 4; }  // 16 bytes of eight keys in different banks
 
 template <typename T, int NG>
 __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
-  constexpr int D = NG * 32, KS = D + 1;
-  extern __shared__ float simt_smem[];
+  constexpr int D = NG * 32, KS = kSimtRow(D);
+  extern __shared__ __align__(16) float simt_smem[];
   float *ks = simt_smem, *vs = ks + kSimtKeys * KS, *qs = vs + kSimtKeys * D;
+  __shared__ float2 weights[4][kSimtKeys];
   let_join_start();
   Item it;
   if (!item_of(a, &it)) return;
   const int tid = threadIdx.x, w = tid / 32, lane = tid % 32;
+  const int own_lim = lane < kCols ? limit_of(a, it, it.cb * kCols + lane) : 0;
+  const int most = __reduce_max_sync(0xffffffffu, own_lim);
+  int lim[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) lim[c] = __shfl_sync(0xffffffffu, own_lim, 2 * w + c);
+  const int k0 = it.chunk * a.chunk, k1 = min(k0 + a.chunk, most);
+
+  // Eight dims of K and of V of a key: NG such pieces a thread. A key past the last stands for zeros.
+  int id[NG];
+  uint32_t kw[NG], vw[NG], kp[NG], vp[NG];
+  auto look_up = [&](int kb) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int j = kb + (tid + 128 * i) / (D / 8);
+      if (j < k1) id[i] = page_entry(a, it.r, j);
+    }
+  };
+  auto fetch = [&](int kb) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int e = tid + 128 * i, j = kb + e / (D / 8), u = e % (D / 8), grp = u / 4, c = u % 4;
+      kw[i] = vw[i] = kp[i] = vp[i] = 0;
+      if (j < k1) {
+        const uint8_t* at = a.kv.page(it.l, it.g, page_in_pool(a, id[i]));
+        const int row = j & ((1 << a.kv.page_shift) - 1);
+        kw[i] = reinterpret_cast<const uint32_t*>(at + a.kv.codes(0, row))[c * NG + grp];
+        const uint16_t* vh = reinterpret_cast<const uint16_t*>(at + a.kv.codes(1, row));
+        vw[i] = vh[2 * c * NG + grp] | uint32_t(vh[(2 * c + 1) * NG + grp]) << 16;
+        kp[i] = reinterpret_cast<const uint32_t*>(at + a.kv.params(0, row))[grp];
+        vp[i] = reinterpret_cast<const uint32_t*>(at + a.kv.params(1, row))[grp];
+      }
+    }
+  };
+  auto unpack = [](float* to, uint32_t codes, uint32_t param) {
+    const float2 sm = __half22float2(u2h(param));
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)  // 2^23 + u less 2^23 + 8, exactly
+      x[e] = fmaf(sm.x, __uint_as_float(((codes >> (4 * e)) & 15u) | 0x4B000000u) - 8388616.f, sm.y);
+    reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  };
+  look_up(k0);
   for (int e = tid; e < kCols * D; e += 128) {
     const int j = it.cb * kCols + e / D;
     float x = 0.f;
@@ -38,96 +85,110 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
     }
     qs[e] = x;
   }
-  int lim[2], most = 0;
-  for (int c = 0; c < kCols; ++c) most = max(most, limit_of(a, it, it.cb * kCols + c));
-#pragma unroll
-  for (int c = 0; c < 2; ++c) lim[c] = limit_of(a, it, it.cb * kCols + 2 * w + c);
-  const int k0 = it.chunk * a.chunk, k1 = min(k0 + a.chunk, most);
+  fetch(k0);
+  look_up(k0 + kSimtKeys);
+
   const float to_log2 = a.scale * kLog2e;
-  float m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, o[2][NG];
+  float m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, o[2][NG];  // sum: of this lane's keys
 #pragma unroll
   for (int c = 0; c < 2; ++c)
 #pragma unroll
     for (int e = 0; e < NG; ++e) o[c][e] = 0.f;
   for (int kb = k0; kb < k1; kb += kSimtKeys) {
     __syncthreads();
-    for (int e = tid; e < kSimtKeys * (D / 8); e += 128) {  // 8 dims of a key, K and V
-      const int key = e / (D / 8), u = e % (D / 8), j = kb + key, grp = u / 4, c = u % 4;
-      float* ko = ks + key * KS + 8 * u;
-      float* vo = vs + key * D + 8 * u;
-      if (j < k1) {
-        const uint8_t* at = a.kv.page(it.l, it.g, page_in_pool(a, page_entry(a, it.r, j)));
-        const int row = j & ((1 << a.kv.page_shift) - 1);
-        const uint32_t kw = reinterpret_cast<const uint32_t*>(at + a.kv.codes(0, row))[c * NG + grp];
-        const uint16_t* vh = reinterpret_cast<const uint16_t*>(at + a.kv.codes(1, row));
-        const uint32_t vw = vh[2 * c * NG + grp] | uint32_t(vh[(2 * c + 1) * NG + grp]) << 16;
-        const float2 kp = __half22float2(reinterpret_cast<const __half2*>(at + a.kv.params(0, row))[grp]);
-        const float2 vp = __half22float2(reinterpret_cast<const __half2*>(at + a.kv.params(1, row))[grp]);
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          ko[x] = fmaf(kp.x, float(int((kw >> (4 * x)) & 15u) - 8), kp.y);
-          vo[x] = fmaf(vp.x, float(int((vw >> (4 * x)) & 15u) - 8), vp.y);
-        }
-      } else {
-#pragma unroll
-        for (int x = 0; x < 8; ++x) ko[x] = vo[x] = 0.f;
-      }
+    for (int i = 0; i < NG; ++i) {
+      const int e = tid + 128 * i, key = e / (D / 8), u = e % (D / 8);
+      unpack(ks + key * KS + 8 * u, kw[i], kp[i]);
+      unpack(vs + key * D + 8 * u, vw[i], vp[i]);
     }
+    fetch(kb + kSimtKeys);
+    look_up(kb + 2 * kSimtKeys);
     __syncthreads();
     float x[2] = {0.f, 0.f};
-    const float* k = ks + lane * KS;
-    const float* q0 = qs + 2 * w * D;
+    const float4* k = reinterpret_cast<const float4*>(ks + lane * KS);
+    const float4* q0 = reinterpret_cast<const float4*>(qs + 2 * w * D);
 #pragma unroll 8
-    for (int e = 0; e < D; ++e) {
-      x[0] = fmaf(q0[e], k[e], x[0]);
-      x[1] = fmaf(q0[D + e], k[e], x[1]);
+    for (int e = 0; e < D / 4; ++e) {
+      const float4 y = k[e];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float4 z = q0[c * (D / 4) + e];
+        x[c] = fmaf(z.w, y.w, fmaf(z.z, y.z, fmaf(z.y, y.y, fmaf(z.x, y.x, x[c]))));
+      }
     }
-    float p[2];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const float y = kb + lane < lim[c] ? x[c] * to_log2 : -INFINITY;
-      float top = y;
+    for (int c = 0; c < 2; ++c) x[c] = kb + lane < lim[c] ? x[c] * to_log2 : -INFINITY;
+    // the reference moves only when a logit passes it by kSimtSlack (log2 units): weights stay below 2^8
+    constexpr float kSimtSlack = 8.f;
+    if (__any_sync(0xffffffffu, x[0] > m[0] + kSimtSlack || x[1] > m[1] + kSimtSlack)) {
 #pragma unroll
-      for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-      const float mn = fmaxf(m[c], top), base = mn == -INFINITY ? 0.f : mn;
-      p[c] = exp2f(y - base);
-      float add = p[c];
+      for (int c = 0; c < 2; ++c) {
+        float top = x[c];
 #pragma unroll
-      for (int s = 16; s > 0; s >>= 1) add += __shfl_xor_sync(0xffffffffu, add, s);
-      const float corr = exp2f(m[c] - base);
-      sum[c] = sum[c] * corr + add;
-      m[c] = mn;
+        for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+        const float mn = fmaxf(m[c], top), corr = mn == -INFINITY ? 1.f : exp2f(m[c] - mn);
+        sum[c] *= corr;
+        m[c] = mn;
 #pragma unroll
-      for (int e = 0; e < NG; ++e) o[c][e] *= corr;
+        for (int e = 0; e < NG; ++e) o[c][e] *= corr;
+      }
     }
-    for (int key = 0; key < kSimtKeys; ++key) {
-      const float p0 = __shfl_sync(0xffffffffu, p[0], key), p1 = __shfl_sync(0xffffffffu, p[1], key);
-      const bool s0 = kb + key < lim[0], s1 = kb + key < lim[1];  // a NaN value reaches only rows that see it
+    float2 p;
+    p.x = exp2f(x[0] - (m[0] == -INFINITY ? 0.f : m[0]));
+    p.y = exp2f(x[1] - (m[1] == -INFINITY ? 0.f : m[1]));
+    sum[0] += p.x;
+    sum[1] += p.y;
+    weights[w][lane] = p;
+    __syncwarp();
+    if (kb + kSimtKeys <= min(lim[0], lim[1])) {
+#pragma unroll 8
+      for (int key = 0; key < kSimtKeys; ++key) {
+        const float2 y = weights[w][key];
+        uint32_t v[NG];
+        load_words<NG>(reinterpret_cast<const uint8_t*>(vs + key * D + NG * lane), v);
 #pragma unroll
-      for (int e = 0; e < NG; ++e) {
-        const float v = vs[key * D + e * 32 + lane];
-        if (s0) o[0][e] = fmaf(p0, v, o[0][e]);
-        if (s1) o[1][e] = fmaf(p1, v, o[1][e]);
+        for (int e = 0; e < NG; ++e) {
+          o[0][e] = fmaf(y.x, __uint_as_float(v[e]), o[0][e]);
+          o[1][e] = fmaf(y.y, __uint_as_float(v[e]), o[1][e]);
+        }
+      }
+    } else if (kb < max(lim[0], lim[1])) {
+#pragma unroll 8
+      for (int key = 0; key < kSimtKeys; ++key) {
+        const float2 y = weights[w][key];
+        const bool s0 = kb + key < lim[0], s1 = kb + key < lim[1];  // a NaN value reaches only rows that see it
+        uint32_t v[NG];
+        load_words<NG>(reinterpret_cast<const uint8_t*>(vs + key * D + NG * lane), v);
+#pragma unroll
+        for (int e = 0; e < NG; ++e) {
+          if (s0) o[0][e] = fmaf(y.x, __uint_as_float(v[e]), o[0][e]);
+          if (s1) o[1][e] = fmaf(y.y, __uint_as_float(v[e]), o[1][e]);
+        }
       }
     }
   }
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], s);
     const int j = it.cb * kCols + 2 * w + c;
     if (j >= it.n * a.kv.G) continue;
 #pragma unroll
-    for (int e = 0; e < NG; ++e) store_out<T>(a, it, j, e * 32 + lane, o[c][e], sum[c]);
+    for (int e = 0; e < NG; ++e) store_out<T>(a, it, j, NG * lane + e, o[c][e], sum[c]);
     if (lane == 0) store_stats(a, it, j, m[c], sum[c], a.chunks == 1);
   }
 }
 
-constexpr int simt_smem_bytes(int d) { return (kSimtKeys * (2 * d + 1) + kCols * d) * int(sizeof(float)); }
+constexpr int simt_smem_bytes(int d) { return (kSimtKeys * (kSimtRow(d) + d) + kCols * d) * int(sizeof(float)); }
 
 // ---------------------------------------------------------------- the join
 // Groups of threads with four dims a thread: kJoin groups share a (layer, row, head) and
 // take every kJoin-th chunk of the request's context, then join in order. One group that
 // walked over 147 chunks took 60 us, eight take 5; over two chunks of 73 000 (row, head)
-// pairs eight groups each (six of them idle) took 200 us.
+// pairs eight groups each (six of them idle) took 200 us. Three to seven chunks (whole
+// calls, one group and eight): 126 pairs 11.8 and 9.1 us, 448 pairs 12.7 and 11.7, 1 792 pairs
+// 26.2 and 28.6, 4 500 pairs 47.9 and 58.6.
 template <typename T, int NG, int kJoin>
 __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
   constexpr int D = NG * 32, kLanes = NG * 8, kPer = 8 / kJoin;
@@ -228,13 +289,14 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(unsigned(chunks >= 8 ? a.part_cols : (a.part_cols + 7) / 8));
+  const bool wide_join = chunks >= 8 || (chunks > 2 && a.part_cols <= 1024);
+  cfg.gridDim = dim3(unsigned(wide_join ? a.part_cols : (a.part_cols + 7) / 8));
   cfg.blockDim = dim3(NG * 64);
   cfg.stream = stream;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
   count_launches(1);
-  return chunks >= 8 ? cudaLaunchKernelEx(&cfg, combine_kernel<T, NG, 8>, a)
+  return wide_join ? cudaLaunchKernelEx(&cfg, combine_kernel<T, NG, 8>, a)
                        : cudaLaunchKernelEx(&cfg, combine_kernel<T, NG, 1>, a);
 }
 
