@@ -31,7 +31,8 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
   __shared__ float2 weights[4][kSimtKeys];
   let_join_start();
   Item it;
-  if (!item_of(a, &it)) return;
+  place_of(a, &it);
+  if (!rows_of(a, &it)) return;
   const int tid = threadIdx.x, w = tid / 32, lane = tid % 32;
   const int own_lim = lane < kCols ? limit_of(a, it, it.cb * kCols + lane) : 0;
   const int most = __reduce_max_sync(0xffffffffu, own_lim);
@@ -395,11 +396,16 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
     }
     cut(most, step, &p.last_chunk, &p.last_chunks);
   } else {
-    // An SM holds two CTAs. One request: one wave of equal chunks. More: eight CTAs for each
-    // place, so that contexts of unequal lengths fill it (64 requests of 2-30k tokens: four 186,
-    // eight 180, sixteen 190 us). At least 256 keys each.
+    // An SM holds two CTAs. One request: one wave of equal chunks. More, on the CUDA cores: eight
+    // CTAs for each place, so that contexts of unequal lengths fill it. On the tensor cores a CTA's
+    // start weighs more, so that only as long as chunks keep 2 048 keys, and one wave else (one row,
+    // 4 KV heads, us with chunks of 256 keys and so: 64 requests of about 300 tokens 18.9 and 11.5,
+    // of 1 000 34.7 and 22.1, of 4 000 63.9 and 52.8, of 16 000, where both are 3 000, 157; 16 requests
+    // of 4 000 34.7 and 24.5, of 16 000 56.9 and 49.7; 5 requests of 4 000 15.9 and 13.1).
     const int64_t items = std::max<int64_t>(1, items_of(kv, s, p.kernel, 1, 1)), places = 2 * 152;
-    const int64_t even = s.R == 1 ? places / items : (8 * places + items - 1) / items;
+    int64_t even = (8 * places + items - 1) / items;
+    if (p.kernel == kAttnMma) even = std::max(places / items, std::min<int64_t>(even, (most + 1023) / 2048));
+    if (s.R == 1) even = places / items;
     p.chunks = int(std::max<int64_t>(1, std::min(even, largest)));
   }
   cut(most, step, &p.chunk, &p.chunks);

@@ -32,7 +32,7 @@ struct Item {
   int l, r, g, cb, chunk, t0, n, len;
 };
 
-// The chunk, KV head, request and layer of unit x, and the request's rows and length.
+// The chunk, KV head, request and layer of unit x.
 __device__ __forceinline__ void decode(const AttnArgs& a, uint32_t x, int chunks, Item* it) {
   it->chunk = int(x % uint32_t(chunks));
   x /= uint32_t(chunks);
@@ -40,15 +40,19 @@ __device__ __forceinline__ void decode(const AttnArgs& a, uint32_t x, int chunks
   x /= uint32_t(a.kv.Hkv);
   it->r = int(x % uint32_t(a.s.R));
   it->l = int(x / uint32_t(a.s.R));
+}
+// The request's rows and length.
+__device__ __forceinline__ void load_rows(const AttnArgs& a, Item* it) {
   it->t0 = a.s.row_off[it->r];
   it->n = a.s.row_off[it->r + 1] - it->t0;
   it->len = cached_len(a.s, a.kv.capacity(), it->r, a.status, threadIdx.x == 0);
 }
 
 // Column blocks of kCols, side by side so that they share the keys in L2; in clusters, the
-// chunks of a context side by side.
+// chunks of a context side by side. The item's place comes first, so that loads which need no
+// more go out beside those of its rows; false from the second step: nothing to do.
 template <bool kCluster = false>
-__device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
+__device__ __forceinline__ void place_of(const AttnArgs& a, Item* it) {
   const uint32_t inner = kCluster ? a.chunks : a.col_blocks;
   uint32_t x = blockIdx.x / inner;
   if (kCluster) {
@@ -58,6 +62,10 @@ __device__ __forceinline__ bool item_of(const AttnArgs& a, Item* it) {
     it->cb = int(blockIdx.x % inner);
     decode(a, x, a.chunks, it);
   }
+}
+template <bool kCluster = false>
+__device__ __forceinline__ bool rows_of(const AttnArgs& a, Item* it) {
+  load_rows(a, it);
   if (it->cb * kCols >= it->n * a.kv.G) return false;
   return kCluster || it->chunk == 0 || it->chunk * a.chunk < it->len;
 }

@@ -98,6 +98,7 @@ __device__ __forceinline__ bool tc_item(const AttnArgs& a, Item* it) {
   uint32_t x = single ? blockIdx.x - units * pairs : blockIdx.x / pairs;
   const int rank = single ? 0 : int(blockIdx.x % pairs);
   decode(a, x, single ? a.last_chunks : a.chunks, it);
+  load_rows(a, it);
   const int tiles = (it->n * a.kv.G + kTileCols - 1) / kTileCols;  // column tiles of the request
   it->cb = single ? tiles / 2 : rank;
   if (single ? !(tiles & 1) : rank >= tiles / 2) return false;
