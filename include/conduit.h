@@ -626,8 +626,8 @@ conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* f
  * bf16 rows with head_dim 64, 96 or 128 run on the tensor cores (fp16 operands:
  * queries exact but for a power of two, values and weights within 2^-11, fp32
  * sums); fp32 rows and other head sizes on the CUDA cores in fp32. Keys enter
- * exactly, or as two fp16 numbers, where a request has at most 8 rows x (Hq/Hkv)
- * or max_len < 2048: lse then carries fp32 rounding only. Else they are within
+ * exactly, or as two fp16 numbers, where no request has rows x (Hq/Hkv) > 8 or
+ * max_len < 2048: lse then carries fp32 rounding only. Else they may be within
  * 2^-11 of themselves (lse to about 2e-6 over 8192 keys). The kernel and the cut
  * into key chunks follow from the sizes, max_len and row_off, so equal calls give
  * equal bits.

@@ -358,12 +358,17 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   PackedAttnPlan p{};
   const int most = int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
   const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
-  // Up to eight columns: the warp-level kernel, whose one block reads the cache once. Then
-  // tcgen05 (16 requests of 8 192 tokens, 28 / 4 heads, both in us: 14 columns 69 and 66, 21: 89
-  // and 68, 63: 181 and 70), but for few columns over a short context, where its start shows
-  // (16 requests of 1 000 tokens: 28 columns 30 and 31, 56: 47 and 39).
+  // Up to eight columns: the warp-level kernel, whose one block reads the cache once. Up to 64: the
+  // kernel with less time by a model, blocks of eight columns at 3.5 us and 9 ns a key on 304 places
+  // after 8 us, or tiles of 128 at 11 us and 1.35 us for 128 keys (2.5 in two parts) on 152 after 18
+  // (28 x 4 heads, 2 and 4 and 8 rows, warp-level / tcgen05, us: one request of 4 000 tokens 9.6 / 15.8,
+  // 11.3 / 16.0, 12.5 / 16.4; 16 of about 4 000 29 / 54, 47 / 52, 84 / 58; 64 of about 1 000 37 / 81,
+  // 56 / 79, 89 / 75; 64 of about 4 000 98 / 137, 159 / 133, 285 / 131).
   const int64_t columns = int64_t(s.max_rows) * kv.G;
-  const bool few = columns <= kCols || (columns <= 4 * kCols && most < 2048);
+  const double units = double(kv.L) * s.R * kv.Hkv;
+  const double warp_us = 8. + units * ((columns + kCols - 1) / kCols) * (3.5 + 0.009 * most) / 304.;
+  const double tc_us = 18. + units * (11. + (most < kExactBelow ? 2.5 : 1.35) / 128. * most) / 152.;
+  const bool few = columns <= kCols || (columns <= 64 && warp_us < tc_us);
   p.kernel = !mma ? kAttnSimt : few ? kAttnMma : kAttnTc;
   const int step = p.kernel == kAttnSimt ? 64 : 256;  // least keys of a chunk
   const int64_t largest = std::max(1, (most + step - 1) / step);
