@@ -624,8 +624,9 @@ conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* f
  *          (fp32 partial results of key chunks); calls that overlap on the GPU
  *          need workspaces of their own
  * bf16 rows with head_dim 64, 96 or 128 run on the tensor cores (fp16 operands:
- * queries exact but for a power of two, values and weights within 2^-11, fp32
- * sums); fp32 rows and other head sizes on the CUDA cores in fp32. Keys enter
+ * queries exact but for a power of two, values within 2^-11, weights within 2^-11
+ * of themselves or 2^-32 of the row's largest, fp32 sums); fp32 rows and other
+ * head sizes on the CUDA cores in fp32. Keys enter
  * exactly, or as two fp16 numbers, where no request has rows x (Hq/Hkv) > 8 or
  * max_len < 2048: lse then carries fp32 rounding only. Else they may be within
  * 2^-11 of themselves (lse to about 2e-6 over 8192 keys). The kernel and the cut

@@ -8,6 +8,14 @@
 namespace conduit {
 constexpr int kCols = 8;  // columns per CTA of the warp-level and CUDA-core kernels
 
+// The tensor-core kernels' weights are fp16 numbers 2^(logit - reference): normal down to 2^-14 and
+// 0 from 2^-25 on, while the fp32 sum counts every weight. So the reference stays kBias (log2 units)
+// below the largest logit, which makes use of the range up to 2^15, and moves only when a logit passes it
+// by kMostWeight. A weight is within 2^-11 of itself or 2^-32 of the row's largest one. (With the
+// largest weight at 1, 262 144 keys of 2^-25 beside it lost 0.7 % of the output.)
+constexpr float kBias = 7.f, kUnbias = 1.f / 128.f;
+constexpr float kMostWeight = 15.f;
+
 struct AttnArgs {
   PackedDev kv;
   SeqsDev s;

@@ -92,10 +92,6 @@ struct Running {
   float o[2 * NG][4];    // dims 32 g + 4 q + {0, 1} and {2, 3} of both columns in o[2 g], o[2 g + 1]
 };
 
-// The weights' reference moves only when a logit passes it by more than this (log2
-// units): weights stay below 2^8, which fp16 and the fp32 sums hold as well as 1.
-constexpr float kSlack = 8.f;
-
 // A tile in shared memory: page after page as in the pool, and of pages of more than 32 tokens
 // the 32 as a page of their own. Offsets of the codes and parameters of tokens 8 i.. of K (v = 0)
 // or V (v = 1); kRun: tokens of a page in the tile.
@@ -152,13 +148,13 @@ __device__ __forceinline__ void tile_step(Running<NG>& st, const uint8_t* box, c
 #pragma unroll
   for (int e = 0; e < 2; ++e)
     top[e] = fmaxf(fmaxf(x[0][e], x[0][e + 2]), fmaxf(x[1][e], x[1][e + 2])) * to_log2[e];
-  if (__any_sync(0xffffffffu, top[0] > st.ref[0] + kSlack || top[1] > st.ref[1] + kSlack)) {
+  if (__any_sync(0xffffffffu, top[0] > st.ref[0] + kMostWeight || top[1] > st.ref[1] + kMostWeight)) {
     float corr[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
 #pragma unroll
       for (int s = 4; s < 32; s <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], s));
-      const float moved = fmaxf(st.ref[e], top[e]);
+      const float moved = fmaxf(st.ref[e], top[e] - kBias);
       corr[e] = moved == -INFINITY ? 1.f : tc::ex2(st.ref[e] - moved);
       st.ref[e] = moved;
       st.sum[e] *= corr[e];
@@ -443,7 +439,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int col = 2 * c + e;
-    if (q == 0) ml[w * kCols + col] = make_float2(st.ref[e], st.sum[e]);
+    if (q == 0) ml[w * kCols + col] = make_float2(st.ref[e] + kBias, st.sum[e] * kUnbias);
 #pragma unroll
     for (int g = 0; g < NG; ++g)
       *reinterpret_cast<float4*>(ow + (w * kCols + col) * kRow + 32 * g + 4 * q) =
@@ -460,7 +456,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) top = fmaxf(top, ml[k * kCols + col].x);
     const float base = top == -INFINITY ? 0.f : top;
-    weight[i * kCols + col] = tc::ex2(ml[i * kCols + col].x - base);
+    weight[i * kCols + col] = tc::ex2(ml[i * kCols + col].x - base) * kUnbias;
     if (i == 0) {
       float total = 0.f;
 #pragma unroll

@@ -40,7 +40,6 @@ constexpr uint32_t kBlock = 128 * 128;        // 128 rows of 64 fp16, swizzled
 constexpr uint32_t kSCols = 128, kPCol = 64, kOCol = 256;
 constexpr int kHalf = kKeys / 2;              // keys of a load
 constexpr int kRing = 3;                      // loads under way
-constexpr float kSlack = 8.f;                 // as in packed_attn_mma.cu
 
 template <int NG>
 struct Sizes {
@@ -557,9 +556,9 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
         const float2 down = make_float2(low, low);
         float top = edge ? weigh<true>(sb, up, down, left, p, &add) : weigh<false>(sb, up, down, left, p, &add);
         top *= to_log2;
-        if (pass || !__any_sync(0xffffffffu, top > ref + kSlack)) break;
+        if (pass || !__any_sync(0xffffffffu, top > ref + kMostWeight)) break;
         // the reference moves: what was summed so far is scaled, and the weights are taken again
-        const float moved = fmaxf(ref, top), corr = moved == -INFINITY ? 1.f : tc::ex2(ref - moved);
+        const float moved = fmaxf(ref, top - kBias), corr = moved == -INFINITY ? 1.f : tc::ex2(ref - moved);
         ref = moved;
         sum = make_float2(sum.x * corr, sum.y * corr);
         if (t > 0) {
@@ -583,7 +582,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     }
     // without keys there is nothing to wait for but the other warps' queries, over which the rows go out
     if (ok) ok = count > 0 ? wait_warp(&bars.o_full[x], 0, abort) : wait_warp(&bars.q_full, 0, abort);
-    float total = sum.x + sum.y, own_w = 1.f, b_w = 0.f;
+    ref += kBias;
+    float total = (sum.x + sum.y) * kUnbias, own_w = kUnbias, b_w = 0.f;
     bool join = false;
     if (split) {
       if (x == 1) {
@@ -595,9 +595,10 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
         join = true;
         const float2 b = of_b[at];
         const float top = fmaxf(ref, b.x), base = top == -INFINITY ? 0.f : top;
-        own_w = tc::ex2(ref - base);
-        b_w = tc::ex2(b.x - base);
-        total = own_w * total + b_w * b.y;
+        const float wa = tc::ex2(ref - base), wb = tc::ex2(b.x - base);
+        total = wa * total + wb * b.y;
+        own_w = wa * kUnbias;
+        b_w = wb * kUnbias;
         ref = top;
       }
     }
