@@ -626,12 +626,13 @@ conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* f
  * bf16 rows with head_dim 64, 96 or 128 run on the tensor cores (fp16 operands:
  * queries exact but for a power of two, values within 2^-11, weights within 2^-11
  * of themselves or 2^-32 of the row's largest, fp32 sums); fp32 rows and other
- * head sizes on the CUDA cores in fp32. Keys enter
- * exactly, or as two fp16 numbers, where no request has rows x (Hq/Hkv) > 8 or
- * max_len < 2048: lse then carries fp32 rounding only. Else they may be within
- * 2^-11 of themselves (lse to about 2e-6 over 8192 keys). The kernel and the cut
- * into key chunks follow from the sizes, max_len and row_off, so equal calls give
- * equal bits.
+ * head sizes on the CUDA cores in fp32. Where no request has rows x (Hq/Hkv) > 8,
+ * and for every row that sees fewer than 2048 keys, keys enter exactly or as two
+ * fp16 numbers: lse then carries fp32 rounding only. For other rows a key may be
+ * within 2^-11 of itself, and so a logit within 2^-11 of scale sum |q||k|; in lse
+ * that averages over the keys that count (2e-6 of it over 8192 of like weight). The
+ * kernel and the cut into key chunks follow from the sizes, max_len and row_off,
+ * the form of the keys from what the rows see, so equal calls give equal bits.
  */
 conduit_status conduit_packed_attn_workspace_size(const conduit_packed_kv* kv, const conduit_seqs* seqs,
                                                   int32_t dtype, size_t* bytes);

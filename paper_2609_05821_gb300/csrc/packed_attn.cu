@@ -262,18 +262,11 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
     a.lse[(int64_t(l) * a.kv.Hq + h) * a.s.T + t] = sum == 0.f ? -INFINITY : kLn2 * (base + log2f(sum));
 }
 
-// The tcgen05 kernel's keys are within 2^-11 of their values, and so a logit within 2^-11 of sum
-// |q||k|: nothing beside the rounding of a bf16 output, and in a log-sum-exp an error that falls
-// with the number of keys that count (2 x 10^-4 of it for one key, 5 x 10^-6 for 2 000, 2 x 10^-6
-// for 8 192). For shorter contexts keys come as two fp16 numbers, whether or not a log-sum-exp is
-// asked for, so that outputs do not depend on that.
-constexpr int kExactBelow = 2048;
-
 template <typename T, int NG>
 cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
   cudaError_t err;
   if (plan.kernel == kAttnTc) {
-    err = launch_packed_attn_tc(a, plan.items, a.s.max_len < kExactBelow, stream);
+    err = launch_packed_attn_tc(a, plan.items, stream);
   } else if (plan.kernel == kAttnMma) {
     err = launch_packed_attn_mma(a, plan.items, plan.cluster, stream);
   } else {
@@ -373,7 +366,8 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   const int step = p.kernel == kAttnSimt ? 64 : 256;  // least keys of a chunk
   const int64_t largest = std::max(1, (most + step - 1) / step);
   if (p.kernel == kAttnTc) {
-    // One CTA per SM: the chunks with the least time by a model of the pass, 11 us for a CTA and
+    // One CTA per SM: the chunks with the least time by a model of the pass where every row sees
+    // max_len keys, 11 us for a CTA and
     // 1.8 us for 128 keys of two column tiles (3.3 of keys in two parts), three quarters of it for
     // one, and of the join, 12 bytes a partial value at 5 TB/s after a launch of 5 us. Either all
     // blocks have the same chunks (two layers x 16 requests x 8 192 keys, 28 / 4 heads of 96: one

@@ -16,6 +16,15 @@ constexpr int kCols = 8;  // columns per CTA of the warp-level and CUDA-core ker
 constexpr float kBias = 7.f, kUnbias = 1.f / 128.f;
 constexpr float kMostWeight = 15.f;
 
+// tcgen05: a key as one fp16 number is within 2^-11 of its value, and so a logit within 2^-11 of
+// scale sum |q||k|: nothing beside the rounding of a bf16 output, and in a log-sum-exp an error that falls
+// with the number of keys that count (2 x 10^-4 of it for one key, 2 x 10^-6 for 8 192 of like
+// weight). So a block with a column that sees fewer keys than this, if any, takes its keys as the sum of two
+// fp16 numbers, a tile in both key buffers, whose logits keep fp32's precision: 170 us for 32-128 rows over 2 000 keys, where one fp16
+// number takes 114. It goes by what the columns see and not by whether a log-sum-exp
+// is asked for, so that outputs do not depend on that.
+constexpr int kExactBelow = 2048;
+
 struct AttnArgs {
   PackedDev kv;
   SeqsDev s;
@@ -198,7 +207,6 @@ __device__ __forceinline__ bool finite_pair(uint32_t p) {
 // (packed_attn_tc.cu): bf16 rows, head_dim 64, 96, 128.
 // `cluster`: the chunks of a context form a cluster, which joins them itself.
 cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, bool cluster, cudaStream_t stream);
-// `exact`: logits in fp32's precision.
-cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, bool exact, cudaStream_t stream);
+cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream);
 
 }  // namespace conduit

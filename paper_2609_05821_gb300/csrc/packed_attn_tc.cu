@@ -26,6 +26,8 @@
 // unpacks; a CTA another 20 000 (item and limits 2 500, queries 8 000-11 500, rows out 7 000, the
 // next CTA's launch 2 000). Measured: 32-128 rows of 16 requests over 8 192 keys, two layers of
 // 28 x 4 heads of 128, 317 us (1.0 PFLOP/s); 96 dims 329, 64 dims 250.
+#include <type_traits>
+
 #include "packed_attn.cuh"
 
 namespace conduit {
@@ -223,17 +225,14 @@ __device__ __forceinline__ float weigh(uint32_t sb, float2 up, float2 down, int 
   return top;
 }
 
-// kExact: keys as the sum of two fp16 numbers (a tile in both key buffers), so that logits keep
-// fp32's precision: 186 us for the same rows over 2 000 keys, where one fp16 number would take about
-// 115.
-template <int NG, bool kExact>
+template <int NG>
 __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   using Z = Sizes<NG>;
   constexpr int D = Z::D;
   extern __shared__ uint8_t dynamic[];
   __shared__ Bars bars;
   __shared__ uint32_t tmem_slot;
-  __shared__ int seen_most, seen_least, poison[NG], abort_flag;
+  __shared__ int seen_most, seen_least, seen_few, poison[NG], abort_flag;
   __shared__ float2 of_b[kTileCols];  // split: B's (reference, sum)
   let_join_start();
   // Blocks with two column tiles come first and those with one, which take half of the time, last.
@@ -267,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     tc::mbar_init(&bars.drained, 1);
     tc::fence_barrier_init();
     seen_most = 0;
-    seen_least = INT32_MAX;
+    seen_least = seen_few = INT32_MAX;
     for (int g = 0; g < NG; ++g) poison[g] = INT32_MAX;
     abort_flag = 0;
   }
@@ -279,9 +278,11 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   const int lim = live ? limit_of(a, it, col) : INT32_MAX;
   if (warp >= kSoftWarp) {
     const int hi = __reduce_max_sync(0xffffffffu, live ? lim : 0), lo = __reduce_min_sync(0xffffffffu, lim);
+    const int few = __reduce_min_sync(0xffffffffu, lim > 0 ? lim : INT32_MAX);
     if (lane == 0) {
       atomicMax(&seen_most, hi);
       atomicMin(&seen_least, lo);
+      atomicMin(&seen_few, few);
     }
   }
   tc::tc_fence_before();
@@ -290,6 +291,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   const uint32_t tmem = tmem_slot;
   const int least = seen_least, k0 = it.chunk * chunk, k1 = min(k0 + chunk, seen_most);
   const int tiles = k1 > k0 ? (k1 - k0 + kKeys - 1) / kKeys : 0;
+  // keys in two parts, whatever the chunk
+  const bool exact = __shfl_sync(0xffffffffu, int(seen_few < kExactBelow), 0) != 0;
 
   // 128 registers a thread at launch: 2 x 88 + 2 x 168 per four warpgroups
   if (warp < kSoftWarp) {
@@ -339,6 +342,10 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     // that their chunks fall into different banks of the swizzled tile; values: side by side.
     // Every warp sees every copy land and says so before its slot is used again, also where
     // another four warps unpack it: none can take a phase of a slot for the one two before it.
+    // Either form of the keys has a copy of this loop and of the MMAs' (one copy that asks at every
+    // tile: 361 us for 8 192 keys instead of 316).
+    auto unpack = [&](auto form) {
+    constexpr bool kExact = decltype(form)::value;
     const int c = lane & 3, i8 = lane >> 2, run_shift = min(6, a.kv.page_shift);
     int unit = warp - kUnpackWarp;  // the next one of this warp
     for (int load = 0; load < 2 * tiles; ++load) {
@@ -368,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
         // use before that: this wait cannot mistake its phase either.)
         if (mine && t >= 2 && !(kExact && !v))
           ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
-        // kExact has one key buffer, whose every use every warp sees
+        // keys in two parts have one buffer, whose every use every warp sees
         if (kExact && ok && t >= 1 && !(load & 1)) ok = wait_warp(&bars.k_free[0], (t - 1) & 1, abort);
       }
       if (!ok) {
@@ -382,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       if (!v) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (kExact)
+          if constexpr (kExact)
             unpack_keys_exact<NG>(tile, tile + Z::kTile, x[i], token + 8 * i, c);
           else
             unpack_keys<NG>(tile, x[i], token + 8 * i, c);
@@ -398,10 +405,17 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(v ? &bars.v_full[stage] : &bars.k_full[kExact ? 0 : stage]);
     }
+    };
+    if (exact)
+      unpack(std::true_type{});
+    else
+      unpack(std::false_type{});
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------------ MMAs
     // the whole warp walks the schedule on values from one lane, so that the operands live in
     // uniform registers
+    auto products = [&](auto form) {
+    constexpr bool kExact = decltype(form)::value;
     const uint32_t leader = lane == 0;
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     const int all = __shfl_sync(0xffffffffu, tiles, 0);
@@ -421,11 +435,15 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
       }
       const uint64_t dk = tc::desc_sw128(k_at + stage * Z::kTile);
       const uint64_t dx = dq + (halves ? 0 : (x * Z::kTile) >> 4);
+      // (both parts in one unrolled row: descriptors spill and the other copy slows down, 342 us)
+#pragma unroll 1
+      for (int part = 0; part < (kExact ? 2 : 1); ++part) {  // the second: what the keys' first parts left out
+        const uint64_t dp = dk + (part ? Z::kTile >> 4 : 0);
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-        const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
-        tc::mma_bf16_if(leader, tm + x * kSCols, dx + off, dk + off, idesc_s, kk > 0);
-        if (kExact) tc::mma_bf16_if(leader, tm + x * kSCols, dx + off, dk + off + (Z::kTile >> 4), idesc_s, true);
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
+          tc::mma_bf16_if(leader, tm + x * kSCols, dx + off, dp + off, idesc_s, kk > 0 || part > 0);
+        }
       }
       tc::mma_commit_if(leader, &bars.s_full[x]);
       if (halves || x == 1) tc::mma_commit_if(leader, &bars.k_free[stage]);
@@ -460,6 +478,11 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     tc::mma_commit_if(leader, &bars.drained);  // every MMA issued above is done once this arrives
     tc::mbar_wait(&bars.drained, 0);
     __syncwarp();
+    };
+    if (exact)
+      products(std::true_type{});
+    else
+      products(std::false_type{});
   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 168;" ::: "memory");
@@ -706,23 +729,23 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
   }
 }
 
-template <int NG, bool kExact>
+template <int NG>
 cudaError_t launch(const AttnArgs& a, int64_t items, cudaStream_t stream) {
   constexpr uint32_t kSmem = Sizes<NG>::kSmem;
-  cudaError_t err = cudaFuncSetAttribute(packed_attn_tc<NG, kExact>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  cudaError_t err = cudaFuncSetAttribute(packed_attn_tc<NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (err) return err;
-  packed_attn_tc<NG, kExact><<<unsigned(items), kThreads, kSmem, stream>>>(a);
+  packed_attn_tc<NG><<<unsigned(items), kThreads, kSmem, stream>>>(a);
   count_launches(1);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, bool exact, cudaStream_t stream) {
+cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream) {
   switch (a.kv.d) {
-    case 64: return exact ? launch<2, true>(a, items, stream) : launch<2, false>(a, items, stream);
-    case 96: return exact ? launch<3, true>(a, items, stream) : launch<3, false>(a, items, stream);
-    default: return exact ? launch<4, true>(a, items, stream) : launch<4, false>(a, items, stream);
+    case 64: return launch<2>(a, items, stream);
+    case 96: return launch<3>(a, items, stream);
+    default: return launch<4>(a, items, stream);
   }
 }
 

@@ -61,3 +61,56 @@ def test_weights_far_below_the_largest(C, d, n, rows, below):
     # sums count n terms in fp32
     gl = lse[0].double().cpu().numpy()
     assert np.all(np.abs(gl - wl) <= e[..., 0].T + 2.0 ** -22 * np.abs(wl) + n * 2.0 ** -24 + 2.0 ** -21)
+
+
+def _between_halves(rng, n, hkv, d):
+    """Keys that the cache holds exactly, almost all of them half way between two fp16 numbers, on the
+    same side of the one they round to: group scale 2^-11, mid 1, codes 1 and 5."""
+    c = rng.choice([1, 5], size=(n, hkv, d // 32, 32))
+    c[..., 0], c[..., 1] = -8, 7
+    return (1 + c * 2.0 ** -11).reshape(n, hkv, d)
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_rows_that_see_few_keys_have_exact_logits(C, d):
+    """Many rows, in a call whose max_len is long: rows that see less than 2,048 keys carry fp32 rounding
+    only in their log-sum-exp, whatever max_len and the other rows. A key in one fp16 number
+    would put a logit off by 0.9 x 2^-11 of its size here."""
+    rng = np.random.default_rng(d)
+    hkv, G, ps = 2, 7, 16
+    lens, rows = (37, 2047, 2600, 3000, 130), (37, 40, 64, 40, 12)
+    T, most = sum(rows), 4096
+    need = [-(-n // ps) for n in lens]
+    first = np.concatenate([[0], np.cumsum(need)])
+    table = torch.zeros((len(lens), most // ps), dtype=torch.int32)
+    for r, n in enumerate(need):
+        table[r, :n] = torch.arange(first[r], first[r] + n)
+    kv = C.PackedKv.empty(1, int(first[-1]), hkv * G, hkv, d, ps, table)
+    K = [_between_halves(rng, n, hkv, d) for n in lens]
+    V = [rng.choice([-1.0, 1.0, 2.0], size=(n, hkv, d // 32, 1)).repeat(32, -1).reshape(n, hkv, d) for n in lens]
+    dev_lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    dev = lambda x: torch.from_numpy(np.concatenate(x)).float().cuda()[None]
+    C.conduit_packed_append(kv, C.Seqs(np.concatenate([[0], np.cumsum(lens)]), dev_lens, most), dev(K), dev(V))
+    limits = np.concatenate([np.arange(1, 38), np.full(40, 2047), rng.integers(0, 2601, 64), rng.integers(2048, 3001, 40),
+                             np.arange(119, 131)])
+    limits[80:83] = 0, 1, 2600
+    q = torch.ones((1, T, hkv * G, d), dtype=BF, device="cuda")
+    seqs = C.Seqs(np.concatenate([[0], np.cumsum(rows)]), dev_lens, most)
+    lse = torch.zeros((1, hkv * G, T), device="cuda")
+    scale = float(np.float32(10 / d))
+    out = C.conduit_packed_attn(kv, seqs, q, scale=scale, lse=lse,
+                                limits=torch.from_numpy(limits.astype(np.int32)).cuda())
+    t = 0
+    for r, (n, c) in enumerate(zip(lens, rows)):
+        seen = limits[t:t + c]
+        wo, wl, A, big = R.attend(q[0, t:t + c].double().cpu().numpy(), K[r], V[r], seen, scale)
+        gl, got = lse[0, :, t:t + c].double().cpu().numpy(), out[0, t:t + c].double().cpu().numpy()
+        assert np.array_equal(np.isneginf(gl), np.isneginf(wl))
+        few = np.broadcast_to(seen < 2048, gl.shape)
+        e = (d * 2.0 ** -23 + np.where(few, 0.0, 2.0 ** -11)) * A.T
+        room = e + 2.0 ** -22 * np.abs(wl) + n * 2.0 ** -24 + 2.0 ** -21
+        fin = np.isfinite(wl)
+        assert np.all(np.abs(gl[fin] - wl[fin]) <= room[fin]), (r, float(np.max(np.abs(gl[fin] - wl[fin]))))
+        tol = ((np.expm1(2 * e.T) + 2.0 ** -10 + (n + 16) * 2.0 ** -24) * big)[..., None] + 2.0 ** -8 * np.abs(wo)
+        assert np.all(np.abs(got - wo) <= tol), r
+        t += c
