@@ -661,6 +661,13 @@ def _addr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _table_holds(kv, num_requests: int):
+    """The kernels read row r of the page table for every request r of a call."""
+    if kv.struct.page_size and kv.page_table.shape[0] < num_requests:
+        raise ConduitError(ERR_INVALID_ARG, f"the page table has {kv.page_table.shape[0]} rows, fewer than "
+                                            f"there are requests ({num_requests})")
+
+
 def _rows(t: torch.Tensor, name: str, layers: int, rows: int, heads: int, d: int, dtype=None):
     """Strided rows [L][T][H][d] (or [T][H][d] of one layer) as a conduit_rows reference."""
     shape, stride = t.shape, t.stride()
@@ -694,6 +701,7 @@ def conduit_rope(rope: Rope, x: torch.Tensor, pos: torch.Tensor, out=None, inver
 
 def _append_args(kv, seqs: Seqs, k, v, rope, pos, q, q_out):
     L, T, Hkv, d = kv.num_layers, seqs.num_rows, kv.num_kv_heads, kv.head_dim
+    _table_holds(kv, seqs.num_requests)
     if q is not None and q_out is None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     rows = [_rows(k, "k", L, T, Hkv, d), _rows(v, "v", L, T, Hkv, d, k.dtype)]
@@ -726,8 +734,8 @@ def conduit_packed_read(kv: PackedKv, batch: Batch, dst: KvCache, first=None, st
     """Tokens first[r] .. of every request of a 4-bit cache into dst, as the batch lays it out."""
     if first is not None and (first.dtype != torch.int32 or first.numel() != batch.num_requests):
         raise ConduitError(ERR_INVALID_ARG, "first must be int32 with one entry per request")
-    if batch.num_requests > kv.page_table.shape[0]:
-        raise ConduitError(ERR_INVALID_ARG, "the page table has fewer rows than the batch has requests")
+    _table_holds(kv, batch.num_requests)
+    _table_holds(dst, batch.num_requests)
     _check(_lib.conduit_packed_read(kv.ref(), _addr(first), dst.ref(), batch.ref(), _addr(status),
                                     _stream_ptr(stream)))
 
@@ -746,8 +754,7 @@ def conduit_packed_attn(kv: PackedKv, seqs: Seqs, q: torch.Tensor, scale: Option
     """Attention of rows q [L, T, Hq, d] over a 4-bit cache. limits int32 [T]: keys each row sees
     (None: causal at the end of the context); lse fp32 [L, Hq, T] receives the log-sum-exp."""
     L, T, Hq, d = kv.num_layers, seqs.num_rows, kv.num_q_heads, kv.head_dim
-    if seqs.num_requests > kv.page_table.shape[0]:
-        raise ConduitError(ERR_INVALID_ARG, "the page table has fewer rows than there are requests")
+    _table_holds(kv, seqs.num_requests)
     if limits is not None and (limits.dtype != torch.int32 or limits.numel() != T or not limits.is_contiguous()):
         raise ConduitError(ERR_INVALID_ARG, "limits must be contiguous int32 with one entry per row")
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() != L * Hq * T or not lse.is_contiguous()):
