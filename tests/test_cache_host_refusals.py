@@ -23,3 +23,10 @@ def test_append_needs_a_page_table_row_per_request(C):
 def test_read_needs_a_row_of_the_destinations_page_table_per_request(C):
     batch = C.Batch([0, 5, 9], [0, 5, 9], [0, 1, 2], [0, 1, 2], device="cpu")
     _expect(C, C.ERR_INVALID_ARG, C.conduit_packed_read, _packed(C), batch, _paged(C, R=1), match="page table")
+
+
+def test_read_refuses_strided_starts(C):
+    batch = C.Batch([0, 5, 9], [0, 5, 9], [0, 1, 2], [0, 1, 2], device="cpu")
+    dst = C.KvCache(torch.zeros((1, 2, 9, 64), dtype=BF), torch.zeros((1, 2, 9, 64), dtype=BF), 4)
+    first = torch.arange(4, dtype=torch.int32)[::2]
+    _expect(C, C.ERR_INVALID_ARG, C.conduit_packed_read, _packed(C), batch, dst, first=first, match="first")
