@@ -36,37 +36,46 @@ class PackedContexts:
                                    table, device)
         self.rope, self.max_len, self.num_requests = rope, max_len, num_requests
         self.lens = torch.zeros(num_requests, dtype=torch.int32, device=device)
+        self._grown = torch.zeros_like(self.lens)  # the lengths with a call's rows, until the call is accepted
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
 
-    def _seqs(self, rows: Sequence[int]) -> C.Seqs:
+    def _seqs(self, rows: Sequence[int], lens: torch.Tensor) -> C.Seqs:
+        if len(rows) != self.num_requests or min(rows, default=0) < 0:
+            raise C.ConduitError(C.ERR_INVALID_ARG, f"rows needs a count >= 0 for each of {self.num_requests} requests")
         off = [0]
         for n in rows:
             off.append(off[-1] + int(n))
-        return C.Seqs(off, self.lens, self.max_len)
+        return C.Seqs(off, lens, self.max_len)
 
     def append(self, rows: Sequence[int], k, v, pos=None, q=None):
         """New tokens, rows[r] of request r: keys turned and packed, queries turned. Returns the turned
-        queries (None without q). Rows k, v [L, T, Hkv, d], q [L, T, Hq, d], pos int32 [A, T]."""
-        self.lens += torch.tensor([int(n) for n in rows], dtype=torch.int32, device=self.lens.device)
-        return C.conduit_packed_append(self.kv, self._seqs(rows), k, v, self.rope, pos, q, status=self.status)
+        queries (None without q). Rows k, v [L, T, Hkv, d], q [L, T, Hq, d], pos int32 [A, T]. A call that
+        raises leaves the contexts as they were."""
+        seqs = self._seqs(rows, self._grown)
+        more = torch.tensor([int(n) for n in rows], dtype=torch.int32, device=self.lens.device)
+        torch.add(self.lens, more, out=self._grown)
+        q_rot = C.conduit_packed_append(self.kv, seqs, k, v, self.rope, pos, q, status=self.status)
+        self.lens.copy_(self._grown)
+        return q_rot
 
     def attend(self, rows: Sequence[int], q, limits=None, lse=None):
         """Attention of the newest rows[r] tokens of each request over its context."""
-        return C.conduit_packed_attn(self.kv, self._seqs(rows), q, limits=limits, lse=lse, status=self.status)
+        return C.conduit_packed_attn(self.kv, self._seqs(rows, self.lens), q, limits=limits, lse=lse, status=self.status)
 
     def decoder(self, dtype: torch.dtype = torch.bfloat16):
         """A one-token step: step(q, k, v, pos) appends a row per request and returns their attention
         [L, R, Hq, d]. Its buffers are allocated here, so that it can be captured."""
         kv, R = self.kv, self.num_requests
-        seqs = self._seqs([1] * R)
+        seqs, grown = self._seqs([1] * R, self.lens), self._seqs([1] * R, self._grown)
         shape = (kv.num_layers, R, kv.num_q_heads, kv.head_dim)
         q_rot, out = (torch.empty(shape, dtype=dtype, device=self.lens.device) for _ in range(2))
         need = C.conduit_packed_attn_workspace_size(kv, seqs, dtype)
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=self.lens.device)
 
         def step(q, k, v, pos=None):
-            self.lens.add_(1)
-            C.conduit_packed_append(kv, seqs, k, v, self.rope, pos, q, q_rot, status=self.status)
+            torch.add(self.lens, 1, out=self._grown)
+            C.conduit_packed_append(kv, grown, k, v, self.rope, pos, q, q_rot, status=self.status)
+            self.lens.copy_(self._grown)
             return C.conduit_packed_attn(kv, seqs, q_rot, out=out, workspace=workspace, status=self.status)
 
         return step

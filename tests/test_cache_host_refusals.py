@@ -30,3 +30,29 @@ def test_read_refuses_strided_starts(C):
     dst = C.KvCache(torch.zeros((1, 2, 9, 64), dtype=BF), torch.zeros((1, 2, 9, 64), dtype=BF), 4)
     first = torch.arange(4, dtype=torch.int32)[::2]
     _expect(C, C.ERR_INVALID_ARG, C.conduit_packed_read, _packed(C), batch, dst, first=first, match="first")
+
+
+def _contexts(C, lens=(5, 7)):
+    from paper_2609_05821_gb300 import context
+    ctx = context.PackedContexts(len(lens), 40, 1, 4, 2, 64, device="cpu")
+    ctx.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    return ctx
+
+
+@pytest.mark.parametrize("rows,given", [([3, 2], 4), ([3], 3), ([3, 2, 1], 6), ([6, -1], 5), ([], 0)])
+def test_a_refused_append_leaves_the_lengths(C, rows, given):
+    ctx = _contexts(C)
+    kw = _append_kw(C, T=given)
+    _expect(C, C.ERR_INVALID_ARG, ctx.append, rows, kw["k"], kw["v"])
+    assert ctx.lens.tolist() == [5, 7]
+    _expect(C, C.ERR_INVALID_ARG, ctx.attend, rows, kw["q"])
+
+
+def test_a_refused_step_leaves_the_lengths(C):
+    ctx = _contexts(C)
+    step = ctx.decoder()
+    for bad in (dict(d=32), dict(T=3), dict(dtype=torch.float32)):
+        kw = _append_kw(C, **{"T": 2, **bad})
+        with pytest.raises(C.ConduitError):
+            step(kw["q"], kw["k"], kw["v"])
+        assert ctx.lens.tolist() == [5, 7]
