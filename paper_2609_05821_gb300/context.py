@@ -14,7 +14,10 @@ be scored and refreshed is taken up into a plain cache.
     ctx.take_up(batch, kv)                            # values into a cache that conduit_score reads
 
 The lengths live on the device (``ctx.lens``) and advance in place, so a captured
-step can be replayed while the contexts grow. Every buffer belongs to the object;
+step can be replayed while the contexts grow. A request whose new rows do not fit into
+max_len keeps its tokens and its length, none of the rows is written and ``check`` says so; what
+the same step's attention returns for such rows is not theirs. A context ends by setting
+its length (``ctx.lens[r] = 0``). Every buffer belongs to the object;
 its calls run on the caller's current stream.
 """
 
@@ -25,6 +28,9 @@ from typing import Optional, Sequence
 import torch
 
 from . import conduit as C
+
+
+_NO_SLOT = 2 ** 31 - 1  # a length whose rows all lie past any context: flagged, and not written
 
 
 class PackedContexts:
@@ -53,9 +59,10 @@ class PackedContexts:
         raises leaves the contexts as they were."""
         seqs = self._seqs(rows, self._grown)
         more = torch.tensor([int(n) for n in rows], dtype=torch.int32, device=self.lens.device)
-        torch.add(self.lens, more, out=self._grown)
+        fits = more <= self.max_len - self.lens
+        self._grown.copy_(torch.where(fits, self.lens + more, _NO_SLOT))
         q_rot = C.conduit_packed_append(self.kv, seqs, k, v, self.rope, pos, q, status=self.status)
-        self.lens.copy_(self._grown)
+        self.lens.copy_(torch.where(fits, self._grown, self.lens))
         return q_rot
 
     def attend(self, rows: Sequence[int], q, limits=None, lse=None):
@@ -75,7 +82,7 @@ class PackedContexts:
         def step(q, k, v, pos=None):
             torch.add(self.lens, 1, out=self._grown)
             C.conduit_packed_append(kv, grown, k, v, self.rope, pos, q, q_rot, status=self.status)
-            self.lens.copy_(self._grown)
+            torch.clamp(self._grown, max=self.max_len, out=self.lens)
             return C.conduit_packed_attn(kv, seqs, q_rot, out=out, workspace=workspace, status=self.status)
 
         return step
