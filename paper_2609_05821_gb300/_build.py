@@ -73,9 +73,10 @@ def build(verbose: bool = False, extra_flags=(), variant: str = "") -> str:
 
 def build_test_hooks(verbose: bool = False) -> str:
     """The test-only library libconduit_testhooks.so: bounded device waits give
-    up after 1 ms instead of 1 s, and conduit_test_withhold_v_tile(n) makes the
-    scoring kernel's V producer skip one tile (no copy, no arrive), so a test
-    can run the timeout path without a fault. Never loaded by the package."""
+    up after 1 ms instead of 1 s, conduit_test_withhold_v_tile(n) makes the
+    scoring kernel's V producer skip one tile (no copy, no arrive) and
+    conduit_test_withhold_packed_load(n) the attention over a 4-bit cache one
+    load, so a test can run the timeout path without a fault. Never loaded by the package."""
     return build(verbose, ("-DCONDUIT_TEST_HOOKS", "-DCONDUIT_WAIT_NS=1000000ull"), "testhooks")
 
 

@@ -347,6 +347,13 @@ void cut(int most, int step, int* chunk, int* chunks) {
 
 }  // namespace
 
+#ifdef CONDUIT_TEST_HOOKS
+// Test builds only (never in libconduit.so): the next attention launches over a 4-bit cache leave out
+// load n of each warp or CTA of the tensor-core kernels (n < 0: none), so that its bounded waits run out.
+int32_t g_test_withhold_load = -1;
+extern "C" void conduit_test_withhold_packed_load(int32_t n) { g_test_withhold_load = n; }
+#endif
+
 PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype) {
   PackedAttnPlan p{};
   const int most = int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
@@ -426,6 +433,9 @@ cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const Pack
   AttnArgs a{kv, s, q, out, lse, limits, scale, plan.chunk, plan.chunks, 0, plan.last_chunk, plan.last_chunks,
              plan.part_cols, nullptr, nullptr, status};
   a.col_blocks = int(blocks_of(kv, s, plan.kernel));
+#ifdef CONDUIT_TEST_HOOKS
+  a.withhold = g_test_withhold_load;
+#endif
   a.part_ml = static_cast<float2*>(scratch);
   a.part_o = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats_bytes(plan));
   return dtype == CONDUIT_BF16 ? launch_t<__nv_bfloat16>(a, plan, stream) : launch_t<float>(a, plan, stream);

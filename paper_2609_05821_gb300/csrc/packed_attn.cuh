@@ -38,6 +38,9 @@ struct AttnArgs {
   float2* part_ml;        // [chunks][part_cols] (M in log2 units, sum)
   float* part_o;          // [chunks][part_cols][d]
   int32_t* status;
+#ifdef CONDUIT_TEST_HOOKS
+  int32_t withhold;  // test builds: this load of each warp (warp-level kernel) or CTA (tcgen05) is not made (-1: none)
+#endif
 };
 
 // The join is launched while the chunks are still worked on; it waits for all of them.

@@ -341,6 +341,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   auto fill = [&](int n) {
     const int stage = n % kStages, kb = k0 + (w + n * kWarps) * kTile;
     const int tokens = min(k1 - kb, kTile);
+#ifdef CONDUIT_TEST_HOOKS
+    if (n == a.withhold) {  // neither copies nor an arrive: the wait for this tile runs out
+      next_page = page_in(n + 1);
+      return;
+    }
+#endif
     if (lane == 0)  // whole runs
       tc::mbar_arrive_expect_tx(&full[w][stage], uint32_t((tokens + kRun - 1) & -kRun) * (D + D / 4));
     __syncwarp();
@@ -411,7 +417,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) packed_attn_mma(AttnArgs a) {
   bool ok = true;
   for (int n = 0; n < mine; ++n) {
     const int stage = n % kStages, kb = k0 + (w + n * kWarps) * kTile;
-    ok = tc::mbar_wait(&full[w][stage], uint32_t(n / kStages) & 1u);
+    // lanes time their waits apart; the products and votes below need all of them or none
+    ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[w][stage], uint32_t(n / kStages) & 1u));
     if (!ok) break;
     const uint8_t* box = ring + stage * kBox;
     if (kb + kTile > least)

@@ -326,6 +326,9 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
                            (kb & ((1 << a.kv.page_shift) - 1)) * row_bytes;
       next = page_at(issued + 1);
       if (issued >= kRing && !(ok = wait_warp(&bars.raw_free[slot], (issued / kRing - 1) & 1, abort))) break;
+#ifdef CONDUIT_TEST_HOOKS
+      if (issued == a.withhold) continue;  // neither copies nor an arrive: the waits for this load run out
+#endif
       if (lane == 0)  // whole runs
         tc::mbar_arrive_expect_tx(&bars.raw_full[slot],
                                   uint32_t((tokens + (1 << run_shift) - 1) >> run_shift << run_shift) * (D + D / 4));
