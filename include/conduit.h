@@ -633,6 +633,7 @@ conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* f
  * that averages over the keys that count (2e-6 of it over 8192 of like weight). The
  * kernel and the cut into key chunks follow from the sizes, max_len and row_off,
  * the form of the keys from what the rows see, so equal calls give equal bits.
+ * UNSUPPORTED: max_len and a page-table row of more than 2^31 - 2^20 tokens.
  */
 conduit_status conduit_packed_attn_workspace_size(const conduit_packed_kv* kv, const conduit_seqs* seqs,
                                                   int32_t dtype, size_t* bytes);

@@ -4,6 +4,8 @@
 
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "internal.cuh"
 
 namespace conduit {
@@ -83,6 +85,12 @@ struct PackedAttnPlan {
   bool cluster;   // the chunks of a context join inside a cluster
   size_t scratch;
 };
+// Keys of the longest context that a call allows. A key's place is a 32-bit number, and so is the end of
+// the last chunk, which lies less than 2^20 past the last key.
+inline int packed_attn_reach(const PackedDev& kv, const SeqsDev& s) {
+  return int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
+}
+constexpr int kMaxReach = INT32_MAX - (1 << 20) + 1;
 PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype);
 cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const PackedAttnPlan& plan, int dtype,
                                const RowsDev& q, float scale, const int32_t* limits, const RowsDev& out,

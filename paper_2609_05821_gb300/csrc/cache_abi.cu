@@ -117,6 +117,12 @@ conduit_status make_packed(const conduit_packed_kv* kv, PackedDev* out) {
   return CONDUIT_OK;
 }
 
+conduit_status check_reach(const PackedDev& kv, const SeqsDev& s) {
+  if (packed_attn_reach(kv, s) > kMaxReach)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "contexts of more than %d tokens (min of max_len and a page-table row)", kMaxReach);
+  return CONDUIT_OK;
+}
+
 // The rows of an append: k, v and, both or neither, q and q_out.
 struct AppendRows {
   RowsDev k, v, q, q_out;
@@ -258,7 +264,9 @@ conduit_status conduit_packed_attn_workspace_size(const conduit_packed_kv* kv, c
   PackedDev kd;
   SeqsDev sd;
   if (!bytes) return fail(CONDUIT_ERR_INVALID_ARG, "bytes is NULL");
-  if ((st = make_packed(kv, &kd)) || (st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype))) return st;
+  if ((st = make_packed(kv, &kd)) || (st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype)) ||
+      (st = check_reach(kd, sd)))
+    return st;
   *bytes = align_up(packed_attn_plan(kd, sd, dtype).scratch);
   return CONDUIT_OK;
 }
@@ -271,7 +279,9 @@ conduit_status conduit_packed_attn(const conduit_packed_kv* kv, const conduit_se
   PackedDev kd;
   SeqsDev sd;
   RowsDev qd, od;
-  if ((st = make_packed(kv, &kd)) || (st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype))) return st;
+  if ((st = make_packed(kv, &kd)) || (st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype)) ||
+      (st = check_reach(kd, sd)))
+    return st;
   if (!(scale >= 0.f) || !std::isfinite(scale))
     return fail(CONDUIT_ERR_INVALID_ARG, "scale must be finite and >= 0 (0: 1/sqrt(head_dim))");
   if (sd.T == 0) return CONDUIT_OK;

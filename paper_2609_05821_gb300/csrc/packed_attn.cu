@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
       t = t0 + j / a.kv.G, h = g * a.kv.G + j % a.kv.G, chunk = a.last_chunk;
     }
     const int len = cached_len(a.s, a.kv.capacity(), r, nullptr, false);
-    n = on ? max(1, (len + chunk - 1) / chunk) : 0;
+    n = !on ? 0 : len > chunk ? (len - 1) / chunk + 1 : 1;
   }
   wait_for_chunks();
   float top = -INFINITY;
@@ -342,7 +342,7 @@ double pass_time(int64_t pairs, int64_t singles, double tp, double ts) {
 void cut(int most, int step, int* chunk, int* chunks) {
   *chunk = std::max(step, (most + *chunks - 1) / *chunks);
   *chunk = (*chunk + step - 1) / step * step;
-  *chunks = std::max(1, (most + *chunk - 1) / *chunk);
+  *chunks = most > *chunk ? (most - 1) / *chunk + 1 : 1;
 }
 
 }  // namespace
@@ -356,7 +356,7 @@ extern "C" void conduit_test_withhold_packed_load(int32_t n) { g_test_withhold_l
 
 PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype) {
   PackedAttnPlan p{};
-  const int most = int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
+  const int most = packed_attn_reach(kv, s);
   const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
   // Up to eight columns: the warp-level kernel, whose one block reads the cache once. Up to 64: the
   // kernel with less time by a model, blocks of eight columns at 3.5 us and 9 ns a key on 304 places

@@ -56,3 +56,19 @@ def test_a_refused_step_leaves_the_lengths(C):
         with pytest.raises(C.ConduitError):
             step(kw["q"], kw["k"], kw["v"])
         assert ctx.lens.tolist() == [5, 7]
+
+
+def test_attention_refuses_contexts_whose_chunks_pass_32_bits(C):
+    """A key's place is counted in 32 bits, whole chunks past the last key included."""
+    pages = 2 ** 21 - 1  # of 1024 tokens
+    pool = torch.zeros((1, 1, 1, C.packed_page_bytes(64, 1024)), dtype=torch.uint8)
+    kv = C.PackedKv(pool, 1, 64, 1024, torch.zeros((1, pages), dtype=torch.int32))
+    for dtype in (BF, torch.float32):
+        for max_len in (2 ** 31 - 1, 2 ** 31 - 2 ** 20 + 1):
+            seqs = _seqs(C, (0, 1), max_len)
+            _expect(C, C.ERR_UNSUPPORTED, C.conduit_packed_attn_workspace_size, kv, seqs, dtype, match="tokens")
+            _expect(C, C.ERR_UNSUPPORTED, C.conduit_packed_attn, kv, seqs, torch.zeros((1, 1, 1, 64), dtype=dtype),
+                    workspace=torch.zeros(8, dtype=torch.uint8), match="tokens")
+        assert C.conduit_packed_attn_workspace_size(kv, _seqs(C, (0, 1), 2 ** 31 - 2 ** 20), dtype) > 0
+        narrow = _packed(C)  # what the table holds counts, where that is less
+        assert C.conduit_packed_attn_workspace_size(narrow, _seqs(C, (0, 1), 2 ** 31 - 1), dtype) == 0

@@ -114,3 +114,24 @@ def test_rows_that_see_few_keys_have_exact_logits(C, d):
         tol = ((np.expm1(2 * e.T) + 2.0 ** -10 + (n + 16) * 2.0 ** -24) * big)[..., None] + 2.0 ** -8 * np.abs(wo)
         assert np.all(np.abs(got - wo) <= tol), r
         t += c
+
+
+def test_context_of_two_thousand_million_keys(C):
+    """The longest context: all keys alike, values 0 but for the last 3,000 pages, which are 1. The output is their
+    share. Sums of a lane count up to 2^17 equal weights one by one: at most 2^17 x 2^-24 off."""
+    d, ps, n, last = 64, 1024, 2 ** 31 - 2 ** 20, 3000
+    table = torch.zeros((1, n // ps), dtype=torch.int32)
+    table[0, -last:] = 1
+    kv = C.PackedKv.empty(1, 2, 1, 1, d, ps, table)
+    fill = C.PackedKv(kv.pool, 1, d, ps, torch.arange(2, dtype=torch.int32)[None])
+    k = torch.zeros((1, 2 * ps, 1, d), device="cuda")
+    v = torch.cat([torch.zeros_like(k[:, :ps]), torch.ones_like(k[:, ps:])], 1)
+    both = torch.tensor([2 * ps], dtype=torch.int32, device="cuda")
+    C.conduit_packed_append(fill, C.Seqs([0, 2 * ps], both, 2 * ps), k, v)
+    seqs = C.Seqs([0, 1], torch.tensor([n], dtype=torch.int32, device="cuda"), n)
+    lse, status = torch.zeros((1, 1, 1), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = C.conduit_packed_attn(kv, seqs, torch.ones((1, 1, 1, d), dtype=BF, device="cuda"), lse=lse, status=status)
+    assert C.conduit_read_status(status) == C.OK
+    share = last * ps / n
+    assert torch.all((out.double() - share).abs() <= (2 * 2.0 ** -7 + 2.0 ** -8) * share)
+    assert abs(float(lse[0, 0, 0]) - np.log(n)) <= 2.0 ** -7 + 2.0 ** -19
