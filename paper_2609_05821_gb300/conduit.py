@@ -668,6 +668,15 @@ def _table_holds(kv, num_requests: int):
                                             f"there are requests ({num_requests})")
 
 
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """A buffer of a call on `stream` (None: the current one). It is of that stream's memory: one of the current
+    stream could still be in use there when the call writes to it, or in use again before the call is done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _rows(t: torch.Tensor, name: str, layers: int, rows: int, heads: int, d: int, dtype=None):
     """Strided rows [L][T][H][d] (or [T][H][d] of one layer) as a conduit_rows reference."""
     shape, stride = t.shape, t.stride()
@@ -692,18 +701,18 @@ def conduit_rope(rope: Rope, x: torch.Tensor, pos: torch.Tensor, out=None, inver
     if len(shape) not in (3, 4):
         raise ConduitError(ERR_INVALID_ARG, "x must be [L, T, H, d] or [T, H, d]")
     L, (T, H, d) = (shape[0], shape[1:]) if len(shape) == 4 else (1, shape)
-    out = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    out = _new(shape, x.dtype, x.device, stream) if out is None else out
     _check(_lib.conduit_rope(rope.ref(), _addr(rope.positions(pos, T)), L, T, H, d, _dtype_code(x),
                              _rows(x, "x", L, T, H, d), _rows(out, "out", L, T, H, d, x.dtype), int(inverse),
                              _addr(status), _stream_ptr(stream)))
     return out
 
 
-def _append_args(kv, seqs: Seqs, k, v, rope, pos, q, q_out):
+def _append_args(kv, seqs: Seqs, k, v, rope, pos, q, q_out, stream):
     L, T, Hkv, d = kv.num_layers, seqs.num_rows, kv.num_kv_heads, kv.head_dim
     _table_holds(kv, seqs.num_requests)
     if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _new(q.shape, q.dtype, q.device, stream)
     rows = [_rows(k, "k", L, T, Hkv, d), _rows(v, "v", L, T, Hkv, d, k.dtype)]
     rows += [None if t is None else _rows(t, name, L, T, kv.num_q_heads, d, k.dtype)
              for t, name in ((q, "q"), (q_out, "q_out"))]
@@ -716,7 +725,7 @@ def conduit_kv_append(kv: KvCache, seqs: Seqs, k: torch.Tensor, v: torch.Tensor,
     [L, T, Hq, d] is turned in the same launch. Returns q_out (None without q)."""
     if k.dtype != kv.dtype:
         raise ConduitError(ERR_INVALID_ARG, f"k is {k.dtype}, the cache {kv.dtype}")
-    turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out)
+    turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out, stream)
     _check(_lib.conduit_kv_append(kv.ref(), seqs.ref(), *turn, *rows, _addr(status), _stream_ptr(stream)))
     return q_out
 
@@ -724,7 +733,7 @@ def conduit_kv_append(kv: KvCache, seqs: Seqs, k: torch.Tensor, v: torch.Tensor,
 def conduit_packed_append(kv: PackedKv, seqs: Seqs, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
                           pos=None, q=None, q_out=None, status=None, stream=None):
     """conduit_kv_append into a 4-bit cache. Returns q_out (None without q)."""
-    turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out)
+    turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out, stream)
     _check(_lib.conduit_packed_append(kv.ref(), seqs.ref(), *turn, _dtype_code(k), *rows, _addr(status),
                                       _stream_ptr(stream)))
     return q_out
@@ -760,9 +769,11 @@ def conduit_packed_attn(kv: PackedKv, seqs: Seqs, q: torch.Tensor, scale: Option
         raise ConduitError(ERR_INVALID_ARG, "limits must be contiguous int32 with one entry per row")
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() != L * Hq * T or not lse.is_contiguous()):
         raise ConduitError(ERR_INVALID_ARG, "lse must be contiguous fp32 [L, Hq, T]")
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else out
     rows = _rows(q, "q", L, T, Hq, d), _rows(out, "out", L, T, Hq, d, q.dtype)
-    ws = _workspace(lambda: conduit_packed_attn_workspace_size(kv, seqs, q.dtype), q.device, workspace)
+    ws = workspace
+    if ws is None:
+        ws = _new(max(conduit_packed_attn_workspace_size(kv, seqs, q.dtype), 1), torch.uint8, q.device, stream)
     _check(_lib.conduit_packed_attn(kv.ref(), seqs.ref(), _dtype_code(q), rows[0], scale or 0.0, _addr(limits),
                                     rows[1], _addr(lse), _addr(ws), ws.numel(), _addr(status), _stream_ptr(stream)))
     return out
