@@ -740,12 +740,15 @@ def conduit_packed_append(kv: PackedKv, seqs: Seqs, k: torch.Tensor, v: torch.Te
 
 
 def conduit_packed_read(kv: PackedKv, batch: Batch, dst: KvCache, first=None, status=None, stream=None):
-    """Tokens first[r] .. of every request of a 4-bit cache into dst, as the batch lays it out."""
+    """Tokens first[r] .. of every request of a 4-bit cache into dst, as the batch lays it out (a contiguous
+    dst has the batch's tokens)."""
     if first is not None and (first.dtype != torch.int32 or first.numel() != batch.num_requests or
                               not first.is_contiguous()):
         raise ConduitError(ERR_INVALID_ARG, "first must be contiguous int32 with one entry per request")
     _table_holds(kv, batch.num_requests)
     _table_holds(dst, batch.num_requests)
+    if not dst.struct.page_size and dst.k.shape[2] != _last(batch.tok_off):
+        raise ConduitError(ERR_INVALID_ARG, f"dst holds {dst.k.shape[2]} tokens, the batch has {batch.n_tot}")
     _check(_lib.conduit_packed_read(kv.ref(), _addr(first), dst.ref(), batch.ref(), _addr(status),
                                     _stream_ptr(stream)))
 

@@ -72,3 +72,11 @@ def test_attention_refuses_contexts_whose_chunks_pass_32_bits(C):
         assert C.conduit_packed_attn_workspace_size(kv, _seqs(C, (0, 1), 2 ** 31 - 2 ** 20), dtype) > 0
         narrow = _packed(C)  # what the table holds counts, where that is less
         assert C.conduit_packed_attn_workspace_size(narrow, _seqs(C, (0, 1), 2 ** 31 - 1), dtype) == 0
+
+
+@pytest.mark.parametrize("tokens", [8, 10])
+def test_read_refuses_a_destination_of_other_tokens(C, tokens):
+    """A contiguous cache of the batch's 9 tokens is written with their stride; any other size is not one."""
+    batch = C.Batch([0, 5, 9], [0, 5, 9], [0, 1, 2], [0, 1, 2], device="cpu")
+    dst = C.KvCache(torch.zeros((1, 2, tokens, 64), dtype=BF), torch.zeros((1, 2, tokens, 64), dtype=BF), 4)
+    _expect(C, C.ERR_INVALID_ARG, C.conduit_packed_read, _packed(C), batch, dst, match="tokens")
