@@ -212,6 +212,7 @@ class Batch:
         self.q_off_dev = self.q_off.to(dev)
         self.num_requests = self.tok_off.numel() - 1
         self.num_images = self.img_off.numel() - 1
+        self.num_tokens = int(self.tok_off[-1]) if self.tok_off.numel() else 0  # reading a tensor at each call costs 2 us
         self.struct = ConduitBatch(
             self.num_requests, self.num_images,
             self.tok_off.data_ptr(), self.img_off.data_ptr(),
@@ -255,6 +256,8 @@ class KvCache:
             P, max_pages = 0, 0
         self.num_layers, self.num_kv_heads, self.head_dim = L, Hkv, d
         self.num_q_heads = num_q_heads
+        # rows of the page table, or tokens of a contiguous cache
+        self.table_rows, self.num_tokens = (self.page_table.shape[0], None) if page_size else (None, k.shape[2])
         self.struct = ConduitKV(L, num_q_heads, Hkv, d, _dtype_code(k), page_size, P, max_pages,
                                 k.data_ptr(), v.data_ptr(),
                                 self.page_table.data_ptr() if page_size else None)
@@ -637,7 +640,7 @@ class PackedKv:
         self.pool = pool
         self.page_table = page_table.to(device=pool.device, dtype=torch.int32).contiguous()
         self.num_layers, self.num_kv_heads, self.num_q_heads = L, Hkv, num_q_heads
-        self.head_dim, self.page_size = head_dim, page_size
+        self.head_dim, self.page_size, self.table_rows = head_dim, page_size, self.page_table.shape[0]
         self.struct = ConduitPackedKV(L, num_q_heads, Hkv, head_dim, page_size, P, self.page_table.shape[1],
                                       pool.data_ptr(), self.page_table.data_ptr())
 
@@ -663,8 +666,8 @@ def _addr(t: Optional[torch.Tensor]):
 
 def _table_holds(kv, num_requests: int):
     """The kernels read row r of the page table for every request r of a call."""
-    if kv.struct.page_size and kv.page_table.shape[0] < num_requests:
-        raise ConduitError(ERR_INVALID_ARG, f"the page table has {kv.page_table.shape[0]} rows, fewer than "
+    if kv.table_rows is not None and kv.table_rows < num_requests:
+        raise ConduitError(ERR_INVALID_ARG, f"the page table has {kv.table_rows} rows, fewer than "
                                             f"there are requests ({num_requests})")
 
 
@@ -747,8 +750,8 @@ def conduit_packed_read(kv: PackedKv, batch: Batch, dst: KvCache, first=None, st
         raise ConduitError(ERR_INVALID_ARG, "first must be contiguous int32 with one entry per request")
     _table_holds(kv, batch.num_requests)
     _table_holds(dst, batch.num_requests)
-    if not dst.struct.page_size and dst.k.shape[2] != _last(batch.tok_off):
-        raise ConduitError(ERR_INVALID_ARG, f"dst holds {dst.k.shape[2]} tokens, the batch has {batch.n_tot}")
+    if dst.num_tokens is not None and dst.num_tokens != batch.num_tokens:
+        raise ConduitError(ERR_INVALID_ARG, f"dst holds {dst.num_tokens} tokens, the batch has {batch.num_tokens}")
     _check(_lib.conduit_packed_read(kv.ref(), _addr(first), dst.ref(), batch.ref(), _addr(status),
                                     _stream_ptr(stream)))
 
