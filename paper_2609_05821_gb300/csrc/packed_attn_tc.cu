@@ -25,7 +25,8 @@
 // shared memory), 1 200-1 500 of softmax, 1 000 for each 32 tokens of keys or values that a warp
 // unpacks; a CTA another 20 000 (item and limits 2 500, queries 8 000-11 500, rows out 7 000, the
 // next CTA's launch 2 000). Measured: 32-128 rows of 16 requests over 8 192 keys, two layers of
-// 28 x 4 heads of 128, 317 us (1.0 PFLOP/s); 96 dims 329, 64 dims 250.
+// 28 x 4 heads of 128, 325 us (0.98 PFLOP/s); 96 dims 339, 64 dims 250. Causal prompts, one layer: 8 192
+// tokens 552, four of 4 096 tokens 831.
 #include <type_traits>
 
 #include "packed_attn.cuh"
@@ -345,8 +346,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     // that their chunks fall into different banks of the swizzled tile; values: side by side.
     // Every warp sees every copy land and says so before its slot is used again, also where
     // another four warps unpack it: none can take a phase of a slot for the one two before it.
-    // Either form of the keys has a copy of this loop and of the MMAs' (one copy that asks at every
-    // tile: 361 us for 8 192 keys instead of 316).
+    // Either form of the keys has a copy of this loop (one copy that asks at every tile: 333 us for
+    // 8 192 keys instead of 325, 357 instead of 339 with 96 dims).
     auto unpack = [&](auto form) {
     constexpr bool kExact = decltype(form)::value;
     const int c = lane & 3, i8 = lane >> 2, run_shift = min(6, a.kv.page_shift);
@@ -417,9 +418,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     // ------------------------------------------------------------------ MMAs
     // the whole warp walks the schedule on values from one lane, so that the operands live in
     // uniform registers
-    auto products = [&](auto form) {
-    constexpr bool kExact = decltype(form)::value;
     const uint32_t leader = lane == 0;
+    const int one = __shfl_sync(0xffffffffu, exact ? 0 : 1, 0);  // 0: keys in two parts, in one buffer
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     const int all = __shfl_sync(0xffffffffu, tiles, 0);
     const bool halves = __shfl_sync(0xffffffffu, int(split), 0) != 0;
@@ -431,18 +431,20 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     // stream that reads it and freed by the last.
     bool ok = true;
     auto score = [&](int x, int tile) {
-      const int stage = kExact ? 0 : tile & 1;
+      const int stage = tile & one;
       if (halves || x == 0) {
-        if (!(ok = wait_warp(&bars.k_full[stage], (kExact ? tile : tile >> 1) & 1, abort))) return;
+        if (!(ok = wait_warp(&bars.k_full[stage], (tile >> one) & 1, abort))) return;
         tc::tc_fence_after();
       }
       const uint64_t dk = tc::desc_sw128(k_at + stage * Z::kTile);
       const uint64_t dx = dq + (halves ? 0 : (x * Z::kTile) >> 4);
-      // (both parts in one unrolled row: descriptors spill and the other copy slows down, 342 us)
+      // One short loop for both forms of the keys. Its code counts where blocks of both are at work at a time:
+      // with a copy for either, 8 192 keys took 317 us instead of 325, but causal prompts of 4 x 4 096 tokens
+      // 902 instead of 831 and 32-128 rows over 2 100 keys 233 instead of 203.
 #pragma unroll 1
-      for (int part = 0; part < (kExact ? 2 : 1); ++part) {  // the second: what the keys' first parts left out
+      for (int part = 0; part < 2 - one; ++part) {  // the second: what the keys' first parts left out
         const uint64_t dp = dk + (part ? Z::kTile >> 4 : 0);
-#pragma unroll
+#pragma unroll 4
         for (int kk = 0; kk < D / 16; ++kk) {
           const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
           tc::mma_bf16_if(leader, tm + x * kSCols, dx + off, dp + off, idesc_s, kk > 0 || part > 0);
@@ -481,11 +483,6 @@ __global__ void __launch_bounds__(kThreads, 1) packed_attn_tc(AttnArgs a) {
     tc::mma_commit_if(leader, &bars.drained);  // every MMA issued above is done once this arrives
     tc::mbar_wait(&bars.drained, 0);
     __syncwarp();
-    };
-    if (exact)
-      products(std::true_type{});
-    else
-      products(std::false_type{});
   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 168;" ::: "memory");
