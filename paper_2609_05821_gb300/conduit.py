@@ -564,7 +564,8 @@ def conduit_refresh_attn(kv: KvCache, batch: Batch, idx, idx_off, idx_off_dev, q
 
 def rope_table(theta: float, rot_dim: int, max_pos: int, device="cuda") -> torch.Tensor:
     """Cosines and sines of positions 0 .. max_pos - 1 for frequencies theta^(-2 p / rot_dim), fp32
-    [max_pos, rot_dim/2, 2]; the angles are formed in fp64."""
+    [max_pos, rot_dim/2, 2]; the angles are formed in fp64. One sequence of frequencies over all pairs,
+    whatever their axes: a model whose axes each begin at frequency 1 brings a table of its own."""
     half = rot_dim // 2
     freq = float(theta) ** (-torch.arange(half, dtype=torch.float64, device=device) / half)
     angle = torch.arange(max_pos, dtype=torch.float64, device=device)[:, None] * freq

@@ -5,7 +5,8 @@
 // c = clamp(rint((x - m)/s), -8, 7); a value stands for m + s c. Every operation is
 // a separately rounded fp32 one, so that a plain program finds the same codes.
 // Bound: the rows once, and d + d/4 bytes per token and KV head of the cache; the append
-// beside it by its issue slots (78 % busy: rotation, range, codes and their places). Measured, 28
+// beside it by its issue slots (78 % busy: rotation, range, codes and their places, and at 72 registers
+// a thread spills of 64 bytes in bf16 and 152 in fp32, read once each). Measured, 28
 // layers of 8 192 tokens, 4 heads of 128 in bf16: append 176 us (3.5 TB/s), read 119 us (5.2 TB/s).
 #include <algorithm>
 

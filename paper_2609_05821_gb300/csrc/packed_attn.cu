@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
       t = t0 + j / a.kv.G, h = g * a.kv.G + j % a.kv.G, chunk = a.last_chunk;
     }
     const int len = cached_len(a.s, a.kv.capacity(), r, nullptr, false);
-    n = !on ? 0 : len > chunk ? (len - 1) / chunk + 1 : 1;
+    n = on ? (len - 1) / chunk + 1 : 0;  // one chunk where there is no key
   }
   wait_for_chunks();
   float top = -INFINITY;
@@ -358,6 +358,7 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   PackedAttnPlan p{};
   const int most = packed_attn_reach(kv, s);
   const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
+  // (The models here and below have the times of 128 dims; 64 and 96 go by them too.)
   // Up to eight columns: the warp-level kernel, whose one block reads the cache once. Up to 64: the
   // kernel with less time by a model, blocks of eight columns at 3.5 us and 9 ns a key on 304 places
   // after 8 us, or tiles of 128 at 11 us and 1.35 us for 128 keys (2.5 in two parts) on 152 after 18
@@ -404,7 +405,8 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   } else {
     // An SM holds two CTAs. One request: one wave of equal chunks. More, on the CUDA cores: eight
     // CTAs for each place, so that contexts of unequal lengths fill it. On the tensor cores a CTA's
-    // start weighs more, so that only as long as chunks keep 2 048 keys, and one wave else (one row,
+    // start weighs more, so that only as long as chunks keep about 2 048 keys (the last one no fewer than
+    // 1 281), and one wave else (one row,
     // 4 KV heads, us with chunks of 256 keys and so: 64 requests of about 300 tokens 18.9 and 11.5,
     // of 1 000 34.7 and 22.1, of 4 000 63.9 and 52.8, of 16 000, where both are 3 000, 157; 16 requests
     // of 4 000 34.7 and 24.5, of 16 000 56.9 and 49.7; 5 requests of 4 000 15.9 and 13.1).

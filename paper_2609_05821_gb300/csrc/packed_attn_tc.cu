@@ -21,10 +21,10 @@
 // O_A, O_B at [256, 512).
 //
 // Bound: the chain S, softmax, P V, next S of each column tile, beside the other's. A key tile
-// of two column tiles takes 3 500 cycles: 2 960 of MMAs (95 each, held up by the operands in
+// of two column tiles takes 3 600 cycles: 2 960 of MMAs (95 each, held up by the operands in
 // shared memory), 1 200-1 500 of softmax, 1 000 for each 32 tokens of keys or values that a warp
-// unpacks; a CTA another 20 000 (item and limits 2 500, queries 8 000-11 500, rows out 7 000, the
-// next CTA's launch 2 000). Measured: 32-128 rows of 16 requests over 8 192 keys, two layers of
+// unpacks; with keys in two parts 6 700. A CTA another 20 000-28 000 (item and limits 2 600, queries
+// 8 000-13 000, first logits 1 400-2 000, rows out 6 000-11 000, the next CTA's launch 2 000). Measured: 32-128 rows of 16 requests over 8 192 keys, two layers of
 // 28 x 4 heads of 128, 325 us (0.98 PFLOP/s); 96 dims 339, 64 dims 250. Causal prompts, one layer: 8 192
 // tokens 552, four of 4 096 tokens 831.
 #include <type_traits>
