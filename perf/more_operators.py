@@ -27,7 +27,7 @@ own = False
 
 BLOCK = 16
 TOP = 448.0             # the largest e4m3 number
-E_LO, E_HI = -100, 119  # exponents of a scale
+E_LO, E_HI = -40, 119   # exponents of a scale
 
 BASE = {
     "kind": "attend", "dtype": "bf16", "layers": 1, "hq": 28, "hkv": 4, "d": 128, "page": 16, "requests": 1,
