@@ -643,6 +643,115 @@ conduit_status conduit_packed_attn(const conduit_packed_kv* kv, const conduit_se
                                    size_t workspace_bytes, int32_t* status, void* stream);
 
 /*
+ * A cache held in 8 bits, next to the one in 4: half of bf16's bytes, keys and values with four
+ * significant bits each. Blocks of 16 tokens of a layer and KV head share a scale, K and V apart:
+ *   top = the block's largest |x|,  e = least whole number with top <= 448 2^e, in [-40, 119]
+ *   code = e4m3(x 2^-e), half to even, +-448 for what lies beyond;  it stands for code 2^e
+ * An append into a block that earlier tokens have (`was`: its e before) takes
+ *   e = max(was, e of the call's tokens),  earlier codes become e4m3(code 2^(was - e))
+ * which is exact but for codes that fall below 2^-6. NaN and infinities are held as NaN, take no part in
+ * `top` and set NONFINITE.
+ * pool is [L][P][Hkv][page_size / 16 blocks][32 d + 16 bytes]; a block is
+ *   K codes [2][d/16][8 tokens][16 dims]  (token 8 a + t, dim 16 c + e at [a][c][t][e])
+ *   V codes [d][4][2][2]                  (dim i, token 8 b + 2 a + c at [i][a][b][c])
+ *   the scales 2^e of K and of V (fp32), then 8 bytes of nothing
+ * so that tensor-core operands of both come out of shared memory as they lie. Rows that no token
+ * has may hold anything; they reach no result.
+ */
+typedef struct conduit_fp8_kv {
+  int32_t num_layers;        /* L */
+  int32_t num_q_heads;       /* Hq, a multiple of Hkv */
+  int32_t num_kv_heads;      /* Hkv */
+  int32_t head_dim;          /* d, a multiple of 32 in [32, 256] */
+  int32_t page_size;         /* a power of two in [16, 1024] */
+  int32_t num_pages;         /* P */
+  int32_t max_pages_per_req; /* row length of page_table */
+  void* pool;                /* device, 16-byte aligned */
+  const int32_t* page_table; /* device [R][max_pages_per_req] */
+} conduit_fp8_kv;
+
+/* Bytes of one page of one layer and KV head; -1 for sizes that are not supported. */
+int64_t conduit_fp8_page_bytes(int32_t head_dim, int32_t page_size);
+
+/*
+ * conduit_kv_append into an 8-bit cache; arguments and errors are those of conduit_packed_append.
+ * Two requests of one call must not append to the same block of 16 tokens.
+ */
+conduit_status conduit_fp8_append(const conduit_fp8_kv* kv, const conduit_seqs* seqs,
+                                  const conduit_rotary* rope, const int32_t* pos, int32_t dtype,
+                                  const conduit_rows* k, const conduit_rows* v,
+                                  const conduit_rows* q, const conduit_rows* q_out,
+                                  int32_t* status, void* stream);
+
+/* conduit_packed_read from an 8-bit cache: the values, exact in fp32 and (but for its range) in bf16. */
+conduit_status conduit_fp8_read(const conduit_fp8_kv* kv, const int32_t* first,
+                                const conduit_kv* dst, const conduit_batch* batch,
+                                int32_t* status, void* stream);
+
+/*
+ * conduit_packed_attn over an 8-bit cache: the same rows, limits, results, workspace rules and errors. bf16
+ * rows with head_dim 64, 96 or 128 run on the tensor cores: keys, values and queries (but for a power of two)
+ * exact in fp16, weights times the scale of their value within 2^-11 of themselves or 2^-32 of the row's
+ * largest, fp32 sums; so lse carries fp32 rounding only. fp32 rows and other head sizes run on the CUDA cores in fp32.
+ */
+conduit_status conduit_fp8_attn_workspace_size(const conduit_fp8_kv* kv, const conduit_seqs* seqs,
+                                               int32_t dtype, size_t* bytes);
+conduit_status conduit_fp8_attn(const conduit_fp8_kv* kv, const conduit_seqs* seqs, int32_t dtype,
+                                const conduit_rows* q, float scale, const int32_t* limits,
+                                const conduit_rows* out, float* lse, void* workspace,
+                                size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
+ * Beam search. A group is `width` beams (rows g width .. g width + width - 1 of the call) of one request.
+ *
+ * The best continuations of each group over its beams and the vocabulary:
+ *   s(b, v) = sums[b] + logits[b][v] - ln sum_u exp(logits[b][u])
+ * the num_out largest, descending, equal ones in the order of (b, v). Sums in fp32, scores compared in fp64.
+ *  logits  device [G width][vocab] of dtype, rows row_stride elements apart (>= vocab), aligned to the element
+ *  sums    device fp32 [G width]: log-probabilities so far; -inf leaves a beam out
+ *  score   device fp32 [G][num_out]
+ *  parent  device int32 [G][num_out]: the row of the call that is continued (g width + beam)
+ *  token   device int32 [G][num_out]
+ * A logit of -inf is never chosen. Where a group has fewer candidates than num_out, the rest have score -inf,
+ * parent g width and token 0. A beam whose logits hold a NaN or +inf, or whose sum is one, is left
+ * out and sets CONDUIT_FLAG_NONFINITE.
+ * width and num_out in [1, 32], vocab >= 1. G = 0 is no work.
+ */
+conduit_status conduit_beam_select(const void* logits, int32_t dtype, int64_t row_stride,
+                                   int32_t num_groups, int32_t width, int32_t vocab, const float* sums,
+                                   int32_t num_out, float* score, int32_t* parent, int32_t* token,
+                                   int32_t* status, void* stream);
+
+/*
+ * Contexts follow the beams: beam b (request b of the cache) takes over the context of row parent[b] of
+ * its group. Whole pages are shared, the page that has been begun is copied:
+ *   n = len[parent[b]],  w = n / page_size (whole pages)
+ *   page_table[b][i] = page_table[parent[b]][i] for i < w,  home[b][i] for i >= w;  len[b] = n
+ *   the n - w page_size rows in use of page home[parent[b]][w] go to page home[b][w], all layers
+ * all beams of a group at once (parent may be any map within the group), in place.
+ *  parent      device int32 [G width], rows of the call (conduit_beam_select's)
+ *  home        device int32 [G width][max_pages_per_req]: pages of which each belongs to one beam and one
+ *              place. A beam appends to its own pages only; a page is never appended to once it is full,
+ *              so beams may go on sharing it
+ *  page_table  device int32 [G width][max_pages_per_req], the cache's own, written
+ *  len         device int32 [G width], written
+ * A beam that starts anew has the row home[b] in page_table and length 0; a prompt appended to one beam of
+ * a group reaches the others by parent = that beam. All beams that are continued must have one length per
+ * group, and the begun page of each must be its own. A group where that does not hold, or with a parent
+ * outside of the group, a length outside [0, capacity] or a begun page outside [0, num_pages), is left as it is
+ * and sets CONDUIT_FLAG_INDEX. width in [1, 32]. G = 0 is no work.
+ */
+conduit_status conduit_kv_reorder(const conduit_kv* kv, int32_t num_groups, int32_t width,
+                                  const int32_t* parent, const int32_t* home, int32_t* page_table,
+                                  int32_t* len, int32_t* status, void* stream);
+conduit_status conduit_packed_reorder(const conduit_packed_kv* kv, int32_t num_groups, int32_t width,
+                                      const int32_t* parent, const int32_t* home, int32_t* page_table,
+                                      int32_t* len, int32_t* status, void* stream);
+conduit_status conduit_fp8_reorder(const conduit_fp8_kv* kv, int32_t num_groups, int32_t width,
+                                   const int32_t* parent, const int32_t* home, int32_t* page_table,
+                                   int32_t* len, int32_t* status, void* stream);
+
+/*
  * Number of kernels this library has enqueued in this process (launched, or
  * recorded into a stream capture) since it was loaded. Diagnostic only.
  */

@@ -142,6 +142,15 @@ def _load():
         "conduit_packed_read": (st, [P, P, P, P, P, P]),
         "conduit_packed_attn_workspace_size": (st, [P, P, I32, ctypes.POINTER(SZ)]),
         "conduit_packed_attn": (st, [P, P, I32, P, ctypes.c_float, P, P, P, P, SZ, P, P]),
+        "conduit_fp8_page_bytes": (ctypes.c_int64, [I32, I32]),
+        "conduit_fp8_append": (st, [P, P, P, P, I32, P, P, P, P, P, P]),
+        "conduit_fp8_read": (st, [P, P, P, P, P, P]),
+        "conduit_fp8_attn_workspace_size": (st, [P, P, I32, ctypes.POINTER(SZ)]),
+        "conduit_fp8_attn": (st, [P, P, I32, P, ctypes.c_float, P, P, P, P, SZ, P, P]),
+        "conduit_beam_select": (st, [P, I32, ctypes.c_int64, I32, I32, I32, P, I32, P, P, P, P, P]),
+        "conduit_kv_reorder": (st, [P, I32, I32, P, P, P, P, P, P]),
+        "conduit_packed_reorder": (st, [P, I32, I32, P, P, P, P, P, P]),
+        "conduit_fp8_reorder": (st, [P, I32, I32, P, P, P, P, P, P]),
         "conduit_launch_count": (ctypes.c_int64, []),
         "conduit_clear_status": (st, [P, P]),
         "conduit_read_status": (st, [P, P, ctypes.POINTER(I32)]),
@@ -625,15 +634,24 @@ def packed_page_bytes(head_dim: int, page_size: int) -> int:
     return int(_lib.conduit_packed_page_bytes(int(head_dim), int(page_size)))
 
 
+def fp8_page_bytes(head_dim: int, page_size: int) -> int:
+    """Bytes of one page of one layer and KV head of an 8-bit cache (-1: sizes not supported)."""
+    return int(_lib.conduit_fp8_page_bytes(int(head_dim), int(page_size)))
+
+
 class PackedKv:
     """A paged cache held in 4 bits (conduit_packed_kv): pool uint8 [L][P][Hkv][page bytes]."""
+
+    bits = 4
+    page_bytes = staticmethod(packed_page_bytes)
+    _sizes = "head_dim must be a multiple of 32 in [32, 256], page_size a power of two in [8, 1024]"
 
     def __init__(self, pool: torch.Tensor, num_q_heads: int, head_dim: int, page_size: int,
                  page_table: torch.Tensor):
         if pool.dtype != torch.uint8 or pool.dim() != 4 or not pool.is_contiguous():
             raise ConduitError(ERR_INVALID_ARG, "pool must be contiguous uint8 [L, P, Hkv, page bytes]")
         L, P, Hkv, nbytes = pool.shape
-        want = packed_page_bytes(head_dim, page_size)
+        want = self.page_bytes(head_dim, page_size)
         if want >= 0 and nbytes != want:
             raise ConduitError(ERR_INVALID_ARG, f"a page of the pool has {nbytes} bytes, {want} needed")
         if page_table.dim() != 2:
@@ -649,15 +667,29 @@ class PackedKv:
     def empty(cls, num_layers: int, num_pages: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
               page_size: int, page_table: torch.Tensor, device="cuda"):
         """A cache with a pool of its own."""
-        nbytes = packed_page_bytes(head_dim, page_size)
+        nbytes = cls.page_bytes(head_dim, page_size)
         if nbytes < 0:
-            raise ConduitError(ERR_UNSUPPORTED, "head_dim must be a multiple of 32 in [32, 256], "
-                                                "page_size a power of two in [8, 1024]")
+            raise ConduitError(ERR_UNSUPPORTED, cls._sizes)
         pool = torch.empty((num_layers, num_pages, num_kv_heads, nbytes), dtype=torch.uint8, device=device)
         return cls(pool, num_q_heads, head_dim, page_size, page_table)
 
     def ref(self):
         return ctypes.byref(self.struct)
+
+
+class Fp8Kv(PackedKv):
+    """A paged cache held in 8 bits with a scale for each block of 16 tokens and head (conduit_fp8_kv, whose fields
+    are those of conduit_packed_kv): pool uint8 [L][P][Hkv][page bytes]."""
+
+    bits = 8
+    page_bytes = staticmethod(fp8_page_bytes)
+    _sizes = "head_dim must be a multiple of 32 in [32, 256], page_size a power of two in [16, 1024]"
+
+
+def _of(kv: PackedKv, bits: int):
+    """The C calls of the 4-bit and the 8-bit cache differ in the layout of a page alone."""
+    if getattr(kv, "bits", None) != bits:
+        raise ConduitError(ERR_INVALID_ARG, "kv must be a PackedKv" if bits == 4 else "kv must be an Fp8Kv")
 
 
 def _addr(t: Optional[torch.Tensor]):
@@ -734,18 +766,28 @@ def conduit_kv_append(kv: KvCache, seqs: Seqs, k: torch.Tensor, v: torch.Tensor,
     return q_out
 
 
-def conduit_packed_append(kv: PackedKv, seqs: Seqs, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
-                          pos=None, q=None, q_out=None, status=None, stream=None):
-    """conduit_kv_append into a 4-bit cache. Returns q_out (None without q)."""
+def _append(fn, kv: PackedKv, seqs: Seqs, k, v, rope, pos, q, q_out, status, stream):
     turn, rows, q_out = _append_args(kv, seqs, k, v, rope, pos, q, q_out, stream)
-    _check(_lib.conduit_packed_append(kv.ref(), seqs.ref(), *turn, _dtype_code(k), *rows, _addr(status),
-                                      _stream_ptr(stream)))
+    _check(fn(kv.ref(), seqs.ref(), *turn, _dtype_code(k), *rows, _addr(status), _stream_ptr(stream)))
     return q_out
 
 
-def conduit_packed_read(kv: PackedKv, batch: Batch, dst: KvCache, first=None, status=None, stream=None):
-    """Tokens first[r] .. of every request of a 4-bit cache into dst, as the batch lays it out (a contiguous
-    dst has the batch's tokens)."""
+def conduit_packed_append(kv: PackedKv, seqs: Seqs, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
+                          pos=None, q=None, q_out=None, status=None, stream=None):
+    """conduit_kv_append into a 4-bit cache. Returns q_out (None without q)."""
+    _of(kv, 4)
+    return _append(_lib.conduit_packed_append, kv, seqs, k, v, rope, pos, q, q_out, status, stream)
+
+
+def conduit_fp8_append(kv: Fp8Kv, seqs: Seqs, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
+                       pos=None, q=None, q_out=None, status=None, stream=None):
+    """conduit_kv_append into an 8-bit cache; a part filled block's earlier tokens take over its new scale. Returns
+    q_out (None without q)."""
+    _of(kv, 8)
+    return _append(_lib.conduit_fp8_append, kv, seqs, k, v, rope, pos, q, q_out, status, stream)
+
+
+def _read(fn, kv: PackedKv, batch: Batch, dst: KvCache, first, status, stream):
     if first is not None and (first.dtype != torch.int32 or first.numel() != batch.num_requests or
                               not first.is_contiguous()):
         raise ConduitError(ERR_INVALID_ARG, "first must be contiguous int32 with one entry per request")
@@ -753,23 +795,43 @@ def conduit_packed_read(kv: PackedKv, batch: Batch, dst: KvCache, first=None, st
     _table_holds(dst, batch.num_requests)
     if dst.num_tokens is not None and dst.num_tokens != batch.num_tokens:
         raise ConduitError(ERR_INVALID_ARG, f"dst holds {dst.num_tokens} tokens, the batch has {batch.num_tokens}")
-    _check(_lib.conduit_packed_read(kv.ref(), _addr(first), dst.ref(), batch.ref(), _addr(status),
-                                    _stream_ptr(stream)))
+    _check(fn(kv.ref(), _addr(first), dst.ref(), batch.ref(), _addr(status), _stream_ptr(stream)))
 
 
-def conduit_packed_attn_workspace_size(kv: PackedKv, seqs: Seqs, dtype: Optional[torch.dtype] = None) -> int:
-    """Workspace of conduit_packed_attn for rows of `dtype` (None: enough for either)."""
+def conduit_packed_read(kv: PackedKv, batch: Batch, dst: KvCache, first=None, status=None, stream=None):
+    """Tokens first[r] .. of every request of a 4-bit cache into dst, as the batch lays it out (a contiguous
+    dst has the batch's tokens)."""
+    _of(kv, 4)
+    _read(_lib.conduit_packed_read, kv, batch, dst, first, status, stream)
+
+
+def conduit_fp8_read(kv: Fp8Kv, batch: Batch, dst: KvCache, first=None, status=None, stream=None):
+    """conduit_packed_read from an 8-bit cache."""
+    _of(kv, 8)
+    _read(_lib.conduit_fp8_read, kv, batch, dst, first, status, stream)
+
+
+def _attn_workspace_size(fn, kv: PackedKv, seqs: Seqs, dtype: Optional[torch.dtype]) -> int:
     n, most = ctypes.c_size_t(0), 0
     for code in ((F32, BF16) if dtype is None else (F32,) if dtype == torch.float32 else (BF16,)):
-        _check(_lib.conduit_packed_attn_workspace_size(kv.ref(), seqs.ref(), code, ctypes.byref(n)))
+        _check(fn(kv.ref(), seqs.ref(), code, ctypes.byref(n)))
         most = max(most, int(n.value))
     return most
 
 
-def conduit_packed_attn(kv: PackedKv, seqs: Seqs, q: torch.Tensor, scale: Optional[float] = None, limits=None,
-                        out=None, lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
-    """Attention of rows q [L, T, Hq, d] over a 4-bit cache. limits int32 [T]: keys each row sees
-    (None: causal at the end of the context); lse fp32 [L, Hq, T] receives the log-sum-exp."""
+def conduit_packed_attn_workspace_size(kv: PackedKv, seqs: Seqs, dtype: Optional[torch.dtype] = None) -> int:
+    """Workspace of conduit_packed_attn for rows of `dtype` (None: enough for either)."""
+    _of(kv, 4)
+    return _attn_workspace_size(_lib.conduit_packed_attn_workspace_size, kv, seqs, dtype)
+
+
+def conduit_fp8_attn_workspace_size(kv: Fp8Kv, seqs: Seqs, dtype: Optional[torch.dtype] = None) -> int:
+    """Workspace of conduit_fp8_attn for rows of `dtype` (None: enough for either)."""
+    _of(kv, 8)
+    return _attn_workspace_size(_lib.conduit_fp8_attn_workspace_size, kv, seqs, dtype)
+
+
+def _attn(fn, size, kv: PackedKv, seqs: Seqs, q, scale, limits, out, lse, workspace, status, stream) -> torch.Tensor:
     L, T, Hq, d = kv.num_layers, seqs.num_rows, kv.num_q_heads, kv.head_dim
     _table_holds(kv, seqs.num_requests)
     if limits is not None and (limits.dtype != torch.int32 or limits.numel() != T or not limits.is_contiguous()):
@@ -780,10 +842,96 @@ def conduit_packed_attn(kv: PackedKv, seqs: Seqs, q: torch.Tensor, scale: Option
     rows = _rows(q, "q", L, T, Hq, d), _rows(out, "out", L, T, Hq, d, q.dtype)
     ws = workspace
     if ws is None:
-        ws = _new(max(conduit_packed_attn_workspace_size(kv, seqs, q.dtype), 1), torch.uint8, q.device, stream)
-    _check(_lib.conduit_packed_attn(kv.ref(), seqs.ref(), _dtype_code(q), rows[0], scale or 0.0, _addr(limits),
-                                    rows[1], _addr(lse), _addr(ws), ws.numel(), _addr(status), _stream_ptr(stream)))
+        ws = _new(max(_attn_workspace_size(size, kv, seqs, q.dtype), 1), torch.uint8, q.device, stream)
+    _check(fn(kv.ref(), seqs.ref(), _dtype_code(q), rows[0], scale or 0.0, _addr(limits), rows[1], _addr(lse), _addr(ws),
+              ws.numel(), _addr(status), _stream_ptr(stream)))
     return out
+
+
+def conduit_packed_attn(kv: PackedKv, seqs: Seqs, q: torch.Tensor, scale: Optional[float] = None, limits=None,
+                        out=None, lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
+    """Attention of rows q [L, T, Hq, d] over a 4-bit cache. limits int32 [T]: keys each row sees
+    (None: causal at the end of the context); lse fp32 [L, Hq, T] receives the log-sum-exp."""
+    _of(kv, 4)
+    return _attn(_lib.conduit_packed_attn, _lib.conduit_packed_attn_workspace_size, kv, seqs, q, scale, limits, out, lse,
+                 workspace, status, stream)
+
+
+def conduit_fp8_attn(kv: Fp8Kv, seqs: Seqs, q: torch.Tensor, scale: Optional[float] = None, limits=None, out=None,
+                     lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
+    """conduit_packed_attn over an 8-bit cache."""
+    _of(kv, 8)
+    return _attn(_lib.conduit_fp8_attn, _lib.conduit_fp8_attn_workspace_size, kv, seqs, q, scale, limits, out, lse,
+                 workspace, status, stream)
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ConduitError(ERR_INVALID_ARG, f"{name} is on {t.device}, not on {device}")
+
+
+def conduit_beam_select(logits: torch.Tensor, sums: torch.Tensor, width: int, num_out: Optional[int] = None, score=None,
+                        parent=None, token=None, status=None, stream=None):
+    """The num_out (None: width) best continuations of every group of `width` beams. logits [G width, vocab] (any row
+    stride, contiguous rows), sums fp32 [G width]. Returns (score fp32, parent int32, token int32), each
+    [G, num_out]; parent counts rows of the call."""
+    if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ConduitError(ERR_INVALID_ARG, "logits must be [G * width, vocab] with contiguous rows")
+    n, vocab = logits.shape
+    if width < 1 or n % width:
+        raise ConduitError(ERR_INVALID_ARG, f"{n} rows of logits are not groups of {width}")
+    if sums.dtype != torch.float32 or sums.numel() != n or not sums.is_contiguous():
+        raise ConduitError(ERR_INVALID_ARG, f"sums must be contiguous fp32 [{n}]")
+    groups, num_out = n // width, width if num_out is None else num_out
+    _same_device(logits.device, sums=sums, score=score, parent=parent, token=token, status=status)
+    got = []
+    for t, dtype, name in ((score, torch.float32, "score"), (parent, torch.int32, "parent"), (token, torch.int32, "token")):
+        if t is None:
+            t = _new((groups, max(num_out, 0)), dtype, logits.device, stream)
+        elif t.dtype != dtype or t.numel() != groups * num_out or not t.is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, f"{name} must be contiguous {dtype} [{groups}, {num_out}]")
+        got.append(t)
+    stride = logits.stride(0) if n > 1 else max(vocab, 1)
+    _check(_lib.conduit_beam_select(_addr(logits), _dtype_code(logits), stride, groups, int(width), vocab, _addr(sums),
+                                    int(num_out), *map(_addr, got), _addr(status), _stream_ptr(stream)))
+    return tuple(got)
+
+
+def _reorder(fn, kv, parent: torch.Tensor, width: int, home: torch.Tensor, lens: torch.Tensor, status, stream):
+    n = parent.numel()
+    if width < 1 or n % width:
+        raise ConduitError(ERR_INVALID_ARG, f"{n} parents are not groups of {width}")
+    if kv.page_table is None:
+        raise ConduitError(ERR_UNSUPPORTED, "reordering needs a paged cache")
+    _table_holds(kv, n)
+    _same_device(kv.page_table.device, parent=parent, home=home, lens=lens, status=status)
+    for t, count, name in ((parent, n, "parent"), (lens, n, "lens"), (home, n * kv.page_table.shape[1], "home")):
+        if t.dtype != torch.int32 or t.numel() != count or not t.is_contiguous():
+            raise ConduitError(ERR_INVALID_ARG, f"{name} must be contiguous int32 with {count} entries")
+    _check(fn(kv.ref(), n // width, int(width), _addr(parent), _addr(home), _addr(kv.page_table), _addr(lens),
+              _addr(status), _stream_ptr(stream)))
+
+
+def conduit_kv_reorder(kv: KvCache, parent: torch.Tensor, width: int, home: torch.Tensor, lens: torch.Tensor, status=None,
+                       stream=None):
+    """Beam b takes over the context of row parent[b] (int32 [G width], within b's group): kv.page_table and lens
+    (int32 [G width]) are rewritten in place, the begun page is copied into b's own of home (int32 [G width, max_pages])."""
+    _reorder(_lib.conduit_kv_reorder, kv, parent, width, home, lens, status, stream)
+
+
+def conduit_packed_reorder(kv: PackedKv, parent: torch.Tensor, width: int, home: torch.Tensor, lens: torch.Tensor,
+                           status=None, stream=None):
+    """conduit_kv_reorder of a 4-bit cache."""
+    _of(kv, 4)
+    _reorder(_lib.conduit_packed_reorder, kv, parent, width, home, lens, status, stream)
+
+
+def conduit_fp8_reorder(kv: Fp8Kv, parent: torch.Tensor, width: int, home: torch.Tensor, lens: torch.Tensor, status=None,
+                        stream=None):
+    """conduit_kv_reorder of an 8-bit cache."""
+    _of(kv, 8)
+    _reorder(_lib.conduit_fp8_reorder, kv, parent, width, home, lens, status, stream)
 
 
 def conduit_clear_status(status: torch.Tensor, stream=None):

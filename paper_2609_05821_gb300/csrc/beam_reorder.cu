@@ -1,0 +1,112 @@
+// Contexts follow the beams of a search: page tables are gathered and the page that has been begun is copied,
+// in place, in one launch, for caches of any width.
+//
+// A full page is never written again, so beams share it by its number. The page that parent p has begun is its own, home[p][w];
+// beam b gets the rows in use into home[b][w]. A thread owns the same 16 bytes of the begun pages of all beams of a
+// group (and the same column of their tables): it reads what all of them need before it writes, which is all
+// that an arbitrary map of beams asks for. What the copy reads beside that, lengths of parents and places of begun pages, the
+// same launch leaves as it is.
+// Bound: the rows in use, read and written once; small calls by the chain parent, length, page, rows.
+#include "beam.cuh"
+
+namespace conduit {
+namespace {
+
+constexpr unsigned kAll = 0xffffffffu;
+constexpr int kThreads = 256;
+
+// kMost: beams that a thread has in hand.
+template <int kMost>
+__global__ void __launch_bounds__(kThreads)
+    reorder_kernel(PagedPool pool, int width, const int32_t* parent, const int32_t* home, int32_t* table, int32_t* len,
+                   int32_t* status) {
+  const int64_t row0 = int64_t(blockIdx.y) * width;
+  const int lane = threadIdx.x % 32;
+  const bool beam = lane < width;
+  // lane b: beam b
+  const int64_t from64 = beam ? int64_t(parent[row0 + lane]) - row0 : 0;
+  bool fine = from64 >= 0 && from64 < width;
+  const int from = fine ? int(from64) : 0;
+  const int own_n = len[row0 + from], n = __shfl_sync(kAll, own_n, 0);
+  fine &= n >= 0 && int64_t(n) <= int64_t(pool.max_pages) * pool.page_size && own_n == n;
+  fine = __all_sync(kAll, !beam || fine);
+  const int whole = fine ? n / pool.page_size : 0, rest = fine ? n % pool.page_size : 0;
+  int to = 0;
+  if (rest) {
+    bool own = true;
+    if (beam) {
+      to = home[(row0 + lane) * pool.max_pages + whole];
+      own = to >= 0 && to < pool.num_pages && table[(row0 + from) * pool.max_pages + whole] == home[(row0 + from) * pool.max_pages + whole];
+    }
+    fine = __all_sync(kAll, own);
+  }
+  const int source = __shfl_sync(kAll, to, from);
+  if (!fine) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) flag_status(status, CONDUIT_FLAG_INDEX);
+    return;
+  }
+  if (blockIdx.x == 0) {
+    for (int i0 = 0; i0 < pool.max_pages; i0 += kThreads) {
+      const int i = i0 + threadIdx.x;
+      const bool on = i < pool.max_pages;
+      int32_t id[kMost];
+#pragma unroll
+      for (int b = 0; b < kMost; ++b) {
+        const int p = __shfl_sync(kAll, from, b);
+        if (b < width && on)
+          id[b] = i < whole ? table[(row0 + p) * pool.max_pages + i] : home[(row0 + b) * pool.max_pages + i];
+      }
+#pragma unroll
+      for (int b = 0; b < kMost; ++b)
+        if (b < width && on) table[(row0 + b) * pool.max_pages + i] = id[b];
+    }
+    if (threadIdx.x < width && len[row0 + threadIdx.x] != n) len[row0 + threadIdx.x] = n;
+    return;
+  }
+  if (!rest) return;
+  // 16 bytes of a part of the begun page
+  int per_head = 0;
+  for (int k = 0; k < pool.parts; ++k) per_head += pool.part[k].bytes / 16;
+  const int64_t lin = int64_t(blockIdx.x - 1) * kThreads + threadIdx.x;
+  const int64_t unit = lin / per_head;
+  int at = int(lin % per_head), k = 0;
+  while (k + 1 < pool.parts && at >= pool.part[k].bytes / 16) at -= pool.part[k++].bytes / 16;
+  const PagePart part = pool.part[k];
+  const int head = int(unit % pool.heads);
+  const int64_t l = unit / pool.heads;
+  const bool on = l < pool.L && at * 16 < (rest + part.tokens - 1) / part.tokens * part.unit;
+  char* base = part.base + l * part.layer_stride + head * part.head_stride + at * 16;
+  uint4 v[kMost];
+#pragma unroll
+  for (int b = 0; b < kMost; ++b) {
+    const int s = __shfl_sync(kAll, source, b), p = __shfl_sync(kAll, from, b);
+    if (b < width && p != b && on) v[b] = *reinterpret_cast<const uint4*>(base + s * part.page_stride);
+  }
+#pragma unroll
+  for (int b = 0; b < kMost; ++b) {
+    const int t = __shfl_sync(kAll, to, b), p = __shfl_sync(kAll, from, b);
+    if (b < width && p != b && on) *reinterpret_cast<uint4*>(base + t * part.page_stride) = v[b];
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_reorder(const PagedPool& pool, int groups, int width, const int32_t* parent, const int32_t* home,
+                           int32_t* page_table, int32_t* len, int32_t* status, cudaStream_t stream) {
+  int64_t per_head = 0;
+  for (int k = 0; k < pool.parts; ++k) per_head += pool.part[k].bytes / 16;
+  const int64_t threads = per_head * pool.heads * pool.L;
+  const dim3 grid(unsigned(1 + (threads + kThreads - 1) / kThreads), groups);
+  if (width <= 4)
+    reorder_kernel<4><<<grid, kThreads, 0, stream>>>(pool, width, parent, home, page_table, len, status);
+  else if (width <= 8)
+    reorder_kernel<8><<<grid, kThreads, 0, stream>>>(pool, width, parent, home, page_table, len, status);
+  else if (width <= 16)
+    reorder_kernel<16><<<grid, kThreads, 0, stream>>>(pool, width, parent, home, page_table, len, status);
+  else
+    reorder_kernel<32><<<grid, kThreads, 0, stream>>>(pool, width, parent, home, page_table, len, status);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+}  // namespace conduit

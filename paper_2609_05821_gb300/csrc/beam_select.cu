@@ -1,0 +1,337 @@
+// Beam search's selection: the best continuations of a group over its beams and the vocabulary.
+//
+// Mathematics: s(b, v) = sums_b + z_bv - lse_b. Inside a row the order is that of the logits, so one pass
+// over a row gives its running maximum and sum and its n largest logits; rows meet only at the end, with their lse,
+// in fp64 (a float's last bit would decide between beams).
+//
+// Shape: a cluster per group; its warps share the rows out in segments. A warp keeps the n best of
+// its segment sorted across its lanes as 64-bit keys (logit, then the lower index); a value above the worst of
+// them goes to a small buffer, and 32 of those are sorted and merged at a time, so that the threshold is
+// all a value costs beside its exponential. The lists and sums go to the first CTA's shared memory, which ranks what can
+// still be chosen. No scratch in memory, one launch.
+// Bound: the logits once.
+#include "beam.cuh"
+#include "tc_common.cuh"
+
+namespace conduit {
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kClusterMost = 8;
+constexpr int kListsMost = kWarps * kClusterMost;
+constexpr unsigned kAll = 0xffffffffu;
+
+struct SelectArgs {
+  const void* logits;
+  int64_t row_stride;
+  int width, vocab, n, segs;
+  const float* sums;
+  float* score;
+  int32_t *parent, *token;
+  int32_t* status;
+};
+
+struct Shared {
+  uint64_t buffer[kWarps][64];         // values on their way into a warp's list
+  uint64_t list[kListsMost][kMaxBeams];  // the first CTA's: every warp's list, sorted
+  float2 stats[kListsMost];            // (largest, sum of e^(z - largest))
+  double base[kMaxBeams];              // sums - lse, -inf: the row is left out
+  double cand[kListsMost * kMaxBeams];
+  uint64_t cand_at[kListsMost * kMaxBeams];  // (beam, token)
+  double head[kListsMost];
+  uint64_t head_at[kListsMost];
+  double least;
+  uint64_t least_at;
+  int count;
+};
+
+// A key that grows with x, and among equal ones with a lower index; 0 stands for none.
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t at) {
+  uint32_t u = __float_as_uint(x + 0.f);  // -0 as 0
+  u ^= (u >> 31) ? 0xFFFFFFFFu : 0x80000000u;
+  return uint64_t(u) << 32 | (~at);
+}
+__device__ __forceinline__ float value_of(uint64_t key) {
+  uint32_t u = uint32_t(key >> 32);
+  u ^= (u >> 31) ? 0x80000000u : 0xFFFFFFFFu;
+  return __uint_as_float(u);
+}
+__device__ __forceinline__ uint32_t index_of(uint64_t key) { return ~uint32_t(key); }
+
+__device__ __forceinline__ uint64_t compare_exchange(uint64_t k, int mask, bool larger) {
+  const uint64_t other = __shfl_xor_sync(kAll, k, mask);
+  return (k > other) == larger ? k : other;
+}
+
+// The 32 keys of a warp in descending order by lane.
+__device__ __forceinline__ uint64_t sort_down(uint64_t k, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+    for (int mask = size >> 1; mask > 0; mask >>= 1) {
+      const bool down = size == 32 || !(lane & size);
+      k = compare_exchange(k, mask, ((lane & mask) == 0) == down);
+    }
+  return k;
+}
+
+// The 32 largest of two descending lists.
+__device__ __forceinline__ uint64_t merge_down(uint64_t list, uint64_t k, int lane) {
+  const uint64_t back = __shfl_xor_sync(kAll, k, 31);
+  list = list > back ? list : back;
+#pragma unroll
+  for (int mask = 16; mask > 0; mask >>= 1) list = compare_exchange(list, mask, (lane & mask) == 0);
+  return list;
+}
+
+// What a warp knows of its segment.
+struct Best {
+  uint64_t list = 0;         // lane i: the i-th best
+  float threshold = -INFINITY;  // of the n-th best
+  int count = 0;             // of values in the buffer
+  float m = -INFINITY, s = 0.f;  // this lane's largest value and sum of e^(z - m)
+};
+
+__device__ __forceinline__ void flush(Best& b, uint64_t* buffer, int n, int lane) {
+  __syncwarp();
+  const uint64_t k = lane < b.count ? buffer[lane] : 0, rest = lane + 32 < b.count ? buffer[lane + 32] : 0;
+  __syncwarp();
+  if (lane + 32 < b.count) buffer[lane] = rest;
+  b.count = max(b.count - 32, 0);
+  b.list = merge_down(b.list, sort_down(k, lane), lane);
+  const uint64_t worst = __shfl_sync(kAll, b.list, n - 1);
+  b.threshold = worst ? value_of(worst) : -INFINITY;
+}
+
+// N values of each lane, at `at` on; -inf for what is none.
+template <int N>
+__device__ __forceinline__ void take(Best& b, const float (&x)[N], uint32_t at, uint64_t* buffer, int n, int lane) {
+  float top = x[0];
+#pragma unroll
+  for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
+  const float m = fmaxf(b.m, top), base = m == -INFINITY ? 0.f : m;
+  // the difference first: its rounding, and not that of z log2(e), is what the exponential sees
+  float add = 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) add += tc::ex2((x[e] - base) * kLog2e);
+  b.s = fmaf(b.s, tc::ex2((b.m - base) * kLog2e), add);
+  b.m = m;
+  // Values seen before have lower indexes, so one that equals the n-th best of them loses; among this call's own,
+  // which do not come in order, it may not.
+  const float old = b.threshold;
+  if (!__any_sync(kAll, top > old)) return;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const bool in = x[e] > old && x[e] >= b.threshold;
+    const uint32_t who = __ballot_sync(kAll, in);
+    if (!who) continue;
+    if (in) buffer[b.count + __popc(who & ((1u << lane) - 1u))] = key_of(x[e], at + e);
+    b.count += __popc(who);
+    if (b.count >= 32) flush(b, buffer, n, lane);
+  }
+}
+
+template <typename T>
+struct Vec {
+  static constexpr int N = 16 / sizeof(T);
+  uint4 w;
+};
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& w, bool on, float (&x)[16 / sizeof(T)]) {
+  const T* v = reinterpret_cast<const T*>(&w);
+#pragma unroll
+  for (int e = 0; e < int(16 / sizeof(T)); ++e) x[e] = on ? to_float(v[e]) : -INFINITY;
+}
+
+// Descending by score, then by (beam, token).
+__device__ __forceinline__ bool before(double s, uint64_t at, double t, uint64_t other) {
+  return s > t || (s == t && at < other);
+}
+
+__device__ __forceinline__ uint32_t in_first_cta(const void* p) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(0));
+  return at;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) {
+  constexpr int N = 16 / sizeof(T);
+  extern __shared__ __align__(16) uint8_t select_smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(select_smem);
+  uint32_t rank, ctas;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // the first CTA runs before it is written to
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int64_t g = blockIdx.x / ctas;
+  const int id = int(rank) * kWarps + warp, beam = id / a.segs, seg = id % a.segs;
+  uint64_t* buffer = sh.buffer[warp];
+  Best b;
+  if (beam < a.width) {
+    const T* row = static_cast<const T*>(a.logits) + (g * a.width + beam) * a.row_stride;
+    // 16-byte loads from the first boundary on; the first segment takes what lies before it, the last what lies behind
+    const int head = min(int((16 - (reinterpret_cast<uintptr_t>(row) & 15u)) % 16 / sizeof(T)), a.vocab);
+    const int vecs = (a.vocab - head) / N, tail = head + vecs * N;
+    const int v0 = int(int64_t(vecs) * seg / a.segs), v1 = int(int64_t(vecs) * (seg + 1) / a.segs);
+    const uint4* from = reinterpret_cast<const uint4*>(row + head);
+    if (seg == 0 && head > 0) {
+      const float x[1] = {lane < head ? to_float(row[lane]) : -INFINITY};
+      take<1>(b, x, uint32_t(lane), buffer, a.n, lane);
+    }
+    constexpr int kAhead = 4;
+    for (int v = v0; v < v1; v += 32 * kAhead) {
+      uint4 w[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int at = v + 32 * k + lane;
+        if (at < v1) w[k] = __ldcs(from + at);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int at = v + 32 * k + lane;
+        if (v + 32 * k >= v1) break;
+        float x[N];
+        unpack<T>(w[k], at < v1, x);
+        take<N>(b, x, uint32_t(head + at * N), buffer, a.n, lane);
+      }
+    }
+    if (seg == a.segs - 1 && tail < a.vocab) {
+      const float x[1] = {tail + lane < a.vocab ? to_float(row[tail + lane]) : -INFINITY};
+      take<1>(b, x, uint32_t(tail + lane), buffer, a.n, lane);
+    }
+    while (b.count > 0) flush(b, buffer, a.n, lane);
+    // the lanes' sums, in the order of a butterfly
+    float m = b.m;
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, s));
+    b.s *= tc::ex2((b.m - (m == -INFINITY ? 0.f : m)) * kLog2e);
+    b.m = m;
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) b.s += __shfl_xor_sync(kAll, b.s, s);
+  }
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  {
+    const uint32_t list = in_first_cta(&sh.list[id][lane]), stats = in_first_cta(&sh.stats[id]);
+    asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(list), "l"(b.list) : "memory");
+    if (lane == 0) asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(stats), "f"(b.m), "f"(b.s) : "memory");
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (rank != 0) return;
+
+  // ------------------------------------------------- one CTA: rows' sums, then the best of the lists
+  if (threadIdx.x == 0) {
+    sh.count = 0;
+    sh.least = -INFINITY;
+    sh.least_at = ~uint64_t(0);
+  }
+  for (int w = warp; w < a.width; w += kWarps) {
+    float m = -INFINITY;
+    for (int i = lane; i < a.segs; i += 32) m = fmaxf(m, sh.stats[w * a.segs + i].x);
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, s));
+    const float from = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+    for (int i = lane; i < a.segs; i += 32) {
+      const float2 y = sh.stats[w * a.segs + i];
+      sum += y.y * tc::ex2((y.x - from) * kLog2e);
+    }
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(kAll, sum, s);
+    if (lane == 0) {
+      const float before_row = a.sums[g * a.width + w];
+      const bool wild = !(sum < INFINITY) || !(before_row < INFINITY);
+      if (wild) flag_status(a.status, CONDUIT_FLAG_NONFINITE);
+      double base = -INFINITY;
+      if (!wild && sum > 0.f && before_row > -INFINITY) {
+        // ln sum = k ln 2 + ln(1 + f): a float's rounding on a number below 1 alone
+        const int k = int(__float_as_uint(sum) >> 23) - 127;
+        const float f = __uint_as_float((__float_as_uint(sum) & 0x7FFFFFu) | 0x3F800000u) - 1.f;
+        base = double(before_row) - (double(m) + (k * 0.69314718055994530942 + double(log1pf(f))));
+      }
+      sh.base[w] = base;
+    }
+  }
+  __syncthreads();
+  const int lists = a.width * a.segs;
+  auto entry = [&](int list, int i, double* score, uint64_t* at) {
+    const uint64_t key = sh.list[list][i];
+    const int w = list / a.segs;
+    *score = key ? sh.base[w] + double(value_of(key)) : -INFINITY;
+    *at = uint64_t(w) << 32 | index_of(key);
+    return *score > -INFINITY;
+  };
+  // The n-th best of the lists' first entries bounds what can be chosen.
+  if (int(threadIdx.x) < lists) entry(threadIdx.x, 0, &sh.head[threadIdx.x], &sh.head_at[threadIdx.x]);
+  __syncthreads();
+  if (int(threadIdx.x) < lists && lists >= a.n) {
+    const double own = sh.head[threadIdx.x];
+    const uint64_t own_at = sh.head_at[threadIdx.x];
+    int place = 0;
+    for (int i = 0; i < lists; ++i) place += before(sh.head[i], sh.head_at[i], own, own_at);
+    if (place == a.n - 1 && own > -INFINITY) {
+      sh.least = own;
+      sh.least_at = own_at;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < lists * a.n; i += kWarps * 32) {
+    double s;
+    uint64_t at;
+    if (entry(i % lists, i / lists, &s, &at) && !before(sh.least, sh.least_at, s, at)) {
+      const int to = atomicAdd(&sh.count, 1);
+      sh.cand[to] = s;
+      sh.cand_at[to] = at;
+    }
+  }
+  __syncthreads();
+  const int count = sh.count;
+  const int64_t out = g * a.n;
+  for (int i = threadIdx.x; i < count; i += kWarps * 32) {
+    const double own = sh.cand[i];
+    const uint64_t own_at = sh.cand_at[i];
+    int place = 0;
+    for (int j = 0; j < count; ++j) place += before(sh.cand[j], sh.cand_at[j], own, own_at);
+    if (place < a.n) {
+      a.score[out + place] = float(own);
+      a.parent[out + place] = int32_t(g * a.width + int64_t(own_at >> 32));
+      a.token[out + place] = int32_t(uint32_t(own_at));
+    }
+  }
+  for (int i = count + threadIdx.x; i < a.n; i += kWarps * 32) {
+    a.score[out + i] = -INFINITY;
+    a.parent[out + i] = int32_t(g * a.width);
+    a.token[out + i] = 0;
+  }
+}
+
+template <typename T>
+cudaError_t launch(SelectArgs a, int groups, cudaStream_t stream) {
+  cudaError_t err = cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Shared)));
+  if (err) return err;
+  cudaLaunchAttribute cluster{};
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = kClusterMost;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(groups) * kClusterMost);
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = sizeof(Shared);
+  cfg.stream = stream;
+  cfg.attrs = &cluster;
+  cfg.numAttrs = 1;
+  a.segs = kListsMost / a.width;
+  count_launches(1);
+  return cudaLaunchKernelEx(&cfg, beam_select_kernel<T>, a);
+}
+
+}  // namespace
+
+cudaError_t launch_beam_select(const void* logits, int dtype, int64_t row_stride, int groups, int width, int vocab,
+                               const float* sums, int num_out, float* score, int32_t* parent, int32_t* token,
+                               int32_t* status, cudaStream_t stream) {
+  const SelectArgs a{logits, row_stride, width, vocab, num_out, 0, sums, score, parent, token, status};
+  return dtype == CONDUIT_BF16 ? launch<__nv_bfloat16>(a, groups, stream) : launch<float>(a, groups, stream);
+}
+
+}  // namespace conduit

@@ -72,10 +72,11 @@ cudaError_t launch_packed_append(const PackedDev& kv, const SeqsDev& s, const Ro
 cudaError_t launch_packed_read(const PackedDev& kv, const int32_t* first, const KvDev& dst, const BatchDev& b,
                                int max_tokens, int32_t* status, cudaStream_t stream);
 
-// Attention over the 4-bit cache. A plan says how a call is cut; `scratch` bytes
+// Attention over the 4-bit or the 8-bit cache. A plan says how a call is cut; `scratch` bytes
 // of workspace hold the partial results of `chunks` key chunks.
 enum { kAttnSimt = 0, kAttnMma = 1, kAttnTc = 2 };
 struct PackedAttnPlan {
+  int bits;       // of the cache: 4 or 8
   int kernel;     // CUDA cores, warp-level tensor cores, tcgen05
   int chunk;      // keys per chunk
   int chunks;     // of the longest context
@@ -91,7 +92,7 @@ inline int packed_attn_reach(const PackedDev& kv, const SeqsDev& s) {
   return int(std::min<int64_t>(s.max_len, int64_t(kv.max_pages) << kv.page_shift));
 }
 constexpr int kMaxReach = INT32_MAX - (1 << 20) + 1;
-PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype);
+PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype, int bits);
 cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const PackedAttnPlan& plan, int dtype,
                                const RowsDev& q, float scale, const int32_t* limits, const RowsDev& out,
                                float* lse, void* scratch, int32_t* status, cudaStream_t stream);

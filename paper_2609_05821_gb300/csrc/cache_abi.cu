@@ -1,10 +1,12 @@
-// C ABI of the rotary positions, the growing paged cache and the 4-bit cache:
+// C ABI of the rotary positions, the growing paged cache, the 4-bit and the 8-bit cache, and of beam search:
 // host-side argument checks and launches. Every check runs before anything is
 // enqueued; nothing here allocates.
 #include <cmath>
 
 #include "abi_checks.cuh"
+#include "beam.cuh"
 #include "cache.cuh"
+#include "fp8.cuh"
 
 using namespace conduit;
 using namespace conduit::abi;
@@ -93,16 +95,14 @@ conduit_status check_threads(int64_t rows, int64_t per_row, int64_t L) {
   return CONDUIT_OK;
 }
 
-conduit_status make_packed(const conduit_packed_kv* kv, PackedDev* out) {
-  if (!kv) return fail(CONDUIT_ERR_INVALID_ARG, "kv is NULL");
+// The caches of 4 and of 8 bits differ in what a page holds: `bytes` (-1: sizes that are not supported).
+template <typename Kv>
+conduit_status make_pages(const Kv* kv, int64_t bytes, const char* sizes, PackedDev* out) {
   if (kv->num_layers < 1 || kv->num_q_heads < 1 || kv->num_kv_heads < 1)
     return fail(CONDUIT_ERR_INVALID_ARG, "layer and head counts must be >= 1");
   if (kv->num_q_heads % kv->num_kv_heads)
     return fail(CONDUIT_ERR_INVALID_ARG, "num_q_heads must be a multiple of num_kv_heads");
-  const int64_t bytes = conduit_packed_page_bytes(kv->head_dim, kv->page_size);
-  if (bytes < 0)
-    return fail(CONDUIT_ERR_UNSUPPORTED,
-                "head_dim must be a multiple of 32 in [32, 256], page_size a power of two in [8, 1024]");
+  if (bytes < 0) return fail(CONDUIT_ERR_UNSUPPORTED, "%s", sizes);
   if (kv->num_pages < 1 || kv->max_pages_per_req < 1 || !kv->page_table)
     return fail(CONDUIT_ERR_INVALID_ARG, "page_table, num_pages and max_pages_per_req are required");
   if (int64_t(kv->max_pages_per_req) * kv->page_size > INT32_MAX)
@@ -115,6 +115,18 @@ conduit_status make_packed(const conduit_packed_kv* kv, PackedDev* out) {
                    kv->num_kv_heads, kv->num_q_heads / kv->num_kv_heads, kv->head_dim, kv->num_pages,
                    kv->max_pages_per_req, shift, bytes};
   return CONDUIT_OK;
+}
+
+conduit_status make_packed(const conduit_packed_kv* kv, PackedDev* out) {
+  if (!kv) return fail(CONDUIT_ERR_INVALID_ARG, "kv is NULL");
+  return make_pages(kv, conduit_packed_page_bytes(kv->head_dim, kv->page_size),
+                    "head_dim must be a multiple of 32 in [32, 256], page_size a power of two in [8, 1024]", out);
+}
+
+conduit_status make_fp8(const conduit_fp8_kv* kv, PackedDev* out) {
+  if (!kv) return fail(CONDUIT_ERR_INVALID_ARG, "kv is NULL");
+  return make_pages(kv, conduit_fp8_page_bytes(kv->head_dim, kv->page_size),
+                    "head_dim must be a multiple of 32 in [32, 256], page_size a power of two in [16, 1024]", out);
 }
 
 conduit_status check_reach(const PackedDev& kv, const SeqsDev& s) {
@@ -141,6 +153,109 @@ conduit_status make_append_rows(const conduit_rows* k, const conduit_rows* v, co
       (st = check_written(q_out, "q_out", L, T, Hq, d)))
     return st;
   return CONDUIT_OK;
+}
+
+using Append = cudaError_t (*)(const PackedDev&, const SeqsDev&, const RopeDev&, int, const RowsDev&, const RowsDev&,
+                               const RowsDev&, const RowsDev&, int32_t*, cudaStream_t);
+conduit_status append_rows(const PackedDev& kd, const conduit_seqs* seqs, const conduit_rotary* rope, const int32_t* pos,
+                           int32_t dtype, const conduit_rows* k, const conduit_rows* v, const conduit_rows* q,
+                           const conduit_rows* q_out, int32_t* status, void* stream, Append launch, const char* name) {
+  conduit_status st;
+  SeqsDev sd;
+  RopeDev rd;
+  AppendRows rows;
+  if ((st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype)) || (st = make_rope(rope, pos, sd.T, kd.d, false, &rd)))
+    return st;
+  if (sd.T == 0) return CONDUIT_OK;
+  if ((st = make_append_rows(k, v, q, q_out, dtype, kd.L, sd.T, kd.Hq, kd.d, &rows)) ||
+      (st = check_threads(sd.max_rows, (kd.Hq + 2 * int64_t(kd.Hkv)) * kd.d, kd.L)))
+    return st;
+  cudaError_t err = launch(kd, sd, rd, dtype, rows.k, rows.v, rows.q, rows.q_out, status, static_cast<cudaStream_t>(stream));
+  if (err) return cuda_fail(err, name);
+  return CONDUIT_OK;
+}
+
+using Read = cudaError_t (*)(const PackedDev&, const int32_t*, const KvDev&, const BatchDev&, int, int32_t*, cudaStream_t);
+conduit_status read_back(const PackedDev& kd, const int32_t* first, const conduit_kv* dst, const conduit_batch* batch,
+                         int32_t* status, void* stream, Read launch, const char* name) {
+  conduit_status st;
+  if ((st = check_batch(batch)) || (st = check_kv(dst, batch))) return st;
+  if (dst->num_layers != kd.L || dst->num_kv_heads != kd.Hkv || dst->head_dim != kd.d)
+    return fail(CONDUIT_ERR_INVALID_ARG, "dst must have the packed cache's layers, KV heads and head_dim");
+  if (batch->num_requests > kMaxGrid) return fail(CONDUIT_ERR_UNSUPPORTED, "more than %d requests", kMaxGrid);
+  int most = 0;
+  for (int r = 0; r < batch->num_requests; ++r) most = std::max(most, batch->tok_off[r + 1] - batch->tok_off[r]);
+  if ((st = check_threads(most, int64_t(kd.Hkv) * kd.d, kd.L))) return st;
+  cudaError_t err = launch(kd, first, make_kv(dst, batch), make_batch(batch), most, status, static_cast<cudaStream_t>(stream));
+  if (err) return cuda_fail(err, name);
+  return CONDUIT_OK;
+}
+
+conduit_status attn_workspace(const PackedDev& kd, int bits, const conduit_seqs* seqs, int32_t dtype, size_t* bytes) {
+  conduit_status st;
+  SeqsDev sd;
+  if ((st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype)) || (st = check_reach(kd, sd))) return st;
+  *bytes = align_up(packed_attn_plan(kd, sd, dtype, bits).scratch);
+  return CONDUIT_OK;
+}
+
+conduit_status attend(const PackedDev& kd, int bits, const conduit_seqs* seqs, int32_t dtype, const conduit_rows* q,
+                      float scale, const int32_t* limits, const conduit_rows* out, float* lse, void* workspace,
+                      size_t workspace_bytes, int32_t* status, void* stream, const char* name) {
+  conduit_status st;
+  SeqsDev sd;
+  RowsDev qd, od;
+  if ((st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype)) || (st = check_reach(kd, sd))) return st;
+  if (!(scale >= 0.f) || !std::isfinite(scale))
+    return fail(CONDUIT_ERR_INVALID_ARG, "scale must be finite and >= 0 (0: 1/sqrt(head_dim))");
+  if (sd.T == 0) return CONDUIT_OK;
+  if ((st = make_rows(q, "q", dtype, &qd)) || (st = make_rows(out, "out", dtype, &od)) ||
+      (st = check_written(out, "out", kd.L, sd.T, kd.Hq, kd.d)))
+    return st;
+  if (reinterpret_cast<uintptr_t>(limits) % 4 || reinterpret_cast<uintptr_t>(lse) % 4)
+    return fail(CONDUIT_ERR_INVALID_ARG, "limits and lse must be 4-byte aligned");
+  const PackedAttnPlan plan = packed_attn_plan(kd, sd, dtype, bits);
+  if ((st = check_workspace(workspace, workspace_bytes, align_up(plan.scratch)))) return st;
+  if (plan.items > INT32_MAX) return fail(CONDUIT_ERR_UNSUPPORTED, "too many rows, heads and layers for one call");
+  if (scale == 0.f) scale = 1.f / std::sqrt(float(kd.d));
+  cudaError_t err = launch_packed_attn(kd, sd, plan, dtype, qd, scale, limits, od, lse, workspace, status,
+                                       static_cast<cudaStream_t>(stream));
+  if (err) return cuda_fail(err, name);
+  return CONDUIT_OK;
+}
+
+conduit_status check_beams(int32_t groups, int32_t width) {
+  if (groups < 0) return fail(CONDUIT_ERR_INVALID_ARG, "num_groups must be >= 0");
+  if (width < 1 || width > kMaxBeams) return fail(CONDUIT_ERR_INVALID_ARG, "width must be in [1, %d]", kMaxBeams);
+  return CONDUIT_OK;
+}
+
+conduit_status reorder(PagedPool* pool, int32_t groups, int32_t width, const int32_t* parent, const int32_t* home,
+                       int32_t* page_table, int32_t* len, int32_t* status, void* stream) {
+  if (conduit_status st = check_beams(groups, width)) return st;
+  if (groups == 0) return CONDUIT_OK;
+  if (groups > kMaxGrid) return fail(CONDUIT_ERR_UNSUPPORTED, "more than %d groups", kMaxGrid);
+  for (const void* p : {static_cast<const void*>(parent), static_cast<const void*>(home),
+                        static_cast<const void*>(page_table), static_cast<const void*>(len)})
+    if (!p || reinterpret_cast<uintptr_t>(p) % 4)
+      return fail(CONDUIT_ERR_INVALID_ARG, "parent, home, page_table and len are required, 4-byte aligned");
+  int64_t chunks = 0;
+  for (int k = 0; k < pool->parts; ++k) chunks += pool->part[k].bytes / 16;
+  if (chunks * pool->heads * pool->L > int64_t(1) << 38) return fail(CONDUIT_ERR_UNSUPPORTED, "a page holds too much");
+  cudaError_t err = launch_reorder(*pool, groups, width, parent, home, page_table, len, status, static_cast<cudaStream_t>(stream));
+  if (err) return cuda_fail(err, "reorder");
+  return CONDUIT_OK;
+}
+
+// The pages of a quantised cache: one record per layer, page and head, whose parts begin at `offset`.
+PagedPool pool_of(const PackedDev& kv) {
+  PagedPool p{};
+  p.L = kv.L, p.heads = kv.Hkv, p.page_size = 1 << kv.page_shift, p.num_pages = kv.P, p.max_pages = kv.max_pages;
+  return p;
+}
+void add_part(PagedPool* p, const PackedDev& kv, int64_t offset, int unit, int tokens) {
+  p->part[p->parts++] = PagePart{reinterpret_cast<char*>(kv.pool) + offset, kv.page_bytes * kv.Hkv * kv.P,
+                                 kv.page_bytes * kv.Hkv, kv.page_bytes, unit, tokens, p->page_size / tokens * unit};
 }
 
 }  // namespace
@@ -222,82 +337,142 @@ conduit_status conduit_packed_append(const conduit_packed_kv* kv, const conduit_
                                      const conduit_rows* k, const conduit_rows* v,
                                      const conduit_rows* q, const conduit_rows* q_out,
                                      int32_t* status, void* stream) {
-  conduit_status st;
   PackedDev kd;
-  SeqsDev sd;
-  RopeDev rd;
-  AppendRows rows;
-  if ((st = make_packed(kv, &kd)) || (st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype)) ||
-      (st = make_rope(rope, pos, sd.T, kd.d, false, &rd)))
-    return st;
-  if (sd.T == 0) return CONDUIT_OK;
-  if ((st = make_append_rows(k, v, q, q_out, dtype, kd.L, sd.T, kd.Hq, kd.d, &rows)) ||
-      (st = check_threads(sd.max_rows, (kd.Hq + 2 * int64_t(kd.Hkv)) * kd.d, kd.L)))
-    return st;
-  cudaError_t err = launch_packed_append(kd, sd, rd, dtype, rows.k, rows.v, rows.q, rows.q_out, status,
-                                         static_cast<cudaStream_t>(stream));
-  if (err) return cuda_fail(err, "packed_append");
-  return CONDUIT_OK;
+  if (conduit_status st = make_packed(kv, &kd)) return st;
+  return append_rows(kd, seqs, rope, pos, dtype, k, v, q, q_out, status, stream, launch_packed_append, "packed_append");
 }
 
 conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* first,
                                    const conduit_kv* dst, const conduit_batch* batch,
                                    int32_t* status, void* stream) {
-  conduit_status st;
   PackedDev kd;
-  if ((st = make_packed(kv, &kd)) || (st = check_batch(batch)) || (st = check_kv(dst, batch))) return st;
-  if (dst->num_layers != kd.L || dst->num_kv_heads != kd.Hkv || dst->head_dim != kd.d)
-    return fail(CONDUIT_ERR_INVALID_ARG, "dst must have the packed cache's layers, KV heads and head_dim");
-  if (batch->num_requests > kMaxGrid) return fail(CONDUIT_ERR_UNSUPPORTED, "more than %d requests", kMaxGrid);
-  int most = 0;
-  for (int r = 0; r < batch->num_requests; ++r) most = std::max(most, batch->tok_off[r + 1] - batch->tok_off[r]);
-  if ((st = check_threads(most, int64_t(kd.Hkv) * kd.d, kd.L))) return st;
-  cudaError_t err = launch_packed_read(kd, first, make_kv(dst, batch), make_batch(batch), most, status,
-                                       static_cast<cudaStream_t>(stream));
-  if (err) return cuda_fail(err, "packed_read");
-  return CONDUIT_OK;
+  if (conduit_status st = make_packed(kv, &kd)) return st;
+  return read_back(kd, first, dst, batch, status, stream, launch_packed_read, "packed_read");
 }
 
 conduit_status conduit_packed_attn_workspace_size(const conduit_packed_kv* kv, const conduit_seqs* seqs,
                                                   int32_t dtype, size_t* bytes) {
-  conduit_status st;
   PackedDev kd;
-  SeqsDev sd;
   if (!bytes) return fail(CONDUIT_ERR_INVALID_ARG, "bytes is NULL");
-  if ((st = make_packed(kv, &kd)) || (st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype)) ||
-      (st = check_reach(kd, sd)))
-    return st;
-  *bytes = align_up(packed_attn_plan(kd, sd, dtype).scratch);
-  return CONDUIT_OK;
+  if (conduit_status st = make_packed(kv, &kd)) return st;
+  return attn_workspace(kd, 4, seqs, dtype, bytes);
 }
 
 conduit_status conduit_packed_attn(const conduit_packed_kv* kv, const conduit_seqs* seqs, int32_t dtype,
                                    const conduit_rows* q, float scale, const int32_t* limits,
                                    const conduit_rows* out, float* lse, void* workspace,
                                    size_t workspace_bytes, int32_t* status, void* stream) {
-  conduit_status st;
   PackedDev kd;
-  SeqsDev sd;
-  RowsDev qd, od;
-  if ((st = make_packed(kv, &kd)) || (st = make_seqs(seqs, &sd)) || (st = check_dtype(dtype)) ||
-      (st = check_reach(kd, sd)))
-    return st;
-  if (!(scale >= 0.f) || !std::isfinite(scale))
-    return fail(CONDUIT_ERR_INVALID_ARG, "scale must be finite and >= 0 (0: 1/sqrt(head_dim))");
-  if (sd.T == 0) return CONDUIT_OK;
-  if ((st = make_rows(q, "q", dtype, &qd)) || (st = make_rows(out, "out", dtype, &od)) ||
-      (st = check_written(out, "out", kd.L, sd.T, kd.Hq, kd.d)))
-    return st;
-  if (reinterpret_cast<uintptr_t>(limits) % 4 || reinterpret_cast<uintptr_t>(lse) % 4)
-    return fail(CONDUIT_ERR_INVALID_ARG, "limits and lse must be 4-byte aligned");
-  const PackedAttnPlan plan = packed_attn_plan(kd, sd, dtype);
-  if ((st = check_workspace(workspace, workspace_bytes, align_up(plan.scratch)))) return st;
-  if (plan.items > INT32_MAX) return fail(CONDUIT_ERR_UNSUPPORTED, "too many rows, heads and layers for one call");
-  if (scale == 0.f) scale = 1.f / std::sqrt(float(kd.d));
-  cudaError_t err = launch_packed_attn(kd, sd, plan, dtype, qd, scale, limits, od, lse, workspace, status,
-                                       static_cast<cudaStream_t>(stream));
-  if (err) return cuda_fail(err, "packed_attn");
+  if (conduit_status st = make_packed(kv, &kd)) return st;
+  return attend(kd, 4, seqs, dtype, q, scale, limits, out, lse, workspace, workspace_bytes, status, stream,
+                "packed_attn");
+}
+
+int64_t conduit_fp8_page_bytes(int32_t head_dim, int32_t page_size) {
+  if (head_dim < 32 || head_dim > kMaxHeadDim || head_dim % 32) return -1;
+  if (page_size < 16 || page_size > 1024 || (page_size & (page_size - 1))) return -1;
+  return int64_t(page_size / kBlockTokens) * fp8_block_bytes(head_dim);
+}
+
+conduit_status conduit_fp8_append(const conduit_fp8_kv* kv, const conduit_seqs* seqs,
+                                     const conduit_rotary* rope, const int32_t* pos, int32_t dtype,
+                                     const conduit_rows* k, const conduit_rows* v,
+                                     const conduit_rows* q, const conduit_rows* q_out,
+                                     int32_t* status, void* stream) {
+  PackedDev kd;
+  if (conduit_status st = make_fp8(kv, &kd)) return st;
+  return append_rows(kd, seqs, rope, pos, dtype, k, v, q, q_out, status, stream, launch_fp8_append, "fp8_append");
+}
+
+conduit_status conduit_fp8_read(const conduit_fp8_kv* kv, const int32_t* first,
+                                   const conduit_kv* dst, const conduit_batch* batch,
+                                   int32_t* status, void* stream) {
+  PackedDev kd;
+  if (conduit_status st = make_fp8(kv, &kd)) return st;
+  return read_back(kd, first, dst, batch, status, stream, launch_fp8_read, "fp8_read");
+}
+
+conduit_status conduit_fp8_attn_workspace_size(const conduit_fp8_kv* kv, const conduit_seqs* seqs,
+                                                  int32_t dtype, size_t* bytes) {
+  PackedDev kd;
+  if (!bytes) return fail(CONDUIT_ERR_INVALID_ARG, "bytes is NULL");
+  if (conduit_status st = make_fp8(kv, &kd)) return st;
+  return attn_workspace(kd, 8, seqs, dtype, bytes);
+}
+
+conduit_status conduit_fp8_attn(const conduit_fp8_kv* kv, const conduit_seqs* seqs, int32_t dtype,
+                                   const conduit_rows* q, float scale, const int32_t* limits,
+                                   const conduit_rows* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, int32_t* status, void* stream) {
+  PackedDev kd;
+  if (conduit_status st = make_fp8(kv, &kd)) return st;
+  return attend(kd, 8, seqs, dtype, q, scale, limits, out, lse, workspace, workspace_bytes, status, stream,
+                "fp8_attn");
+}
+
+conduit_status conduit_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t num_groups,
+                                   int32_t width, int32_t vocab, const float* sums, int32_t num_out, float* score,
+                                   int32_t* parent, int32_t* token, int32_t* status, void* stream) {
+  conduit_status st;
+  if ((st = check_dtype(dtype)) || (st = check_beams(num_groups, width))) return st;
+  if (num_out < 1 || num_out > kMaxBeams) return fail(CONDUIT_ERR_INVALID_ARG, "num_out must be in [1, %d]", kMaxBeams);
+  if (vocab < 1) return fail(CONDUIT_ERR_INVALID_ARG, "vocab must be >= 1");
+  if (row_stride < vocab) return fail(CONDUIT_ERR_INVALID_ARG, "row_stride must be >= vocab");
+  if (num_groups == 0) return CONDUIT_OK;
+  if (int64_t(num_groups) * width > INT32_MAX || num_groups > 1 << 26)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "too many groups for one call");
+  if (!logits || reinterpret_cast<uintptr_t>(logits) % (dtype == CONDUIT_BF16 ? 2 : 4))
+    return fail(CONDUIT_ERR_INVALID_ARG, "logits is NULL or not aligned to its element");
+  for (const void* p : {static_cast<const void*>(sums), static_cast<const void*>(score),
+                        static_cast<const void*>(parent), static_cast<const void*>(token)})
+    if (!p || reinterpret_cast<uintptr_t>(p) % 4)
+      return fail(CONDUIT_ERR_INVALID_ARG, "sums, score, parent and token are required, 4-byte aligned");
+  cudaError_t err = launch_beam_select(logits, dtype, row_stride, num_groups, width, vocab, sums, num_out, score, parent,
+                                       token, status, static_cast<cudaStream_t>(stream));
+  if (err) return cuda_fail(err, "beam_select");
   return CONDUIT_OK;
+}
+
+conduit_status conduit_kv_reorder(const conduit_kv* kv, int32_t num_groups, int32_t width, const int32_t* parent,
+                                  const int32_t* home, int32_t* page_table, int32_t* len, int32_t* status, void* stream) {
+  conduit_batch none{};
+  if (conduit_status st = check_kv(kv, &none)) return st;
+  if (kv->page_size == 0) return fail(CONDUIT_ERR_UNSUPPORTED, "reordering needs a paged cache");
+  if (int64_t(kv->max_pages_per_req) * kv->page_size > INT32_MAX)
+    return fail(CONDUIT_ERR_UNSUPPORTED, "a page-table row holds more than 2^31 - 1 tokens");
+  const int64_t row = int64_t(kv->head_dim) * (kv->dtype == CONDUIT_BF16 ? 2 : 4), head = row * kv->page_size;
+  if (head > INT32_MAX) return fail(CONDUIT_ERR_UNSUPPORTED, "a page holds too much");
+  PagedPool p{};
+  p.L = kv->num_layers, p.heads = kv->num_kv_heads, p.page_size = kv->page_size, p.num_pages = kv->num_pages;
+  p.max_pages = kv->max_pages_per_req;
+  for (void* base : {kv->k, kv->v})
+    p.part[p.parts++] = PagePart{static_cast<char*>(base), head * p.heads * p.num_pages, head * p.heads, head, int32_t(row), 1,
+                                 int32_t(head)};
+  return reorder(&p, num_groups, width, parent, home, page_table, len, status, stream);
+}
+
+conduit_status conduit_packed_reorder(const conduit_packed_kv* kv, int32_t num_groups, int32_t width,
+                                      const int32_t* parent, const int32_t* home, int32_t* page_table, int32_t* len,
+                                      int32_t* status, void* stream) {
+  PackedDev kd;
+  if (conduit_status st = make_packed(kv, &kd)) return st;
+  PagedPool p = pool_of(kd);
+  // codes of K and V, then their parameters
+  const int64_t codes = int64_t(p.page_size) * (kd.d / 2), params = int64_t(p.page_size) * (kd.d / 8);
+  add_part(&p, kd, 0, kd.d / 2, 1);
+  add_part(&p, kd, codes, kd.d / 2, 1);
+  add_part(&p, kd, 2 * codes, kd.d / 8, 1);
+  add_part(&p, kd, 2 * codes + params, kd.d / 8, 1);
+  return reorder(&p, num_groups, width, parent, home, page_table, len, status, stream);
+}
+
+conduit_status conduit_fp8_reorder(const conduit_fp8_kv* kv, int32_t num_groups, int32_t width, const int32_t* parent,
+                                   const int32_t* home, int32_t* page_table, int32_t* len, int32_t* status, void* stream) {
+  PackedDev kd;
+  if (conduit_status st = make_fp8(kv, &kd)) return st;
+  PagedPool p = pool_of(kd);
+  add_part(&p, kd, 0, fp8_block_bytes(kd.d), kBlockTokens);
+  return reorder(&p, num_groups, width, parent, home, page_table, len, status, stream);
 }
 
 }  // extern "C"

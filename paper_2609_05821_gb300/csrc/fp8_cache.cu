@@ -1,0 +1,473 @@
+// The 8-bit cache: append with rotation and the scales of blocks, and the read back into a plain cache.
+//
+// Mathematics: a block of 16 tokens of a head shares e, the least with max |x| <= 448 2^e;
+// code = e4m3(x 2^-e), a value stands for code 2^e. Powers of two scale exactly, so a value is
+// rounded once, and the rotation's fp32 operations are rounded one by one: a plain program finds the same codes.
+//
+// Shape: a warp owns a block of one head (two heads of 64 dims, four of 32), keys first, then
+// values: both have to be seen whole before the first code. Lane 16 c + u has dims 8 u .. 8 u + 7
+// (and, past 128 dims, 8 (u + 16) ..) of the tokens of parity c, so a row is read in one piece by
+// 16 lanes; the codes of a value column meet in pairs of lanes that swap half of their dims.
+// Bound: the rows once and 2 d + 1 bytes a token and head of the cache.
+#include <algorithm>
+
+#include "fp8.cuh"
+#include "rotate.cuh"
+#include "tc_common.cuh"
+#include "turn8.cuh"
+
+namespace conduit {
+namespace {
+
+constexpr int kThreads = 128;
+
+// Lanes of a head's row, and heads that share a warp.
+__host__ __device__ constexpr int heads_per_warp(int d) { return d <= 32 ? 4 : d <= 64 ? 2 : 1; }
+
+// Where this lane stands: head of the warp's, chunk of 8 dims, parity of its tokens.
+struct Place {
+  int head, u, c;
+  bool on;
+};
+__device__ __forceinline__ Place place_in_warp(int d, int lane) {
+  const int per = 16 / heads_per_warp(d), in = lane & 15;
+  return Place{in / per, in % per, lane >> 4, in % per < d / 8};
+}
+// The largest over the lanes of a head.
+__device__ __forceinline__ float head_max(float x, int d) {
+  constexpr unsigned kAll = 0xffffffffu;
+  x = fmaxf(x, __shfl_xor_sync(kAll, x, 16));
+#pragma unroll
+  for (int s = 1; s < 16; s <<= 1) {
+    const float y = __shfl_xor_sync(kAll, x, s);
+    if (s < 16 / heads_per_warp(d)) x = fmaxf(x, y);
+  }
+  return x;
+}
+
+// Largest |x| of eight numbers; NaN and infinities become NaN and leave it alone. True if there was one.
+__device__ __forceinline__ bool top_of(float (&x)[8], float* top) {
+  float t = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) t = tc::fmax3(t, fabsf(x[e]), fabsf(x[e + 1]));
+  float2 zero = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int e = 0; e < 8; e += 2)  // NaN from NaN and infinities
+    zero = tc::ffma2(make_float2(x[e], x[e + 1]), make_float2(0.f, 0.f), zero);
+  const bool wild = !(zero.x + zero.y == 0.f);
+  if (wild) {
+    t = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (fabsf(x[e]) < INFINITY)
+        t = fmaxf(t, fabsf(x[e]));
+      else
+        x[e] = NAN;
+    }
+  }
+  *top = fmaxf(*top, t);
+  return wild;
+}
+
+// Word of four codes, rescaled by 2^n (n <= 0): exact products, one rounding.
+__device__ __forceinline__ uint32_t rescaled(uint32_t w, float by) {
+  const float2 a = floats_lo(w), b = floats_hi(w);
+  return fp8_pair(a.x * by, a.y * by) | fp8_pair(b.x * by, b.y * by) << 16;
+}
+
+// The tokens of a block that a call writes: bit t of `now`.
+// K: each lane has its chunk of eight tokens of parity c, x[i] of token 2 i + c.
+// Writes codes and scale of one head's keys. `was`: exponent of the earlier tokens' scale, or kLeastExp;
+// older: earlier tokens (bits).
+template <int NC>
+__device__ __forceinline__ void put_keys(uint8_t* block, const Place& p, int d, uint32_t now, uint32_t older, int e,
+                                         int was, const float (&x)[NC][8][8]) {
+  const float down = power_of_two(-e), by = power_of_two(max(was - e, -126));
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const int u = p.u + 16 * n;
+    if (!p.on || u >= d / 8) continue;
+    uint8_t* at = block + (u >> 1) * 128 + (u & 1) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = 2 * i + p.c;
+      uint2* to = reinterpret_cast<uint2*>(at + (t >> 3) * 8 * d + (t & 7) * 16);
+      if (now >> t & 1u) {
+        float y[8];
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+          const float2 z = tc::fmul2(make_float2(x[n][i][k], x[n][i][k + 1]), make_float2(down, down));
+          y[k] = z.x, y[k + 1] = z.y;
+        }
+        *to = make_uint2(fp8_pair(y[0], y[1]) | fp8_pair(y[2], y[3]) << 16, fp8_pair(y[4], y[5]) | fp8_pair(y[6], y[7]) << 16);
+      } else if (was < e && (older >> t & 1u)) {
+        const uint2 w = *to;
+        *to = make_uint2(rescaled(w.x, by), rescaled(w.y, by));
+      }
+    }
+  }
+}
+
+// The same of the values, whose rows are dims: byte 4 a + 2 b + c of a row is token 8 b + 2 a + c, so a
+// lane's codes of tokens 2 a + c and 2 a + 8 + c are the halfword (a, c) and its partner's the other.
+template <int NC>
+__device__ __forceinline__ void put_values(uint8_t* block, const Place& p, int d, uint32_t now, uint32_t older, int e,
+                                           int was, const float (&x)[NC][8][8]) {
+  constexpr unsigned kAll = 0xffffffffu;
+  const float down = power_of_two(-e), by = power_of_two(max(was - e, -126));
+  const bool whole = now == 0xFFFFu;
+  uint32_t mine[4], past[4];  // bytes of word a that the call writes, and that earlier tokens have
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    mine[a] = past[a] = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int t = 8 * (k >> 1) + 2 * a + (k & 1);
+      if (now >> t & 1u) mine[a] |= 0xFFu << (8 * k);
+      if (older >> t & 1u) past[a] |= 0xFFu << (8 * k);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const int u = p.u + 16 * n;
+    uint32_t w[8][2];  // dim k: halfwords a = 0, 1 and a = 2, 3
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      uint32_t h[4];
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float2 y = tc::fmul2(make_float2(x[n][a][k], x[n][a + 4][k]), make_float2(down, down));
+        h[a] = fp8_pair(y.x, y.y);
+      }
+      w[k][0] = h[0] | h[1] << 16;
+      w[k][1] = h[2] | h[3] << 16;
+    }
+    uint4* rows = reinterpret_cast<uint4*>(block + 16 * d + (8 * u + 4 * p.c) * 16);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // parity 0 keeps dims 0-3 and hands on 4-7, parity 1 the other way round
+      uint32_t own[2], got[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        own[j] = p.c ? w[k + 4][j] : w[k][j];
+        got[j] = __shfl_xor_sync(kAll, p.c ? w[k][j] : w[k + 4][j], 16);
+      }
+      const uint32_t even[2] = {p.c ? got[0] : own[0], p.c ? got[1] : own[1]};
+      const uint32_t odd[2] = {p.c ? own[0] : got[0], p.c ? own[1] : got[1]};
+      // even: tokens (2 a, 2 a + 8), odd: (2 a + 1, 2 a + 9)
+      uint4 y = make_uint4(__byte_perm(even[0], odd[0], 0x5140), __byte_perm(even[0], odd[0], 0x7362),
+                           __byte_perm(even[1], odd[1], 0x5140), __byte_perm(even[1], odd[1], 0x7362));
+      if (!p.on || u >= d / 8) continue;
+      if (!whole) {
+        uint4 old = rows[k];
+        if (was < e && older) {
+          auto mixed = [&](uint32_t o, int a) { return (rescaled(o, by) & past[a]) | (o & ~past[a]); };
+          old = make_uint4(mixed(old.x, 0), mixed(old.y, 1), mixed(old.z, 2), mixed(old.w, 3));
+        }
+        y = make_uint4((y.x & mine[0]) | (old.x & ~mine[0]), (y.y & mine[1]) | (old.y & ~mine[1]),
+                       (y.z & mine[2]) | (old.z & ~mine[2]), (y.w & mine[3]) | (old.w & ~mine[3]));
+      }
+      rows[k] = y;
+    }
+  }
+}
+
+// Units below kv_warps: a block of the call's tokens of a head (or the heads that share a warp), one layer. The warps after
+// them rotate queries, a unit of pairs per thread.
+template <typename T, int VEC, int kPairing, int NC>
+__global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 1)
+    fp8_append_kernel(PackedDev kv, SeqsDev s, RopeDev rope, int kv_grid, int blocks, bool wide, RowsDev k, RowsDev v,
+                      RowsDev q, RowsDev q_out, int32_t* status) {
+  const int r = blockIdx.y, l = blockIdx.z;
+  const int t0 = s.row_off[r], n = s.row_off[r + 1] - t0, len = s.len[r];
+  if (n == 0) return;
+  const int begin = len - n;  // slot of the call's first row
+  if (int(blockIdx.x) >= kv_grid) {
+    const uint32_t lin = (blockIdx.x - kv_grid) * uint32_t(kThreads) + threadIdx.x;
+    const uint32_t per = units_per_row<VEC>(rope, kv.d), rest = lin / per;
+    const int u = int(lin - rest * per), i = int(rest / uint32_t(kv.Hq)), h = int(rest - uint32_t(i) * kv.Hq);
+    if (i >= n) return;
+    const int64_t t = int64_t(t0) + i;
+    const int slot = begin + i;
+    bool ok = slot >= 0 && slot < s.max_len && slot < kv.capacity();
+    const int page = kv.page_table[int64_t(r) * kv.max_pages + (ok ? slot >> kv.page_shift : 0)];
+    ok &= page >= 0 && page < kv.P;
+    int pos[CONDUIT_MAX_AXES];
+    if (rope.rot) ok &= load_positions(rope, t, pos);
+    if (!ok) return;  // flagged beside the row's key
+    using C = Chunk<T, VEC>;
+    const Unit un = unit_of<VEC>(rope, kv.d, u);
+    const T* src = static_cast<const T*>(q.p) + l * q.ls + t * q.rs + h * q.hs;
+    T* dst = static_cast<T*>(q_out.p) + l * q_out.ls + t * q_out.rs + h * q_out.hs;
+    C a = *reinterpret_cast<const C*>(src + un.a), b;
+    if (un.b >= 0) b = *reinterpret_cast<const C*>(src + un.b);
+    if (un.turns) {
+      float2 cs[VEC];
+      load_turn<VEC>(rope, pos, u * VEC, cs);
+      turn_chunks<T, VEC>(rope, cs, a, b);
+    }
+    *reinterpret_cast<C*>(dst + un.a) = a;
+    if (un.b >= 0) *reinterpret_cast<C*>(dst + un.b) = b;
+    return;
+  }
+  const int lane = threadIdx.x % 32, hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
+  const uint32_t unit = blockIdx.x * uint32_t(kThreads / 32) + threadIdx.x / 32;
+  const int nth = int(unit / uint32_t(groups)), head0 = int(unit % uint32_t(groups)) * hp;  // heads side by side
+  // slots count from the block of the first row (rows before slot 0 lie in blocks of their own)
+  const int64_t first = (int64_t(begin) >> 4) * 16 + 16 * int64_t(nth);
+  if (nth >= blocks || first >= len) return;
+  const Place p = place_in_warp(kv.d, lane);
+  const int head = head0 + p.head;
+  const bool on = p.on && head < kv.Hkv;
+
+  // which of the block's tokens the call writes
+  const int most = min(s.max_len, kv.capacity());
+  bool in_range = first >= 0 && first < most;
+  int page = kv.page_table[int64_t(r) * kv.max_pages + (in_range ? int(first) >> kv.page_shift : 0)];
+  in_range &= page >= 0 && page < kv.P;
+  const int64_t own_slot = first + (lane & 15);  // lane t looks at token t
+  const bool called = own_slot >= begin && own_slot < len;
+  bool fine = called && in_range && own_slot < most;
+  if (fine && rope.rot) {
+    int pos[CONDUIT_MAX_AXES];
+    fine = load_positions(rope, int64_t(t0) + (own_slot - begin), pos);
+  }
+  const uint32_t asked = __ballot_sync(0xffffffffu, called) & 0xFFFFu, now = __ballot_sync(0xffffffffu, fine) & 0xFFFFu;
+  if (now != asked && lane == 0 && head0 == 0) flag_status(status, CONDUIT_FLAG_INDEX);
+  if (now == 0) return;
+  const int before = int(min(max(int64_t(begin) - first, int64_t(0)), int64_t(16)));
+  const uint32_t older = (1u << before) - 1u;
+
+  uint8_t* block = fp8_block(kv, l, on ? head : 0, page, int(first));
+  float* scales = reinterpret_cast<float*>(block + 32 * kv.d);
+  int was[2] = {kLeastExp, kLeastExp};
+  if (older) {
+    const float2 w = *reinterpret_cast<const float2*>(scales);
+    was[0] = exponent_of(w.x), was[1] = exponent_of(w.y);
+  }
+  const int64_t row0 = int64_t(t0) + (first - begin);  // row of the call of the block's token 0
+  const int64_t k0 = l * k.ls + (on ? head : 0) * k.hs, v0 = l * v.ls + (on ? head : 0) * v.hs;
+  auto row_of = [&](const RowsDev& x, int64_t base, int t) { return static_cast<const T*>(x.p) + base + (row0 + t) * x.rs; };
+
+  bool bad = false;
+  float x[NC][8][8];
+  // keys
+  {
+    Raw8<T> raw[NC][8];
+#pragma unroll
+    for (int m = 0; m < NC; ++m)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int t = 2 * i + p.c, u = p.u + 16 * m;
+        raw[m][i] = Raw8<T>{};
+        if ((now >> t & 1u) && on && u < kv.d / 8) raw[m][i] = load8(row_of(k, k0, t) + 8 * u, wide);
+      }
+    float top = 0.f;
+#pragma unroll
+    for (int m = 0; m < NC; ++m) {
+      const int i0 = 8 * (p.u + 16 * m);
+      const int far0 = i0 >= rope.rot ? i0 : i0 < rope.half ? i0 + rope.half : i0 - rope.half;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int t = 2 * i + p.c;
+        to_floats(raw[m][i], x[m][i]);
+        if (kPairing != kNoTurn && (now >> t & 1u) && on && i0 < kv.d) {
+          int pos[CONDUIT_MAX_AXES];
+          load_positions(rope, row0 + t, pos);
+          float2 cs[8];
+          load_turn8<kPairing>(rope, pos, i0, cs);
+          const T* row = row_of(k, k0, t);
+          Raw8<T> far{};
+          if (kPairing == kChunks) far = load8(row + far0, wide);
+          turn8<kPairing>(rope, row, i0, far, cs, x[m][i]);
+        }
+        bad |= top_of(x[m][i], &top);
+      }
+    }
+    const int e = max(exponent_for(head_max(top, kv.d)), was[0]);
+    put_keys<NC>(block, Place{p.head, p.u, p.c, on}, kv.d, now, older, e, was[0], x);
+    if (on && p.u == 0 && p.c == 0) scales[0] = power_of_two(e);
+  }
+  // values
+  {
+    float top = 0.f;
+#pragma unroll
+    for (int m = 0; m < NC; ++m)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int t = 2 * i + p.c, u = p.u + 16 * m;
+        Raw8<T> raw{};
+        if ((now >> t & 1u) && on && u < kv.d / 8) raw = load8(row_of(v, v0, t) + 8 * u, wide);
+        to_floats(raw, x[m][i]);
+      }
+#pragma unroll
+    for (int m = 0; m < NC; ++m)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) bad |= top_of(x[m][i], &top);
+    const int e = max(exponent_for(head_max(top, kv.d)), was[1]);
+    put_values<NC>(block, Place{p.head, p.u, p.c, on}, kv.d, now, older, e, was[1], x);
+    if (on && p.u == 0 && p.c == 0) scales[1] = power_of_two(e);
+  }
+  if (bad) flag_status(status, CONDUIT_FLAG_NONFINITE);
+}
+
+// Eight numbers as a row's elements.
+template <typename T>
+__device__ __forceinline__ void store8(T* to, const float (&x)[8]) {
+  constexpr int N = 16 / sizeof(T);
+#pragma unroll
+  for (int p = 0; p < 8 / N; ++p) {
+    Chunk<T, N> y;
+#pragma unroll
+    for (int e = 0; e < N; ++e) y.v[e] = from_float<T>(x[p * N + e]);
+    store_once<T, N>(to + p * N, y);
+  }
+}
+
+// A warp turns a block of one head (or of the heads that share a warp) into rows: the mapping of the append.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+    fp8_read_kernel(PackedDev kv, const int32_t* first, KvDev dst, BatchDev b, int32_t* status) {
+  constexpr unsigned kAll = 0xffffffffu;
+  const int r = blockIdx.y, l = blockIdx.z, lane = threadIdx.x % 32;
+  const int t0 = b.tok_off[r], n = b.tok_off[r + 1] - t0;
+  const int64_t from = first ? first[r] : 0;
+  const int hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
+  const uint32_t unit = blockIdx.x * uint32_t(kThreads / 32) + threadIdx.x / 32;
+  const int64_t slot = (from >> 4) * 16 + 16 * int64_t(unit / uint32_t(groups));
+  if (slot >= from + n) return;
+  const int head0 = int(unit % uint32_t(groups)) * hp;
+  const Place p = place_in_warp(kv.d, lane);
+  const int head = head0 + p.head;
+  const bool on = p.on && head < kv.Hkv;
+
+  bool in_range = slot >= 0 && slot < kv.capacity();
+  const int page = kv.page_table[int64_t(r) * kv.max_pages + (in_range ? int(slot) >> kv.page_shift : 0)];
+  in_range &= page >= 0 && page < kv.P;
+  const int64_t own = slot + (lane & 15) - from;  // lane t looks at token t
+  const bool called = own >= 0 && own < n;
+  bool fine = called && in_range;
+  if (fine && dst.page_size) {
+    const int to = dst.page_table[int64_t(r) * dst.max_pages + own / dst.page_size];
+    fine = to >= 0 && to < dst.num_pages;
+  }
+  const uint32_t asked = __ballot_sync(kAll, called) & 0xFFFFu, now = __ballot_sync(kAll, fine) & 0xFFFFu;
+  if (now != asked && lane == 0 && head0 == 0) flag_status(status, CONDUIT_FLAG_INDEX);
+  if (now == 0) return;
+  const uint8_t* block = fp8_block(kv, l, on ? head : 0, page, int(slot));
+  const float2 scale = *reinterpret_cast<const float2*>(block + 32 * kv.d);
+  auto row_at = [&](int t) { return dst.row(l, on ? head : 0, r, int64_t(t0) + slot + t - from, int(slot + t - from)); };
+  for (int u = p.u; u < (kv.d + 127) / 128 * 16; u += 16) {
+    const bool live = on && u < kv.d / 8;
+    uint2 kw[8];
+    uint4 vw[4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = 2 * i + p.c;
+      kw[i] = make_uint2(0, 0);
+      if (live) kw[i] = __ldcs(reinterpret_cast<const uint2*>(block + (t >> 3) * 8 * kv.d + (u >> 1) * 128 + (t & 7) * 16 + (u & 1) * 8));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      vw[j] = make_uint4(0, 0, 0, 0);
+      if (live) vw[j] = __ldcs(reinterpret_cast<const uint4*>(block + 16 * kv.d + (8 * u + 4 * p.c + j) * 16));
+    }
+    // dims of this lane's parity: halfword a of w[dim] holds tokens 2 a + c and 2 a + 8 + c
+    uint32_t w[8][2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t even[2] = {__byte_perm(vw[j].x, vw[j].y, 0x6420), __byte_perm(vw[j].z, vw[j].w, 0x6420)};
+      const uint32_t odd[2] = {__byte_perm(vw[j].x, vw[j].y, 0x7531), __byte_perm(vw[j].z, vw[j].w, 0x7531)};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t keep = p.c ? odd[h] : even[h];
+        const uint32_t got = __shfl_xor_sync(kAll, p.c ? even[h] : odd[h], 16);
+        w[j][h] = p.c ? got : keep;
+        w[j + 4][h] = p.c ? keep : got;
+      }
+    }
+    if (!live) continue;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = 2 * i + p.c;
+      if (!(now >> t & 1u)) continue;
+      const int64_t at = row_at(t) + 8 * u;
+      float x[8], y[8];
+      const float2 z[4] = {floats_lo(kw[i].x), floats_hi(kw[i].x), floats_lo(kw[i].y), floats_hi(kw[i].y)};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 a = tc::fmul2(z[e], make_float2(scale.x, scale.x));
+        x[2 * e] = a.x, x[2 * e + 1] = a.y;
+      }
+      store8(static_cast<T*>(dst.k) + at, x);
+      // token 2 i + c: halfword a = i % 4, its low byte for i < 4
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float2 pair = (i & 1) ? floats_hi(w[e][(i & 3) >> 1]) : floats_lo(w[e][(i & 3) >> 1]);
+        y[e] = (i < 4 ? pair.x : pair.y) * scale.y;
+      }
+      store8(static_cast<T*>(dst.v) + at, y);
+    }
+  }
+}
+
+template <typename T, int VEC, int kPairing>
+cudaError_t append_with(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, bool wide, const RowsDev& k,
+                        const RowsDev& v, const RowsDev& q, const RowsDev& q_out, int32_t* status,
+                        cudaStream_t stream) {
+  const int hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
+  const int blocks = (s.max_rows + 15) / 16 + 1;  // a call's rows begin anywhere in a block
+  constexpr int kWarps = kThreads / 32;
+  const int kv_grid = int((int64_t(blocks) * groups + kWarps - 1) / kWarps);
+  const int64_t q_threads = q.p ? int64_t(s.max_rows) * kv.Hq * units_per_row<VEC>(rope, kv.d) : 0;
+  const int q_grid = int((q_threads + kThreads - 1) / kThreads);
+  const dim3 grid(unsigned(kv_grid + q_grid), s.R, kv.L);
+  if (kv.d <= 128)
+    fp8_append_kernel<T, VEC, kPairing, 1><<<grid, kThreads, 0, stream>>>(kv, s, rope, kv_grid, blocks, wide, k, v, q, q_out, status);
+  else
+    fp8_append_kernel<T, VEC, kPairing, 2><<<grid, kThreads, 0, stream>>>(kv, s, rope, kv_grid, blocks, wide, k, v, q, q_out, status);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+template <typename T, int VEC>
+cudaError_t append(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, bool wide, const RowsDev& k,
+                   const RowsDev& v, const RowsDev& q, const RowsDev& q_out, int32_t* status, cudaStream_t stream) {
+  switch (pairing(rope)) {
+    case kNoTurn: return append_with<T, VEC, kNoTurn>(kv, s, rope, wide, k, v, q, q_out, status, stream);
+    case kChunks: return append_with<T, VEC, kChunks>(kv, s, rope, wide, k, v, q, q_out, status, stream);
+    case kNeighbours: return append_with<T, VEC, kNeighbours>(kv, s, rope, wide, k, v, q, q_out, status, stream);
+    default: return append_with<T, VEC, kAnywhere>(kv, s, rope, wide, k, v, q, q_out, status, stream);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_fp8_append(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, int dtype, const RowsDev& k,
+                              const RowsDev& v, const RowsDev& q, const RowsDev& q_out, int32_t* status,
+                              cudaStream_t stream) {
+  const int vec = dtype == CONDUIT_BF16 ? 8 : 4;
+  const bool wide = rows_aligned(k, vec) && rows_aligned(v, vec);
+  const bool wide_q = q.p && dims_in_chunks(rope, kv.d, vec) && rows_aligned(q, vec) && rows_aligned(q_out, vec);
+  if (dtype == CONDUIT_BF16)
+    return wide_q ? append<__nv_bfloat16, 8>(kv, s, rope, wide, k, v, q, q_out, status, stream)
+                  : append<__nv_bfloat16, 1>(kv, s, rope, wide, k, v, q, q_out, status, stream);
+  return wide_q ? append<float, 4>(kv, s, rope, wide, k, v, q, q_out, status, stream)
+                : append<float, 1>(kv, s, rope, wide, k, v, q, q_out, status, stream);
+}
+
+cudaError_t launch_fp8_read(const PackedDev& kv, const int32_t* first, const KvDev& dst, const BatchDev& b,
+                            int max_tokens, int32_t* status, cudaStream_t stream) {
+  const int hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
+  const int64_t units = (int64_t(max_tokens + 15) / 16 + 1) * groups;
+  constexpr int kWarps = kThreads / 32;
+  const dim3 grid(unsigned((units + kWarps - 1) / kWarps), b.R, kv.L);
+  if (dst.dtype == CONDUIT_BF16)
+    fp8_read_kernel<__nv_bfloat16><<<grid, kThreads, 0, stream>>>(kv, first, dst, b, status);
+  else
+    fp8_read_kernel<float><<<grid, kThreads, 0, stream>>>(kv, first, dst, b, status);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+}  // namespace conduit

@@ -1,4 +1,4 @@
-// Attention over the 4-bit cache: how a call is cut, the CUDA-core kernel (fp32
+// Attention over the 4-bit and the 8-bit cache: how a call is cut, the CUDA-core kernel (fp32
 // rows, head sizes without a tensor-core kernel), and the join of key chunks.
 //
 // Mathematics: x_j = scale <q, K_j>, out = sum_j e^(x_j - M) V_j / sum_j e^(x_j - M) in
@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "fp8.cuh"
 #include "packed_attn.cuh"
 
 namespace conduit {
@@ -23,7 +24,131 @@ namespace {
 constexpr int kSimtKeys = 32;
 constexpr int kSimtRow(int d) { return d + 4; }  // 16 bytes of eight keys in different banks
 
-template <typename T, int NG>
+// The next 32 keys of the 4-bit cache on their way: eight dims of K and of V of a key, NG such pieces a
+// thread. A key past the last stands for zeros.
+template <int NG>
+struct Coming4 {
+  static constexpr int D = NG * 32;
+  int id[NG];
+  uint32_t kw[NG], vw[NG], kp[NG], vp[NG];
+  __device__ __forceinline__ void look_up(const AttnArgs& a, const Item& it, int kb, int k1, int tid) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int j = kb + (tid + 128 * i) / (D / 8);
+      if (j < k1) id[i] = page_entry(a, it.r, j);
+    }
+  }
+  __device__ __forceinline__ void fetch(const AttnArgs& a, const Item& it, int kb, int k1, int tid) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int e = tid + 128 * i, j = kb + e / (D / 8), u = e % (D / 8), grp = u / 4, c = u % 4;
+      kw[i] = vw[i] = kp[i] = vp[i] = 0;
+      if (j < k1) {
+        const uint8_t* at = a.kv.page(it.l, it.g, page_in_pool(a, id[i]));
+        const int row = j & ((1 << a.kv.page_shift) - 1);
+        kw[i] = reinterpret_cast<const uint32_t*>(at + a.kv.codes(0, row))[c * NG + grp];
+        const uint16_t* vh = reinterpret_cast<const uint16_t*>(at + a.kv.codes(1, row));
+        vw[i] = vh[2 * c * NG + grp] | uint32_t(vh[(2 * c + 1) * NG + grp]) << 16;
+        kp[i] = reinterpret_cast<const uint32_t*>(at + a.kv.params(0, row))[grp];
+        vp[i] = reinterpret_cast<const uint32_t*>(at + a.kv.params(1, row))[grp];
+      }
+    }
+  }
+  __device__ __forceinline__ static void unpack(float* to, uint32_t codes, uint32_t param) {
+    const float2 sm = __half22float2(u2h(param));
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)  // 2^23 + u less 2^23 + 8, exactly
+      x[e] = fmaf(sm.x, __uint_as_float(((codes >> (4 * e)) & 15u) | 0x4B000000u) - 8388616.f, sm.y);
+    reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
+  __device__ __forceinline__ void put(float* ks, float* vs, int tid) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int e = tid + 128 * i, key = e / (D / 8), u = e % (D / 8);
+      unpack(ks + key * kSimtRow(D) + 8 * u, kw[i], kp[i]);
+      unpack(vs + key * D + 8 * u, vw[i], vp[i]);
+    }
+  }
+};
+
+// The same of the 8-bit cache, two blocks of 16 tokens: eight dims of K of a key, and a dim of V of a
+// block's tokens.
+template <int NG>
+struct Coming8 {
+  static constexpr int D = NG * 32, NV = (NG + 1) / 2;
+  int kid[NG], vid[NV], seen[NV];  // seen: tokens of the block before the last key
+  uint2 kw[NG];
+  uint4 vw[NV];
+  float kscale[NG], vscale[NV];
+  __device__ __forceinline__ void look_up(const AttnArgs& a, const Item& it, int kb, int k1, int tid) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int j = kb + (tid + 128 * i) / (D / 8);
+      if (j < k1) kid[i] = page_entry(a, it.r, j);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int b = (tid + 128 * i) / D, j = kb + kBlockTokens * b;
+      if (b < 2 && j < k1) vid[i] = page_entry(a, it.r, j);
+    }
+  }
+  __device__ __forceinline__ void fetch(const AttnArgs& a, const Item& it, int kb, int k1, int tid) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int e = tid + 128 * i, j = kb + e / (D / 8), u = e % (D / 8), t = j % kBlockTokens;
+      kw[i] = make_uint2(0, 0);
+      kscale[i] = 0.f;
+      if (j < k1) {
+        const uint8_t* at = fp8_block(a.kv, it.l, it.g, page_in_pool(a, kid[i]), j - t);
+        kw[i] = *reinterpret_cast<const uint2*>(at + (t >> 3) * 8 * D + (u >> 1) * 128 + (t & 7) * 16 + (u & 1) * 8);
+        kscale[i] = reinterpret_cast<const float*>(at + 32 * D)[0];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e = tid + 128 * i, b = e / D, dim = e % D, j = kb + kBlockTokens * b;
+      vw[i] = make_uint4(0, 0, 0, 0);
+      vscale[i] = 0.f;
+      seen[i] = k1 - j;
+      if (b < 2 && j < k1) {
+        const uint8_t* at = fp8_block(a.kv, it.l, it.g, page_in_pool(a, vid[i]), j);
+        vw[i] = *reinterpret_cast<const uint4*>(at + 16 * D + dim * 16);
+        vscale[i] = reinterpret_cast<const float*>(at + 32 * D)[1];
+      }
+    }
+  }
+  __device__ __forceinline__ void put(float* ks, float* vs, int tid) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int e = tid + 128 * i, key = e / (D / 8), u = e % (D / 8);
+      const float2 x[4] = {floats_lo(kw[i].x), floats_hi(kw[i].x), floats_lo(kw[i].y), floats_hi(kw[i].y)};
+      const float s = kscale[i];
+      float4* to = reinterpret_cast<float4*>(ks + key * kSimtRow(D) + 8 * u);
+      to[0] = make_float4(x[0].x * s, x[0].y * s, x[1].x * s, x[1].y * s);
+      to[1] = make_float4(x[2].x * s, x[2].y * s, x[3].x * s, x[3].y * s);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e = tid + 128 * i, b = e / D, dim = e % D;
+      if (b >= 2) continue;
+      const uint32_t w[4] = {vw[i].x, vw[i].y, vw[i].z, vw[i].w};
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const float2 near = floats_lo(w[n]), far = floats_hi(w[n]);  // tokens 2 n, 2 n + 1 and 8 on
+        const float y[4] = {near.x, near.y, far.x, far.y};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int t = 8 * (c >> 1) + 2 * n + (c & 1);
+          vs[(kBlockTokens * b + t) * D + dim] = t < seen[i] ? y[c] * vscale[i] : 0.f;
+        }
+      }
+    }
+  }
+};
+
+template <typename T, int NG, typename Coming>
 __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
   constexpr int D = NG * 32, KS = kSimtRow(D);
   extern __shared__ __align__(16) float simt_smem[];
@@ -41,42 +166,8 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
   for (int c = 0; c < 2; ++c) lim[c] = __shfl_sync(0xffffffffu, own_lim, 2 * w + c);
   const int k0 = it.chunk * a.chunk, k1 = min(k0 + a.chunk, most);
 
-  // Eight dims of K and of V of a key: NG such pieces a thread. A key past the last stands for zeros.
-  int id[NG];
-  uint32_t kw[NG], vw[NG], kp[NG], vp[NG];
-  auto look_up = [&](int kb) {
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      const int j = kb + (tid + 128 * i) / (D / 8);
-      if (j < k1) id[i] = page_entry(a, it.r, j);
-    }
-  };
-  auto fetch = [&](int kb) {
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      const int e = tid + 128 * i, j = kb + e / (D / 8), u = e % (D / 8), grp = u / 4, c = u % 4;
-      kw[i] = vw[i] = kp[i] = vp[i] = 0;
-      if (j < k1) {
-        const uint8_t* at = a.kv.page(it.l, it.g, page_in_pool(a, id[i]));
-        const int row = j & ((1 << a.kv.page_shift) - 1);
-        kw[i] = reinterpret_cast<const uint32_t*>(at + a.kv.codes(0, row))[c * NG + grp];
-        const uint16_t* vh = reinterpret_cast<const uint16_t*>(at + a.kv.codes(1, row));
-        vw[i] = vh[2 * c * NG + grp] | uint32_t(vh[(2 * c + 1) * NG + grp]) << 16;
-        kp[i] = reinterpret_cast<const uint32_t*>(at + a.kv.params(0, row))[grp];
-        vp[i] = reinterpret_cast<const uint32_t*>(at + a.kv.params(1, row))[grp];
-      }
-    }
-  };
-  auto unpack = [](float* to, uint32_t codes, uint32_t param) {
-    const float2 sm = __half22float2(u2h(param));
-    float x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e)  // 2^23 + u less 2^23 + 8, exactly
-      x[e] = fmaf(sm.x, __uint_as_float(((codes >> (4 * e)) & 15u) | 0x4B000000u) - 8388616.f, sm.y);
-    reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
-  };
-  look_up(k0);
+  Coming next;
+  next.look_up(a, it, k0, k1, tid);
   for (int e = tid; e < kCols * D; e += 128) {
     const int j = it.cb * kCols + e / D;
     float x = 0.f;
@@ -86,8 +177,8 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
     }
     qs[e] = x;
   }
-  fetch(k0);
-  look_up(k0 + kSimtKeys);
+  next.fetch(a, it, k0, k1, tid);
+  next.look_up(a, it, k0 + kSimtKeys, k1, tid);
 
   const float to_log2 = a.scale * kLog2e;
   float m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, o[2][NG];  // sum: of this lane's keys
@@ -97,14 +188,9 @@ __global__ void __launch_bounds__(128) packed_attn_simt(AttnArgs a) {
     for (int e = 0; e < NG; ++e) o[c][e] = 0.f;
   for (int kb = k0; kb < k1; kb += kSimtKeys) {
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      const int e = tid + 128 * i, key = e / (D / 8), u = e % (D / 8);
-      unpack(ks + key * KS + 8 * u, kw[i], kp[i]);
-      unpack(vs + key * D + 8 * u, vw[i], vp[i]);
-    }
-    fetch(kb + kSimtKeys);
-    look_up(kb + 2 * kSimtKeys);
+    next.put(ks, vs, tid);
+    next.fetch(a, it, kb + kSimtKeys, k1, tid);
+    next.look_up(a, it, kb + 2 * kSimtKeys, k1, tid);
     __syncthreads();
     float x[2] = {0.f, 0.f};
     const float4* k = reinterpret_cast<const float4*>(ks + lane * KS);
@@ -262,6 +348,16 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
     a.lse[(int64_t(l) * a.kv.Hq + h) * a.s.T + t] = sum == 0.f ? -INFINITY : kLn2 * (base + log2f(sum));
 }
 
+template <typename T, int NG, typename Coming>
+cudaError_t launch_simt(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
+  constexpr int kSmem = simt_smem_bytes(NG * 32);
+  cudaError_t err = cudaFuncSetAttribute(packed_attn_simt<T, NG, Coming>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (err) return err;
+  packed_attn_simt<T, NG, Coming><<<unsigned(plan.items), 128, kSmem, stream>>>(a);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
 template <typename T, int NG>
 cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
   cudaError_t err;
@@ -269,13 +365,10 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
     err = launch_packed_attn_tc(a, plan.items, stream);
   } else if (plan.kernel == kAttnMma) {
     err = launch_packed_attn_mma(a, plan.items, plan.cluster, stream);
+  } else if (plan.bits == 8) {
+    err = launch_simt<T, NG, Coming8<NG>>(a, plan, stream);
   } else {
-    constexpr int kSmem = simt_smem_bytes(NG * 32);
-    err = cudaFuncSetAttribute(packed_attn_simt<T, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (err) return err;
-    packed_attn_simt<T, NG><<<unsigned(plan.items), 128, kSmem, stream>>>(a);
-    count_launches(1);
-    err = cudaGetLastError();
+    err = launch_simt<T, NG, Coming4<NG>>(a, plan, stream);
   }
   const int chunks = std::max(a.chunks, a.last_chunks);
   if (err || chunks == 1 || plan.cluster) return err;
@@ -354,10 +447,11 @@ int32_t g_test_withhold_load = -1;
 extern "C" void conduit_test_withhold_packed_load(int32_t n) { g_test_withhold_load = n; }
 #endif
 
-PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype) {
+PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype, int bits) {
   PackedAttnPlan p{};
+  p.bits = bits;
   const int most = packed_attn_reach(kv, s);
-  const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
+  const bool mma = bits == 4 && dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
   // (The models here and below have the times of 128 dims; 64 and 96 go by them too.)
   // Up to eight columns: the warp-level kernel, whose one block reads the cache once. Up to 64: the
   // kernel with less time by a model, blocks of eight columns at 3.5 us and 9 ns a key on 304 places
