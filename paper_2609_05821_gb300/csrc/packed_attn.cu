@@ -364,7 +364,8 @@ cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_
   if (plan.kernel == kAttnTc) {
     err = launch_packed_attn_tc(a, plan.items, stream);
   } else if (plan.kernel == kAttnMma) {
-    err = launch_packed_attn_mma(a, plan.items, plan.cluster, stream);
+    err = plan.bits == 8 ? launch_fp8_attn_mma(a, plan.items, plan.cluster, stream)
+                         : launch_packed_attn_mma(a, plan.items, plan.cluster, stream);
   } else if (plan.bits == 8) {
     err = launch_simt<T, NG, Coming8<NG>>(a, plan, stream);
   } else {
@@ -451,7 +452,7 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   PackedAttnPlan p{};
   p.bits = bits;
   const int most = packed_attn_reach(kv, s);
-  const bool mma = bits == 4 && dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
+  const bool mma = dtype == CONDUIT_BF16 && (kv.d == 64 || kv.d == 96 || kv.d == 128);
   // (The models here and below have the times of 128 dims; 64 and 96 go by them too.)
   // Up to eight columns: the warp-level kernel, whose one block reads the cache once. Up to 64: the
   // kernel with less time by a model, blocks of eight columns at 3.5 us and 9 ns a key on 304 places
@@ -463,7 +464,7 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   const double units = double(kv.L) * s.R * kv.Hkv;
   const double warp_us = 8. + units * ((columns + kCols - 1) / kCols) * (3.5 + 0.009 * most) / 304.;
   const double tc_us = 18. + units * (11. + (most < kExactBelow ? 2.5 : 1.35) / 128. * most) / 152.;
-  const bool few = columns <= kCols || (columns <= 64 && warp_us < tc_us);
+  const bool few = bits == 8 || columns <= kCols || (columns <= 64 && warp_us < tc_us);
   p.kernel = !mma ? kAttnSimt : few ? kAttnMma : kAttnTc;
   const int step = p.kernel == kAttnSimt ? 64 : 256;  // least keys of a chunk
   const int64_t largest = std::max(1, (most + step - 1) / step);
