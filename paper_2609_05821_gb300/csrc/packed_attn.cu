@@ -362,7 +362,7 @@ template <typename T, int NG>
 cudaError_t launch_ng(const AttnArgs& a, const PackedAttnPlan& plan, cudaStream_t stream) {
   cudaError_t err;
   if (plan.kernel == kAttnTc) {
-    err = launch_packed_attn_tc(a, plan.items, stream);
+    err = plan.bits == 8 ? launch_fp8_attn_tc(a, plan.items, stream) : launch_packed_attn_tc(a, plan.items, stream);
   } else if (plan.kernel == kAttnMma) {
     err = plan.bits == 8 ? launch_fp8_attn_mma(a, plan.items, plan.cluster, stream)
                          : launch_packed_attn_mma(a, plan.items, plan.cluster, stream);
@@ -464,7 +464,7 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   const double units = double(kv.L) * s.R * kv.Hkv;
   const double warp_us = 8. + units * ((columns + kCols - 1) / kCols) * (3.5 + 0.009 * most) / 304.;
   const double tc_us = 18. + units * (11. + (most < kExactBelow ? 2.5 : 1.35) / 128. * most) / 152.;
-  const bool few = bits == 8 || columns <= kCols || (columns <= 64 && warp_us < tc_us);
+  const bool few = columns <= kCols || (columns <= 64 && warp_us < tc_us);
   p.kernel = !mma ? kAttnSimt : few ? kAttnMma : kAttnTc;
   const int step = p.kernel == kAttnSimt ? 64 : 256;  // least keys of a chunk
   const int64_t largest = std::max(1, (most + step - 1) / step);

@@ -211,7 +211,8 @@ __device__ __forceinline__ bool finite_pair(uint32_t p) {
 // `cluster`: the chunks of a context form a cluster, which joins them itself.
 cudaError_t launch_packed_attn_mma(const AttnArgs& a, int64_t items, bool cluster, cudaStream_t stream);
 cudaError_t launch_packed_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream);
-// The same over the 8-bit cache (fp8_attn_mma.cu).
+// The same over the 8-bit cache (fp8_attn_mma.cu, fp8_attn_tc.cu).
 cudaError_t launch_fp8_attn_mma(const AttnArgs& a, int64_t items, bool cluster, cudaStream_t stream);
+cudaError_t launch_fp8_attn_tc(const AttnArgs& a, int64_t items, cudaStream_t stream);
 
 }  // namespace conduit
