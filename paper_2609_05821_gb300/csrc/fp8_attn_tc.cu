@@ -31,7 +31,7 @@ constexpr uint32_t kBlock = 128 * 128;        // 128 rows of 64 fp16, swizzled
 constexpr uint32_t kSCols = 128, kPCol = 64, kOCol = 256;
 constexpr int kLoadKeys = 2 * kBlockTokens;   // keys of a load
 constexpr int kLoads = kKeys / kLoadKeys;     // loads of a key tile
-constexpr int kRing = 3;                      // loads under way
+constexpr int kRing = 4;                      // loads under way
 constexpr int kBlocks = kKeys / kBlockTokens; // blocks of a key tile
 
 template <int NG>
@@ -181,7 +181,6 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
   __shared__ uint32_t tmem_slot;
   __shared__ int seen_most, seen_least, poison[D], poison_any, abort_flag;
   __shared__ Scales scales[4][kBlocks];  // of four key tiles
-  __shared__ float2 of_b[kTileCols];  // split: B's (reference, sum)
   let_join_start();
   // Blocks with two column tiles come first and those with one, which take half of the time, last.
   Item it;
@@ -192,6 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
   const bool partial = (split ? a.last_chunks : a.chunks) > 1;
   uint8_t* base = dynamic + (1024 - (tc::smem_u32(dynamic) & 1023u)) % 1024;
   uint8_t *qt = base, *kt = qt + 2 * Z::kTile, *vt = kt + 2 * Z::kTile, *raw = vt + 2 * Z::kValues;
+  float2* of_b = reinterpret_cast<float2*>(qt + Z::kTile);  // split: B's (reference, sum), where there is no second query tile
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
   volatile int* abort = &abort_flag;
 
@@ -282,14 +282,39 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
       bool ok = wait_warp(&bars.raw_full[slot], (load / kRing) & 1, abort);
       const bool mine = unit < 2 * load + 2;
       const int kb = k0 + load * kLoadKeys, tile_key = (load % kLoads) * kLoadKeys;
-      // Into registers first, so that the next copy into the slot starts while this one is converted.
       // Keys: 16 dims of a token; eight lanes a tile of 8 tokens. Values: 16 tokens of a dim.
-      uint4 x[2 * NG];
-      float2 sc = make_float2(1.f, 1.f);
-      if (ok) {
-        const uint8_t* box = raw + slot * Z::kRaw;
+      const uint8_t* box = raw + slot * Z::kRaw;
+      const uint8_t* from = box + (v ? 16 * D : 0) + lane * 16;
+      const bool edge = v && kb + kLoadKeys > least;  // values that some column does not see
+      // A buffer is free once its last tile but one has been used. (When a load lands, every warp has
+      // stored all units of the tile two before it, and so has passed the wait for the use before
+      // that: this wait cannot mistake its phase either.)
+      auto buffer_free = [&] {
+        return t < 2 || wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
+      };
+      auto put_values = [&](const uint4& w, int i) {
+        const int dim = (i % NG) * 32 + lane, block = tile_key / kBlockTokens + i / NG;
+        uint4 first, second;
+        widen<true>(w, &first, &second);
+        uint8_t* to = vt + stage * Z::kValues + (block >> 2) * (D * 128);
+        *reinterpret_cast<uint4*>(to + tc::sw128_offset(dim, 2 * block & 7)) = first;
+        *reinterpret_cast<uint4*>(to + tc::sw128_offset(dim, (2 * block + 1) & 7)) = second;
+      };
+      if (ok && mine && edge) {
+        // apart from the usual loop, which its code would stretch
+        ok = buffer_free();
+#pragma unroll 1
+        for (int i = 0; ok && i < 2 * NG; ++i) {
+          const uint4 w = *reinterpret_cast<const uint4*>(from + (i / NG) * Z::kBox + (i % NG) * 512);
+          put_values(guard(w, (i % NG) * 32 + lane, kb + (i / NG) * kBlockTokens, k1, least, poison, &poison_any), i);
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars.raw_free[slot]);
+      } else if (ok) {
+        // into registers first, so that the next copy into the slot starts while this one is converted
+        uint4 x[2 * NG];
+        float2 sc = make_float2(1.f, 1.f);
         if (mine) {
-          const uint8_t* from = box + (v ? 16 * D : 0) + lane * 16;
 #pragma unroll
           for (int i = 0; i < 2 * NG; ++i)
             x[i] = *reinterpret_cast<const uint4*>(from + (i / NG) * Z::kBox + (i % NG) * 512);
@@ -298,10 +323,28 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&bars.raw_free[slot]);
-        // A buffer is free once its last tile but one has been used. (When a load lands, every warp has
-        // stored all units of the tile two before it, and so has passed the wait for the use before
-        // that: this wait cannot mistake its phase either.)
-        if (mine && t >= 2) ok = wait_warp(v ? &bars.v_free[stage] : &bars.k_free[stage], ((t >> 1) - 1) & 1, abort);
+        if (mine && (ok = buffer_free())) {
+          if (v) {
+#pragma unroll
+            for (int i = 0; i < 2 * NG; ++i) put_values(x[i], i);
+          } else {
+            if (lane < 2) {
+              const int e = exponent_of(sc.y);
+              scales[t & 3][tile_key / kBlockTokens + lane] = make_float4(sc.x, float(e), power_of_two(-e), 0.f);
+            }
+            // piece 32 i + lane of a block: chunks of 16 dims within halves of 8 tokens
+#pragma unroll
+            for (int i = 0; i < 2 * NG; ++i) {
+              const int piece = (i % NG) * 32 + lane, half = piece / (D / 2), ch = piece % (D / 2) / 8;
+              const int token = tile_key + (i / NG) * kBlockTokens + 8 * half + (piece & 7);
+              uint4 first, second;
+              widen<false>(x[i], &first, &second);
+              uint8_t* to = kt + stage * Z::kTile + (ch >> 2) * kBlock;
+              *reinterpret_cast<uint4*>(to + tc::sw128_offset(token, 2 * ch & 7)) = first;
+              *reinterpret_cast<uint4*>(to + tc::sw128_offset(token, (2 * ch + 1) & 7)) = second;
+            }
+          }
+        }
       }
       if (!ok) {
         if (lane == 0) give_up(a, abort, CONDUIT_SITE_LOAD);
@@ -309,37 +352,6 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
       }
       if (!mine) continue;
       unit += kUnpackWarps;
-      if (!v) {
-        // piece 32 i + lane of a block: chunks of 16 dims within halves of 8 tokens
-        if (lane < 2) {
-          const int e = exponent_of(sc.y);
-          scales[t & 3][tile_key / kBlockTokens + lane] = make_float4(sc.x, float(e), power_of_two(-e), 0.f);
-        }
-        uint8_t* tile = kt + stage * Z::kTile;
-#pragma unroll
-        for (int i = 0; i < 2 * NG; ++i) {
-          const int piece = (i % NG) * 32 + lane, half = piece / (D / 2), ch = piece % (D / 2) / 8;
-          const int token = tile_key + (i / NG) * kBlockTokens + 8 * half + (piece & 7);
-          uint4 first, second;
-          widen<false>(x[i], &first, &second);
-          uint8_t* to = tile + (ch >> 2) * kBlock;
-          *reinterpret_cast<uint4*>(to + tc::sw128_offset(token, 2 * ch & 7)) = first;
-          *reinterpret_cast<uint4*>(to + tc::sw128_offset(token, (2 * ch + 1) & 7)) = second;
-        }
-      } else {
-        uint8_t* tile = vt + stage * Z::kValues;
-        const bool edge = kb + kLoadKeys > least;  // some column does not see all of it
-#pragma unroll
-        for (int i = 0; i < 2 * NG; ++i) {
-          const int dim = (i % NG) * 32 + lane, block = tile_key / kBlockTokens + i / NG;
-          if (edge) x[i] = guard(x[i], dim, kb + (i / NG) * kBlockTokens, k1, least, poison, &poison_any);
-          uint4 first, second;
-          widen<true>(x[i], &first, &second);
-          uint8_t* to = tile + (block >> 2) * (D * 128);
-          *reinterpret_cast<uint4*>(to + tc::sw128_offset(dim, 2 * block & 7)) = first;
-          *reinterpret_cast<uint4*>(to + tc::sw128_offset(dim, (2 * block + 1) & 7)) = second;
-        }
-      }
       tc::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(v ? &bars.v_full[stage] : &bars.k_full[stage]);
