@@ -706,7 +706,9 @@ conduit_status conduit_fp8_attn(const conduit_fp8_kv* kv, const conduit_seqs* se
  *
  * The best continuations of each group over its beams and the vocabulary:
  *   s(b, v) = sums[b] + logits[b][v] - ln sum_u exp(logits[b][u])
- * the num_out largest, descending, equal ones in the order of (b, v). Sums in fp32, scores compared in fp64.
+ * the num_out largest, descending, equal ones in the order of (b, v). The sums of exponentials are fp32, scores are formed
+ * and compared in fp64: inside a beam the order is that of the logits; beams whose scores are within about 10^-6 of one
+ * another may come in either order (equal rows 16 bytes aligned, with equal sums, in theirs).
  *  logits  device [G width][vocab] of dtype, rows row_stride elements apart (>= vocab), aligned to the element
  *  sums    device fp32 [G width]: log-probabilities so far; -inf leaves a beam out
  *  score   device fp32 [G][num_out]

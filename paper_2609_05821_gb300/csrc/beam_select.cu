@@ -31,18 +31,21 @@ struct SelectArgs {
   int32_t* status;
 };
 
+constexpr int kBuffer = 31 + 32 * 8;  // values that wait for a warp's next merge, and one load more
+
 struct Shared {
-  uint64_t buffer[kWarps][64];         // values on their way into a warp's list
   uint64_t list[kListsMost][kMaxBeams];  // the first CTA's: every warp's list, sorted
-  float2 stats[kListsMost];            // (largest, sum of e^(z - largest))
-  double base[kMaxBeams];              // sums - lse, -inf: the row is left out
-  double cand[kListsMost * kMaxBeams];
-  uint64_t cand_at[kListsMost * kMaxBeams];  // (beam, token)
-  double head[kListsMost];
-  uint64_t head_at[kListsMost];
-  double least;
-  uint64_t least_at;
+  float2 stats[kListsMost];              // (largest, sum of e^(z - largest))
+  double base[kMaxBeams];                // sums - lse, -inf: the row is left out
+  uint64_t head[kListsMost], head_at[kListsMost];
+  uint64_t least, least_at;
   int count;
+  union {
+    uint64_t buffer[kWarps][kBuffer + 1];  // values on their way into a warp's list
+    struct {
+      uint64_t score[kListsMost * kMaxBeams], at[kListsMost * kMaxBeams];  // what can still be chosen: rank and (beam, token)
+    } cand;
+  };
 };
 
 // A key that grows with x, and among equal ones with a lower index; 0 stands for none.
@@ -86,24 +89,46 @@ __device__ __forceinline__ uint64_t merge_down(uint64_t list, uint64_t k, int la
 
 // What a warp knows of its segment.
 struct Best {
-  uint64_t list = 0;         // lane i: the i-th best
-  float threshold = -INFINITY;  // of the n-th best
-  int count = 0;             // of values in the buffer
+  uint64_t list = 0;            // lane i: the i-th best
+  float threshold = -INFINITY;  // values up to here are not among the n best
+  int count = 0;                // of values in the buffer
   float m = -INFINITY, s = 0.f;  // this lane's largest value and sum of e^(z - m)
 };
 
-__device__ __forceinline__ void flush(Best& b, uint64_t* buffer, int n, int lane) {
+// The buffer's last 32 values (or all) into the list.
+__device__ __forceinline__ void merge_some(Best& b, const uint64_t* buffer, int n, int lane) {
   __syncwarp();
-  const uint64_t k = lane < b.count ? buffer[lane] : 0, rest = lane + 32 < b.count ? buffer[lane + 32] : 0;
-  __syncwarp();
-  if (lane + 32 < b.count) buffer[lane] = rest;
-  b.count = max(b.count - 32, 0);
+  const int from = max(b.count - 32, 0);
+  const uint64_t k = from + lane < b.count ? buffer[from + lane] : 0;
+  b.count = from;
   b.list = merge_down(b.list, sort_down(k, lane), lane);
   const uint64_t worst = __shfl_sync(kAll, b.list, n - 1);
-  b.threshold = worst ? value_of(worst) : -INFINITY;
+  if (worst) b.threshold = fmaxf(b.threshold, value_of(worst));
+  __syncwarp();
 }
 
-// N values of each lane, at `at` on; -inf for what is none.
+// The next float below x.
+__device__ __forceinline__ float below(float x) {
+  const int u = __float_as_int(x);
+  return x == 0.f ? __int_as_float(0x80000001) : __int_as_float(x > 0.f ? u - 1 : u + 1);
+}
+
+// A lower bound of the n-th best of the lanes' largest values, as a threshold: at least n values lie above it.
+__device__ __forceinline__ float bound(float top, int n, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+    for (int mask = size >> 1; mask > 0; mask >>= 1) {
+      const float other = __shfl_xor_sync(kAll, top, mask);
+      const bool down = size == 32 || !(lane & size), larger = ((lane & mask) == 0) == down;
+      top = larger ? fmaxf(top, other) : fminf(top, other);
+    }
+  top = __shfl_sync(kAll, top, n - 1);
+  return top > -INFINITY ? below(top) : top;
+}
+
+// N values of each lane, at `at` on, -inf for what is none. Values seen before have lower indexes, so that one that
+// equals the worst of the list is not among the n best.
 template <int N>
 __device__ __forceinline__ void take(Best& b, const float (&x)[N], uint32_t at, uint64_t* buffer, int n, int lane) {
   float top = x[0];
@@ -111,31 +136,30 @@ __device__ __forceinline__ void take(Best& b, const float (&x)[N], uint32_t at, 
   for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
   const float m = fmaxf(b.m, top), base = m == -INFINITY ? 0.f : m;
   // the difference first: its rounding, and not that of z log2(e), is what the exponential sees
-  float add = 0.f;
+  float2 add = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int e = 0; e < N; ++e) add += tc::ex2((x[e] - base) * kLog2e);
-  b.s = fmaf(b.s, tc::ex2((b.m - base) * kLog2e), add);
+  for (int e = 0; e < N; e += 2) {
+    const float2 y = tc::fmul2(tc::fadd2(make_float2(x[e], x[e + 1]), make_float2(-base, -base)), make_float2(kLog2e, kLog2e));
+    add = tc::fadd2(add, make_float2(tc::ex2(y.x), tc::ex2(y.y)));
+  }
+  b.s = fmaf(b.s, tc::ex2((b.m - base) * kLog2e), add.x + add.y);
+  if (!__any_sync(kAll, top > b.threshold)) {
+    b.m = m;
+    return;
+  }
+  if (!__any_sync(kAll, b.m > -INFINITY)) b.threshold = fmaxf(b.threshold, bound(top, n, lane));  // the first values
   b.m = m;
-  // Values seen before have lower indexes, so one that equals the n-th best of them loses; among this call's own,
-  // which do not come in order, it may not.
-  const float old = b.threshold;
-  if (!__any_sync(kAll, top > old)) return;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    const bool in = x[e] > old && x[e] >= b.threshold;
+    const bool in = x[e] > b.threshold;
     const uint32_t who = __ballot_sync(kAll, in);
-    if (!who) continue;
     if (in) buffer[b.count + __popc(who & ((1u << lane) - 1u))] = key_of(x[e], at + e);
     b.count += __popc(who);
-    if (b.count >= 32) flush(b, buffer, n, lane);
   }
+#pragma unroll 1
+  while (b.count >= 32) merge_some(b, buffer, n, lane);
 }
 
-template <typename T>
-struct Vec {
-  static constexpr int N = 16 / sizeof(T);
-  uint4 w;
-};
 template <typename T>
 __device__ __forceinline__ void unpack(const uint4& w, bool on, float (&x)[16 / sizeof(T)]) {
   const T* v = reinterpret_cast<const T*>(&w);
@@ -143,8 +167,16 @@ __device__ __forceinline__ void unpack(const uint4& w, bool on, float (&x)[16 / 
   for (int e = 0; e < int(16 / sizeof(T)); ++e) x[e] = on ? to_float(v[e]) : -INFINITY;
 }
 
+// A number that grows with a score.
+__device__ __forceinline__ uint64_t rank_of(double s) {
+  const uint64_t u = uint64_t(__double_as_longlong(s));
+  return u ^ (u >> 63 ? ~uint64_t(0) : uint64_t(1) << 63);
+}
+__device__ __forceinline__ double score_of(uint64_t r) {
+  return __longlong_as_double(int64_t(r ^ (r >> 63 ? uint64_t(1) << 63 : ~uint64_t(0))));
+}
 // Descending by score, then by (beam, token).
-__device__ __forceinline__ bool before(double s, uint64_t at, double t, uint64_t other) {
+__device__ __forceinline__ bool before(uint64_t s, uint64_t at, uint64_t t, uint64_t other) {
   return s > t || (s == t && at < other);
 }
 
@@ -175,32 +207,38 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
     const int vecs = (a.vocab - head) / N, tail = head + vecs * N;
     const int v0 = int(int64_t(vecs) * seg / a.segs), v1 = int(int64_t(vecs) * (seg + 1) / a.segs);
     const uint4* from = reinterpret_cast<const uint4*>(row + head);
-    if (seg == 0 && head > 0) {
-      const float x[1] = {lane < head ? to_float(row[lane]) : -INFINITY};
-      take<1>(b, x, uint32_t(lane), buffer, a.n, lane);
-    }
+    // One body for the elements before the first boundary, the vectors and the elements behind: the code of a merge counts where
+    // every warp is elsewhere in it (a copy at each step of an unrolled loop: 135 us for 64 x 8 rows of 128 003,
+    // half of the issue slots waiting for instructions).
     constexpr int kAhead = 4;
-    for (int v = v0; v < v1; v += 32 * kAhead) {
-      uint4 w[kAhead];
+    const int steps = (v1 - v0 + 31) / 32;
+    uint4 w[kAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int at = v + 32 * k + lane;
-        if (at < v1) w[k] = __ldcs(from + at);
-      }
+    for (int k = 0; k < kAhead; ++k) {
+      const int at = v0 + 32 * k + lane;
+      if (at < v1) w[k] = __ldcs(from + at);
+    }
+#pragma unroll 1
+    for (int step = seg == 0 && head > 0 ? -1 : 0; step < steps + (seg == a.segs - 1 && tail < a.vocab); ++step) {
+      float x[N];
+      uint32_t at;
+      if (step >= 0 && step < steps) {
+        const int v = v0 + 32 * step + lane;
+        unpack<T>(w[0], v < v1, x);
+        at = uint32_t(head + v * N);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int at = v + 32 * k + lane;
-        if (v + 32 * k >= v1) break;
-        float x[N];
-        unpack<T>(w[k], at < v1, x);
-        take<N>(b, x, uint32_t(head + at * N), buffer, a.n, lane);
+        for (int k = 0; k + 1 < kAhead; ++k) w[k] = w[k + 1];
+        if (v + 32 * kAhead < v1) w[kAhead - 1] = __ldcs(from + v + 32 * kAhead);
+      } else {
+        const int first = step < 0 ? 0 : tail, end = step < 0 ? head : a.vocab;
+        at = uint32_t(first + lane);
+        x[0] = first + lane < end ? to_float(row[first + lane]) : -INFINITY;
+#pragma unroll
+        for (int e = 1; e < N; ++e) x[e] = -INFINITY;
       }
+      take<N>(b, x, at, buffer, a.n, lane);
     }
-    if (seg == a.segs - 1 && tail < a.vocab) {
-      const float x[1] = {tail + lane < a.vocab ? to_float(row[tail + lane]) : -INFINITY};
-      take<1>(b, x, uint32_t(tail + lane), buffer, a.n, lane);
-    }
-    while (b.count > 0) flush(b, buffer, a.n, lane);
+    if (b.count > 0) merge_some(b, buffer, a.n, lane);
     // the lanes' sums, in the order of a butterfly
     float m = b.m;
 #pragma unroll
@@ -222,7 +260,7 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
   // ------------------------------------------------- one CTA: rows' sums, then the best of the lists
   if (threadIdx.x == 0) {
     sh.count = 0;
-    sh.least = -INFINITY;
+    sh.least = rank_of(-INFINITY);
     sh.least_at = ~uint64_t(0);
   }
   for (int w = warp; w < a.width; w += kWarps) {
@@ -254,46 +292,44 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
   }
   __syncthreads();
   const int lists = a.width * a.segs;
-  auto entry = [&](int list, int i, double* score, uint64_t* at) {
+  const uint64_t none = rank_of(-INFINITY);
+  auto entry = [&](int list, int i, uint64_t* score, uint64_t* at) {
     const uint64_t key = sh.list[list][i];
     const int w = list / a.segs;
-    *score = key ? sh.base[w] + double(value_of(key)) : -INFINITY;
+    *score = key ? rank_of(sh.base[w] + double(value_of(key))) : none;
     *at = uint64_t(w) << 32 | index_of(key);
-    return *score > -INFINITY;
+    return *score > none;
   };
   // The n-th best of the lists' first entries bounds what can be chosen.
   if (int(threadIdx.x) < lists) entry(threadIdx.x, 0, &sh.head[threadIdx.x], &sh.head_at[threadIdx.x]);
   __syncthreads();
   if (int(threadIdx.x) < lists && lists >= a.n) {
-    const double own = sh.head[threadIdx.x];
-    const uint64_t own_at = sh.head_at[threadIdx.x];
+    const uint64_t own = sh.head[threadIdx.x], own_at = sh.head_at[threadIdx.x];
     int place = 0;
     for (int i = 0; i < lists; ++i) place += before(sh.head[i], sh.head_at[i], own, own_at);
-    if (place == a.n - 1 && own > -INFINITY) {
+    if (place == a.n - 1 && own > none) {
       sh.least = own;
       sh.least_at = own_at;
     }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < lists * a.n; i += kWarps * 32) {
-    double s;
-    uint64_t at;
+    uint64_t s, at;
     if (entry(i % lists, i / lists, &s, &at) && !before(sh.least, sh.least_at, s, at)) {
       const int to = atomicAdd(&sh.count, 1);
-      sh.cand[to] = s;
-      sh.cand_at[to] = at;
+      sh.cand.score[to] = s;
+      sh.cand.at[to] = at;
     }
   }
   __syncthreads();
   const int count = sh.count;
   const int64_t out = g * a.n;
   for (int i = threadIdx.x; i < count; i += kWarps * 32) {
-    const double own = sh.cand[i];
-    const uint64_t own_at = sh.cand_at[i];
+    const uint64_t own = sh.cand.score[i], own_at = sh.cand.at[i];
     int place = 0;
-    for (int j = 0; j < count; ++j) place += before(sh.cand[j], sh.cand_at[j], own, own_at);
+    for (int j = 0; j < count; ++j) place += before(sh.cand.score[j], sh.cand.at[j], own, own_at);
     if (place < a.n) {
-      a.score[out + place] = float(own);
+      a.score[out + place] = float(score_of(own));
       a.parent[out + place] = int32_t(g * a.width + int64_t(own_at >> 32));
       a.token[out + place] = int32_t(uint32_t(own_at));
     }

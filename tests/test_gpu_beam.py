@@ -1,8 +1,9 @@
 """Beam selection and the contexts that follow it, against plain forms.
 
-Selection: the order inside a beam is that of the logits, so the chosen (beam, token) are compared exactly wherever
-the 64-bit scores of neighbours lie further apart than the error of a log-sum-exp in fp32: sums of 2^-22 relative
-exponentials, and the rounding of numbers up to 32 x 2^-24. A score is rounded to fp32 once more.
+Selection: the order inside a beam is that of the logits. A beam's log-sum-exp is off by EPS at most (sums of
+exponentials that are 2^-22 off, and the rounding of numbers up to 32 x 2^-24), the same for all of its candidates and for
+beams of equal rows and sums; so candidates of two unequal beams may change places where their 64-bit scores are within 2 EPS,
+and everything else is compared exactly. A score is rounded to fp32 once more.
 Reordering moves bytes: everything is compared exactly.
 """
 
@@ -52,9 +53,9 @@ def _check_select(C, logits, sums, width, n, status_want=0, **kw):
                 continue
             assert abs(got_s[i] - best[i]) <= EPS + 2.0 ** -24 * abs(best[i]), (g, i, got_s[i], best[i])
             flat = int((got_p[i] - g * width) * V + got_t[i])
-            # equal or clearly ordered neighbours leave one answer
-            near = s[(np.abs(s - best[i]) <= 2 * EPS) & (s != best[i])]
-            if near.size == 0:
+            close = np.unique(np.nonzero(np.abs(s - best[i]) <= 2 * EPS)[0] // V)
+            own = g * width + order[i] // V
+            if all(torch.equal(logits[g * width + w], logits[own]) and sums[g * width + w] == sums[own] for w in close):
                 assert flat == order[i], (g, i, flat, order[i])
             else:
                 assert abs(s[flat] - best[i]) <= 2 * EPS
