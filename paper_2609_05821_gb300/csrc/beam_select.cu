@@ -31,34 +31,40 @@ struct SelectArgs {
   int32_t* status;
 };
 
+constexpr int kStages = 4;            // loads of 16 bytes a lane under way
 constexpr int kBuffer = 31 + 32 * 8;  // values that wait for a warp's next merge, and one load more
 
 struct Shared {
   uint64_t list[kListsMost][kMaxBeams];  // the first CTA's: every warp's list, sorted
   float2 stats[kListsMost];              // (largest, sum of e^(z - largest))
   double base[kMaxBeams];                // sums - lse, -inf: the row is left out
-  uint64_t head[kListsMost], head_at[kListsMost];
-  uint64_t least, least_at;
+  float down[kMaxBeams], up[kMaxBeams];  // bounds of it
+  float sums[kMaxBeams];
+  uint32_t head[kListsMost];             // keys of lower bounds of the lists' first scores
+  float least;
   int count;
   union {
-    uint64_t buffer[kWarps][kBuffer + 1];  // values on their way into a warp's list
+    struct {
+      uint4 ring[kWarps][kStages][32];       // loads under way
+      uint64_t buffer[kWarps][kBuffer + 1];  // values on their way into a warp's list
+    };
     struct {
       uint64_t score[kListsMost * kMaxBeams], at[kListsMost * kMaxBeams];  // what can still be chosen: rank and (beam, token)
     } cand;
   };
 };
 
-// A key that grows with x, and among equal ones with a lower index; 0 stands for none.
-__device__ __forceinline__ uint64_t key_of(float x, uint32_t at) {
-  uint32_t u = __float_as_uint(x + 0.f);  // -0 as 0
-  u ^= (u >> 31) ? 0xFFFFFFFFu : 0x80000000u;
-  return uint64_t(u) << 32 | (~at);
+// A number that grows with x.
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);  // -0 as 0
+  return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
-__device__ __forceinline__ float value_of(uint64_t key) {
-  uint32_t u = uint32_t(key >> 32);
-  u ^= (u >> 31) ? 0x80000000u : 0xFFFFFFFFu;
-  return __uint_as_float(u);
+__device__ __forceinline__ float unordered(uint32_t u) {
+  return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
+// The same, and among equal ones the larger for a lower index; 0 stands for none.
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t at) { return uint64_t(ordered(x)) << 32 | (~at); }
+__device__ __forceinline__ float value_of(uint64_t key) { return unordered(uint32_t(key >> 32)); }
 __device__ __forceinline__ uint32_t index_of(uint64_t key) { return ~uint32_t(key); }
 
 __device__ __forceinline__ uint64_t compare_exchange(uint64_t k, int mask, bool larger) {
@@ -186,6 +192,12 @@ __device__ __forceinline__ uint32_t in_first_cta(const void* p) {
   return at;
 }
 
+// 16 bytes a lane into shared memory; a group for each call, also where a lane has none.
+__device__ __forceinline__ void copy16(void* to, const void* from, bool on) {
+  if (on) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to)), "l"(from) : "memory");
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) {
   constexpr int N = 16 / sizeof(T);
@@ -200,6 +212,7 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
   const int id = int(rank) * kWarps + warp, beam = id / a.segs, seg = id % a.segs;
   uint64_t* buffer = sh.buffer[warp];
   Best b;
+  if (rank == 0 && threadIdx.x < kMaxBeams) sh.sums[threadIdx.x] = int(threadIdx.x) < a.width ? a.sums[g * a.width + threadIdx.x] : 0.f;
   if (beam < a.width) {
     const T* row = static_cast<const T*>(a.logits) + (g * a.width + beam) * a.row_stride;
     // 16-byte loads from the first boundary on; the first segment takes what lies before it, the last what lies behind
@@ -210,25 +223,21 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
     // One body for the elements before the first boundary, the vectors and the elements behind: the code of a merge counts where
     // every warp is elsewhere in it (a copy at each step of an unrolled loop: 135 us for 64 x 8 rows of 128 003,
     // half of the issue slots waiting for instructions).
-    constexpr int kAhead = 4;
     const int steps = (v1 - v0 + 31) / 32;
-    uint4 w[kAhead];
+    uint4* ring = sh.ring[warp][0] + lane;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int at = v0 + 32 * k + lane;
-      if (at < v1) w[k] = __ldcs(from + at);
-    }
+    for (int k = 0; k < kStages; ++k) copy16(ring + 32 * k, from + v0 + 32 * k + lane, v0 + 32 * k + lane < v1);
 #pragma unroll 1
     for (int step = seg == 0 && head > 0 ? -1 : 0; step < steps + (seg == a.segs - 1 && tail < a.vocab); ++step) {
       float x[N];
       uint32_t at;
       if (step >= 0 && step < steps) {
         const int v = v0 + 32 * step + lane;
-        unpack<T>(w[0], v < v1, x);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");  // this lane reads what it copied itself
+        uint4* slot = ring + 32 * (step % kStages);
+        unpack<T>(*slot, v < v1, x);
         at = uint32_t(head + v * N);
-#pragma unroll
-        for (int k = 0; k + 1 < kAhead; ++k) w[k] = w[k + 1];
-        if (v + 32 * kAhead < v1) w[kAhead - 1] = __ldcs(from + v + 32 * kAhead);
+        copy16(slot, from + v + 32 * kStages, v + 32 * kStages < v1);
       } else {
         const int first = step < 0 ? 0 : tail, end = step < 0 ? head : a.vocab;
         at = uint32_t(first + lane);
@@ -260,8 +269,7 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
   // ------------------------------------------------- one CTA: rows' sums, then the best of the lists
   if (threadIdx.x == 0) {
     sh.count = 0;
-    sh.least = rank_of(-INFINITY);
-    sh.least_at = ~uint64_t(0);
+    sh.least = -INFINITY;
   }
   for (int w = warp; w < a.width; w += kWarps) {
     float m = -INFINITY;
@@ -277,7 +285,7 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(kAll, sum, s);
     if (lane == 0) {
-      const float before_row = a.sums[g * a.width + w];
+      const float before_row = sh.sums[w];
       const bool wild = !(sum < INFINITY) || !(before_row < INFINITY);
       if (wild) flag_status(a.status, CONDUIT_FLAG_NONFINITE);
       double base = -INFINITY;
@@ -288,37 +296,41 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
         base = double(before_row) - (double(m) + (k * 0.69314718055994530942 + double(log1pf(f))));
       }
       sh.base[w] = base;
+      sh.down[w] = __double2float_rd(base);
+      sh.up[w] = __double2float_ru(base);
     }
   }
   __syncthreads();
+  // The n-th best of the lists' first entries bounds what can be chosen; in fp32, rounded down, against scores rounded up.
   const int lists = a.width * a.segs;
-  const uint64_t none = rank_of(-INFINITY);
-  auto entry = [&](int list, int i, uint64_t* score, uint64_t* at) {
-    const uint64_t key = sh.list[list][i];
-    const int w = list / a.segs;
-    *score = key ? rank_of(sh.base[w] + double(value_of(key))) : none;
-    *at = uint64_t(w) << 32 | index_of(key);
-    return *score > none;
-  };
-  // The n-th best of the lists' first entries bounds what can be chosen.
-  if (int(threadIdx.x) < lists) entry(threadIdx.x, 0, &sh.head[threadIdx.x], &sh.head_at[threadIdx.x]);
-  __syncthreads();
-  if (int(threadIdx.x) < lists && lists >= a.n) {
-    const uint64_t own = sh.head[threadIdx.x], own_at = sh.head_at[threadIdx.x];
-    int place = 0;
-    for (int i = 0; i < lists; ++i) place += before(sh.head[i], sh.head_at[i], own, own_at);
-    if (place == a.n - 1 && own > none) {
-      sh.least = own;
-      sh.least_at = own_at;
-    }
+  if (threadIdx.x < kListsMost) {
+    const int list = threadIdx.x;
+    const uint64_t key = list < lists ? sh.list[list][0] : 0;
+    const float low = key ? __fadd_rd(sh.down[list / a.segs], value_of(key)) : -INFINITY;
+    sh.head[list] = low > -INFINITY ? ordered(low) : 0;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < lists * a.n; i += kWarps * 32) {
-    uint64_t s, at;
-    if (entry(i % lists, i / lists, &s, &at) && !before(sh.least, sh.least_at, s, at)) {
+  if (threadIdx.x < kListsMost) {
+    const uint32_t own = sh.head[threadIdx.x];
+    int place = 0;
+#pragma unroll 16
+    for (int i = 0; i < kListsMost; ++i) place += sh.head[i] > own || (sh.head[i] == own && i < int(threadIdx.x));
+    if (place == a.n - 1 && own) sh.least = unordered(own);
+  }
+  __syncthreads();
+  constexpr int kPer = kWarps * 32 / kListsMost;  // threads of a list
+  const int list = threadIdx.x / kPer, w = list / a.segs;
+  if (list < lists && sh.up[w] > -INFINITY) {
+    const float least = sh.least, up = sh.up[w];
+    const double base = sh.base[w];
+    for (int i = threadIdx.x % kPer; i < a.n; i += kPer) {
+      const uint64_t key = sh.list[list][i];
+      if (!key || __fadd_ru(up, value_of(key)) < least) break;  // the list goes down
+      const double score = base + double(value_of(key));
+      if (!(score > -INFINITY)) break;
       const int to = atomicAdd(&sh.count, 1);
-      sh.cand.score[to] = s;
-      sh.cand.at[to] = at;
+      sh.cand.score[to] = rank_of(score);
+      sh.cand.at[to] = uint64_t(w) << 32 | index_of(key);
     }
   }
   __syncthreads();
