@@ -4,12 +4,13 @@
 // over a row gives its running maximum and sum and its n largest logits; rows meet only at the end, with their lse,
 // in fp64 (a float's last bit would decide between beams).
 //
-// Shape: a cluster per group; its warps share the rows out in segments. A warp keeps the n best of
-// its segment sorted across its lanes as 64-bit keys (logit, then the lower index); a value above the worst of
-// them goes to a small buffer, and 32 of those are sorted and merged at a time, so that the threshold is
-// all a value costs beside its exponential. The lists and sums go to the first CTA's shared memory, which ranks what can
-// still be chosen. No scratch in memory, one launch.
-// Bound: the logits once.
+// Shape: a cluster per group; its warps share the rows out in segments. While a segment streams by, a lane keeps its running
+// maximum and sum, and the maximum of each of up to 16 blocks of its values: nothing about candidates. The n-th largest
+// of the lanes' maxima bounds the segment's n best from below, so what can be among them lies in the few blocks that reach it, which
+// are read again, 32 at a time; their values above the bound go to a small buffer and, sorted as 64-bit
+// keys (logit, then the lower index), into the list of the n best across the warp's lanes. The lists and sums go to the first CTA's
+// shared memory, which ranks what can still be chosen. No scratch in memory, one launch.
+// Bound: the logits once, and as close behind it the exponentials, one a logit.
 #include "beam.cuh"
 #include "tc_common.cuh"
 
@@ -31,7 +32,8 @@ struct SelectArgs {
   int32_t* status;
 };
 
-constexpr int kStages = 4;            // loads of 16 bytes a lane under way
+constexpr int kAtOnce = 4;            // loads of 16 bytes a lane under way, beside as many in work
+constexpr int kBlocks = 16;           // blocks of a lane's values
 constexpr int kBuffer = 31 + 32 * 8;  // values that wait for a warp's next merge, and one load more
 
 struct Shared {
@@ -45,8 +47,9 @@ struct Shared {
   int count;
   union {
     struct {
-      uint4 ring[kWarps][kStages][32];       // loads under way
       uint64_t buffer[kWarps][kBuffer + 1];  // values on their way into a warp's list
+      float top[kWarps][kBlocks][32];        // largest values of blocks
+      uint32_t block[kWarps][32];            // blocks to read again
     };
     struct {
       uint64_t score[kListsMost * kMaxBeams], at[kListsMost * kMaxBeams];  // what can still be chosen: rank and (beam, token)
@@ -93,30 +96,28 @@ __device__ __forceinline__ uint64_t merge_down(uint64_t list, uint64_t k, int la
   return list;
 }
 
-// What a warp knows of its segment.
-struct Best {
-  uint64_t list = 0;            // lane i: the i-th best
-  float threshold = -INFINITY;  // values up to here are not among the n best
-  int count = 0;                // of values in the buffer
-  float m = -INFINITY, s = 0.f;  // this lane's largest value and sum of e^(z - m)
-};
-
-// The buffer's last 32 values (or all) into the list.
-__device__ __forceinline__ void merge_some(Best& b, const uint64_t* buffer, int n, int lane) {
-  __syncwarp();
-  const int from = max(b.count - 32, 0);
-  const uint64_t k = from + lane < b.count ? buffer[from + lane] : 0;
-  b.count = from;
-  b.list = merge_down(b.list, sort_down(k, lane), lane);
-  const uint64_t worst = __shfl_sync(kAll, b.list, n - 1);
-  if (worst) b.threshold = fmaxf(b.threshold, value_of(worst));
-  __syncwarp();
-}
-
 // The next float below x.
 __device__ __forceinline__ float below(float x) {
   const int u = __float_as_int(x);
   return x == 0.f ? __int_as_float(0x80000001) : __int_as_float(x > 0.f ? u - 1 : u + 1);
+}
+
+// What a warp knows of its segment.
+struct Best {
+  uint64_t list = 0;             // lane i: the i-th best
+  int count = 0;                 // of values in the buffer
+  float m = -INFINITY, s = 0.f;  // this lane's largest value and sum of e^(z - m)
+};
+
+// A list and up to 32 values of the buffer: their best. Not inlined: the code of a sort counts where every warp is
+// elsewhere in it.
+__device__ __noinline__ uint64_t merged(uint64_t list, const uint64_t* from, int count) {
+  const int lane = threadIdx.x % 32;
+  __syncwarp();
+  const uint64_t k = lane < count ? from[lane] : 0;
+  list = merge_down(list, sort_down(k, lane), lane);
+  __syncwarp();
+  return list;
 }
 
 // A lower bound of the n-th best of the lanes' largest values, as a threshold: at least n values lie above it.
@@ -133,13 +134,26 @@ __device__ __forceinline__ float bound(float top, int n, int lane) {
   return top > -INFINITY ? below(top) : top;
 }
 
-// N values of each lane, at `at` on, -inf for what is none. Values seen before have lower indexes, so that one that
-// equals the worst of the list is not among the n best.
+// Values of each lane, at `at` on, above `limit` into the buffer, and 32 of those at a time into the list.
 template <int N>
-__device__ __forceinline__ void take(Best& b, const float (&x)[N], uint32_t at, uint64_t* buffer, int n, int lane) {
-  float top = x[0];
+__device__ __forceinline__ void keep(Best& b, const float (&x)[N], uint32_t at, float limit, uint64_t* buffer, int lane) {
 #pragma unroll
-  for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
+  for (int e = 0; e < N; ++e) {
+    const bool in = x[e] > limit;
+    const uint32_t who = __ballot_sync(kAll, in);
+    if (in) buffer[b.count + __popc(who & ((1u << lane) - 1u))] = key_of(x[e], at + e);
+    b.count += __popc(who);
+  }
+#pragma unroll 1
+  while (b.count >= 32) {
+    b.count -= 32;
+    b.list = merged(b.list, buffer + b.count, 32);
+  }
+}
+
+// N values' part of a lane's maximum and sum.
+template <int N>
+__device__ __forceinline__ void add_up(Best& b, const float (&x)[N], float top) {
   const float m = fmaxf(b.m, top), base = m == -INFINITY ? 0.f : m;
   // the difference first: its rounding, and not that of z log2(e), is what the exponential sees
   float2 add = make_float2(0.f, 0.f);
@@ -149,21 +163,7 @@ __device__ __forceinline__ void take(Best& b, const float (&x)[N], uint32_t at, 
     add = tc::fadd2(add, make_float2(tc::ex2(y.x), tc::ex2(y.y)));
   }
   b.s = fmaf(b.s, tc::ex2((b.m - base) * kLog2e), add.x + add.y);
-  if (!__any_sync(kAll, top > b.threshold)) {
-    b.m = m;
-    return;
-  }
-  if (!__any_sync(kAll, b.m > -INFINITY)) b.threshold = fmaxf(b.threshold, bound(top, n, lane));  // the first values
   b.m = m;
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const bool in = x[e] > b.threshold;
-    const uint32_t who = __ballot_sync(kAll, in);
-    if (in) buffer[b.count + __popc(who & ((1u << lane) - 1u))] = key_of(x[e], at + e);
-    b.count += __popc(who);
-  }
-#pragma unroll 1
-  while (b.count >= 32) merge_some(b, buffer, n, lane);
 }
 
 template <typename T>
@@ -192,14 +192,8 @@ __device__ __forceinline__ uint32_t in_first_cta(const void* p) {
   return at;
 }
 
-// 16 bytes a lane into shared memory; a group for each call, also where a lane has none.
-__device__ __forceinline__ void copy16(void* to, const void* from, bool on) {
-  if (on) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to)), "l"(from) : "memory");
-  asm volatile("cp.async.commit_group;" ::: "memory");
-}
-
 template <typename T>
-__global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 2) beam_select_kernel(SelectArgs a) {
   constexpr int N = 16 / sizeof(T);
   extern __shared__ __align__(16) uint8_t select_smem[];
   Shared& sh = *reinterpret_cast<Shared*>(select_smem);
@@ -220,34 +214,97 @@ __global__ void __launch_bounds__(kWarps * 32) beam_select_kernel(SelectArgs a) 
     const int vecs = (a.vocab - head) / N, tail = head + vecs * N;
     const int v0 = int(int64_t(vecs) * seg / a.segs), v1 = int(int64_t(vecs) * (seg + 1) / a.segs);
     const uint4* from = reinterpret_cast<const uint4*>(row + head);
-    // One body for the elements before the first boundary, the vectors and the elements behind: the code of a merge counts where
-    // every warp is elsewhere in it (a copy at each step of an unrolled loop: 135 us for 64 x 8 rows of 128 003,
-    // half of the issue slots waiting for instructions).
-    const int steps = (v1 - v0 + 31) / 32;
-    uint4* ring = sh.ring[warp][0] + lane;
+    // elements of their own: before the first boundary, behind the last
+    const float ends[2][2] = {{seg == 0 && lane < head ? to_float(row[lane]) : -INFINITY, -INFINITY},
+                              {seg == a.segs - 1 && tail + lane < a.vocab ? to_float(row[tail + lane]) : -INFINITY, -INFINITY}};
+    add_up<2>(b, ends[0], ends[0][0]);
+    add_up<2>(b, ends[1], ends[1][0]);
+    const int loads = (v1 - v0 + 32 * kAtOnce - 1) / (32 * kAtOnce), per_block = max(1, (loads + kBlocks - 1) / kBlocks);
+    auto load = [&](int i, uint4 (&w)[kAtOnce]) {
 #pragma unroll
-    for (int k = 0; k < kStages; ++k) copy16(ring + 32 * k, from + v0 + 32 * k + lane, v0 + 32 * k + lane < v1);
-#pragma unroll 1
-    for (int step = seg == 0 && head > 0 ? -1 : 0; step < steps + (seg == a.segs - 1 && tail < a.vocab); ++step) {
-      float x[N];
-      uint32_t at;
-      if (step >= 0 && step < steps) {
-        const int v = v0 + 32 * step + lane;
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");  // this lane reads what it copied itself
-        uint4* slot = ring + 32 * (step % kStages);
-        unpack<T>(*slot, v < v1, x);
-        at = uint32_t(head + v * N);
-        copy16(slot, from + v + 32 * kStages, v + 32 * kStages < v1);
-      } else {
-        const int first = step < 0 ? 0 : tail, end = step < 0 ? head : a.vocab;
-        at = uint32_t(first + lane);
-        x[0] = first + lane < end ? to_float(row[first + lane]) : -INFINITY;
-#pragma unroll
-        for (int e = 1; e < N; ++e) x[e] = -INFINITY;
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int v = v0 + 32 * (kAtOnce * i + k) + lane;
+        if (v < v1) w[k] = __ldcs(from + v);
       }
-      take<N>(b, x, at, buffer, a.n, lane);
+    };
+    float block_top = -INFINITY;
+    int left = per_block, at_block = 0;
+    auto work = [&](int i, const uint4 (&w)[kAtOnce]) {
+      float x[kAtOnce * N];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        float y[N];
+        unpack<T>(w[k], v0 + 32 * (kAtOnce * i + k) + lane < v1, y);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[k * N + e] = y[e];
+      }
+      float top = x[0];
+#pragma unroll
+      for (int e = 1; e + 1 < kAtOnce * N; e += 2) top = tc::fmax3(top, x[e], x[e + 1]);
+      top = fmaxf(top, x[kAtOnce * N - 1]);
+      add_up<kAtOnce * N>(b, x, top);
+      block_top = fmaxf(block_top, top);
+      if (--left == 0 || i == loads - 1) {
+        sh.top[warp][at_block++][lane] = block_top;
+        block_top = -INFINITY;
+        left = per_block;
+      }
+    };
+    {
+      uint4 w0[kAtOnce], w1[kAtOnce];  // in turn, so that no copy of one waits for its loads
+      load(0, w0);
+#pragma unroll 1
+      for (int i = 0; i < loads; i += 2) {
+        load(i + 1, w1);
+        work(i, w0);
+        if (i + 1 >= loads) break;
+        load(i + 2, w0);
+        work(i + 1, w1);
+      }
     }
-    if (b.count > 0) merge_some(b, buffer, a.n, lane);
+    // What can be among the n best. In the order of the indexes up to a batch of blocks, so that a value that equals the worst of a full
+    // list from batches before has n better ones.
+    float limit = bound(b.m, a.n, lane);
+    auto tighten = [&] {
+      const uint64_t worst = __shfl_sync(kAll, b.list, a.n - 1);
+      if (worst) limit = fmaxf(limit, value_of(worst));
+    };
+    if (seg == 0) keep<2>(b, ends[0], uint32_t(lane), limit, buffer, lane);
+    uint32_t* ids = sh.block[warp];
+    int found = 0;
+#pragma unroll 1
+    for (int j = 0; j <= at_block; ++j) {
+      const bool in = j < at_block && sh.top[warp][j][lane] > limit;
+      const uint32_t who = __ballot_sync(kAll, in);
+      if (found > 0 && (j == at_block || found + __popc(who) > 32)) {
+        __syncwarp();
+        const uint32_t id = lane < found ? ids[lane] : 0;
+        const int i0 = int(id >> 5) * per_block, i1 = min(i0 + per_block, loads);
+#pragma unroll 1
+        for (int i = 0; i < per_block; ++i) {
+          uint4 w[kAtOnce];
+          const int v = v0 + 32 * kAtOnce * (i0 + i) + int(id & 31u);
+          const bool on = lane < found && i0 + i < i1;
+#pragma unroll
+          for (int k = 0; k < kAtOnce; ++k)
+            if (on && v + 32 * k < v1) w[k] = from[v + 32 * k];
+#pragma unroll
+          for (int k = 0; k < kAtOnce; ++k) {
+            float y[N];
+            unpack<T>(w[k], on && v + 32 * k < v1, y);
+            keep<N>(b, y, uint32_t(head + (v + 32 * k) * N), limit, buffer, lane);
+          }
+        }
+        tighten();
+        found = 0;
+        __syncwarp();
+      }
+      // (a block that the tightened limit leaves out holds nothing above it)
+      if (in) ids[found + __popc(who & ((1u << lane) - 1u))] = uint32_t(j) << 5 | uint32_t(lane);
+      found += __popc(who);
+    }
+    if (seg == a.segs - 1) keep<2>(b, ends[1], uint32_t(tail + lane), limit, buffer, lane);
+    if (b.count > 0) b.list = merged(b.list, buffer, b.count);
     // the lanes' sums, in the order of a butterfly
     float m = b.m;
 #pragma unroll
@@ -359,16 +416,19 @@ cudaError_t launch(SelectArgs a, int groups, cudaStream_t stream) {
   if (err) return err;
   cudaLaunchAttribute cluster{};
   cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = kClusterMost;
+  // Two CTAs of 100 registers a thread on an SM: clusters of eight while all of them run at a time, else of four (64 groups of
+  // 8 rows of 128 003: 38 us, 45 in clusters of eight; four CTAs an SM with half of the loads under way 43).
+  const int ctas = groups * kClusterMost <= 2 * 152 ? kClusterMost : kClusterMost / 2;
+  cluster.val.clusterDim.x = ctas;
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(unsigned(groups) * kClusterMost);
+  cfg.gridDim = dim3(unsigned(groups) * ctas);
   cfg.blockDim = dim3(kWarps * 32);
   cfg.dynamicSmemBytes = sizeof(Shared);
   cfg.stream = stream;
   cfg.attrs = &cluster;
   cfg.numAttrs = 1;
-  a.segs = kListsMost / a.width;
+  a.segs = ctas * kWarps / a.width;
   count_launches(1);
   return cudaLaunchKernelEx(&cfg, beam_select_kernel<T>, a);
 }
