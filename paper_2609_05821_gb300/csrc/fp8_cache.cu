@@ -7,7 +7,9 @@
 // Shape: a warp owns a block of one head (two heads of 64 dims, four of 32), keys first, then
 // values: both have to be seen whole before the first code. Lane 16 c + u has dims 8 u .. 8 u + 7
 // (and, past 128 dims, 8 (u + 16) ..) of the tokens of parity c, so a row is read in one piece by
-// 16 lanes; the codes of a value column meet in pairs of lanes that swap half of their dims.
+// 16 lanes; the codes of a value column meet in pairs of lanes that swap half of their dims. A CTA stays with a
+// block of tokens over its heads and layers: cosines and signed sines of the block's tokens lie in shared memory, dim by dim,
+// and the next unit's keys are on their way while a unit's values are packed.
 // Bound: the rows once and 2 d + 1 bytes a token and head of the cache.
 #include <algorithm>
 
@@ -45,28 +47,29 @@ __device__ __forceinline__ float head_max(float x, int d) {
   return x;
 }
 
-// Largest |x| of eight numbers; NaN and infinities become NaN and leave it alone. True if there was one.
-__device__ __forceinline__ bool top_of(float (&x)[8], float* top) {
-  float t = 0.f;
+// Largest |x| of eight numbers into top; wild becomes NaN where one is not finite.
+__device__ __forceinline__ void look_at(const float (&x)[8], float* top, float2* wild) {
 #pragma unroll
-  for (int e = 0; e < 8; e += 2) t = tc::fmax3(t, fabsf(x[e]), fabsf(x[e + 1]));
-  float2 zero = make_float2(0.f, 0.f);
-#pragma unroll
-  for (int e = 0; e < 8; e += 2)  // NaN from NaN and infinities
-    zero = tc::ffma2(make_float2(x[e], x[e + 1]), make_float2(0.f, 0.f), zero);
-  const bool wild = !(zero.x + zero.y == 0.f);
-  if (wild) {
-    t = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (fabsf(x[e]) < INFINITY)
-        t = fmaxf(t, fabsf(x[e]));
-      else
-        x[e] = NAN;
-    }
+  for (int e = 0; e < 8; e += 2) {
+    *top = tc::fmax3(*top, fabsf(x[e]), fabsf(x[e + 1]));
+    *wild = tc::ffma2(make_float2(x[e], x[e + 1]), make_float2(0.f, 0.f), *wild);
   }
-  *top = fmaxf(*top, t);
-  return wild;
+}
+// NaN and infinities of a lane's numbers become NaN and leave the largest alone.
+template <int NC>
+__device__ __forceinline__ void mend(float (&x)[NC][8][8], float* top) {
+  *top = 0.f;
+#pragma unroll
+  for (int m = 0; m < NC; ++m)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (fabsf(x[m][i][e]) < INFINITY)
+          *top = fmaxf(*top, fabsf(x[m][i][e]));
+        else
+          x[m][i][e] = NAN;
+      }
 }
 
 // Word of four codes, rescaled by 2^n (n <= 0): exact products, one rounding.
@@ -172,13 +175,13 @@ __device__ __forceinline__ void put_values(uint8_t* block, const Place& p, int d
   }
 }
 
-// Units below kv_warps: a block of the call's tokens of a head (or the heads that share a warp), one layer. The warps after
-// them rotate queries, a unit of pairs per thread.
+// CTAs below kv_grid: a block of the call's tokens, its heads and layers dealt out over the warps of grid.z. Those after
+// them rotate queries, a unit of pairs per thread, and walk over the layers.
 template <typename T, int VEC, int kPairing, int NC>
 __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 1)
-    fp8_append_kernel(PackedDev kv, SeqsDev s, RopeDev rope, int kv_grid, int blocks, bool wide, RowsDev k, RowsDev v,
+    fp8_append_kernel(PackedDev kv, SeqsDev s, RopeDev rope, int kv_grid, bool wide, RowsDev k, RowsDev v,
                       RowsDev q, RowsDev q_out, int32_t* status) {
-  const int r = blockIdx.y, l = blockIdx.z;
+  const int r = blockIdx.y;
   const int t0 = s.row_off[r], n = s.row_off[r + 1] - t0, len = s.len[r];
   if (n == 0) return;
   const int begin = len - n;  // slot of the call's first row
@@ -197,28 +200,24 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 1)
     if (!ok) return;  // flagged beside the row's key
     using C = Chunk<T, VEC>;
     const Unit un = unit_of<VEC>(rope, kv.d, u);
-    const T* src = static_cast<const T*>(q.p) + l * q.ls + t * q.rs + h * q.hs;
-    T* dst = static_cast<T*>(q_out.p) + l * q_out.ls + t * q_out.rs + h * q_out.hs;
-    C a = *reinterpret_cast<const C*>(src + un.a), b;
-    if (un.b >= 0) b = *reinterpret_cast<const C*>(src + un.b);
-    if (un.turns) {
-      float2 cs[VEC];
-      load_turn<VEC>(rope, pos, u * VEC, cs);
-      turn_chunks<T, VEC>(rope, cs, a, b);
+    float2 cs[VEC];
+    if (un.turns) load_turn<VEC>(rope, pos, u * VEC, cs);
+    for (int l = blockIdx.z; l < kv.L; l += gridDim.z) {
+      const T* src = static_cast<const T*>(q.p) + l * q.ls + t * q.rs + h * q.hs;
+      T* dst = static_cast<T*>(q_out.p) + l * q_out.ls + t * q_out.rs + h * q_out.hs;
+      C a = *reinterpret_cast<const C*>(src + un.a), b;
+      if (un.b >= 0) b = *reinterpret_cast<const C*>(src + un.b);
+      if (un.turns) turn_chunks<T, VEC>(rope, cs, a, b);
+      *reinterpret_cast<C*>(dst + un.a) = a;
+      if (un.b >= 0) *reinterpret_cast<C*>(dst + un.b) = b;
     }
-    *reinterpret_cast<C*>(dst + un.a) = a;
-    if (un.b >= 0) *reinterpret_cast<C*>(dst + un.b) = b;
     return;
   }
-  const int lane = threadIdx.x % 32, hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
-  const uint32_t unit = blockIdx.x * uint32_t(kThreads / 32) + threadIdx.x / 32;
-  const int nth = int(unit / uint32_t(groups)), head0 = int(unit % uint32_t(groups)) * hp;  // heads side by side
   // slots count from the block of the first row (rows before slot 0 lie in blocks of their own)
-  const int64_t first = (int64_t(begin) >> 4) * 16 + 16 * int64_t(nth);
-  if (nth >= blocks || first >= len) return;
+  const int64_t first = (int64_t(begin) >> 4) * 16 + 16 * int64_t(blockIdx.x);
+  if (first >= len) return;
+  const int lane = threadIdx.x % 32, hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
   const Place p = place_in_warp(kv.d, lane);
-  const int head = head0 + p.head;
-  const bool on = p.on && head < kv.Hkv;
 
   // which of the block's tokens the call writes
   const int most = min(s.max_len, kv.capacity());
@@ -233,80 +232,160 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 1)
     fine = load_positions(rope, int64_t(t0) + (own_slot - begin), pos);
   }
   const uint32_t asked = __ballot_sync(0xffffffffu, called) & 0xFFFFu, now = __ballot_sync(0xffffffffu, fine) & 0xFFFFu;
-  if (now != asked && lane == 0 && head0 == 0) flag_status(status, CONDUIT_FLAG_INDEX);
+  if (now != asked && threadIdx.x == 0 && blockIdx.z == 0) flag_status(status, CONDUIT_FLAG_INDEX);
   if (now == 0) return;
   const int before = int(min(max(int64_t(begin) - first, int64_t(0)), int64_t(16)));
   const uint32_t older = (1u << before) - 1u;
-
-  uint8_t* block = fp8_block(kv, l, on ? head : 0, page, int(first));
-  float* scales = reinterpret_cast<float*>(block + 32 * kv.d);
-  int was[2] = {kLeastExp, kLeastExp};
-  if (older) {
-    const float2 w = *reinterpret_cast<const float2*>(scales);
-    was[0] = exponent_of(w.x), was[1] = exponent_of(w.y);
-  }
   const int64_t row0 = int64_t(t0) + (first - begin);  // row of the call of the block's token 0
-  const int64_t k0 = l * k.ls + (on ? head : 0) * k.hs, v0 = l * v.ls + (on ? head : 0) * v.hs;
-  auto row_of = [&](const RowsDev& x, int64_t base, int t) { return static_cast<const T*>(x.p) + base + (row0 + t) * x.rs; };
 
-  bool bad = false;
-  float x[NC][8][8];
-  // keys
-  {
-    Raw8<T> raw[NC][8];
+  extern __shared__ __align__(16) float turns[];  // [16][d] cosines, then signed sines
+  float *cosines = turns, *sines = turns + kBlockTokens * kv.d;
+  if (kPairing != kNoTurn) {
+    const int chunks = kv.d / 8;
+    for (int e = threadIdx.x; e < kBlockTokens * chunks; e += kThreads) {
+      const int t = e / chunks, i0 = e % chunks * 8;
+      float c8[8], s8[8];
+      float2 cs[8];
 #pragma unroll
-    for (int m = 0; m < NC; ++m)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int t = 2 * i + p.c, u = p.u + 16 * m;
-        raw[m][i] = Raw8<T>{};
-        if ((now >> t & 1u) && on && u < kv.d / 8) raw[m][i] = load8(row_of(k, k0, t) + 8 * u, wide);
+      for (int k = 0; k < 8; ++k) cs[k] = make_float2(1.f, 0.f);
+      if (now >> t & 1u) {
+        int pos[CONDUIT_MAX_AXES];
+        load_positions(rope, row0 + t, pos);
+        load_turn8<kPairing>(rope, pos, i0, cs);
       }
-    float top = 0.f;
 #pragma unroll
-    for (int m = 0; m < NC; ++m) {
-      const int i0 = 8 * (p.u + 16 * m);
-      const int far0 = i0 >= rope.rot ? i0 : i0 < rope.half ? i0 + rope.half : i0 - rope.half;
+      for (int k = 0; k < 8; ++k) c8[k] = cs[k].x, s8[k] = cs[k].y;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int t = 2 * i + p.c;
-        to_floats(raw[m][i], x[m][i]);
-        if (kPairing != kNoTurn && (now >> t & 1u) && on && i0 < kv.d) {
-          int pos[CONDUIT_MAX_AXES];
-          load_positions(rope, row0 + t, pos);
-          float2 cs[8];
-          load_turn8<kPairing>(rope, pos, i0, cs);
-          const T* row = row_of(k, k0, t);
-          Raw8<T> far{};
-          if (kPairing == kChunks) far = load8(row + far0, wide);
-          turn8<kPairing>(rope, row, i0, far, cs, x[m][i]);
-        }
-        bad |= top_of(x[m][i], &top);
+      for (int k = 0; k < 8; k += 4) {
+        *reinterpret_cast<float4*>(cosines + t * kv.d + i0 + k) = make_float4(c8[k], c8[k + 1], c8[k + 2], c8[k + 3]);
+        *reinterpret_cast<float4*>(sines + t * kv.d + i0 + k) = make_float4(s8[k], s8[k + 1], s8[k + 2], s8[k + 3]);
       }
     }
-    const int e = max(exponent_for(head_max(top, kv.d)), was[0]);
-    put_keys<NC>(block, Place{p.head, p.u, p.c, on}, kv.d, now, older, e, was[0], x);
-    if (on && p.u == 0 && p.c == 0) scales[0] = power_of_two(e);
+    __syncthreads();
   }
-  // values
-  {
-    float top = 0.f;
+
+  constexpr bool kAhead = NC == 1 && sizeof(T) == 2;  // registers for a unit's keys beside another's values
+  const uint32_t mine = (now >> p.c) & 0x5555u;       // bit 2 i: token 2 i + c
+  const int units = groups * kv.L, step = gridDim.z * (kThreads / 32);
+  int unit = blockIdx.z * (kThreads / 32) + threadIdx.x / 32;
+  auto head_of = [&](int n) { return n % groups * hp + p.head; };
+  auto load_rows = [&](const RowsDev& x, int n, Raw8<T> (&raw)[NC][8]) {
+    const int head = head_of(n), l = n / groups;
+    const bool on = n < units && p.on && head < kv.Hkv;
+    const T* row = static_cast<const T*>(x.p) + l * x.ls + (on ? head : 0) * x.hs + (row0 + p.c) * x.rs + 8 * p.u;
 #pragma unroll
-    for (int m = 0; m < NC; ++m)
+    for (int i = 0; i < 8; ++i, row += 2 * x.rs)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int t = 2 * i + p.c, u = p.u + 16 * m;
-        Raw8<T> raw{};
-        if ((now >> t & 1u) && on && u < kv.d / 8) raw = load8(row_of(v, v0, t) + 8 * u, wide);
-        to_floats(raw, x[m][i]);
+      for (int m = 0; m < NC; ++m) {
+        raw[m][i] = Raw8<T>{};
+        if ((mine >> (2 * i) & 1u) && on && p.u + 16 * m < kv.d / 8) raw[m][i] = load8(row + 128 * m, wide);
       }
+  };
+  bool bad = false;
+  Raw8<T> k_raw[NC][8], v_raw[NC][8];
+  if (kAhead) load_rows(k, unit, k_raw);
+  for (; unit < units; unit += step) {
+    const int head = head_of(unit), l = unit / groups;
+    const bool on = p.on && head < kv.Hkv;
+    const Place here{p.head, p.u, p.c, on};
+    uint8_t* block = fp8_block(kv, l, on ? head : 0, page, int(first));
+    float* scales = reinterpret_cast<float*>(block + 32 * kv.d);
+    int was[2] = {kLeastExp, kLeastExp};
+    if (older) {
+      const float2 w = *reinterpret_cast<const float2*>(scales);
+      was[0] = exponent_of(w.x), was[1] = exponent_of(w.y);
+    }
+    if (!kAhead) load_rows(k, unit, k_raw);
+    if (kAhead) load_rows(v, unit, v_raw);
+    float x[NC][8][8];
+    {
+      const T* rows = static_cast<const T*>(k.p) + l * k.ls + (on ? head : 0) * k.hs + row0 * k.rs;
+      float top = 0.f;
+      float2 wild = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int m = 0; m < NC; ++m)
+      for (int m = 0; m < NC; ++m) {
+        const int i0 = 8 * (p.u + 16 * m);
+        const int far0 = i0 >= rope.rot ? i0 : i0 < rope.half ? i0 + rope.half : i0 - rope.half;
+        const bool turns_here = kPairing != kNoTurn && i0 < rope.rot && on;
+        // the other half of a chunk's pairs is another lane's chunk of the same head
+        const int far_lane = (lane & 16) | ((lane & 15) + (far0 - i0) / 8);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) bad |= top_of(x[m][i], &top);
-    const int e = max(exponent_for(head_max(top, kv.d)), was[1]);
-    put_values<NC>(block, Place{p.head, p.u, p.c, on}, kv.d, now, older, e, was[1], x);
-    if (on && p.u == 0 && p.c == 0) scales[1] = power_of_two(e);
+        for (int i = 0; i < 8; ++i) {
+          to_floats(k_raw[m][i], x[m][i]);
+          if (kPairing == kNoTurn) {
+            look_at(x[m][i], &top, &wild);
+            continue;
+          }
+          const int t = 2 * i + p.c;
+          float other[8];
+          if (kPairing == kChunks) {
+            Raw8<T> far{};
+            if (NC == 1) {
+#pragma unroll
+              for (int c = 0; c < int(sizeof(T) / 2); ++c) {
+                far.w[c].x = __shfl_sync(0xffffffffu, k_raw[m][i].w[c].x, far_lane);
+                far.w[c].y = __shfl_sync(0xffffffffu, k_raw[m][i].w[c].y, far_lane);
+                far.w[c].z = __shfl_sync(0xffffffffu, k_raw[m][i].w[c].z, far_lane);
+                far.w[c].w = __shfl_sync(0xffffffffu, k_raw[m][i].w[c].w, far_lane);
+              }
+            } else if (turns_here && (mine >> (2 * i) & 1u)) {
+              far = load8(rows + t * k.rs + far0, wide);
+            }
+            to_floats(far, other);
+          } else if (kPairing == kNeighbours) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) other[e] = x[m][i][e ^ 1];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int at = i0 + e;
+              const int j = rope.layout == CONDUIT_ROPE_PAIRS ? at ^ 1 : at < rope.half ? at + rope.half : at - rope.half;
+              other[e] = turns_here && (mine >> (2 * i) & 1u) && at < rope.rot ? to_float(rows[t * k.rs + j]) : 0.f;
+            }
+          }
+          if (turns_here) {
+            const float* c8 = cosines + t * kv.d + i0;
+            const float* s8 = sines + t * kv.d + i0;
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+              const float4 c = *reinterpret_cast<const float4*>(c8 + e), s = *reinterpret_cast<const float4*>(s8 + e);
+              const float own[4] = {x[m][i][e], x[m][i][e + 1], x[m][i][e + 2], x[m][i][e + 3]};
+              // the products are rounded before they are added; a dim past rot has cosine 1 and sine 0
+              const float2 a0 = tc::fmul2(make_float2(own[0], own[1]), make_float2(c.x, c.y));
+              const float2 b0 = tc::fmul2(make_float2(other[e], other[e + 1]), make_float2(s.x, s.y));
+              const float2 a1 = tc::fmul2(make_float2(own[2], own[3]), make_float2(c.z, c.w));
+              const float2 b1 = tc::fmul2(make_float2(other[e + 2], other[e + 3]), make_float2(s.z, s.w));
+              const float2 y0 = add_rounded(a0, b0), y1 = add_rounded(a1, b1);
+              x[m][i][e] = y0.x, x[m][i][e + 1] = y0.y, x[m][i][e + 2] = y1.x, x[m][i][e + 3] = y1.y;
+            }
+          }
+          look_at(x[m][i], &top, &wild);
+        }
+      }
+      if (!(wild.x + wild.y == 0.f)) bad = true, mend(x, &top);
+      const int e = max(exponent_for(head_max(top, kv.d)), was[0]);
+      put_keys<NC>(block, here, kv.d, now, older, e, was[0], x);
+      if (on && p.u == 0 && p.c == 0) scales[0] = power_of_two(e);
+    }
+    if (kAhead)
+      load_rows(k, unit + step, k_raw);
+    else
+      load_rows(v, unit, v_raw);
+    {
+      float top = 0.f;
+      float2 wild = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int m = 0; m < NC; ++m)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          to_floats(v_raw[m][i], x[m][i]);
+          look_at(x[m][i], &top, &wild);
+        }
+      if (!(wild.x + wild.y == 0.f)) bad = true, mend(x, &top);
+      const int e = max(exponent_for(head_max(top, kv.d)), was[1]);
+      put_values<NC>(block, here, kv.d, now, older, e, was[1], x);
+      if (on && p.u == 0 && p.c == 0) scales[1] = power_of_two(e);
+    }
   }
   if (bad) flag_status(status, CONDUIT_FLAG_NONFINITE);
 }
@@ -418,14 +497,18 @@ cudaError_t append_with(const PackedDev& kv, const SeqsDev& s, const RopeDev& ro
   const int hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
   const int blocks = (s.max_rows + 15) / 16 + 1;  // a call's rows begin anywhere in a block
   constexpr int kWarps = kThreads / 32;
-  const int kv_grid = int((int64_t(blocks) * groups + kWarps - 1) / kWarps);
   const int64_t q_threads = q.p ? int64_t(s.max_rows) * kv.Hq * units_per_row<VEC>(rope, kv.d) : 0;
   const int q_grid = int((q_threads + kThreads - 1) / kThreads);
-  const dim3 grid(unsigned(kv_grid + q_grid), s.R, kv.L);
+  // Units of a warp: as many as leave eight CTAs for each place of the device, at most 16.
+  const int64_t warps = (int64_t(groups) * kv.L + kWarps - 1) / kWarps;
+  const int64_t most = std::max<int64_t>(1, int64_t(blocks) * s.R * warps / (8 * 3 * 152));
+  const int per = int(std::min<int64_t>({most, warps, 16}));
+  const dim3 grid(unsigned(blocks + q_grid), s.R, unsigned((warps + per - 1) / per));
+  const int smem = kPairing == kNoTurn ? 0 : 2 * kBlockTokens * kv.d * int(sizeof(float));
   if (kv.d <= 128)
-    fp8_append_kernel<T, VEC, kPairing, 1><<<grid, kThreads, 0, stream>>>(kv, s, rope, kv_grid, blocks, wide, k, v, q, q_out, status);
+    fp8_append_kernel<T, VEC, kPairing, 1><<<grid, kThreads, smem, stream>>>(kv, s, rope, blocks, wide, k, v, q, q_out, status);
   else
-    fp8_append_kernel<T, VEC, kPairing, 2><<<grid, kThreads, 0, stream>>>(kv, s, rope, kv_grid, blocks, wide, k, v, q, q_out, status);
+    fp8_append_kernel<T, VEC, kPairing, 2><<<grid, kThreads, smem, stream>>>(kv, s, rope, blocks, wide, k, v, q, q_out, status);
   count_launches(1);
   return cudaGetLastError();
 }
