@@ -8,10 +8,13 @@
 // values: both have to be seen whole before the first code. Lane 16 c + u has dims 8 u .. 8 u + 7
 // (and, past 128 dims, 8 (u + 16) ..) of the tokens of parity c, so a row is read in one piece by
 // 16 lanes; the codes of a value column meet in pairs of lanes that swap half of their dims. A CTA stays with a
-// block of tokens over its heads and layers: cosines and signed sines of the block's tokens lie in shared memory, dim by dim,
-// and the next unit's keys are on their way while a unit's values are packed.
+// block of tokens over its heads and layers: cosines and signed sines of the block's tokens lie in shared memory, dim by dim.
+// Rows pass through shared memory too, each of a warp's two buffers filled again as soon as it has been read: the values of
+// a unit are on their way while its keys are packed, the next unit's keys meanwhile (in registers: 316 us for append and read of
+// 28 layers of 8 192 tokens, 281 so).
 // Bound: the rows once and 2 d + 1 bytes a token and head of the cache.
 #include <algorithm>
+#include <type_traits>
 
 #include "fp8.cuh"
 #include "rotate.cuh"
@@ -82,7 +85,8 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float by) {
 // K: each lane has its chunk of eight tokens of parity c, x[i] of token 2 i + c.
 // Writes codes and scale of one head's keys. `was`: exponent of the earlier tokens' scale, or kLeastExp;
 // older: earlier tokens (bits).
-template <int NC>
+// kWhole: all of them, so that nothing was there before.
+template <int NC, bool kWhole>
 __device__ __forceinline__ void put_keys(uint8_t* block, const Place& p, int d, uint32_t now, uint32_t older, int e,
                                          int was, const float (&x)[NC][8][8]) {
   const float down = power_of_two(-e), by = power_of_two(max(was - e, -126));
@@ -95,7 +99,7 @@ __device__ __forceinline__ void put_keys(uint8_t* block, const Place& p, int d, 
     for (int i = 0; i < 8; ++i) {
       const int t = 2 * i + p.c;
       uint2* to = reinterpret_cast<uint2*>(at + (t >> 3) * 8 * d + (t & 7) * 16);
-      if (now >> t & 1u) {
+      if (kWhole || (now >> t & 1u)) {
         float y[8];
 #pragma unroll
         for (int k = 0; k < 8; k += 2) {
@@ -113,16 +117,16 @@ __device__ __forceinline__ void put_keys(uint8_t* block, const Place& p, int d, 
 
 // The same of the values, whose rows are dims: byte 4 a + 2 b + c of a row is token 8 b + 2 a + c, so a
 // lane's codes of tokens 2 a + c and 2 a + 8 + c are the halfword (a, c) and its partner's the other.
-template <int NC>
+template <int NC, bool kWhole>
 __device__ __forceinline__ void put_values(uint8_t* block, const Place& p, int d, uint32_t now, uint32_t older, int e,
                                            int was, const float (&x)[NC][8][8]) {
   constexpr unsigned kAll = 0xffffffffu;
   const float down = power_of_two(-e), by = power_of_two(max(was - e, -126));
-  const bool whole = now == 0xFFFFu;
   uint32_t mine[4], past[4];  // bytes of word a that the call writes, and that earlier tokens have
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     mine[a] = past[a] = 0;
+    if (kWhole) continue;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int t = 8 * (k >> 1) + 2 * a + (k & 1);
@@ -161,7 +165,7 @@ __device__ __forceinline__ void put_values(uint8_t* block, const Place& p, int d
       uint4 y = make_uint4(__byte_perm(even[0], odd[0], 0x5140), __byte_perm(even[0], odd[0], 0x7362),
                            __byte_perm(even[1], odd[1], 0x5140), __byte_perm(even[1], odd[1], 0x7362));
       if (!p.on || u >= d / 8) continue;
-      if (!whole) {
+      if (!kWhole) {
         uint4 old = rows[k];
         if (was < e && older) {
           auto mixed = [&](uint32_t o, int a) { return (rescaled(o, by) & past[a]) | (o & ~past[a]); };
@@ -177,10 +181,11 @@ __device__ __forceinline__ void put_values(uint8_t* block, const Place& p, int d
 
 // CTAs below kv_grid: a block of the call's tokens, its heads and layers dealt out over the warps of grid.z. Those after
 // them rotate queries, a unit of pairs per thread, and walk over the layers.
-template <typename T, int VEC, int kPairing, int NC>
-__global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 1)
-    fp8_append_kernel(PackedDev kv, SeqsDev s, RopeDev rope, int kv_grid, bool wide, RowsDev k, RowsDev v,
-                      RowsDev q, RowsDev q_out, int32_t* status) {
+template <typename T, bool kWide, int kPairing, int NC>
+__global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 2)
+    fp8_append_kernel(PackedDev kv, SeqsDev s, RopeDev rope, int kv_grid, RowsDev k, RowsDev v, RowsDev q, RowsDev q_out,
+                      int32_t* status) {
+  constexpr int VEC = kWide ? 16 / int(sizeof(T)) : 1;
   const int r = blockIdx.y;
   const int t0 = s.row_off[r], n = s.row_off[r + 1] - t0, len = s.len[r];
   if (n == 0) return;
@@ -238,7 +243,8 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 1)
   const uint32_t older = (1u << before) - 1u;
   const int64_t row0 = int64_t(t0) + (first - begin);  // row of the call of the block's token 0
 
-  extern __shared__ __align__(16) float turns[];  // [16][d] cosines, then signed sines
+  // [16][2][d / 8][4] cosines, then signed sines: dims 8 u + 4 h .. of a token at [h][u], so that the lanes of a row read side by side
+  extern __shared__ __align__(16) float turns[];
   float *cosines = turns, *sines = turns + kBlockTokens * kv.d;
   if (kPairing != kNoTurn) {
     const int chunks = kv.d / 8;
@@ -257,136 +263,159 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 1)
       for (int k = 0; k < 8; ++k) c8[k] = cs[k].x, s8[k] = cs[k].y;
 #pragma unroll
       for (int k = 0; k < 8; k += 4) {
-        *reinterpret_cast<float4*>(cosines + t * kv.d + i0 + k) = make_float4(c8[k], c8[k + 1], c8[k + 2], c8[k + 3]);
-        *reinterpret_cast<float4*>(sines + t * kv.d + i0 + k) = make_float4(s8[k], s8[k + 1], s8[k + 2], s8[k + 3]);
+        const int at = t * kv.d + (k * kv.d + 4 * i0) / 8;
+        *reinterpret_cast<float4*>(cosines + at) = make_float4(c8[k], c8[k + 1], c8[k + 2], c8[k + 3]);
+        *reinterpret_cast<float4*>(sines + at) = make_float4(s8[k], s8[k + 1], s8[k + 2], s8[k + 3]);
       }
     }
     __syncthreads();
   }
 
-  constexpr bool kAhead = NC == 1 && sizeof(T) == 2;  // registers for a unit's keys beside another's values
   const uint32_t mine = (now >> p.c) & 0x5555u;       // bit 2 i: token 2 i + c
-  const int units = groups * kv.L, step = gridDim.z * (kThreads / 32);
-  int unit = blockIdx.z * (kThreads / 32) + threadIdx.x / 32;
+  const int units = groups * kv.L, step = gridDim.z * (kThreads / 32), first_unit = blockIdx.z * (kThreads / 32) + threadIdx.x / 32;
+  // this warp's rows: 16 tokens of a unit's keys, and of its values
+  const int row_bytes = hp * kv.d * int(sizeof(T));
+  uint8_t* rows_at = reinterpret_cast<uint8_t*>(turns) + (kPairing == kNoTurn ? 0 : 2 * kBlockTokens * kv.d * int(sizeof(float))) +
+                     threadIdx.x / 32 * 2 * kBlockTokens * row_bytes;
   auto head_of = [&](int n) { return n % groups * hp + p.head; };
-  auto load_rows = [&](const RowsDev& x, int n, Raw8<T> (&raw)[NC][8]) {
-    const int head = head_of(n), l = n / groups;
-    const bool on = n < units && p.on && head < kv.Hkv;
-    const T* row = static_cast<const T*>(x.p) + l * x.ls + (on ? head : 0) * x.hs + (row0 + p.c) * x.rs + 8 * p.u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i, row += 2 * x.rs)
-#pragma unroll
-      for (int m = 0; m < NC; ++m) {
-        raw[m][i] = Raw8<T>{};
-        if ((mine >> (2 * i) & 1u) && on && p.u + 16 * m < kv.d / 8) raw[m][i] = load8(row + 128 * m, wide);
-      }
-  };
   bool bad = false;
-  Raw8<T> k_raw[NC][8], v_raw[NC][8];
-  if (kAhead) load_rows(k, unit, k_raw);
-  for (; unit < units; unit += step) {
-    const int head = head_of(unit), l = unit / groups;
-    const bool on = p.on && head < kv.Hkv;
-    const Place here{p.head, p.u, p.c, on};
-    uint8_t* block = fp8_block(kv, l, on ? head : 0, page, int(first));
-    float* scales = reinterpret_cast<float*>(block + 32 * kv.d);
-    int was[2] = {kLeastExp, kLeastExp};
-    if (older) {
-      const float2 w = *reinterpret_cast<const float2*>(scales);
-      was[0] = exponent_of(w.x), was[1] = exponent_of(w.y);
-    }
-    if (!kAhead) load_rows(k, unit, k_raw);
-    if (kAhead) load_rows(v, unit, v_raw);
-    float x[NC][8][8];
-    {
-      const T* rows = static_cast<const T*>(k.p) + l * k.ls + (on ? head : 0) * k.hs + row0 * k.rs;
-      float top = 0.f;
-      float2 wild = make_float2(0.f, 0.f);
+  auto work = [&](auto all) {
+    constexpr bool kWhole = decltype(all)::value;  // the call writes every token of the block
+    // dim i0 of this lane's token 2 i + c and head (a lane without a chunk is at the first one; what it reads is left out)
+    auto row_at = [&](int which, int i, int i0) {
+      return reinterpret_cast<T*>(rows_at + (which * kBlockTokens + 2 * i + p.c) * row_bytes) + p.head * kv.d + i0;
+    };
+    auto copy_rows = [&](const RowsDev& x, int which, int n) {
+      const int head = head_of(n), l = n / groups;
+      if (n < units && p.on && head < kv.Hkv) {
+        const T* row = static_cast<const T*>(x.p) + l * x.ls + head * x.hs + (row0 + p.c) * x.rs + 8 * p.u;
 #pragma unroll
-      for (int m = 0; m < NC; ++m) {
-        const int i0 = 8 * (p.u + 16 * m);
-        const int far0 = i0 >= rope.rot ? i0 : i0 < rope.half ? i0 + rope.half : i0 - rope.half;
-        const bool turns_here = kPairing != kNoTurn && i0 < rope.rot && on;
-        // the other half of a chunk's pairs is another lane's chunk of the same head
-        const int far_lane = (lane & 16) | ((lane & 15) + (far0 - i0) / 8);
+        for (int i = 0; i < 8; ++i, row += 2 * x.rs) {
+          if (!kWhole && !(mine >> (2 * i) & 1u)) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          to_floats(k_raw[m][i], x[m][i]);
-          if (kPairing == kNoTurn) {
-            look_at(x[m][i], &top, &wild);
-            continue;
-          }
-          const int t = 2 * i + p.c;
-          float other[8];
-          if (kPairing == kChunks) {
-            Raw8<T> far{};
-            if (NC == 1) {
+          for (int m = 0; m < NC; ++m) {
+            if (NC > 1 && p.u + 16 * m >= kv.d / 8) continue;
+            T* to = row_at(which, i, 8 * (p.u + 16 * m));
+            if (kWide) {
 #pragma unroll
-              for (int c = 0; c < int(sizeof(T) / 2); ++c) {
-                far.w[c].x = __shfl_sync(0xffffffffu, k_raw[m][i].w[c].x, far_lane);
-                far.w[c].y = __shfl_sync(0xffffffffu, k_raw[m][i].w[c].y, far_lane);
-                far.w[c].z = __shfl_sync(0xffffffffu, k_raw[m][i].w[c].z, far_lane);
-                far.w[c].w = __shfl_sync(0xffffffffu, k_raw[m][i].w[c].w, far_lane);
-              }
-            } else if (turns_here && (mine >> (2 * i) & 1u)) {
-              far = load8(rows + t * k.rs + far0, wide);
-            }
-            to_floats(far, other);
-          } else if (kPairing == kNeighbours) {
+              for (int c = 0; c < int(sizeof(T) / 2); ++c)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to) + 16 * c),
+                             "l"(row + 128 * m + 16 / sizeof(T) * c)
+                             : "memory");
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) other[e] = x[m][i][e ^ 1];
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int at = i0 + e;
-              const int j = rope.layout == CONDUIT_ROPE_PAIRS ? at ^ 1 : at < rope.half ? at + rope.half : at - rope.half;
-              other[e] = turns_here && (mine >> (2 * i) & 1u) && at < rope.rot ? to_float(rows[t * k.rs + j]) : 0.f;
+              for (int e = 0; e < 8; ++e) to[e] = row[128 * m + e];
             }
           }
-          if (turns_here) {
-            const float* c8 = cosines + t * kv.d + i0;
-            const float* s8 = sines + t * kv.d + i0;
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-              const float4 c = *reinterpret_cast<const float4*>(c8 + e), s = *reinterpret_cast<const float4*>(s8 + e);
-              const float own[4] = {x[m][i][e], x[m][i][e + 1], x[m][i][e + 2], x[m][i][e + 3]};
-              // the products are rounded before they are added; a dim past rot has cosine 1 and sine 0
-              const float2 a0 = tc::fmul2(make_float2(own[0], own[1]), make_float2(c.x, c.y));
-              const float2 b0 = tc::fmul2(make_float2(other[e], other[e + 1]), make_float2(s.x, s.y));
-              const float2 a1 = tc::fmul2(make_float2(own[2], own[3]), make_float2(c.z, c.w));
-              const float2 b1 = tc::fmul2(make_float2(other[e + 2], other[e + 3]), make_float2(s.z, s.w));
-              const float2 y0 = add_rounded(a0, b0), y1 = add_rounded(a1, b1);
-              x[m][i][e] = y0.x, x[m][i][e + 1] = y0.y, x[m][i][e + 2] = y1.x, x[m][i][e + 3] = y1.y;
-            }
-          }
-          look_at(x[m][i], &top, &wild);
         }
       }
-      if (!(wild.x + wild.y == 0.f)) bad = true, mend(x, &top);
-      const int e = max(exponent_for(head_max(top, kv.d)), was[0]);
-      put_keys<NC>(block, here, kv.d, now, older, e, was[0], x);
-      if (on && p.u == 0 && p.c == 0) scales[0] = power_of_two(e);
-    }
-    if (kAhead)
-      load_rows(k, unit + step, k_raw);
-    else
-      load_rows(v, unit, v_raw);
-    {
-      float top = 0.f;
-      float2 wild = make_float2(0.f, 0.f);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto rows_here = [&] {  // all but the last rows that this warp has asked for
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+      __syncwarp();
+    };
+    copy_rows(k, 0, first_unit);
+    copy_rows(v, 1, first_unit);
+#pragma unroll 1
+    for (int unit = first_unit; unit < units; unit += step) {
+      const int head = head_of(unit), l = unit / groups;
+      const bool on = p.on && head < kv.Hkv;
+      const Place here{p.head, p.u, p.c, on};
+      uint8_t* block = fp8_block(kv, l, on ? head : 0, page, int(first));
+      float* scales = reinterpret_cast<float*>(block + 32 * kv.d);
+      int was[2] = {kLeastExp, kLeastExp};
+      if (!kWhole && older) {
+        const float2 w = *reinterpret_cast<const float2*>(scales);
+        was[0] = exponent_of(w.x), was[1] = exponent_of(w.y);
+      }
+      float x[NC][8][8];
+      // A lane's numbers of a token and chunk; zeros where the call has none.
+      auto read = [&](int which, int m, int i, float (&y)[8]) {
+        Raw8<T> raw{};
+        const int u = p.u + 16 * m;
+        if ((kWhole || (mine >> (2 * i) & 1u)) && (NC == 1 || u < kv.d / 8)) raw = load8(row_at(which, i, p.on ? 8 * u : 0), true);
+        to_floats(raw, y);
+      };
+      {
+        float top = 0.f;
+        float2 wild = make_float2(0.f, 0.f);
+        rows_here();
 #pragma unroll
-      for (int m = 0; m < NC; ++m)
+        for (int m = 0; m < NC; ++m) {
+          const int i0 = p.on ? 8 * (p.u + 16 * m) : 0;
+          const int far0 = i0 < rope.half ? i0 + rope.half : i0 - rope.half;
+          const bool turns_here = kPairing != kNoTurn && i0 < rope.rot && (NC == 1 || i0 < kv.d);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          to_floats(v_raw[m][i], x[m][i]);
-          look_at(x[m][i], &top, &wild);
+          for (int i = 0; i < 8; ++i) {
+            read(0, m, i, x[m][i]);
+            if (turns_here && (kWhole || (mine >> (2 * i) & 1u))) {
+              const int t = 2 * i + p.c;
+              float other[8];
+              if (kPairing == kChunks) {
+                to_floats(load8(row_at(0, i, far0), true), other);
+              } else if (kPairing == kNeighbours) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) other[e] = x[m][i][e ^ 1];
+              } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  const int at = i0 + e;
+                  const int j = rope.layout == CONDUIT_ROPE_PAIRS ? at ^ 1 : at < rope.half ? at + rope.half : at - rope.half;
+                  other[e] = at < rope.rot ? to_float(*row_at(0, i, j)) : 0.f;
+                }
+              }
+              const float* c8 = cosines + t * kv.d + i0 / 2;
+              const float* s8 = sines + t * kv.d + i0 / 2;
+#pragma unroll
+              for (int e = 0; e < 8; e += 4) {
+                const float4 c = *reinterpret_cast<const float4*>(c8 + e * kv.d / 8), s = *reinterpret_cast<const float4*>(s8 + e * kv.d / 8);
+                const float own[4] = {x[m][i][e], x[m][i][e + 1], x[m][i][e + 2], x[m][i][e + 3]};
+                // the products are rounded before they are added; a dim past rot has cosine 1 and sine 0
+                const float2 a0 = tc::fmul2(make_float2(own[0], own[1]), make_float2(c.x, c.y));
+                const float2 b0 = tc::fmul2(make_float2(other[e], other[e + 1]), make_float2(s.x, s.y));
+                const float2 a1 = tc::fmul2(make_float2(own[2], own[3]), make_float2(c.z, c.w));
+                const float2 b1 = tc::fmul2(make_float2(other[e + 2], other[e + 3]), make_float2(s.z, s.w));
+                const float2 y0 = add_rounded(a0, b0), y1 = add_rounded(a1, b1);
+                x[m][i][e] = y0.x, x[m][i][e + 1] = y0.y, x[m][i][e + 2] = y1.x, x[m][i][e + 3] = y1.y;
+              }
+            }
+            look_at(x[m][i], &top, &wild);
+          }
         }
-      if (!(wild.x + wild.y == 0.f)) bad = true, mend(x, &top);
-      const int e = max(exponent_for(head_max(top, kv.d)), was[1]);
-      put_values<NC>(block, here, kv.d, now, older, e, was[1], x);
-      if (on && p.u == 0 && p.c == 0) scales[1] = power_of_two(e);
+        __syncwarp();
+        copy_rows(k, 0, unit + step);
+        if (!(wild.x + wild.y == 0.f)) bad |= on, mend(x, &top);
+        if (!on) top = 0.f;
+        const int e = max(exponent_for(head_max(top, kv.d)), was[0]);
+        put_keys<NC, kWhole>(block, here, kv.d, now, older, e, was[0], x);
+        if (on && p.u == 0 && p.c == 0) scales[0] = power_of_two(e);
+      }
+      {
+        float top = 0.f;
+        float2 wild = make_float2(0.f, 0.f);
+        rows_here();
+#pragma unroll
+        for (int m = 0; m < NC; ++m)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            read(1, m, i, x[m][i]);
+            look_at(x[m][i], &top, &wild);
+          }
+        __syncwarp();
+        copy_rows(v, 1, unit + step);
+        if (!(wild.x + wild.y == 0.f)) bad |= on, mend(x, &top);
+        if (!on) top = 0.f;
+        const int e = max(exponent_for(head_max(top, kv.d)), was[1]);
+        put_values<NC, kWhole>(block, here, kv.d, now, older, e, was[1], x);
+        if (on && p.u == 0 && p.c == 0) scales[1] = power_of_two(e);
+      }
     }
-  }
+  };
+  if (now == 0xFFFFu)
+    work(std::true_type{});
+  else
+    work(std::false_type{});
   if (bad) flag_status(status, CONDUIT_FLAG_NONFINITE);
 }
 
@@ -490,37 +519,40 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-template <typename T, int VEC, int kPairing>
-cudaError_t append_with(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, bool wide, const RowsDev& k,
-                        const RowsDev& v, const RowsDev& q, const RowsDev& q_out, int32_t* status,
-                        cudaStream_t stream) {
+template <typename T, bool kWide, int kPairing>
+cudaError_t append_with(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, const RowsDev& k, const RowsDev& v,
+                        const RowsDev& q, const RowsDev& q_out, int32_t* status, cudaStream_t stream) {
   const int hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
   const int blocks = (s.max_rows + 15) / 16 + 1;  // a call's rows begin anywhere in a block
-  constexpr int kWarps = kThreads / 32;
+  constexpr int kWarps = kThreads / 32, VEC = kWide ? 16 / int(sizeof(T)) : 1;
   const int64_t q_threads = q.p ? int64_t(s.max_rows) * kv.Hq * units_per_row<VEC>(rope, kv.d) : 0;
   const int q_grid = int((q_threads + kThreads - 1) / kThreads);
-  // Units of a warp: as many as leave eight CTAs for each place of the device, at most 16.
+  // Units of a warp: as many as leave four CTAs for each place of the device, at most seven (28 layers of 8 192 tokens, append
+  // and read: four 300 us, seven 282, fourteen 284). Three CTAs an SM: with four, which spill, 327 us, with two 286.
   const int64_t warps = (int64_t(groups) * kv.L + kWarps - 1) / kWarps;
-  const int64_t most = std::max<int64_t>(1, int64_t(blocks) * s.R * warps / (8 * 3 * 152));
-  const int per = int(std::min<int64_t>({most, warps, 16}));
+  const int64_t most = std::max<int64_t>(1, int64_t(blocks) * s.R * warps / (4 * 3 * 152));
+  const int per = int(std::min<int64_t>({most, warps, 7}));
   const dim3 grid(unsigned(blocks + q_grid), s.R, unsigned((warps + per - 1) / per));
-  const int smem = kPairing == kNoTurn ? 0 : 2 * kBlockTokens * kv.d * int(sizeof(float));
-  if (kv.d <= 128)
-    fp8_append_kernel<T, VEC, kPairing, 1><<<grid, kThreads, smem, stream>>>(kv, s, rope, blocks, wide, k, v, q, q_out, status);
-  else
-    fp8_append_kernel<T, VEC, kPairing, 2><<<grid, kThreads, smem, stream>>>(kv, s, rope, blocks, wide, k, v, q, q_out, status);
-  count_launches(1);
-  return cudaGetLastError();
+  const int smem = (kPairing == kNoTurn ? 0 : 2 * kBlockTokens * kv.d * int(sizeof(float))) +
+                   kWarps * 2 * kBlockTokens * hp * kv.d * int(sizeof(T));
+  auto run = [&](auto kernel) {
+    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (err) return err;
+    kernel<<<grid, kThreads, smem, stream>>>(kv, s, rope, blocks, k, v, q, q_out, status);
+    count_launches(1);
+    return cudaGetLastError();
+  };
+  return kv.d <= 128 ? run(fp8_append_kernel<T, kWide, kPairing, 1>) : run(fp8_append_kernel<T, kWide, kPairing, 2>);
 }
 
-template <typename T, int VEC>
-cudaError_t append(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, bool wide, const RowsDev& k,
-                   const RowsDev& v, const RowsDev& q, const RowsDev& q_out, int32_t* status, cudaStream_t stream) {
+template <typename T, bool kWide>
+cudaError_t append(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, const RowsDev& k, const RowsDev& v,
+                   const RowsDev& q, const RowsDev& q_out, int32_t* status, cudaStream_t stream) {
   switch (pairing(rope)) {
-    case kNoTurn: return append_with<T, VEC, kNoTurn>(kv, s, rope, wide, k, v, q, q_out, status, stream);
-    case kChunks: return append_with<T, VEC, kChunks>(kv, s, rope, wide, k, v, q, q_out, status, stream);
-    case kNeighbours: return append_with<T, VEC, kNeighbours>(kv, s, rope, wide, k, v, q, q_out, status, stream);
-    default: return append_with<T, VEC, kAnywhere>(kv, s, rope, wide, k, v, q, q_out, status, stream);
+    case kNoTurn: return append_with<T, kWide, kNoTurn>(kv, s, rope, k, v, q, q_out, status, stream);
+    case kChunks: return append_with<T, kWide, kChunks>(kv, s, rope, k, v, q, q_out, status, stream);
+    case kNeighbours: return append_with<T, kWide, kNeighbours>(kv, s, rope, k, v, q, q_out, status, stream);
+    default: return append_with<T, kWide, kAnywhere>(kv, s, rope, k, v, q, q_out, status, stream);
   }
 }
 
@@ -529,14 +561,15 @@ cudaError_t append(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, b
 cudaError_t launch_fp8_append(const PackedDev& kv, const SeqsDev& s, const RopeDev& rope, int dtype, const RowsDev& k,
                               const RowsDev& v, const RowsDev& q, const RowsDev& q_out, int32_t* status,
                               cudaStream_t stream) {
+  // 16-byte copies where every row of the call allows them (queries: and their pairs come in whole chunks)
   const int vec = dtype == CONDUIT_BF16 ? 8 : 4;
-  const bool wide = rows_aligned(k, vec) && rows_aligned(v, vec);
-  const bool wide_q = q.p && dims_in_chunks(rope, kv.d, vec) && rows_aligned(q, vec) && rows_aligned(q_out, vec);
+  const bool wide = rows_aligned(k, vec) && rows_aligned(v, vec) &&
+                    (!q.p || (dims_in_chunks(rope, kv.d, vec) && rows_aligned(q, vec) && rows_aligned(q_out, vec)));
   if (dtype == CONDUIT_BF16)
-    return wide_q ? append<__nv_bfloat16, 8>(kv, s, rope, wide, k, v, q, q_out, status, stream)
-                  : append<__nv_bfloat16, 1>(kv, s, rope, wide, k, v, q, q_out, status, stream);
-  return wide_q ? append<float, 4>(kv, s, rope, wide, k, v, q, q_out, status, stream)
-                : append<float, 1>(kv, s, rope, wide, k, v, q, q_out, status, stream);
+    return wide ? append<__nv_bfloat16, true>(kv, s, rope, k, v, q, q_out, status, stream)
+                : append<__nv_bfloat16, false>(kv, s, rope, k, v, q, q_out, status, stream);
+  return wide ? append<float, true>(kv, s, rope, k, v, q, q_out, status, stream)
+              : append<float, false>(kv, s, rope, k, v, q, q_out, status, stream);
 }
 
 cudaError_t launch_fp8_read(const PackedDev& kv, const int32_t* first, const KvDev& dst, const BatchDev& b,
