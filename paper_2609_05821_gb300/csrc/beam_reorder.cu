@@ -7,6 +7,8 @@
 // that an arbitrary map of beams asks for. What the copy reads beside that, lengths of parents and places of begun pages, the
 // same launch leaves as it is.
 // Bound: the rows in use, read and written once; small calls by the chain parent, length, page, rows.
+#include <algorithm>
+
 #include "beam.cuh"
 
 namespace conduit {
@@ -64,28 +66,37 @@ __global__ void __launch_bounds__(kThreads)
     return;
   }
   if (!rest) return;
-  // 16 bytes of a part of the begun page
-  int per_head = 0;
-  for (int k = 0; k < pool.parts; ++k) per_head += pool.part[k].bytes / 16;
-  const int64_t lin = int64_t(blockIdx.x - 1) * kThreads + threadIdx.x;
-  const int64_t unit = lin / per_head;
-  int at = int(lin % per_head), k = 0;
-  while (k + 1 < pool.parts && at >= pool.part[k].bytes / 16) at -= pool.part[k++].bytes / 16;
-  const PagePart part = pool.part[k];
-  const int head = int(unit % pool.heads);
-  const int64_t l = unit / pool.heads;
-  const bool on = l < pool.L && at * 16 < (rest + part.tokens - 1) / part.tokens * part.unit;
-  char* base = part.base + l * part.layer_stride + head * part.head_stride + at * 16;
-  uint4 v[kMost];
+  // the beams that take another one's rows over: (page read, page written)
+  __shared__ int2 moves[kMaxBeams];
+  const uint32_t moved = __ballot_sync(kAll, beam && from != lane);
+  if (threadIdx.x < 32 && (moved >> lane & 1u)) moves[__popc(moved & ((1u << lane) - 1u))] = make_int2(source, to);
+  __syncthreads();
+  const int count = __popc(moved);
+  int used[4], all = 0;  // 16-byte chunks in use of a part of a head's page
 #pragma unroll
-  for (int b = 0; b < kMost; ++b) {
-    const int s = __shfl_sync(kAll, source, b), p = __shfl_sync(kAll, from, b);
-    if (b < width && p != b && on) v[b] = *reinterpret_cast<const uint4*>(base + s * part.page_stride);
+  for (int k = 0; k < 4; ++k) {
+    used[k] = k < pool.parts ? ((rest + pool.part[k].tokens - 1) / pool.part[k].tokens * pool.part[k].unit + 15) / 16 : 0;
+    all += used[k];
   }
+  // A CTA stays for several heads: the chain of loads above costs as much as a head's rows (a CTA for each 256 chunks of the
+  // page: 73 us for 32 groups of 8 beams, 28 layers).
+  for (int u = blockIdx.x - 1; u < pool.L * pool.heads; u += gridDim.x - 1) {
+    const int l = u / pool.heads, head = u % pool.heads;
+    for (int c = threadIdx.x; c < all; c += kThreads) {
+      int at = c, k = 0;
 #pragma unroll
-  for (int b = 0; b < kMost; ++b) {
-    const int t = __shfl_sync(kAll, to, b), p = __shfl_sync(kAll, from, b);
-    if (b < width && p != b && on) *reinterpret_cast<uint4*>(base + t * part.page_stride) = v[b];
+      for (int j = 0; j < 3; ++j)
+        if (k == j && at >= used[j]) at -= used[j], ++k;
+      const PagePart& part = pool.part[k];
+      char* base = part.base + l * part.layer_stride + head * part.head_stride + int64_t(at) * 16;
+      uint4 v[kMost];
+#pragma unroll
+      for (int b = 0; b < kMost; ++b)
+        if (b < count) v[b] = *reinterpret_cast<const uint4*>(base + moves[b].x * part.page_stride);
+#pragma unroll
+      for (int b = 0; b < kMost; ++b)
+        if (b < count) *reinterpret_cast<uint4*>(base + moves[b].y * part.page_stride) = v[b];
+    }
   }
 }
 
@@ -93,10 +104,9 @@ __global__ void __launch_bounds__(kThreads)
 
 cudaError_t launch_reorder(const PagedPool& pool, int groups, int width, const int32_t* parent, const int32_t* home,
                            int32_t* page_table, int32_t* len, int32_t* status, cudaStream_t stream) {
-  int64_t per_head = 0;
-  for (int k = 0; k < pool.parts; ++k) per_head += pool.part[k].bytes / 16;
-  const int64_t threads = per_head * pool.heads * pool.L;
-  const dim3 grid(unsigned(1 + (threads + kThreads - 1) / kThreads), groups);
+  // about three waves of CTAs
+  const int64_t units = int64_t(pool.L) * pool.heads, most = std::max(1, 3 * 4 * 152 / groups);
+  const dim3 grid(unsigned(1 + std::min(units, most)), groups);
   if (width <= 4)
     reorder_kernel<4><<<grid, kThreads, 0, stream>>>(pool, width, parent, home, page_table, len, status);
   else if (width <= 8)

@@ -239,9 +239,7 @@ conduit_status reorder(PagedPool* pool, int32_t groups, int32_t width, const int
                         static_cast<const void*>(page_table), static_cast<const void*>(len)})
     if (!p || reinterpret_cast<uintptr_t>(p) % 4)
       return fail(CONDUIT_ERR_INVALID_ARG, "parent, home, page_table and len are required, 4-byte aligned");
-  int64_t chunks = 0;
-  for (int k = 0; k < pool->parts; ++k) chunks += pool->part[k].bytes / 16;
-  if (chunks * pool->heads * pool->L > int64_t(1) << 38) return fail(CONDUIT_ERR_UNSUPPORTED, "a page holds too much");
+  if (int64_t(pool->L) * pool->heads > INT32_MAX) return fail(CONDUIT_ERR_UNSUPPORTED, "too many layers and heads");
   cudaError_t err = launch_reorder(*pool, groups, width, parent, home, page_table, len, status, static_cast<cudaStream_t>(stream));
   if (err) return cuda_fail(err, "reorder");
   return CONDUIT_OK;
