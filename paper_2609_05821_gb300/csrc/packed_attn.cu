@@ -462,8 +462,11 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
   // 56 / 79, 89 / 75; 64 of about 4 000 98 / 137, 159 / 133, 285 / 131).
   const int64_t columns = int64_t(s.max_rows) * kv.G;
   const double units = double(kv.L) * s.R * kv.Hkv;
-  const double warp_us = 8. + units * ((columns + kCols - 1) / kCols) * (3.5 + 0.009 * most) / 304.;
-  const double tc_us = 18. + units * (11. + (most < kExactBelow ? 2.5 : 1.35) / 128. * most) / 152.;
+  // The same with 8 bits: 5.8 ns a key (16 requests of about 4 000, 3 and 4 and 6 rows 35 / 58, 39 / 54, 65 / 62; 64 of about
+  // 1 000 37 / 56, 45 / 57, 66 / 53; 64 of about 4 000 104 / 152, 131 / 154, 197 / 175; 16 of about 16 000 101 / 143, 139 / 155,
+  // 158 / 143).
+  const double warp_us = 8. + units * ((columns + kCols - 1) / kCols) * (3.5 + (bits == 8 ? 0.0058 : 0.009) * most) / 304.;
+  const double tc_us = 18. + units * (11. + (bits == 4 && most < kExactBelow ? 2.5 : 1.35) / 128. * most) / 152.;
   const bool few = columns <= kCols || (columns <= 64 && warp_us < tc_us);
   p.kernel = !mma ? kAttnSimt : few ? kAttnMma : kAttnTc;
   const int step = p.kernel == kAttnSimt ? 64 : 256;  // least keys of a chunk
@@ -483,16 +486,25 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
       singles += tiles & 1;
     }
     const int64_t heads = int64_t(kv.L) * kv.Hkv, items = heads * (pairs + singles);
-    const double keys = (most < kExactBelow ? 3.3 : 1.8) / 128. * most, all = double(kv.L) * s.T * kv.Hq;
+    const double per = bits == 8 ? 1.9 : most < kExactBelow ? 3.3 : 1.8;
+    const double keys = per / 128. * most, all = double(kv.L) * s.T * kv.Hq;
     auto join = [&](int64_t c, double cols) { return c > 1 ? 5. + c * cols * kv.d * 12. / 5e6 : 0.; };
+    // 8 bits: the mean of that and of the same contexts with lengths spread evenly up to max_len, half as many keys on as many SMs,
+    // so that unequal lengths find CTAs to even them out (16 requests of 2 000-30 000 tokens, 4 rows: 210 us in two chunks, 155 so).
+    auto spread = [&](int64_t n_pairs, int64_t n_singles, int64_t cp, int64_t cs, double tp, double ts) {
+      const double even = pass_time(n_pairs * cp, n_singles * cs, tp, ts);
+      if (bits != 8) return even;
+      const double work = n_pairs * (0.5 * (cp + 1)) * tp + n_singles * (0.5 * (cs + 1)) * ts;
+      return 0.5 * (even + std::max(work / 152. + 0.5 * (n_pairs ? tp : ts), n_pairs ? tp : ts));
+    };
     double best = 0;
     for (int64_t c = 1; c <= std::min<int64_t>(largest, 64) && (c == 1 || items * c <= 8 * 152); ++c) {
       const double tp = 11. + keys / c, ts = 11. + 0.75 * keys / c;
-      const double us = pass_time(heads * pairs * c, heads * singles * c, tp, ts) + join(c, all);
+      const double us = spread(heads * pairs, heads * singles, c, c, tp, ts) + join(c, all);
       if (c == 1 || us < best) best = us, p.chunks = p.last_chunks = int(c);
     }
     for (int64_t c = 2; pairs && singles && items <= 8 * 152 && c <= std::min<int64_t>(largest, 8); ++c) {
-      const double us = pass_time(heads * pairs, heads * singles * c, 11. + keys, 11. + 0.75 * keys / c) +
+      const double us = spread(heads * pairs, heads * singles, 1, c, 11. + keys, 11. + 0.75 * keys / c) +
                         join(c, double(heads * singles * 128));
       if (us < best) best = us, p.chunks = 1, p.last_chunks = int(c);
     }
