@@ -738,7 +738,9 @@ conduit_status conduit_beam_select(const void* logits, int32_t dtype, int64_t ro
  *  page_table  device int32 [G width][max_pages_per_req], the cache's own, written
  *  len         device int32 [G width], written
  * A beam that starts anew has the row home[b] in page_table and length 0; a prompt appended to one beam of
- * a group reaches the others by parent = that beam. All beams that are continued must have one length per
+ * a group reaches the others by parent = that beam. Lengths may be cut for a whole group at a time, to whole pages, and
+ * the group be reordered (each beam its own parent, if nothing else) before the next append: entries past the length are
+ * home's only then. All beams that are continued must have one length per
  * group, and the begun page of each must be its own. A group where that does not hold, or with a parent
  * outside of the group, a length outside [0, capacity] or a begun page outside [0, num_pages), is left as it is
  * and sets CONDUIT_FLAG_INDEX. width in [1, 32]. G = 0 is no work.

@@ -239,6 +239,7 @@ conduit_status reorder(PagedPool* pool, int32_t groups, int32_t width, const int
                         static_cast<const void*>(page_table), static_cast<const void*>(len)})
     if (!p || reinterpret_cast<uintptr_t>(p) % 4)
       return fail(CONDUIT_ERR_INVALID_ARG, "parent, home, page_table and len are required, 4-byte aligned");
+  if (home == page_table) return fail(CONDUIT_ERR_INVALID_ARG, "home must be another table than page_table");
   if (int64_t(pool->L) * pool->heads > INT32_MAX) return fail(CONDUIT_ERR_UNSUPPORTED, "too many layers and heads");
   cudaError_t err = launch_reorder(*pool, groups, width, parent, home, page_table, len, status, static_cast<cudaStream_t>(stream));
   if (err) return cuda_fail(err, "reorder");

@@ -532,7 +532,7 @@ cudaError_t append_with(const PackedDev& kv, const SeqsDev& s, const RopeDev& ro
   const int64_t warps = (int64_t(groups) * kv.L + kWarps - 1) / kWarps;
   const int64_t most = std::max<int64_t>(1, int64_t(blocks) * s.R * warps / (4 * 3 * 152));
   const int per = int(std::min<int64_t>({most, warps, 7}));
-  const dim3 grid(unsigned(blocks + q_grid), s.R, unsigned((warps + per - 1) / per));
+  const dim3 grid(unsigned(blocks + q_grid), s.R, unsigned(std::min<int64_t>((warps + per - 1) / per, 65535)));
   const int smem = (kPairing == kNoTurn ? 0 : 2 * kBlockTokens * kv.d * int(sizeof(float))) +
                    kWarps * 2 * kBlockTokens * hp * kv.d * int(sizeof(T));
   auto run = [&](auto kernel) {

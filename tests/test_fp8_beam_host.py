@@ -142,4 +142,5 @@ def test_reorder_refusals(C):
     _expect(C, C.ERR_INVALID_ARG, run, _fp8(C, R=33), i32(33), 33, i32((33, 3)), i32(33), match="width")
     flat = torch.zeros((1, 2, 9, 64), dtype=BF)
     _expect(C, C.ERR_UNSUPPORTED, C.conduit_kv_reorder, C.KvCache(flat, flat.clone(), 4), i32(4), 2, home, i32(4), match="paged")
+    _expect(C, C.ERR_INVALID_ARG, run, kv, i32(4), 2, kv.page_table, i32(4), match="home")
     run(kv, i32(0), 2, i32((0, 3)), i32(0))  # no groups: no work

@@ -290,3 +290,14 @@ def test_reorder_from_the_first_beam_and_captured(C):
     for b in range(4):
         assert kv.page_table[b, :2].tolist() == home[0, :2].tolist() and kv.page_table[b, 2:].tolist() == home[b, 2:].tolist()
         assert torch.equal(kv.k[:, home[b, 2], :, :5], k[:, home[0, 2], :, :5])
+
+
+def test_a_group_that_is_cut_to_whole_pages(C):
+    """After lengths are cut, a reordering of each beam to itself gives every beam its own pages from there on."""
+    kv, home, parts, _ = _make(C, "fp8", 1, 1, 32, 16, 3, 4, 9)
+    kv.page_table[1:, :3] = home[0, :3]  # beams 1 and 2 share the first one's pages
+    lens = torch.full((3,), 16, dtype=torch.int32, device="cuda")
+    pool = kv.pool.clone()
+    C.conduit_fp8_reorder(kv, torch.arange(3, dtype=torch.int32, device="cuda"), 3, home, lens)
+    assert torch.equal(kv.page_table[:, 1:], home[:, 1:]) and torch.equal(kv.page_table[:, 0], home[0, :1].expand(3))
+    assert torch.equal(kv.pool, pool) and lens.tolist() == [16] * 3
