@@ -81,15 +81,10 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float by) {
   return fp8_pair(a.x * by, a.y * by) | fp8_pair(b.x * by, b.y * by) << 16;
 }
 
-// The tokens of a block that a call writes: bit t of `now`.
-// K: each lane has its chunk of eight tokens of parity c, x[i] of token 2 i + c.
-// Writes codes and scale of one head's keys. `was`: exponent of the earlier tokens' scale, or kLeastExp;
-// older: earlier tokens (bits).
-// kWhole: all of them, so that nothing was there before.
-template <int NC, bool kWhole>
-__device__ __forceinline__ void put_keys(uint8_t* block, const Place& p, int d, uint32_t now, uint32_t older, int e,
-                                         int was, const float (&x)[NC][8][8]) {
-  const float down = power_of_two(-e), by = power_of_two(max(was - e, -126));
+// A whole block's codes. K: each lane has its chunk of eight tokens of parity c, x[i] of token 2 i + c.
+template <int NC>
+__device__ __forceinline__ void put_keys(uint8_t* block, const Place& p, int d, int e, const float (&x)[NC][8][8]) {
+  const float down = power_of_two(-e);
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
     const int u = p.u + 16 * n;
@@ -98,42 +93,24 @@ __device__ __forceinline__ void put_keys(uint8_t* block, const Place& p, int d, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int t = 2 * i + p.c;
-      uint2* to = reinterpret_cast<uint2*>(at + (t >> 3) * 8 * d + (t & 7) * 16);
-      if (kWhole || (now >> t & 1u)) {
-        float y[8];
+      float y[8];
 #pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-          const float2 z = tc::fmul2(make_float2(x[n][i][k], x[n][i][k + 1]), make_float2(down, down));
-          y[k] = z.x, y[k + 1] = z.y;
-        }
-        *to = make_uint2(fp8_pair(y[0], y[1]) | fp8_pair(y[2], y[3]) << 16, fp8_pair(y[4], y[5]) | fp8_pair(y[6], y[7]) << 16);
-      } else if (was < e && (older >> t & 1u)) {
-        const uint2 w = *to;
-        *to = make_uint2(rescaled(w.x, by), rescaled(w.y, by));
+      for (int k = 0; k < 8; k += 2) {
+        const float2 z = tc::fmul2(make_float2(x[n][i][k], x[n][i][k + 1]), make_float2(down, down));
+        y[k] = z.x, y[k + 1] = z.y;
       }
+      *reinterpret_cast<uint2*>(at + (t >> 3) * 8 * d + (t & 7) * 16) =
+          make_uint2(fp8_pair(y[0], y[1]) | fp8_pair(y[2], y[3]) << 16, fp8_pair(y[4], y[5]) | fp8_pair(y[6], y[7]) << 16);
     }
   }
 }
 
 // The same of the values, whose rows are dims: byte 4 a + 2 b + c of a row is token 8 b + 2 a + c, so a
 // lane's codes of tokens 2 a + c and 2 a + 8 + c are the halfword (a, c) and its partner's the other.
-template <int NC, bool kWhole>
-__device__ __forceinline__ void put_values(uint8_t* block, const Place& p, int d, uint32_t now, uint32_t older, int e,
-                                           int was, const float (&x)[NC][8][8]) {
+template <int NC>
+__device__ __forceinline__ void put_values(uint8_t* block, const Place& p, int d, int e, const float (&x)[NC][8][8]) {
   constexpr unsigned kAll = 0xffffffffu;
-  const float down = power_of_two(-e), by = power_of_two(max(was - e, -126));
-  uint32_t mine[4], past[4];  // bytes of word a that the call writes, and that earlier tokens have
-#pragma unroll
-  for (int a = 0; a < 4; ++a) {
-    mine[a] = past[a] = 0;
-    if (kWhole) continue;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int t = 8 * (k >> 1) + 2 * a + (k & 1);
-      if (now >> t & 1u) mine[a] |= 0xFFu << (8 * k);
-      if (older >> t & 1u) past[a] |= 0xFFu << (8 * k);
-    }
-  }
+  const float down = power_of_two(-e);
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
     const int u = p.u + 16 * n;
@@ -162,19 +139,9 @@ __device__ __forceinline__ void put_values(uint8_t* block, const Place& p, int d
       const uint32_t even[2] = {p.c ? got[0] : own[0], p.c ? got[1] : own[1]};
       const uint32_t odd[2] = {p.c ? own[0] : got[0], p.c ? own[1] : got[1]};
       // even: tokens (2 a, 2 a + 8), odd: (2 a + 1, 2 a + 9)
-      uint4 y = make_uint4(__byte_perm(even[0], odd[0], 0x5140), __byte_perm(even[0], odd[0], 0x7362),
-                           __byte_perm(even[1], odd[1], 0x5140), __byte_perm(even[1], odd[1], 0x7362));
-      if (!p.on || u >= d / 8) continue;
-      if (!kWhole) {
-        uint4 old = rows[k];
-        if (was < e && older) {
-          auto mixed = [&](uint32_t o, int a) { return (rescaled(o, by) & past[a]) | (o & ~past[a]); };
-          old = make_uint4(mixed(old.x, 0), mixed(old.y, 1), mixed(old.z, 2), mixed(old.w, 3));
-        }
-        y = make_uint4((y.x & mine[0]) | (old.x & ~mine[0]), (y.y & mine[1]) | (old.y & ~mine[1]),
-                       (y.z & mine[2]) | (old.z & ~mine[2]), (y.w & mine[3]) | (old.w & ~mine[3]));
-      }
-      rows[k] = y;
+      if (p.on && u < d / 8)
+        rows[k] = make_uint4(__byte_perm(even[0], odd[0], 0x5140), __byte_perm(even[0], odd[0], 0x7362),
+                             __byte_perm(even[1], odd[1], 0x5140), __byte_perm(even[1], odd[1], 0x7362));
     }
   }
 }
@@ -224,198 +191,259 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 2)
   const int lane = threadIdx.x % 32, hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
   const Place p = place_in_warp(kv.d, lane);
 
-  // which of the block's tokens the call writes
-  const int most = min(s.max_len, kv.capacity());
-  bool in_range = first >= 0 && first < most;
-  int page = kv.page_table[int64_t(r) * kv.max_pages + (in_range ? int(first) >> kv.page_shift : 0)];
-  in_range &= page >= 0 && page < kv.P;
+  // Which of the block's tokens belong to the call. Their rows, page, positions and cosines go out together: a decoding
+  // step is a chain of loads, and none of these waits for another but the cosines for the positions.
   const int64_t own_slot = first + (lane & 15);  // lane t looks at token t
   const bool called = own_slot >= begin && own_slot < len;
-  bool fine = called && in_range && own_slot < most;
-  if (fine && rope.rot) {
-    int pos[CONDUIT_MAX_AXES];
-    fine = load_positions(rope, int64_t(t0) + (own_slot - begin), pos);
-  }
-  const uint32_t asked = __ballot_sync(0xffffffffu, called) & 0xFFFFu, now = __ballot_sync(0xffffffffu, fine) & 0xFFFFu;
-  if (now != asked && threadIdx.x == 0 && blockIdx.z == 0) flag_status(status, CONDUIT_FLAG_INDEX);
-  if (now == 0) return;
-  const int before = int(min(max(int64_t(begin) - first, int64_t(0)), int64_t(16)));
-  const uint32_t older = (1u << before) - 1u;
+  const uint32_t asked = __ballot_sync(0xffffffffu, called) & 0xFFFFu, my_asked = (asked >> p.c) & 0x5555u;  // bit 2 i: token 2 i + c
   const int64_t row0 = int64_t(t0) + (first - begin);  // row of the call of the block's token 0
-
+  const int units = groups * kv.L, step = gridDim.z * (kThreads / 32), first_unit = blockIdx.z * (kThreads / 32) + threadIdx.x / 32;
   // [16][2][d / 8][4] cosines, then signed sines: dims 8 u + 4 h .. of a token at [h][u], so that the lanes of a row read side by side
   extern __shared__ __align__(16) float turns[];
   float *cosines = turns, *sines = turns + kBlockTokens * kv.d;
-  if (kPairing != kNoTurn) {
-    const int chunks = kv.d / 8;
-    for (int e = threadIdx.x; e < kBlockTokens * chunks; e += kThreads) {
-      const int t = e / chunks, i0 = e % chunks * 8;
-      float c8[8], s8[8];
-      float2 cs[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) cs[k] = make_float2(1.f, 0.f);
-      if (now >> t & 1u) {
-        int pos[CONDUIT_MAX_AXES];
-        load_positions(rope, row0 + t, pos);
-        load_turn8<kPairing>(rope, pos, i0, cs);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) c8[k] = cs[k].x, s8[k] = cs[k].y;
-#pragma unroll
-      for (int k = 0; k < 8; k += 4) {
-        const int at = t * kv.d + (k * kv.d + 4 * i0) / 8;
-        *reinterpret_cast<float4*>(cosines + at) = make_float4(c8[k], c8[k + 1], c8[k + 2], c8[k + 3]);
-        *reinterpret_cast<float4*>(sines + at) = make_float4(s8[k], s8[k + 1], s8[k + 2], s8[k + 3]);
-      }
-    }
-    __syncthreads();
-  }
-
-  const uint32_t mine = (now >> p.c) & 0x5555u;       // bit 2 i: token 2 i + c
-  const int units = groups * kv.L, step = gridDim.z * (kThreads / 32), first_unit = blockIdx.z * (kThreads / 32) + threadIdx.x / 32;
   // this warp's rows: 16 tokens of a unit's keys, and of its values
   const int row_bytes = hp * kv.d * int(sizeof(T));
   uint8_t* rows_at = reinterpret_cast<uint8_t*>(turns) + (kPairing == kNoTurn ? 0 : 2 * kBlockTokens * kv.d * int(sizeof(float))) +
                      threadIdx.x / 32 * 2 * kBlockTokens * row_bytes;
   auto head_of = [&](int n) { return n % groups * hp + p.head; };
-  bool bad = false;
-  auto work = [&](auto all) {
-    constexpr bool kWhole = decltype(all)::value;  // the call writes every token of the block
-    // dim i0 of this lane's token 2 i + c and head (a lane without a chunk is at the first one; what it reads is left out)
-    auto row_at = [&](int which, int i, int i0) {
-      return reinterpret_cast<T*>(rows_at + (which * kBlockTokens + 2 * i + p.c) * row_bytes) + p.head * kv.d + i0;
-    };
-    auto copy_rows = [&](const RowsDev& x, int which, int n) {
-      const int head = head_of(n), l = n / groups;
-      if (n < units && p.on && head < kv.Hkv) {
-        const T* row = static_cast<const T*>(x.p) + l * x.ls + head * x.hs + (row0 + p.c) * x.rs + 8 * p.u;
+  // dim i0 of this lane's token 2 i + c and head (a lane without a chunk is at the first one; what it reads is left out)
+  auto row_at = [&](int which, int i, int i0) {
+    return reinterpret_cast<T*>(rows_at + (which * kBlockTokens + 2 * i + p.c) * row_bytes) + p.head * kv.d + i0;
+  };
+  auto copy_rows = [&](auto all, const RowsDev& x, int which, int n) {
+    const int head = head_of(n), l = n / groups;
+    if (n < units && p.on && head < kv.Hkv) {
+      const T* row = static_cast<const T*>(x.p) + l * x.ls + head * x.hs + (row0 + p.c) * x.rs + 8 * p.u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i, row += 2 * x.rs) {
-          if (!kWhole && !(mine >> (2 * i) & 1u)) continue;
-#pragma unroll
-          for (int m = 0; m < NC; ++m) {
-            if (NC > 1 && p.u + 16 * m >= kv.d / 8) continue;
-            T* to = row_at(which, i, 8 * (p.u + 16 * m));
-            if (kWide) {
-#pragma unroll
-              for (int c = 0; c < int(sizeof(T) / 2); ++c)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to) + 16 * c),
-                             "l"(row + 128 * m + 16 / sizeof(T) * c)
-                             : "memory");
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) to[e] = row[128 * m + e];
-            }
-          }
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    auto rows_here = [&] {  // all but the last rows that this warp has asked for
-      asm volatile("cp.async.wait_group 1;" ::: "memory");
-      __syncwarp();
-    };
-    copy_rows(k, 0, first_unit);
-    copy_rows(v, 1, first_unit);
-#pragma unroll 1
-    for (int unit = first_unit; unit < units; unit += step) {
-      const int head = head_of(unit), l = unit / groups;
-      const bool on = p.on && head < kv.Hkv;
-      const Place here{p.head, p.u, p.c, on};
-      uint8_t* block = fp8_block(kv, l, on ? head : 0, page, int(first));
-      float* scales = reinterpret_cast<float*>(block + 32 * kv.d);
-      int was[2] = {kLeastExp, kLeastExp};
-      if (!kWhole && older) {
-        const float2 w = *reinterpret_cast<const float2*>(scales);
-        was[0] = exponent_of(w.x), was[1] = exponent_of(w.y);
-      }
-      float x[NC][8][8];
-      // A lane's numbers of a token and chunk; zeros where the call has none.
-      auto read = [&](int which, int m, int i, float (&y)[8]) {
-        Raw8<T> raw{};
-        const int u = p.u + 16 * m;
-        if ((kWhole || (mine >> (2 * i) & 1u)) && (NC == 1 || u < kv.d / 8)) raw = load8(row_at(which, i, p.on ? 8 * u : 0), true);
-        to_floats(raw, y);
-      };
-      {
-        float top = 0.f;
-        float2 wild = make_float2(0.f, 0.f);
-        rows_here();
+      for (int i = 0; i < 8; ++i, row += 2 * x.rs) {
+        if (!decltype(all)::value && !(my_asked >> (2 * i) & 1u)) continue;
 #pragma unroll
         for (int m = 0; m < NC; ++m) {
-          const int i0 = p.on ? 8 * (p.u + 16 * m) : 0;
-          const int far0 = i0 < rope.half ? i0 + rope.half : i0 - rope.half;
-          const bool turns_here = kPairing != kNoTurn && i0 < rope.rot && (NC == 1 || i0 < kv.d);
+          if (NC > 1 && p.u + 16 * m >= kv.d / 8) continue;
+          T* to = row_at(which, i, 8 * (p.u + 16 * m));
+          if (kWide) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            read(0, m, i, x[m][i]);
-            if (turns_here && (kWhole || (mine >> (2 * i) & 1u))) {
-              const int t = 2 * i + p.c;
-              float other[8];
-              if (kPairing == kChunks) {
-                to_floats(load8(row_at(0, i, far0), true), other);
-              } else if (kPairing == kNeighbours) {
+            for (int c = 0; c < int(sizeof(T) / 2); ++c)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to) + 16 * c),
+                           "l"(row + 128 * m + 16 / sizeof(T) * c)
+                           : "memory");
+          } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) other[e] = x[m][i][e ^ 1];
-              } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  const int at = i0 + e;
-                  const int j = rope.layout == CONDUIT_ROPE_PAIRS ? at ^ 1 : at < rope.half ? at + rope.half : at - rope.half;
-                  other[e] = at < rope.rot ? to_float(*row_at(0, i, j)) : 0.f;
-                }
-              }
-              const float* c8 = cosines + t * kv.d + i0 / 2;
-              const float* s8 = sines + t * kv.d + i0 / 2;
-#pragma unroll
-              for (int e = 0; e < 8; e += 4) {
-                const float4 c = *reinterpret_cast<const float4*>(c8 + e * kv.d / 8), s = *reinterpret_cast<const float4*>(s8 + e * kv.d / 8);
-                const float own[4] = {x[m][i][e], x[m][i][e + 1], x[m][i][e + 2], x[m][i][e + 3]};
-                // the products are rounded before they are added; a dim past rot has cosine 1 and sine 0
-                const float2 a0 = tc::fmul2(make_float2(own[0], own[1]), make_float2(c.x, c.y));
-                const float2 b0 = tc::fmul2(make_float2(other[e], other[e + 1]), make_float2(s.x, s.y));
-                const float2 a1 = tc::fmul2(make_float2(own[2], own[3]), make_float2(c.z, c.w));
-                const float2 b1 = tc::fmul2(make_float2(other[e + 2], other[e + 3]), make_float2(s.z, s.w));
-                const float2 y0 = add_rounded(a0, b0), y1 = add_rounded(a1, b1);
-                x[m][i][e] = y0.x, x[m][i][e + 1] = y0.y, x[m][i][e + 2] = y1.x, x[m][i][e + 3] = y1.y;
-              }
-            }
-            look_at(x[m][i], &top, &wild);
+            for (int e = 0; e < 8; ++e) to[e] = row[128 * m + e];
           }
         }
-        __syncwarp();
-        copy_rows(k, 0, unit + step);
-        if (!(wild.x + wild.y == 0.f)) bad |= on, mend(x, &top);
-        if (!on) top = 0.f;
-        const int e = max(exponent_for(head_max(top, kv.d)), was[0]);
-        put_keys<NC, kWhole>(block, here, kv.d, now, older, e, was[0], x);
-        if (on && p.u == 0 && p.c == 0) scales[0] = power_of_two(e);
       }
-      {
-        float top = 0.f;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  copy_rows(std::false_type{}, k, 0, first_unit);
+  copy_rows(std::false_type{}, v, 1, first_unit);
+
+  const int most = min(s.max_len, kv.capacity());
+  bool in_range = first >= 0 && first < most;
+  const int page = kv.page_table[int64_t(r) * kv.max_pages + (in_range ? int(first) >> kv.page_shift : 0)];
+  bool fine = called;
+  if (called && rope.rot) {
+    int pos[CONDUIT_MAX_AXES];
+    fine = load_positions(rope, int64_t(t0) + (own_slot - begin), pos);
+  }
+  if (kPairing != kNoTurn) {
+    const int chunks = kv.d / 8;
+    for (int e = threadIdx.x; e < kBlockTokens * chunks; e += kThreads) {
+      const int t = e / chunks, i0 = e % chunks * 8;
+      if (!(asked >> t & 1u)) continue;
+      int pos[CONDUIT_MAX_AXES];
+      if (!load_positions(rope, row0 + t, pos)) continue;
+      float2 cs[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) cs[k] = make_float2(1.f, 0.f);
+      load_turn8<kPairing>(rope, pos, i0, cs);
+#pragma unroll
+      for (int k = 0; k < 8; k += 4) {
+        const int at = t * kv.d + (k * kv.d + 4 * i0) / 8;
+        *reinterpret_cast<float4*>(cosines + at) = make_float4(cs[k].x, cs[k + 1].x, cs[k + 2].x, cs[k + 3].x);
+        *reinterpret_cast<float4*>(sines + at) = make_float4(cs[k].y, cs[k + 1].y, cs[k + 2].y, cs[k + 3].y);
+      }
+    }
+  }
+  in_range &= page >= 0 && page < kv.P;
+  const uint32_t now = __ballot_sync(0xffffffffu, fine && in_range && own_slot < most) & 0xFFFFu;  // the tokens that are written
+  if (now != asked && threadIdx.x == 0 && blockIdx.z == 0) flag_status(status, CONDUIT_FLAG_INDEX);
+  if (now == 0) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return;
+  }
+  const int before = int(min(max(int64_t(begin) - first, int64_t(0)), int64_t(16)));
+  const uint32_t older = (1u << before) - 1u, mine = (now >> p.c) & 0x5555u;
+  if (kPairing != kNoTurn) __syncthreads();
+
+  auto rows_here = [&] {  // all but the last rows that this warp has asked for
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncwarp();
+  };
+  // A lane's eight numbers of token 2 i + c from dim i0 on, keys turned.
+  auto numbers = [&](int which, int i, int i0, float (&y)[8]) {
+    to_floats(load8(row_at(which, i, i0), true), y);
+    if (which || kPairing == kNoTurn || i0 >= rope.rot) return;
+    const int t = 2 * i + p.c;
+    float other[8];
+    if (kPairing == kChunks) {
+      to_floats(load8(row_at(0, i, i0 < rope.half ? i0 + rope.half : i0 - rope.half), true), other);
+    } else if (kPairing == kNeighbours) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) other[e] = y[e ^ 1];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = i0 + e;
+        const int j = rope.layout == CONDUIT_ROPE_PAIRS ? at ^ 1 : at < rope.half ? at + rope.half : at - rope.half;
+        other[e] = at < rope.rot ? to_float(*row_at(0, i, j)) : 0.f;
+      }
+    }
+    const float *c8 = cosines + t * kv.d + i0 / 2, *s8 = sines + t * kv.d + i0 / 2;
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) {
+      const float4 c = *reinterpret_cast<const float4*>(c8 + e * kv.d / 8), s = *reinterpret_cast<const float4*>(s8 + e * kv.d / 8);
+      // the products are rounded before they are added; a dim past rot has cosine 1 and sine 0
+      const float2 a0 = tc::fmul2(make_float2(y[e], y[e + 1]), make_float2(c.x, c.y));
+      const float2 b0 = tc::fmul2(make_float2(other[e], other[e + 1]), make_float2(s.x, s.y));
+      const float2 a1 = tc::fmul2(make_float2(y[e + 2], y[e + 3]), make_float2(c.z, c.w));
+      const float2 b1 = tc::fmul2(make_float2(other[e + 2], other[e + 3]), make_float2(s.z, s.w));
+      const float2 y0 = add_rounded(a0, b0), y1 = add_rounded(a1, b1);
+      y[e] = y0.x, y[e + 1] = y0.y, y[e + 2] = y1.x, y[e + 3] = y1.y;
+    }
+  };
+  bool bad = false;
+  if (now == 0xFFFFu) {  // whole blocks: everything in registers between one reading and one writing
+#pragma unroll 1
+    for (int unit = first_unit; unit < units; unit += step) {
+      const int head = head_of(unit);
+      const bool on = p.on && head < kv.Hkv;
+      const Place here{p.head, p.u, p.c, on};
+      uint8_t* block = fp8_block(kv, unit / groups, on ? head : 0, page, int(first));
+      float* scales = reinterpret_cast<float*>(block + 32 * kv.d);
+      float x[NC][8][8];
+      auto gather = [&](auto which, float* top) {
         float2 wild = make_float2(0.f, 0.f);
+        *top = 0.f;
         rows_here();
 #pragma unroll
         for (int m = 0; m < NC; ++m)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            read(1, m, i, x[m][i]);
-            look_at(x[m][i], &top, &wild);
+            const int i0 = p.on ? 8 * (p.u + 16 * m) : 0;
+            if (NC == 1 || i0 < kv.d) {
+              numbers(decltype(which)::value, i, i0, x[m][i]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[m][i][e] = 0.f;
+            }
+            look_at(x[m][i], top, &wild);
           }
         __syncwarp();
-        copy_rows(v, 1, unit + step);
-        if (!(wild.x + wild.y == 0.f)) bad |= on, mend(x, &top);
-        if (!on) top = 0.f;
-        const int e = max(exponent_for(head_max(top, kv.d)), was[1]);
-        put_values<NC, kWhole>(block, here, kv.d, now, older, e, was[1], x);
-        if (on && p.u == 0 && p.c == 0) scales[1] = power_of_two(e);
+        copy_rows(std::true_type{}, decltype(which)::value ? v : k, decltype(which)::value, unit + step);
+        if (!(wild.x + wild.y == 0.f)) bad |= on, mend(x, top);
+        if (!on) *top = 0.f;
+      };
+      float top;
+      gather(std::integral_constant<int, 0>{}, &top);
+      int e = exponent_for(head_max(top, kv.d));
+      put_keys<NC>(block, here, kv.d, e, x);
+      if (on && p.u == 0 && p.c == 0) scales[0] = power_of_two(e);
+      gather(std::integral_constant<int, 1>{}, &top);
+      e = exponent_for(head_max(top, kv.d));
+      put_values<NC>(block, here, kv.d, e, x);
+      if (on && p.u == 0 && p.c == 0) scales[1] = power_of_two(e);
+    }
+  } else {
+    // Part filled blocks, token by token and read twice (largest number, codes): a decoding step fetches this
+    // code once a call, and its length is what the call takes (with all tokens' steps laid out 19 us for a step of 64 requests).
+#pragma unroll 1
+    for (int unit = first_unit; unit < units; unit += step) {
+      const int head = head_of(unit);
+      const bool on = p.on && head < kv.Hkv;
+      uint8_t* block = fp8_block(kv, unit / groups, on ? head : 0, page, int(first));
+      float* scales = reinterpret_cast<float*>(block + 32 * kv.d);
+      float2 was2 = make_float2(0.f, 0.f);
+      if (older) was2 = *reinterpret_cast<const float2*>(scales);
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which) {
+        rows_here();
+        const int was = older ? exponent_of(which ? was2.y : was2.x) : kLeastExp;
+        int e = was;
+        float down = 0.f;
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+          float top = 0.f;
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) {
+            if (!(now >> (2 * i) & 3u)) continue;
+#pragma unroll 1
+            for (int u = p.u; u < kv.d / 8; u += 16) {
+              if (!on || !(mine >> (2 * i) & 1u)) continue;
+              float y[8];
+              numbers(which, i, 8 * u, y);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const bool finite = fabsf(y[k]) < INFINITY;
+                bad |= !finite;
+                y[k] = finite ? y[k] : NAN;
+                top = fmaxf(top, fabsf(y[k]));
+              }
+              if (pass == 0) continue;
+              const int t = 2 * i + p.c;
+              uint32_t w[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k)
+                w[k] = fp8_pair(y[4 * k] * down, y[4 * k + 1] * down) | fp8_pair(y[4 * k + 2] * down, y[4 * k + 3] * down) << 16;
+              if (which == 0) {
+                *reinterpret_cast<uint2*>(block + (t >> 3) * 8 * kv.d + (u >> 1) * 128 + (t & 7) * 16 + (u & 1) * 8) = make_uint2(w[0], w[1]);
+              } else {
+                uint8_t* to = block + 16 * kv.d + 8 * u * 16 + (t & 7) / 2 * 4 + (t >> 3) * 2 + (t & 1);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) to[16 * k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
+              }
+            }
+          }
+          if (pass == 1) break;
+          e = max(exponent_for(head_max(top, kv.d)), was);
+          down = power_of_two(-e);
+          if (__any_sync(0xffffffffu, on && older && was < e)) {  // (every lane of a head alike)
+            const float by = power_of_two(max(was - e, -126));
+            if (on && was < e) {
+#pragma unroll 1
+              for (int u = p.u; u < kv.d / 8; u += 16) {
+                if (which == 0) {
+#pragma unroll 1
+                  for (int t = p.c; t < before; t += 2) {
+                    uint2* at = reinterpret_cast<uint2*>(block + (t >> 3) * 8 * kv.d + (u >> 1) * 128 + (t & 7) * 16 + (u & 1) * 8);
+                    const uint2 w = *at;
+                    *at = make_uint2(rescaled(w.x, by), rescaled(w.y, by));
+                  }
+                } else {
+#pragma unroll 1
+                  for (int k = 0; k < 16; ++k) {  // words of dims 8 u + 4 c .. of four tokens each
+                    const int a = k & 3;
+                    uint32_t past = 0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                      if (8 * (j >> 1) + 2 * a + (j & 1) < before) past |= 0xFFu << (8 * j);
+                    uint32_t* at = reinterpret_cast<uint32_t*>(block + 16 * kv.d + (8 * u + 4 * p.c + (k >> 2)) * 16) + a;
+                    const uint32_t w = *at;
+                    *at = (rescaled(w, by) & past) | (w & ~past);
+                  }
+                }
+              }
+            }
+            __syncwarp();  // before other lanes write bytes of the same words
+          }
+        }
+        __syncwarp();
+        copy_rows(std::false_type{}, which ? v : k, which, unit + step);
+        if (on && p.u == 0 && p.c == 0) scales[which] = power_of_two(e);
       }
     }
-  };
-  if (now == 0xFFFFu)
-    work(std::true_type{});
-  else
-    work(std::false_type{});
+  }
   if (bad) flag_status(status, CONDUIT_FLAG_NONFINITE);
 }
 
