@@ -376,32 +376,41 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 2)
         for (int pass = 0; pass < 2; ++pass) {
           float top = 0.f;
 #pragma unroll 1
-          for (int i = 0; i < 8; ++i) {
-            if (!(now >> (2 * i) & 3u)) continue;
+          for (int i = 0; i < 8; i += 2) {  // two tokens of each parity side by side; what the call has none of is read and dropped
+            if (!(now >> (2 * i) & 15u)) continue;
 #pragma unroll 1
             for (int u = p.u; u < kv.d / 8; u += 16) {
-              if (!on || !(mine >> (2 * i) & 1u)) continue;
-              float y[8];
-              numbers(which, i, 8 * u, y);
+              if (!on) continue;
+              float y[2][8];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const bool finite = fabsf(y[k]) < INFINITY;
-                bad |= !finite;
-                y[k] = finite ? y[k] : NAN;
-                top = fmaxf(top, fabsf(y[k]));
+              for (int j = 0; j < 2; ++j) numbers(which, i + j, 8 * u, y[j]);
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const bool live = mine >> (2 * (i + j)) & 1u;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const bool finite = fabsf(y[j][k]) < INFINITY;
+                  bad |= live && !finite;
+                  y[j][k] = finite ? y[j][k] : NAN;
+                  top = fmaxf(top, live ? fabsf(y[j][k]) : 0.f);
+                }
               }
               if (pass == 0) continue;
-              const int t = 2 * i + p.c;
-              uint32_t w[2];
 #pragma unroll
-              for (int k = 0; k < 2; ++k)
-                w[k] = fp8_pair(y[4 * k] * down, y[4 * k + 1] * down) | fp8_pair(y[4 * k + 2] * down, y[4 * k + 3] * down) << 16;
-              if (which == 0) {
-                *reinterpret_cast<uint2*>(block + (t >> 3) * 8 * kv.d + (u >> 1) * 128 + (t & 7) * 16 + (u & 1) * 8) = make_uint2(w[0], w[1]);
-              } else {
-                uint8_t* to = block + 16 * kv.d + 8 * u * 16 + (t & 7) / 2 * 4 + (t >> 3) * 2 + (t & 1);
+              for (int j = 0; j < 2; ++j) {
+                if (!(mine >> (2 * (i + j)) & 1u)) continue;
+                const int t = 2 * (i + j) + p.c;
+                uint32_t w[2];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) to[16 * k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
+                for (int k = 0; k < 2; ++k)
+                  w[k] = fp8_pair(y[j][4 * k] * down, y[j][4 * k + 1] * down) | fp8_pair(y[j][4 * k + 2] * down, y[j][4 * k + 3] * down) << 16;
+                if (which == 0) {
+                  *reinterpret_cast<uint2*>(block + (t >> 3) * 8 * kv.d + (u >> 1) * 128 + (t & 7) * 16 + (u & 1) * 8) = make_uint2(w[0], w[1]);
+                } else {
+                  uint8_t* to = block + 16 * kv.d + 8 * u * 16 + (t & 7) / 2 * 4 + (t >> 3) * 2 + (t & 1);
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) to[16 * k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
+                }
               }
             }
           }
