@@ -10,7 +10,9 @@
 // are read again, 32 at a time; their values above the bound go to a small buffer and, sorted as 64-bit
 // keys (logit, then the lower index), into the list of the n best across the warp's lanes. The lists and sums go to the first CTA's
 // shared memory, which ranks what can still be chosen. No scratch in memory, one launch.
-// Bound: the logits once, and as close behind it the exponentials, one a logit.
+// Bound: the logits once, and as close behind it the exponentials, one a logit. Measured: 64 groups of 8 rows of 128 003 bf16
+// logits, 16 of them chosen, 38 us (3.4 TB/s; about 10 us are its start and what follows the last logit: blocks read again, lists
+// merged and ranked); 4 rows of 32 000 in fp32 9.5 us. With candidates sought at every step: 69 us.
 #include "beam.cuh"
 #include "tc_common.cuh"
 
@@ -416,7 +418,7 @@ cudaError_t launch(SelectArgs a, int groups, cudaStream_t stream) {
   if (err) return err;
   cudaLaunchAttribute cluster{};
   cluster.id = cudaLaunchAttributeClusterDimension;
-  // Two CTAs of 100 registers a thread on an SM: clusters of eight while all of them run at a time, else of four (64 groups of
+  // Two CTAs of 108 registers a thread on an SM: clusters of eight while all of them run at a time, else of four (64 groups of
   // 8 rows of 128 003: 38 us, 45 in clusters of eight; four CTAs an SM with half of the loads under way 43).
   const int ctas = groups * kClusterMost <= 2 * 152 ? kClusterMost : kClusterMost / 2;
   cluster.val.clusterDim.x = ctas;

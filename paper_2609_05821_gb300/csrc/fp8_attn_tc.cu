@@ -16,6 +16,12 @@
 // order, so S_x(t + 1) may overwrite P_x(t), and S_x(t + 1) says that P_x(t) V(t) is done.
 // TMEM: S_A, S_B at columns [0, 256) with P over their upper halves,
 // O_A, O_B at [256, 512). A block with one column tile: A takes the even key tiles, B the odd ones.
+//
+// Bound: the chain S, softmax, P V, next S of each column tile beside the other's, and under it the shared memory that
+// feeds the MMAs (a key tile: 192 KB of operands and 128 KB of codes in, out and widened). Measured: 32-128
+// rows of 16 requests over 8 192 keys, two layers of 28 x 4 heads of 128, 325 us (0.98 PFLOP/s, tensor pipe 45 % busy); causal
+// prompts, one layer: 8 192 tokens 514 us, four of 4 096 tokens 610. Three loads under way instead of four, and the
+// guarded values in the usual loop: 395 us.
 #include "fp8.cuh"
 #include "packed_attn.cuh"
 

@@ -1,4 +1,4 @@
-// What the attention kernels over the 4-bit cache share: the arguments of a call,
+// What the attention kernels over the 4-bit and the 8-bit cache share: the arguments of a call,
 // a CTA's share of it, and the stores of final rows and partial results.
 #pragma once
 
@@ -16,7 +16,7 @@ constexpr int kCols = 8;  // columns per CTA of the warp-level and CUDA-core ker
 constexpr float kBias = 7.f, kUnbias = 1.f / 128.f;
 constexpr float kMostWeight = 15.f;
 
-// tcgen05: a key as one fp16 number is within 2^-11 of its value, and so a logit within 2^-11 of
+// tcgen05, 4 bits: a key as one fp16 number is within 2^-11 of its value, and so a logit within 2^-11 of
 // scale sum |q||k|: nothing beside the rounding of a bf16 output, and in a log-sum-exp an error that falls
 // with the number of keys that count (2 x 10^-4 of it for one key, 2 x 10^-6 for 8 192 of like
 // weight). So a block with a column that sees fewer keys than this, if any, takes its keys as the sum of two
