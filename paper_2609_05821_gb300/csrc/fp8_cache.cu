@@ -158,16 +158,16 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 2)
   const int r = blockIdx.y;
   const int t0 = s.row_off[r], n = s.row_off[r + 1] - t0, len = s.len[r];
   if (n == 0) return;
-  const int begin = len - n;  // slot of the call's first row
+  const int64_t begin = int64_t(len) - n;  // slot of the call's first row
   if (int(blockIdx.x) >= kv_grid) {
     const uint32_t lin = (blockIdx.x - kv_grid) * uint32_t(kThreads) + threadIdx.x;
     const uint32_t per = units_per_row<VEC>(rope, kv.d), rest = lin / per;
     const int u = int(lin - rest * per), i = int(rest / uint32_t(kv.Hq)), h = int(rest - uint32_t(i) * kv.Hq);
     if (i >= n) return;
     const int64_t t = int64_t(t0) + i;
-    const int slot = begin + i;
+    const int64_t slot = begin + i;
     bool ok = slot >= 0 && slot < s.max_len && slot < kv.capacity();
-    const int page = kv.page_table[int64_t(r) * kv.max_pages + (ok ? slot >> kv.page_shift : 0)];
+    const int page = kv.page_table[int64_t(r) * kv.max_pages + (ok ? int(slot) >> kv.page_shift : 0)];
     ok &= page >= 0 && page < kv.P;
     int pos[CONDUIT_MAX_AXES];
     if (rope.rot) ok &= load_positions(rope, t, pos);
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 2)
     return;
   }
   // slots count from the block of the first row (rows before slot 0 lie in blocks of their own)
-  const int64_t first = (int64_t(begin) >> 4) * 16 + 16 * int64_t(blockIdx.x);
+  const int64_t first = (begin >> 4) * 16 + 16 * int64_t(blockIdx.x);
   if (first >= len) return;
   const int lane = threadIdx.x % 32, hp = heads_per_warp(kv.d), groups = (kv.Hkv + hp - 1) / hp;
   const Place p = place_in_warp(kv.d, lane);
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, NC == 1 ? 3 : 2)
     asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
-  const int before = int(min(max(int64_t(begin) - first, int64_t(0)), int64_t(16)));
+  const int before = int(min(max(begin - first, int64_t(0)), int64_t(16)));
   const uint32_t older = (1u << before) - 1u, mine = (now >> p.c) & 0x5555u;
   if (kPairing != kNoTurn) __syncthreads();
 

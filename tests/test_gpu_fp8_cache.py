@@ -284,3 +284,17 @@ def test_append_is_captured_and_replayed(C):
                 cache.plain[0][r][g][1].append(at[r], f[0, r:r + 1, 2 + g])
             at[r] += 1
     assert np.array_equal(cache.kv.pool.cpu().numpy(), cache.put())
+
+
+def test_lengths_that_no_context_has(C):
+    """Lengths below the call's rows, negative ones and the ends of 32 bits: flagged, nothing written."""
+    cache = Cache(C, 7, 1, 2, 1, 64, 16, 2, 32)
+    x = torch.randn((1, 6, 4, 64), generator=torch.Generator().manual_seed(4)).cuda()
+    before = cache.kv.pool.clone()
+    for lens in ((0, 0), (-1, -2 ** 31), (2 ** 31 - 1, -2 ** 31 + 2), (36, 2 ** 31 - 1)):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        q_out = torch.full((1, 6, 2, 64), 9.0, device="cuda")
+        seqs = C.Seqs([0, 3, 6], torch.tensor(lens, dtype=torch.int32, device="cuda"), 32)
+        C.conduit_fp8_append(cache.kv, seqs, x[:, :, :1], x[:, :, 1:2], q=x[:, :, 2:], q_out=q_out, status=status)
+        assert C.conduit_read_status(status) == C.ERR_INDEX
+        assert torch.equal(cache.kv.pool, before) and (q_out == 9.0).all()
