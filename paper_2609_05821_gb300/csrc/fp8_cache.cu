@@ -575,8 +575,10 @@ cudaError_t append_with(const PackedDev& kv, const SeqsDev& s, const RopeDev& ro
   const int smem = (kPairing == kNoTurn ? 0 : 2 * kBlockTokens * kv.d * int(sizeof(float))) +
                    kWarps * 2 * kBlockTokens * hp * kv.d * int(sizeof(T));
   auto run = [&](auto kernel) {
-    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (err) return err;
+    if (smem > 48 * 1024) {  // (a microsecond of a decoding step's call otherwise)
+      cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (err) return err;
+    }
     kernel<<<grid, kThreads, smem, stream>>>(kv, s, rope, blocks, k, v, q, q_out, status);
     count_launches(1);
     return cudaGetLastError();
