@@ -4,8 +4,9 @@
 // Mathematics. Codes are exact in fp16, and so are the queries (bf16 scaled to fp16's range by a power of two per row),
 // so only fp32 sums round; a block's key scale multiplies its logits. The scale of its values, 2^v, joins the exponent of its
 // weights: w_j = 2^(x_j + v - reference), with which the codes themselves are summed, while the denominator takes
-// w_j 2^-v. The reference follows the largest x + v, so that fp16's range of weights goes to what counts in the output,
-// however far the blocks' scales lie apart.
+// w_j 2^-v. The reference follows the largest x + v, so that fp16's range of weights goes to what counts in the output.
+// The fp32 sum holds weights down to 2^-126: scales up to 2^100 apart leave 2^-33 of the largest weight, and what a reference that
+// rises by as much leaves of a sum from before (least scale 2^-40, so 2^47 at least) is a normal number.
 //
 // Shape. mma with the tokens (then the dims) as the 16 rows and up to 8 (row, query head) columns as n. A block of
 // 16 tokens is one bulk copy; its K codes lie in the pool as the 8 x 16-byte tiles that ldmatrix reads without bank conflicts, its

@@ -228,6 +228,32 @@ def test_scales_far_apart(C, dtype, rows):
         _check([[[(k, v)]]], (n,), (rows,), q, lim, out, lse, d ** -0.5, dtype == BF)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("sizes", [(0.0, 2.0 ** 68, 1.0), (2.0 ** 68, 0.0, 2.0 ** -30), (2.0 ** -30, 1.0, 2.0 ** 68)])
+def test_scales_as_far_apart_as_allowed(C, dtype, rows, sizes):
+    """Value scales 2^100 apart, in every order: the smaller blocks' weights still count in the denominator."""
+    n, d = 2048, 128
+    rng = np.random.default_rng(14)
+    k, v = F.Blocks(n, d), F.Blocks(n, d)
+    y = rng.uniform(0.5, 1.75, (n, d)).astype(np.float32)  # one sign: a lost denominator shows whole
+    for b in range(n // 16):
+        y[16 * b:16 * b + 16] *= np.float32(sizes[b % 3])
+    k.append(0, 0.1 * rng.standard_normal((n, d)).astype(np.float32))
+    v.append(0, y)
+    assert max(v.exp) - min(v.exp) <= 100
+    pool = np.full((1, n // 16, 1, 32 * d + 16), 0xFF, dtype=np.uint8)
+    for b in range(n // 16):
+        F.put_block(pool[0, b, 0], k, v, b)
+    kv = C.Fp8Kv(torch.from_numpy(pool).cuda(), 2, d, 16, torch.arange(n // 16, dtype=torch.int32)[None])
+    q = torch.randn((1, rows, 2, d), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").to(dtype)
+    for limit in (17, 33, 49, n):
+        lim = torch.full((rows,), limit, dtype=torch.int32, device="cuda")
+        lse = torch.zeros((1, 2, rows), device="cuda")
+        out = C.conduit_fp8_attn(kv, _seqs(C, (n,), (rows,)), q, limits=lim, lse=lse)
+        _check([[[(k, v)]]], (n,), (rows,), q, lim, out, lse, d ** -0.5, dtype == BF)
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_small_weights_keep_their_share(C, rows):
     """A quarter of a million keys whose weights are 2^-24 of the largest one: together 2^-6 of the output."""
