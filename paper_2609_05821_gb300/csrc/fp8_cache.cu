@@ -13,8 +13,8 @@
 // a unit are on their way while its keys are packed, the next unit's keys meanwhile (in registers: 316 us for append and read of
 // 28 layers of 8 192 tokens, 281 so).
 // Bound: the rows once and 2 d + 1 bytes a token and head of the cache. Measured, 28 layers of 8 192 tokens, 4 heads of 128 in
-// bf16: append 159 us (4.4 TB/s; stores of 8 and 16 bytes a lane take two thirds of the load/store unit's slots, and 168 registers leave
-// 12 warps an SM), read 102 us (6.9 TB/s, at the copy rate). One token of 64 requests: append 10 us, read 6.
+// bf16: append 159 us (4.4 TB/s; the load/store unit is 66 % busy, nearly half of it the keys' reads from shared memory, and 168
+// registers leave 12 warps an SM), read 102 us (6.9 TB/s, at the copy rate). One token of 64 requests: append 10 us, read 6.
 #include <algorithm>
 #include <type_traits>
 
