@@ -713,7 +713,7 @@ conduit_status conduit_fp8_attn(const conduit_fp8_kv* kv, const conduit_seqs* se
  * another may come in either order (equal rows 16 bytes aligned, with equal sums, in theirs).
  *  logits  device [G width][vocab] of dtype, rows row_stride elements apart (>= vocab), aligned to the element
  *  sums    device fp32 [G width]: log-probabilities so far; -inf leaves a beam out
- *  score   device fp32 [G][num_out]
+ *  score   device fp32 [G][num_out]; may be sums where num_out is width
  *  parent  device int32 [G][num_out]: the row of the call that is continued (g width + beam)
  *  token   device int32 [G][num_out]
  * A logit of -inf is never chosen. Where a group has fewer candidates than num_out, the rest have score -inf,

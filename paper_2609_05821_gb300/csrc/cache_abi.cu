@@ -426,6 +426,8 @@ conduit_status conduit_beam_select(const void* logits, int32_t dtype, int64_t ro
                         static_cast<const void*>(parent), static_cast<const void*>(token)})
     if (!p || reinterpret_cast<uintptr_t>(p) % 4)
       return fail(CONDUIT_ERR_INVALID_ARG, "sums, score, parent and token are required, 4-byte aligned");
+  if (score == sums && num_out != width)
+    return fail(CONDUIT_ERR_INVALID_ARG, "score may be sums where num_out is width only");
   cudaError_t err = launch_beam_select(logits, dtype, row_stride, num_groups, width, vocab, sums, num_out, score, parent,
                                        token, status, static_cast<cudaStream_t>(stream));
   if (err) return cuda_fail(err, "beam_select");

@@ -129,6 +129,13 @@ def test_select_refusals(C):
     assert [x.shape for x in got] == [(0, 2)] * 3
 
 
+def test_select_in_place_refusals(C):
+    """Scores over the sums of other groups, which may not have been read."""
+    z, buf = torch.zeros((4, 10)), torch.zeros(8)
+    _expect(C, C.ERR_INVALID_ARG, C.conduit_beam_select, z, buf[:4], 2, 4, score=buf.view(2, 4), match="may be sums")
+    _expect(C, C.ERR_INVALID_ARG, C.conduit_beam_select, z, buf[:4], 2, 1, score=buf[:2].view(2, 1), match="may be sums")
+
+
 def test_reorder_refusals(C):
     kv = _fp8(C, R=4)
     i32 = lambda n: torch.zeros(n, dtype=torch.int32)

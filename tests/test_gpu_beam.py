@@ -132,6 +132,17 @@ def test_select_large_and_small_logits(C):
         assert np.allclose(score[0].double().cpu().numpy(), best, rtol=2.0 ** -22, atol=EPS)
 
 
+def test_select_over_its_sums(C):
+    """Scores take the place of the sums: the same bits as beside them."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    z = 3 * torch.randn((4 * 90, 1003), generator=g, device="cuda")
+    sums = -5 * torch.rand(4 * 90, generator=g, device="cuda")
+    want = C.conduit_beam_select(z, sums, 4)
+    buf = sums.clone()
+    got = C.conduit_beam_select(z, buf, 4, score=buf.view(90, 4))
+    assert got[0].data_ptr() == buf.data_ptr() and all(torch.equal(a, b) for a, b in zip(want, got))
+
+
 def test_select_is_captured_and_repeats_bits(C):
     z = torch.randn((16, 70001), generator=torch.Generator().manual_seed(3)).cuda().to(BF)
     sums = torch.zeros(16, device="cuda")
