@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) beam_select_kernel(SelectArgs 
     const uint4* from = reinterpret_cast<const uint4*>(row + head);
     // elements of their own: before the first boundary, behind the last
     const float ends[2][2] = {{seg == 0 && lane < head ? to_float(row[lane]) : -INFINITY, -INFINITY},
-                              {seg == a.segs - 1 && tail + lane < a.vocab ? to_float(row[tail + lane]) : -INFINITY, -INFINITY}};
+                              {seg == a.segs - 1 && lane < a.vocab - tail ? to_float(row[int64_t(tail) + lane]) : -INFINITY, -INFINITY}};
     add_up<2>(b, ends[0], ends[0][0]);
     add_up<2>(b, ends[1], ends[1][0]);
     const int loads = (v1 - v0 + 32 * kAtOnce - 1) / (32 * kAtOnce), per_block = max(1, (loads + kBlocks - 1) / kBlocks);
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) beam_select_kernel(SelectArgs 
           for (int k = 0; k < kAtOnce; ++k) {
             float y[N];
             unpack<T>(w[k], on && v + 32 * k < v1, y);
-            keep<N>(b, y, uint32_t(head + (v + 32 * k) * N), limit, buffer, lane);
+            keep<N>(b, y, uint32_t(head) + uint32_t(v + 32 * k) * N, limit, buffer, lane);
           }
         }
         tighten();
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) beam_select_kernel(SelectArgs 
       if (in) ids[found + __popc(who & ((1u << lane) - 1u))] = uint32_t(j) << 5 | uint32_t(lane);
       found += __popc(who);
     }
-    if (seg == a.segs - 1) keep<2>(b, ends[1], uint32_t(tail + lane), limit, buffer, lane);
+    if (seg == a.segs - 1) keep<2>(b, ends[1], uint32_t(tail) + lane, limit, buffer, lane);
     if (b.count > 0) b.list = merged(b.list, buffer, b.count);
     // the lanes' sums, in the order of a butterfly
     float m = b.m;
