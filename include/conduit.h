@@ -692,9 +692,9 @@ conduit_status conduit_fp8_read(const conduit_fp8_kv* kv, const int32_t* first,
  * conduit_packed_attn over an 8-bit cache: the same rows, limits, results, workspace rules and errors. bf16
  * rows with head_dim 64, 96 or 128 run on the tensor cores: keys, values and queries (but for a power of two)
  * exact in fp16, weights times the scale of their value within 2^-11 of themselves or 2^-32 of the row's
- * largest, fp32 sums; so lse carries fp32 rounding only. fp32 rows and other head sizes run on the CUDA cores in fp32.
- * On the tensor cores a head's value scales count in full where they lie within 2^100 of each other, always so for values
- * up to 2^68; farther apart by 2^D, weights below 2^(D - 133) of that of the largest value are lost from the denominator.
+ * largest, fp32 sums; so lse carries fp32 rounding only (of logits plus the exponents of their value scales, where those
+ * differ). Every key counts in the denominator at its weight, wherever in their range the scales of its and of other
+ * values lie. fp32 rows and other head sizes run on the CUDA cores in fp32.
  */
 conduit_status conduit_fp8_attn_workspace_size(const conduit_fp8_kv* kv, const conduit_seqs* seqs,
                                                int32_t dtype, size_t* bytes);

@@ -75,7 +75,10 @@ __device__ __forceinline__ void join_warps(const AttnArgs& a, const Item& it, co
     if (i == 0) {
       float total = 0.f;
 #pragma unroll
-      for (int k = 0; k < kWarps; ++k) total = fmaf(tc::ex2(ml[k * kCols + col].x - base), ml[k * kCols + col].y, total);
+      for (int k = 0; k < kWarps; ++k) {
+        const float by = ml[k * kCols + col].x - base;
+        total = add_scaled(total, ml[k * kCols + col].y, by, tc::ex2(by));
+      }
       weight[kWarps * kCols + col] = total;
       const int j = it.cb * kCols + col;
       if (kCluster)
@@ -128,7 +131,7 @@ __device__ __forceinline__ void join_warps(const AttnArgs& a, const Item& it, co
       for (int k = 0; k < 8; ++k) {
         if (k >= C) continue;
         const float wgt = tc::ex2(st[k].x - base);
-        total = fmaf(wgt, st[k].y, total);
+        total = add_scaled(total, st[k].y, st[k].x - base, wgt);
         out.x = fmaf(wgt, o[k].x, out.x);
         out.y = fmaf(wgt, o[k].y, out.y);
         out.z = fmaf(wgt, o[k].z, out.z);

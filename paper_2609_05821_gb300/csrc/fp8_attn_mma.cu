@@ -5,8 +5,7 @@
 // so only fp32 sums round; a block's key scale multiplies its logits. The scale of its values, 2^v, joins the exponent of its
 // weights: w_j = 2^(x_j + v - reference), with which the codes themselves are summed, while the denominator takes
 // w_j 2^-v. The reference follows the largest x + v, so that fp16's range of weights goes to what counts in the output.
-// The fp32 sum holds weights down to 2^-126: scales up to 2^100 apart leave 2^-33 of the largest weight, and what a reference that
-// rises by as much leaves of a sum from before (least scale 2^-40, so 2^47 at least) is a normal number.
+// Where w_j would leave fp32's range (value scales 2^60 apart and more) the denominator takes 2^(x - reference) itself.
 //
 // Shape. mma with the tokens (then the dims) as the 16 rows and up to 8 (row, query head) columns as n. A block of
 // 16 tokens is one bulk copy; its K codes lie in the pool as the 8 x 16-byte tiles that ldmatrix reads without bank conflicts, its
@@ -80,10 +79,10 @@ __device__ __forceinline__ void block_step(Running<NG>& st, const uint8_t* box, 
     for (int e = 0; e < 2; ++e) {
 #pragma unroll
       for (int s = 4; s < 32; s <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], s));
-      const float moved = fmaxf(st.ref[e], top[e] - kBias);
-      corr[e] = moved == -INFINITY ? 1.f : tc::ex2(st.ref[e] - moved);
+      const float moved = fmaxf(st.ref[e], top[e] - kBias), by = st.ref[e] - moved;
+      corr[e] = moved == -INFINITY ? 1.f : tc::ex2(by);
       st.ref[e] = moved;
-      st.sum[e] *= corr[e];
+      st.sum[e] = scaled_down(st.sum[e], by, corr[e]);
     }
 #pragma unroll
     for (int t = 0; t < 2 * NG; ++t)
@@ -92,10 +91,15 @@ __device__ __forceinline__ void block_step(Running<NG>& st, const uint8_t* box, 
   }
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const float base = (kEdge && st.ref[e] == -INFINITY ? 0.f : st.ref[e]) - v_log2;
-    x[e] = tc::ex2(x[e] - base);
-    x[e + 2] = tc::ex2(x[e + 2] - base);
-    st.sum[e] = fmaf(x[e] + x[e + 2], v_down, st.sum[e]);
+    const float base = (kEdge && st.ref[e] == -INFINITY ? 0.f : st.ref[e]) - v_log2, x0 = x[e], x1 = x[e + 2];
+    x[e] = tc::ex2(x0 - base);
+    x[e + 2] = tc::ex2(x1 - base);
+    if (top[e] < st.ref[e] - kFarBelow) {
+      const float lifted = st.ref[e] - kLift;
+      st.sum[e] = fmaf(tc::ex2(x0 - lifted) + tc::ex2(x1 - lifted), kUnlift, st.sum[e]);
+    } else {
+      st.sum[e] = fmaf(x[e] + x[e + 2], v_down, st.sum[e]);
+    }
   }
   // tokens 2 c, 2 c + 1 and 8 on of column q
   const uint32_t b0 = transpose8x8(h2u(__floats2half2_rn(x[0], x[1])));

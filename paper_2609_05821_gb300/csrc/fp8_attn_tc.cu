@@ -22,6 +22,8 @@
 // rows of 16 requests over 8 192 keys, two layers of 28 x 4 heads of 128, 325 us (0.98 PFLOP/s, tensor pipe 45 % busy); causal
 // prompts, one layer: 8 192 tokens 514 us, four of 4 096 tokens 610. Three loads under way instead of four, and the
 // guarded values in the usual loop: 395 us.
+#include <type_traits>
+
 #include "fp8.cuh"
 #include "packed_attn.cuh"
 
@@ -39,6 +41,9 @@ constexpr int kLoadKeys = 2 * kBlockTokens;   // keys of a load
 constexpr int kLoads = kKeys / kLoadKeys;     // loads of a key tile
 constexpr int kRing = 4;                      // loads under way
 constexpr int kBlocks = kKeys / kBlockTokens; // blocks of a key tile
+// While no value scale is above 2^kNear, all lie within 2^80 of each other, and a weight down to 2^-46 of its column's largest stays
+// in fp32's range. From the first key tile on that has a larger one the denominator goes by weigh_apart.
+constexpr float kNear = 40.f;
 
 template <int NG>
 struct Sizes {
@@ -176,6 +181,35 @@ __device__ __forceinline__ float weigh(uint32_t sb, const Scales* scales, float 
     }
   }
   return top;
+}
+
+// Their sum without v alone, for value scales that lie far apart: a block whose weights are all far below the reference counts by
+// its logits, others as in weigh.
+__device__ __forceinline__ float weigh_apart(uint32_t sb, const Scales* scales, float to_log2, float low, int left) {
+  float add = 0.f;
+#pragma unroll 1
+  for (int b = 0; b < kBlocks; ++b, left -= kBlockTokens) {
+    float s[kBlockTokens];
+    tc::tmem_ld16(sb + kBlockTokens * b, s);
+    const Scales sc = scales[b];
+    const float up1 = fmaxf(sc.x * to_log2, 1.1754944e-38f);
+    float block_top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < kBlockTokens; ++e) {
+      if (e >= left) s[e] = -INFINITY;
+      block_top = fmaxf(block_top, s[e]);
+    }
+    const bool far = fmaf(block_top, up1, sc.y) < -low - kFarBelow;
+    const float down1 = (far ? kLift : sc.y) + low;
+    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int e = 0; e < kBlockTokens; e += 2) {
+      const float2 y = tc::ffma2(make_float2(s[e], s[e + 1]), make_float2(up1, up1), make_float2(down1, down1));
+      sum = tc::fadd2(sum, make_float2(tc::ex2(y.x), tc::ex2(y.y)));
+    }
+    add = fmaf(sum.x + sum.y, far ? kUnlift : sc.z, add);
+  }
+  return add;
 }
 
 template <int NG>
@@ -504,42 +538,53 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
     float sum = 0.f;
     bool ok = true;
     const int count = split ? (tiles + 1 - x) / 2 : tiles;
-    for (int t = 0; t < count; ++t) {
-      if (!(ok = wait_warp(&bars.s_full[x], t & 1, abort))) break;
-      tc::tc_fence_after();
-      const int tile_id = split ? 2 * t + x : t, kb = k0 + tile_id * kKeys;
-      const int left = lim - kb;  // keys of the tile that the column sees
-      const bool edge = kb + kKeys > least;
-      uint32_t p[4][16];
-      float add;
-      for (int pass = 0;; ++pass) {
-        const float low = ref == -INFINITY ? 0.f : -ref;
-        const float top = edge ? weigh<true>(sb, scales[tile_id & 3], to_log2, low, left, p, &add)
-                               : weigh<false>(sb, scales[tile_id & 3], to_log2, low, left, p, &add);
-        if (pass || !__any_sync(0xffffffffu, top > ref + kMostWeight)) break;
-        // the reference moves: what was summed so far is scaled, and the weights are taken again
-        const float moved = fmaxf(ref, top - kBias), corr = moved == -INFINITY ? 1.f : tc::ex2(ref - moved);
-        ref = moved;
-        sum *= corr;
-        if (t > 0) {
+    int t = 0;
+    // One key tile after the other. kFar: value scales may lie anywhere; else it ends at the first tile that has one above
+    // kNear. Two loops: in one, what the second needs beside the first's weights cost the kernel 3 % of its time, so 1.5 %.
+    auto walk = [&](auto far) {
+      constexpr bool kFar = decltype(far)::value;
+      for (; t < count; ++t) {
+        if (!(ok = wait_warp(&bars.s_full[x], t & 1, abort))) break;
+        tc::tc_fence_after();
+        const int tile_id = split ? 2 * t + x : t, kb = k0 + tile_id * kKeys;
+        const Scales* sc = scales[tile_id & 3];
+        if (!kFar && __any_sync(0xffffffffu, sc[lane & (kBlocks - 1)].y > kNear)) break;
+        const int left = lim - kb;  // keys of the tile that the column sees
+        const bool edge = kb + kKeys > least;
+        uint32_t p[4][16];
+        float add;
+        for (int pass = 0;; ++pass) {
+          const float low = ref == -INFINITY ? 0.f : -ref;
+          const float top = kFar || edge ? weigh<true>(sb, sc, to_log2, low, left, p, &add)
+                                 : weigh<false>(sb, sc, to_log2, low, left, p, &add);
+          if (pass || !__any_sync(0xffffffffu, top > ref + kMostWeight)) break;
+          // the reference moves: what was summed so far is scaled, and the weights are taken again
+          const float moved = fmaxf(ref, top - kBias), by = ref - moved, corr = moved == -INFINITY ? 1.f : tc::ex2(by);
+          ref = moved;
+          sum = kFar ? scaled_down(sum, by, corr) : sum * corr;
+          if (t > 0) {
 #pragma unroll 1
-          for (int b = 0; b < D / 32; ++b) {
-            float o[32];
-            tc::tmem_ld32(ob + 32 * b, o);
+            for (int b = 0; b < D / 32; ++b) {
+              float o[32];
+              tc::tmem_ld32(ob + 32 * b, o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] *= corr;
-            tc::tmem_st32(ob + 32 * b, o);
+              for (int e = 0; e < 32; ++e) o[e] *= corr;
+              tc::tmem_st32(ob + 32 * b, o);
+            }
           }
         }
-      }
-      sum += add;
+        if (kFar) add = weigh_apart(sb, sc, to_log2, ref == -INFINITY ? 0.f : -ref, left);
+        sum += add;
 #pragma unroll
-      for (int b = 0; b < 4; ++b) tc::tmem_st16_nowait(sb + kPCol + 16 * b, p[b]);
-      tc::tmem_wait_st();
-      tc::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&bars.p_full[x]);
-    }
+        for (int b = 0; b < 4; ++b) tc::tmem_st16_nowait(sb + kPCol + 16 * b, p[b]);
+        tc::tmem_wait_st();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars.p_full[x]);
+      }
+    };
+    walk(std::false_type{});
+    if (ok && t < count) walk(std::true_type{});
     // without keys there is nothing to wait for but the other warps' queries, over which the rows go out
     if (ok) ok = count > 0 ? wait_warp(&bars.o_full[x], 0, abort) : wait_warp(&bars.q_full, 0, abort);
     ref += kBias;
@@ -556,7 +601,10 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
         const float2 b = of_b[at];
         const float top = fmaxf(ref, b.x), base = top == -INFINITY ? 0.f : top;
         const float wa = tc::ex2(ref - base), wb = tc::ex2(b.x - base);
-        total = wa * total + wb * b.y;
+        if (fminf(ref, b.x) - base < kLeastFactor)
+          total = add_scaled(scaled_down(total, ref - base, wa), b.y, b.x - base, wb);
+        else
+          total = wa * total + wb * b.y;
         own_w = wa * kUnbias;
         b_w = wb * kUnbias;
         ref = top;

@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
   for (int c = of; c < n; c += kJoin) {
     const float2 ml = a.part_ml[c * cols + col];
     const float wgt = exp2f(ml.x - base);
-    sum = fmaf(wgt, ml.y, sum);
+    sum = add_scaled(sum, ml.y, ml.x - base, wgt);
     const float4 po = *reinterpret_cast<const float4*>(a.part_o + (c * cols + col) * D + 4 * lane);
     o.x = fmaf(wgt, po.x, o.x);
     o.y = fmaf(wgt, po.y, o.y);

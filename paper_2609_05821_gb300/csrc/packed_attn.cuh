@@ -16,6 +16,28 @@ constexpr int kCols = 8;  // columns per CTA of the warp-level and CUDA-core ker
 constexpr float kBias = 7.f, kUnbias = 1.f / 128.f;
 constexpr float kMostWeight = 15.f;
 
+// The 8-bit cache's references follow logit + log2 of the value scale, which lies in [-40, 119], so a sum of weights without
+// their value scales lies between 2^-119 (its largest weight's share) and 2^47 times the number of keys, and two references may be
+// 2^159 apart and more where both sums count alike. A factor below kLeastFactor is applied in two halves, since
+// 2^by alone would leave fp32's range.
+constexpr float kLeastFactor = -100.f;  // log2
+// y 2^by for by <= 0; power: 2^by, 1 where by is NaN (from -inf to -inf).
+__device__ __forceinline__ float scaled_down(float y, float by, float power) {
+  if (by < kLeastFactor) {
+    const float half = tc::ex2(0.5f * by);
+    return y * half * half;
+  }
+  return y * power;
+}
+// sum + y 2^by.
+__device__ __forceinline__ float add_scaled(float sum, float y, float by, float power) {
+  return by < kLeastFactor ? sum + scaled_down(y, by, power) : fmaf(power, y, sum);
+}
+// Weights whose product with their value scale is 2^kFarBelow or less of the reference count by their logits alone, held
+// 2^kLift up: with its scale such a weight may leave fp32's range while it counts in full in the denominator (zeros beside values of
+// 2^100: a log-sum-exp off by ln 2, and the output half of it).
+constexpr float kFarBelow = 60.f, kLift = 40.f, kUnlift = 1.f / 1099511627776.f;
+
 // tcgen05, 4 bits: a key as one fp16 number is within 2^-11 of its value, and so a logit within 2^-11 of
 // scale sum |q||k|: nothing beside the rounding of a bf16 output, and in a log-sum-exp an error that falls
 // with the number of keys that count (2 x 10^-4 of it for one key, 2 x 10^-6 for 8 192 of like
