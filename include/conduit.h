@@ -624,11 +624,12 @@ conduit_status conduit_packed_read(const conduit_packed_kv* kv, const int32_t* f
  *          (fp32 partial results of key chunks); calls that overlap on the GPU
  *          need workspaces of their own
  * bf16 rows with head_dim 64, 96 or 128 run on the tensor cores (fp16 operands:
- * queries exact but for a power of two, values within 2^-11, weights within 2^-11
- * of themselves or 2^-32 of the row's largest, fp32 sums); fp32 rows and other
+ * queries exact but for a power of two down to 2^-25 of their row's largest |q| and
+ * within 2^-33 of it below, values within 2^-11, weights within 2^-11 of themselves or 2^-32 of the row's largest, fp32 sums); fp32 rows and other
  * head sizes on the CUDA cores in fp32. Where no request has rows x (Hq/Hkv) > 8,
  * and for every row that sees fewer than 2048 keys, keys enter exactly or as two
- * fp16 numbers: lse then carries fp32 rounding only. For other rows a key may be
+ * fp16 numbers: lse then carries fp32 rounding only (and scale 2^-33 max |q| sum |k|
+ * over dims of such small queries). For other rows a key may be
  * within 2^-11 of itself, and so a logit within 2^-11 of scale sum |q||k|; in lse
  * that averages over the keys that count (2e-6 of it over 8192 of like weight). The
  * kernel and the cut into key chunks follow from the sizes, max_len and row_off,
@@ -690,9 +691,10 @@ conduit_status conduit_fp8_read(const conduit_fp8_kv* kv, const int32_t* first,
 
 /*
  * conduit_packed_attn over an 8-bit cache: the same rows, limits, results, workspace rules and errors. bf16
- * rows with head_dim 64, 96 or 128 run on the tensor cores: keys, values and queries (but for a power of two)
- * exact in fp16, weights times the scale of their value within 2^-11 of themselves or 2^-32 of the row's
- * largest, fp32 sums; so lse carries fp32 rounding only (of logits plus the exponents of their value scales, where those
+ * rows with head_dim 64, 96 or 128 run on the tensor cores: keys and values exact in fp16, queries too (but for a power
+ * of two) down to 2^-32 of their row's largest |q| and within 2^-40 of it below, so that a logit may be off by
+ * scale 2^-40 max |q| sum |k| over such dims; weights times the scale of their value within 2^-11 of themselves or 2^-32 of the
+ * row's largest, fp32 sums. Beside such queries lse carries fp32 rounding only (of logits plus the exponents of their value scales, where those
  * differ). Every key counts in the denominator at its weight, wherever in their range the scales of its and of other
  * values lie. fp32 rows and other head sizes run on the CUDA cores in fp32.
  */

@@ -1,8 +1,9 @@
 // Attention over the 8-bit cache for few rows (decoding, drafts): warp-level tensor cores, one pass over
 // the codes.
 //
-// Mathematics. Codes are exact in fp16, and so are the queries (bf16 scaled to fp16's range by a power of two per row),
-// so only fp32 sums round; a block's key scale multiplies its logits. The scale of its values, 2^v, joins the exponent of its
+// Mathematics. Codes are exact in fp16, and so are the queries (bf16, scaled by a power of two per row so that the largest lies
+// in [2^15, 2^16)) down to 2^-32 of their row's largest; what is smaller is off by 2^-40 of it at most, fp16's step at its
+// low end. Beside that only fp32 sums round; a block's key scale multiplies its logits. The scale of its values, 2^v, joins the exponent of its
 // weights: w_j = 2^(x_j + v - reference), with which the codes themselves are summed, while the denominator takes
 // w_j 2^-v. The reference follows the largest x + v, so that fp16's range of weights goes to what counts in the output.
 // Where w_j would leave fp32's range (value scales 2^60 apart and more) the denominator takes 2^(x - reference) itself.
@@ -235,7 +236,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fp8_attn_mma(AttnArgs a) {
   for (int s = 0; s < kStages; ++s)
     if (s < mine) fill(s);
 
-  // Queries of column q in the operand layout, scaled by 2^-shift so that the largest lies in [256, 512).
+  // Queries of column q in the operand layout, scaled by 2^-shift so that the largest lies in [2^15, 2^16), or below that where it is
+  // small: from 2^109 on every bf16 number is a multiple of fp16's least one.
   uint32_t bq[2 * NG][2];
   float to_log2[2];
   {
@@ -251,18 +253,15 @@ __global__ void __launch_bounds__(kWarps * 32, 2) fp8_attn_mma(AttnArgs a) {
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    int shift = int(__float_as_uint(top) >> 23) - 127 - 8;  // top < 2^(shift + 9)
+    int shift = max(int(__float_as_uint(top) >> 23) - 127 - 15, -109);  // top < 2^(shift + 16)
     if (!(top < INFINITY) || top == 0.f) shift = 0;
-    // 2^-shift and 2^shift in two factors, each a normal number
-    const float f1 = power_of_two(-(shift / 2)), f2 = power_of_two(-(shift - shift / 2));
-    const float g1 = power_of_two(shift / 2), g2 = power_of_two(shift - shift / 2);
-    const float back = a.scale * kLog2e * g1 * g2;
+    const float up = power_of_two(-shift), back = a.scale * kLog2e * power_of_two(shift);
 #pragma unroll
     for (int e = 0; e < 2; ++e) to_log2[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e));
 #pragma unroll
     for (int g = 0; g < 2 * NG; ++g) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[g][e] = x[g][e] * f1 * f2;
+      for (int e = 0; e < 4; ++e) x[g][e] *= up;
       bq[g][0] = h2u(__floats2half2_rn(x[g][0], x[g][1]));
       bq[g][1] = h2u(__floats2half2_rn(x[g][2], x[g][3]));
     }

@@ -1,6 +1,6 @@
 // Attention over the 8-bit cache for many rows (query prefixes, recomputed rows): tcgen05.
 //
-// Mathematics: as in fp8_attn_mma.cu: codes and queries exact in fp16, the scales of keys on the logits, those of
+// Mathematics: as in fp8_attn_mma.cu: codes exact in fp16, queries as there, the scales of keys on the logits, those of
 // values in the exponents of the weights, which are rounded to fp16; logits, statistics and outputs in fp32
 // (tensor memory).
 //
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
     float to_log2;
     {
       // Queries into the swizzled tile, two columns at a time, each scaled by a power of two so that
-      // its largest lies in [256, 512) (or below, if that takes more than 2^126).
+      // its largest lies in [2^15, 2^16) (or below, if that takes more than 2^109).
       constexpr int kUse = D / 8;  // lanes with eight dims of a column
       const bool wide = ((reinterpret_cast<uintptr_t>(a.q.p) | uint64_t(2 * (a.q.ls | a.q.rs | a.q.hs))) & 15u) == 0;
       const int64_t own = it.l * a.q.ls + int64_t(it.t0 + own_i) * a.q.rs + own_h * a.q.hs;
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_attn_tc(AttnArgs a) {
 #pragma unroll
         for (int o = 1; o < 16; o <<= 1) top = bf16_max2(top, __shfl_xor_sync(0xffffffffu, top, o));
         top = max(top & 0xFFFFu, top >> 16);
-        int shift = max(int(top >> 7) - 127 - 8, -126);
+        int shift = max(int(top >> 7) - 127 - 15, -109);
         if (top >= 0x7F80u || top == 0) shift = 0;
         const int got = __shfl_sync(0xffffffffu, shift, (lane & 1) << 4);
         if (lane >> 1 == k) own_shift = got;

@@ -3,8 +3,8 @@
 //
 // Mathematics. A group of 32 dims of token t is m_t + s_t c, c in -8..7. Logits come group by
 // group: x = sum_g s_tg (sum c q) + m_tg (sum q), with the codes exact in fp16 and the
-// queries exact too (bf16 scaled to fp16's range by a power of two per row), so only fp32 sums
-// round (to 6 x 10^-8 of a log-sum-exp). Values are formed as fp16 m + s c (2^-11 relative),
+// queries exact too (bf16 scaled by a power of two per row to fp16's range) down to 2^-25 of their
+// row's largest and within 2^-33 of it below, so beside that only fp32 sums round (to 6 x 10^-8 of a log-sum-exp). Values are formed as fp16 m + s c (2^-11 relative),
 // weights rounded to fp16: both below the rounding of a bf16 output. (Codes with their offset
 // left on, taken off in fp32, cost no instruction less on the pipe that counts and lost
 // precision: fp16's 1024 + u 6 x 10^-6 of a log-sum-exp, bf16's 128 + u 178 us for the batch of
