@@ -73,6 +73,10 @@ struct Coming4 {
   }
 };
 
+// Values of the 8-bit cache reach 2^128 and weights 2^8, so their fp32 sums are held 2^-40 down: with 2^31 keys they stay below
+// fp32's largest number, and the least value, 2^-49, is still 2^37 above its least normal one.
+constexpr float kValueDown = 1.f / 1099511627776.f, kValueUp = 1099511627776.f;
+
 // The same of the 8-bit cache, two blocks of 16 tokens: eight dims of K of a key, and a dim of V of a
 // block's tokens.
 template <int NG>
@@ -115,7 +119,7 @@ struct Coming8 {
       if (b < 2 && j < k1) {
         const uint8_t* at = fp8_block(a.kv, it.l, it.g, page_in_pool(a, vid[i]), j);
         vw[i] = *reinterpret_cast<const uint4*>(at + 16 * D + dim * 16);
-        vscale[i] = reinterpret_cast<const float*>(at + 32 * D)[1];
+        vscale[i] = reinterpret_cast<const float*>(at + 32 * D)[1] * kValueDown;
       }
     }
   }
@@ -338,7 +342,7 @@ __global__ void __launch_bounds__(NG * 64) combine_kernel(AttnArgs a) {
     }
   }
   if (!on) return;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = sum == 0.f ? 0.f : a.v_up / sum;
   T* to = static_cast<T*>(a.out.p) + l * a.out.ls + int64_t(t) * a.out.rs + h * a.out.hs + 4 * lane;
   to[0] = from_float<T>(o.x * inv);
   to[1] = from_float<T>(o.y * inv);
@@ -539,7 +543,8 @@ PackedAttnPlan packed_attn_plan(const PackedDev& kv, const SeqsDev& s, int dtype
 cudaError_t launch_packed_attn(const PackedDev& kv, const SeqsDev& s, const PackedAttnPlan& plan, int dtype,
                                const RowsDev& q, float scale, const int32_t* limits, const RowsDev& out,
                                float* lse, void* scratch, int32_t* status, cudaStream_t stream) {
-  AttnArgs a{kv, s, q, out, lse, limits, scale, plan.chunk, plan.chunks, 0, plan.last_chunk, plan.last_chunks,
+  const float v_up = plan.bits == 8 && plan.kernel == kAttnSimt ? kValueUp : 1.f;
+  AttnArgs a{kv, s, q, out, lse, limits, scale, v_up, plan.chunk, plan.chunks, 0, plan.last_chunk, plan.last_chunks,
              plan.part_cols, nullptr, nullptr, status};
   a.col_blocks = int(blocks_of(kv, s, plan.kernel));
 #ifdef CONDUIT_TEST_HOOKS

@@ -54,6 +54,7 @@ struct AttnArgs {
   float* lse;             // or NULL
   const int32_t* limits;  // or NULL
   float scale;
+  float v_up;             // CUDA cores, 8 bits: outputs are summed 2^-40 down (kValueDown), 1 elsewhere
   int chunk, chunks, col_blocks;
   int last_chunk, last_chunks;  // tcgen05: of blocks with one column tile
   int64_t part_cols;      // columns with partial results: L T Hq, or L R Hkv 128 where only those blocks have them
@@ -137,7 +138,7 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const Item& it, int
   const int i = j / a.kv.G, h = it.g * a.kv.G + j % a.kv.G;
   if (a.chunks == 1) {
     T* to = static_cast<T*>(a.out.p) + it.l * a.out.ls + int64_t(it.t0 + i) * a.out.rs + h * a.out.hs;
-    to[dd] = from_float<T>(sum == 0.f ? 0.f : o / sum);
+    to[dd] = from_float<T>(sum == 0.f ? 0.f : o / sum * a.v_up);
   } else {
     const int64_t cols = int64_t(a.kv.L) * a.s.T * a.kv.Hq;
     const int64_t col = (int64_t(it.l) * a.s.T + it.t0 + i) * a.kv.Hq + h;

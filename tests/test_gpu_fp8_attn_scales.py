@@ -56,12 +56,14 @@ SIZES = [
 ]
 
 
-@pytest.mark.parametrize("dtype", [BF])
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("n", [96, 2064, 9008])
 @pytest.mark.parametrize("rows", [1, 3, 40, 200])
 def test_scales_anywhere_in_their_range(C, dtype, rows, n):
     """Zeros and small values beside values of up to 2^127, in every order: each key counts in the denominator. One warp's
     and several warps' blocks, a cluster's and a workspace's chunks, one column tile and two."""
+    if dtype == F32 and rows > 3:
+        pytest.skip("the kernel of few rows")
     d = 64 if n == 96 else 128
     rng = np.random.default_rng(n + rows)
     for sizes in SIZES:
@@ -87,6 +89,34 @@ def test_scales_anywhere_in_their_range(C, dtype, rows, n):
             assert np.all(off <= e.T + 2.0 ** -22 * np.abs(wl) + limit * 2.0 ** -23 + 2.0 ** -21), (sizes, limit, off.max())
         again, lse2 = _attend(C, kv, n, q, n)
         assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("dtype,d", [(F32, 64), (F32, 128), (F32, 256), (BF, 32), (BF, 160)])
+@pytest.mark.parametrize("n", [96, 5008])
+def test_large_values_on_the_cuda_cores(C, dtype, d, n):
+    """Values of up to 2^127: fp32 sums of weights times values stay in range, in one chunk and in several; and values near the
+    least keep their bits."""
+    rng = np.random.default_rng(n + d)
+    for size in (2.0 ** 126, 2.0 ** 110, 2.0 ** -40):
+        k, v = F.Blocks(n, d), F.Blocks(n, d)
+        y = (rng.uniform(0.5, 1.75, (n, d)) * size).astype(np.float32)
+        y[:, ::3] *= -1
+        x = (0.1 * rng.standard_normal((n, d))).astype(np.float32)
+        x[n // 2:] *= 30  # logits that rise along the context: weights above 1
+        k.append(0, x)
+        v.append(0, y)
+        kv = _one_head(C, 2, k, v)
+        q = torch.randn((1, 2, 2, d), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").to(dtype)
+        K, V = k.values(n)[:, None], v.values(n)[:, None]
+        for limit in (40, n):
+            out, lse = _attend(C, kv, n, q, limit)
+            wo, wl, A, big = R.attend(q[0].double().cpu().numpy(), K, V, np.full(2, limit), d ** -0.5)
+            e = (d + 4) * 2.0 ** -23 * A
+            tol = ((np.expm1(2 * e) + (limit + 16) * 2.0 ** -23) * big)[..., None]
+            tol = tol + (2.0 ** -8 if dtype == BF else 2.0 ** -22) * np.abs(wo)
+            assert np.all(np.abs(out[0].double().cpu().numpy() - wo) <= tol), (size, limit)
+            off = np.abs(lse[0].double().cpu().numpy() - wl)
+            assert np.all(off <= e.T + 2.0 ** -22 * np.abs(wl) + limit * 2.0 ** -23 + 2.0 ** -21), (size, limit)
 
 
 @pytest.mark.parametrize("rows", [1, 40])
