@@ -711,8 +711,10 @@ conduit_status conduit_fp8_attn(const conduit_fp8_kv* kv, const conduit_seqs* se
  * The best continuations of each group over its beams and the vocabulary:
  *   s(b, v) = sums[b] + logits[b][v] - ln sum_u exp(logits[b][u])
  * the num_out largest, descending, equal ones in the order of (b, v). The sums of exponentials are fp32, scores are formed
- * and compared in fp64: inside a beam the order is that of the logits; beams whose scores are within about 10^-6 of one
- * another may come in either order (equal rows 16 bytes aligned, with equal sums, in theirs).
+ * and compared in fp64: inside a beam the order is that of the logits. A beam's ln sum is within (21 + ln vocab) 2^-22 (8 10^-6
+ * for 128 000 logits; a tenth of it and less is usual), and beams whose scores lie within twice that may come in either order. Equal
+ * rows with equal sums have equal scores, and come in their order, where they begin at the same place within 16 bytes (as rows do
+ * whose row_stride is a multiple of 16 bytes).
  *  logits  device [G width][vocab] of dtype, rows row_stride elements apart (>= vocab), aligned to the element
  *  sums    device fp32 [G width]: log-probabilities so far; -inf leaves a beam out
  *  score   device fp32 [G][num_out]; may be sums where num_out is width

@@ -1,8 +1,14 @@
 // Beam search's selection: the best continuations of a group over its beams and the vocabulary.
 //
 // Mathematics: s(b, v) = sums_b + z_bv - lse_b. Inside a row the order is that of the logits, so one pass
-// over a row gives its running maximum and sum and its n largest logits; rows meet only at the end, with their lse,
-// in fp64 (a float's last bit would decide between beams).
+// over a row gives its running sum of exponentials and its n largest logits; rows meet only at the end, with their lse, in fp64,
+// so that between two beams the errors of their sums decide and nothing beside them.
+//
+// Precision of a row's lse, with u = 2^-24: an exponential carries 2.25 |z - reference| u of its argument (difference, product, log2 e)
+// and 4 u of ex2, and the same again when a reference moves; over the row's shares that is 3.25 u (ln vocab + 12) + 16 u at most. A load's
+// sum is a tree, loads are added with a compensation, so the sums add 26 u whatever the vocabulary, the logarithm 2 u:
+// (21 + ln vocab) 2^-22 in all, 7.8e-6 for 128 003 logits. Measured on flat levels below a peak and on slow rises: the rounding of
+// the score, 5e-7 (without the compensation and with a reference that follows the maximum: 1.4e-5, 390 loads a lane).
 //
 // Shape: a cluster per group; its warps share the rows out in segments. While a segment streams by, a lane keeps its running
 // maximum and sum, and the maximum of each of up to 16 blocks of its values: nothing about candidates. The n-th largest
@@ -11,7 +17,7 @@
 // keys (logit, then the lower index), into the list of the n best across the warp's lanes. The lists and sums go to the first CTA's
 // shared memory, which ranks what can still be chosen. No scratch in memory, one launch.
 // Bound: the logits once, and as close behind it the exponentials, one a logit. Measured: 64 groups of 8 rows of 128 003 bf16
-// logits, 16 of them chosen, 38 us (3.4 TB/s; about 10 us are its start and what follows the last logit: blocks read again, lists
+// logits, 16 of them chosen, 39 us (3.4 TB/s; about 10 us are its start and what follows the last logit: blocks read again, lists
 // merged and ranked); 4 rows of 32 000 in fp32 9.5 us. With candidates sought at every step: 69 us.
 #include "beam.cuh"
 #include "tc_common.cuh"
@@ -40,7 +46,7 @@ constexpr int kBuffer = 31 + 32 * 8;  // values that wait for a warp's next merg
 
 struct Shared {
   uint64_t list[kListsMost][kMaxBeams];  // the first CTA's: every warp's list, sorted
-  float2 stats[kListsMost];              // (largest, sum of e^(z - largest))
+  float2 stats[kListsMost];              // (reference, sum of e^(z - reference))
   double base[kMaxBeams];                // sums - lse, -inf: the row is left out
   float down[kMaxBeams], up[kMaxBeams];  // bounds of it
   float sums[kMaxBeams];
@@ -106,9 +112,10 @@ __device__ __forceinline__ float below(float x) {
 
 // What a warp knows of its segment.
 struct Best {
-  uint64_t list = 0;             // lane i: the i-th best
-  int count = 0;                 // of values in the buffer
-  float m = -INFINITY, s = 0.f;  // this lane's largest value and sum of e^(z - m)
+  uint64_t list = 0;    // lane i: the i-th best
+  int count = 0;        // of values in the buffer
+  float m = -INFINITY;  // this lane's largest value
+  float ref = -INFINITY, s = 0.f, over = 0.f;  // its sum of e^(z - ref) is s - over
 };
 
 // A list and up to 32 values of the buffer: their best. Not inlined: the code of a sort counts where every warp is
@@ -153,19 +160,29 @@ __device__ __forceinline__ void keep(Best& b, const float (&x)[N], uint32_t at, 
   }
 }
 
-// N values' part of a lane's maximum and sum.
+// N values' part of a lane's maximum and sum. The reference moves by more than kSlack or not at all: a row that rises slowly
+// would otherwise scale its sum at every load, and each time is another error of the exponential's.
+constexpr float kSlack = 4.f;
 template <int N>
 __device__ __forceinline__ void add_up(Best& b, const float (&x)[N], float top) {
-  const float m = fmaxf(b.m, top), base = m == -INFINITY ? 0.f : m;
+  const bool moves = top > b.ref + kSlack;
+  const float ref = moves ? top : b.ref, base = ref == -INFINITY ? 0.f : ref;
   // the difference first: its rounding, and not that of z log2(e), is what the exponential sees
-  float2 add = make_float2(0.f, 0.f);
+  constexpr int kSums = N >= 8 ? 4 : 1;
+  float2 add[kSums];
 #pragma unroll
-  for (int e = 0; e < N; e += 2) {
-    const float2 y = tc::fmul2(tc::fadd2(make_float2(x[e], x[e + 1]), make_float2(-base, -base)), make_float2(kLog2e, kLog2e));
-    add = tc::fadd2(add, make_float2(tc::ex2(y.x), tc::ex2(y.y)));
+  for (int e = 0; e < N / 2; ++e) {
+    const float2 d = tc::fadd2(make_float2(x[2 * e], x[2 * e + 1]), make_float2(-base, -base));
+    const float2 y = tc::fmul2(d, make_float2(kLog2e, kLog2e)), w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
+    add[e % kSums] = e < kSums ? w : tc::fadd2(add[e % kSums], w);
   }
-  b.s = fmaf(b.s, tc::ex2((b.m - base) * kLog2e), add.x + add.y);
-  b.m = m;
+  if constexpr (kSums == 4) add[0] = tc::fadd2(tc::fadd2(add[0], add[1]), tc::fadd2(add[2], add[3]));
+  const float corr = tc::ex2((b.ref - base) * kLog2e);  // 1 where it stays
+  const float was = b.s * corr, more = add[0].x + add[0].y - b.over * corr;
+  b.s = was + more;
+  b.over = (b.s - was) - more;
+  b.ref = ref;
+  b.m = fmaxf(b.m, top);
 }
 
 template <typename T>
@@ -308,11 +325,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) beam_select_kernel(SelectArgs 
     if (seg == a.segs - 1) keep<2>(b, ends[1], uint32_t(tail) + lane, limit, buffer, lane);
     if (b.count > 0) b.list = merged(b.list, buffer, b.count);
     // the lanes' sums, in the order of a butterfly
-    float m = b.m;
+    float m = b.ref;
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, s));
-    b.s *= tc::ex2((b.m - (m == -INFINITY ? 0.f : m)) * kLog2e);
-    b.m = m;
+    b.s = (b.s - b.over) * tc::ex2((b.ref - (m == -INFINITY ? 0.f : m)) * kLog2e);
+    b.ref = m;
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) b.s += __shfl_xor_sync(kAll, b.s, s);
   }
@@ -320,7 +337,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) beam_select_kernel(SelectArgs 
   {
     const uint32_t list = in_first_cta(&sh.list[id][lane]), stats = in_first_cta(&sh.stats[id]);
     asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(list), "l"(b.list) : "memory");
-    if (lane == 0) asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(stats), "f"(b.m), "f"(b.s) : "memory");
+    if (lane == 0) asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(stats), "f"(b.ref), "f"(b.s) : "memory");
   }
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (rank != 0) return;
