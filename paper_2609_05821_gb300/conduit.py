@@ -926,6 +926,8 @@ def conduit_kv_reorder(kv: KvCache, parent: torch.Tensor, width: int, home: torc
                        stream=None):
     """Beam b takes over the context of row parent[b] (int32 [G width], within b's group): kv.page_table and lens
     (int32 [G width]) are rewritten in place, the begun page is copied into b's own of home (int32 [G width, max_pages])."""
+    if not isinstance(kv, KvCache):
+        raise ConduitError(ERR_INVALID_ARG, "kv must be a KvCache")
     _reorder(_lib.conduit_kv_reorder, kv, parent, width, home, lens, status, stream)
 
 
