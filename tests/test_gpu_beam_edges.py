@@ -90,3 +90,16 @@ def test_equal_rows_come_in_their_order(C):
         z[:] = row.to(dtype)
         score, parent, token = C.conduit_beam_select(z, torch.full((8,), -1.5, device="cuda"), 8, 8)
         assert parent[0].tolist() == list(range(8)) and len(set(token[0].tolist())) == 1 and len(set(score[0].tolist())) == 1
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("L,hkv,d,ps,G,width,lens", [
+    (2, 3, 8, 5, 3, 3, (13, 0, 99)),
+    (1, 1, 8, 1, 2, 4, (7, 1)),
+    (3, 2, 24, 12, 2, 17, (1, 47)),
+    (1, 5, 40, 100, 4, 2, (99, 100, 101, 3)),
+])
+def test_reorder_over_odd_heads_and_pages(C, kind, L, hkv, d, ps, G, width, lens):
+    """Heads of 8 dims, whose rows are 16 bytes, and pages of any number of tokens."""
+    from tests import test_gpu_beam
+    test_gpu_beam.test_reorder(C, kind, L, hkv, d, ps, G, width, lens)
