@@ -871,11 +871,7 @@ def _same_device(device, **tensors):
             raise ConduitError(ERR_INVALID_ARG, f"{name} is on {t.device}, not on {device}")
 
 
-def _fits_int32(**sizes):
-    """ctypes would cut a larger number to its low 32 bits."""
-    for name, n in sizes.items():
-        if n >= 2 ** 31:
-            raise ConduitError(ERR_UNSUPPORTED, f"{n} {name}: more than 2^31 - 1")
+_MOST = 2 ** 31 - 1  # of a size; ctypes would cut a larger one to its low 32 bits
 
 
 def conduit_beam_select(logits: torch.Tensor, sums: torch.Tensor, width: int, num_out: Optional[int] = None, score=None,
@@ -892,7 +888,8 @@ def conduit_beam_select(logits: torch.Tensor, sums: torch.Tensor, width: int, nu
     if sums.dtype is not torch.float32 or sums.numel() != n or not sums.is_contiguous():
         raise ConduitError(ERR_INVALID_ARG, f"sums must be contiguous fp32 [{n}]")
     groups, num_out = n // width, width if num_out is None else int(num_out)
-    _fits_int32(vocab=vocab, num_out=num_out, groups=groups)
+    if vocab > _MOST or groups > _MOST or num_out > _MOST:
+        raise ConduitError(ERR_UNSUPPORTED, f"vocab {vocab}, num_out {num_out} or {groups} groups: more than 2^31 - 1")
     _same_device(logits.device, sums=sums, score=score, parent=parent, token=token, status=status)
     if stream is None and score is None and parent is None and token is None:
         # the cheapest way to three tensors of their own (torch.empty: 4 us more for the call)
@@ -919,7 +916,8 @@ def _reorder(fn, kv, parent: torch.Tensor, width: int, home: torch.Tensor, lens:
     n = parent.numel()
     if width < 1 or n % width:
         raise ConduitError(ERR_INVALID_ARG, f"{n} parents are not groups of {width}")
-    _fits_int32(groups=n // width)
+    if n // width > _MOST:
+        raise ConduitError(ERR_UNSUPPORTED, f"{n // width} groups: more than 2^31 - 1")
     if kv.page_table is None:
         raise ConduitError(ERR_UNSUPPORTED, "reordering needs a paged cache")
     _table_holds(kv, n)
