@@ -6,8 +6,10 @@
 // group (and the same column of their tables): it reads what all of them need before it writes, which is all
 // that an arbitrary map of beams asks for. What the copy reads beside that, lengths of parents and places of begun pages, the
 // same launch leaves as it is.
-// Bound: the rows in use, read and written once; small calls by the chain parent, length, page, rows. Measured: 32 groups of 8
-// beams, 28 layers of 4 heads of 128 in bf16, pages of 32 tokens, 38 us (191 MB read and written, 5.0 TB/s); one group of 4 beams 6 us.
+// Bound: the rows in use of the pages begun, read once a parent and written once a child; small calls by the chain parent, length,
+// page, rows. Measured: 32 groups of 8 beams, 28 layers of 4 heads of 128 in bf16, pages of 32 tokens, 38 us (47 MB from HBM, 96 MB
+// written: 21 us of bytes; a parent's rows are loaded again for each child, from L2). Not HBM (30 % busy) but that chain
+// at the start of each CTA, three waves of them, with the rows of about two heads behind it; one group of 4 beams 6 us.
 #include <algorithm>
 
 #include "beam.cuh"

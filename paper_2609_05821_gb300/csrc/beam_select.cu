@@ -435,8 +435,8 @@ cudaError_t launch(SelectArgs a, int groups, cudaStream_t stream) {
   if (err) return err;
   cudaLaunchAttribute cluster{};
   cluster.id = cudaLaunchAttributeClusterDimension;
-  // Two CTAs of 108 registers a thread on an SM: clusters of eight while all of them run at a time, else of four (64 groups of
-  // 8 rows of 128 003: 38 us, 45 in clusters of eight; four CTAs an SM with half of the loads under way 43).
+  // Two CTAs of 112 registers a thread on an SM: clusters of eight while all of them run at a time, else of four (64 groups of
+  // 8 rows of 128 003: 39 us, 45 in clusters of eight; four CTAs an SM with half of the loads under way 43).
   const int ctas = groups * kClusterMost <= 2 * 152 ? kClusterMost : kClusterMost / 2;
   cluster.val.clusterDim.x = ctas;
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;

@@ -15,8 +15,8 @@
 // block-wide barrier is met before the end, where the warps' results are joined.
 //
 // Bound: 2 d + 1 bytes per token and KV head from HBM. Measured: one row each of 64 requests of 2 000-30 000 tokens, 28 x 4
-// heads of 128, 175 us with the join (6.0 TB/s, 89 % of the copy rate; 36 % of the issue slots); one of 262 145 tokens, 32 x 8
-// heads, 92 us (5.8 TB/s). Two or four column blocks in a CTA of their own SM share the conversions but leave half of the
+// heads of 128, 176 us with the join (6.0 TB/s, 88 % of the copy rate; 38 % of the issue slots); one of 262 145 tokens, 32 x 8
+// heads, 93 us (5.8 TB/s). Two or four column blocks in a CTA of their own SM share the conversions but leave half of the
 // warps: 2 rows of 64 requests of about 4 000 tokens 83 us with blocks of their own, 99 and 136 so.
 #include "attn_warps.cuh"
 #include "fp8.cuh"

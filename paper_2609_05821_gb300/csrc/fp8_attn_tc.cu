@@ -19,7 +19,7 @@
 //
 // Bound: the chain S, softmax, P V, next S of each column tile beside the other's, and under it the shared memory that
 // feeds the MMAs (a key tile: 192 KB of operands and 128 KB of codes in, out and widened). Measured: 32-128
-// rows of 16 requests over 8 192 keys, two layers of 28 x 4 heads of 128, 325 us (0.98 PFLOP/s, tensor pipe 45 % busy); causal
+// rows of 16 requests over 8 192 keys, two layers of 28 x 4 heads of 128, 331 us (0.96 PFLOP/s, tensor pipe 44 % busy); causal
 // prompts, one layer: 8 192 tokens 514 us, four of 4 096 tokens 610. Three loads under way instead of four, and the
 // guarded values in the usual loop: 395 us.
 #include <type_traits>
