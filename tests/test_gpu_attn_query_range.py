@@ -59,14 +59,11 @@ def _check(C, attn, kv, k, v, q, scale, below, step):
     assert np.all(off <= e.T + 2.0 ** -22 * np.abs(wl) + n * 2.0 ** -23 + 2.0 ** -21), (off.max(), e.max())
 
 
-@pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("d", [64, 96, 128])
-@pytest.mark.parametrize("rows", [1, 5, 40, 150])
-@pytest.mark.parametrize("power", [20, 30, 34, 38, 44, 80])
+@pytest.mark.parametrize("dtype,d,rows,power", [(BF, d, rows, power) for d in (64, 96, 128) for rows in (1, 5, 40, 150)
+                                                for power in (20, 30, 34, 38, 44)] +
+                         [(F32, 128, rows, power) for rows in (1, 5) for power in (20, 38, 80)])
 def test_unequal_queries_over_8_bits(C, dtype, d, rows, power):
     """A dim 2^power larger than the others meets zero keys, so that the logits come from the small dims alone."""
-    if (dtype == F32 and (rows > 40 or d == 64)) or (dtype == BF and power == 80):
-        pytest.skip("the kernel of the other cases, or no bound to speak of")
     n, hq = 208, 2
     rng = np.random.default_rng(power)
     k = rng.standard_normal((n, d))
