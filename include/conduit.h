@@ -694,8 +694,8 @@ conduit_status conduit_fp8_read(const conduit_fp8_kv* kv, const int32_t* first,
  * rows with head_dim 64, 96 or 128 run on the tensor cores: keys and values exact in fp16, queries too (but for a power
  * of two) down to 2^-32 of their row's largest |q| and within 2^-40 of it below, so that a logit may be off by
  * scale 2^-40 max |q| sum |k| over such dims; weights times the scale of their value within 2^-11 of themselves or 2^-32 of the
- * row's largest, fp32 sums. Beside such queries lse carries fp32 rounding only (of logits plus the exponents of their value scales, where those
- * differ). Every key counts in the denominator at its weight, wherever in their range the scales of its and of other
+ * row's largest, fp32 sums. Beside such queries lse carries fp32 rounding only (of logits plus the exponents of their
+ * value scales, where those differ). Every key counts in the denominator at its weight, wherever in their range the scales of its and of other
  * values lie. fp32 rows and other head sizes run on the CUDA cores in fp32.
  */
 conduit_status conduit_fp8_attn_workspace_size(const conduit_fp8_kv* kv, const conduit_seqs* seqs,
@@ -711,8 +711,8 @@ conduit_status conduit_fp8_attn(const conduit_fp8_kv* kv, const conduit_seqs* se
  * The best continuations of each group over its beams and the vocabulary:
  *   s(b, v) = sums[b] + logits[b][v] - ln sum_u exp(logits[b][u])
  * the num_out largest, descending, equal ones in the order of (b, v). The sums of exponentials are fp32, scores are formed
- * and compared in fp64: inside a beam the order is that of the logits. A beam's ln sum is within (21 + ln vocab) 2^-22 (8 10^-6
- * for 128 000 logits; a tenth of it and less is usual), and beams whose scores lie within twice that may come in either order. Equal
+ * and compared in fp64: inside a beam the order is that of the logits. A beam's ln sum is within (21 + ln vocab) 2^-22 (8e-6 for
+ * 128 000 logits; a tenth of it and less is usual), and beams whose scores lie within twice that may come in either order. Equal
  * rows with equal sums have equal scores, and come in their order, where they begin at the same place within 16 bytes (as rows do
  * whose row_stride is a multiple of 16 bytes).
  *  logits  device [G width][vocab] of dtype, rows row_stride elements apart (>= vocab), aligned to the element
